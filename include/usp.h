@@ -48,6 +48,8 @@ typedef enum {
 
 /* Format version written by usp_encode and reported by usp_info. */
 #define USP_FORMAT_VERSION 2
+/* The same for usp_encode_q: records of 8-bit values. */
+#define USP_FORMAT_VERSION_Q 3
 
 /*
  * usp_encode -- one-time conversion of W and its keep-mask into the compressed
@@ -177,7 +179,8 @@ usp_status usp_plan(const usp_matrix *A, int64_t N, char *buf, size_t len);
 /*
  * usp_densify -- writes W with the mask applied (pruned entries as +0) into a
  * dense row-major M x K fp16 device buffer Wd with row stride ldw >= K, by the
- * same on-chip decode the product uses. Asynchronous on `stream`. For checks.
+ * same on-chip decode the product uses; 8-bit values times their row's scale,
+ * rounded to fp16. Asynchronous on `stream`. For checks.
  */
 usp_status usp_densify(const usp_matrix *A, void *Wd, int64_t ldw, void *stream);
 
@@ -193,7 +196,7 @@ typedef struct {
     int64_t nnz;            /* kept entries */
     size_t device_bytes;    /* bytes of the encoding the product streams from HBM */
     size_t table_bytes;     /* bytes of the per-tile offset table (also streamed) */
-    int32_t format_version; /* USP_FORMAT_VERSION */
+    int32_t format_version; /* USP_FORMAT_VERSION, or USP_FORMAT_VERSION_Q for 8-bit weights */
     int32_t tile_rows, tile_k; /* tile geometry of the encoding */
     int32_t device;
 } usp_info_t;
@@ -201,8 +204,162 @@ typedef struct {
 /* usp_info -- shape, size and geometry of an encoding. */
 usp_status usp_info(const usp_matrix *A, usp_info_t *info);
 
-/* usp_free -- releases the handle and its device memory. NULL is accepted.
- * The caller guarantees no usp_spmm/usp_densify on it is still in flight.
+/* ---- 8-bit weights and tokens ------------------------------------------------
+ *
+ * W = diag(w_scale) Wq and X = Xq diag(x_scale): 8-bit integers with one fp32 scale
+ * per output channel and one per token. The products are summed exactly in 32-bit
+ * integers; the scales, the bias, the activation and the residual are applied in
+ * fp32, then the one rounding to fp16. A handle of 8-bit weights is used with
+ * usp_spmm_q, usp_densify, usp_decode_q, usp_info, usp_plan, usp_workspace_size,
+ * usp_group_create and usp_free; usp_spmm and its variants and usp_decode refuse
+ * it, as usp_spmm_q refuses a handle of fp16 weights (USP_ERR_INVALID_ARG).
+ */
+
+/* Most columns of an 8-bit weight (its integer sums stay below 2^31) and of the
+ * experts of a group. */
+#define USP_MAX_K_Q 129024
+
+/*
+ * usp_encode_q -- usp_encode for 8-bit weights.
+ *   W      host pointer, M x K int8 (the whole range, -128 included), row stride ldw >= K
+ *   scale  host pointer, M fp32 scales, one per row (finite)
+ *   K      <= USP_MAX_K_Q
+ * Everything else as usp_encode.
+ */
+usp_status usp_encode_q(const int8_t *W, int64_t ldw, const uint8_t *mask, int64_t ldm, const float *scale,
+                        int64_t M, int64_t K, int device, usp_matrix **out);
+
+/* usp_decode_q -- host-side inverse of usp_encode_q: M x K int8, M x K mask bytes, M scales. Blocking. */
+usp_status usp_decode_q(const usp_matrix *A, int8_t *W_out, uint8_t *mask_out, float *scale_out);
+
+/*
+ * usp_quantize -- tokens in 8 bits: per token n, a = max_k |X[n, k]|, x_scale[n] = a / 127
+ * and Xq[n, k] = X[n, k] * (127 / a) rounded to the nearest integer, ties to even (all in
+ * fp32; a = 0 gives zeros and scale 0). A token that holds a NaN or an infinity gets zeros
+ * and the scale NaN, so its products are NaN.
+ *   X        device pointer, fp16, token n at X + n * ldx, ldx >= K
+ *   Xq       device pointer, int8, token n at Xq + n * ldq, ldq >= K
+ *   x_scale  device pointer, fp32 [N]
+ *   N, K     >= 1
+ *   device   the HIP device of the pointers and of `stream`
+ * Asynchronous on `stream`; no allocation, capturable.
+ */
+usp_status usp_quantize(const void *X, int64_t ldx, int64_t N, int64_t K, void *Xq, int64_t ldq, float *x_scale,
+                        int device, void *stream);
+
+/*
+ * usp_spmm_q -- Y = act(W X + bias) + residual with 8-bit W and X, on the handle's device.
+ *   Xq       device pointer, int8, token n at Xq + n * ldx, ldx >= K
+ *   x_scale  device pointer, fp32 [N], 4-byte aligned
+ *   workspace  16-byte aligned, to >= usp_workspace_size(A, N) bytes (may be NULL when that is
+ *       0); must not be used by another in-flight call. It needs no clearing, and the region that
+ *       usp_spmm expects cleared is left alone, so that one workspace can serve both.
+ * Xq with a base or stride that is no multiple of 4 bytes is copied first. Everything else --
+ * Y, bias, residual, activation, asynchrony, capture, reproducibility -- as usp_spmm_ex.
+ */
+usp_status usp_spmm_q(const usp_matrix *A, const void *Xq, int64_t ldx, const float *x_scale, void *Y, int64_t ldy,
+                      int64_t N, const void *bias, const void *residual, int64_t ldr, int activation,
+                      void *workspace, size_t ws_bytes, void *stream);
+
+/* ---- Products grouped by expert ---------------------------------------------- */
+
+typedef struct usp_group usp_group; /* opaque; a list of encoded experts */
+
+/*
+ * usp_group_create -- a group of E experts: handles of the same shape and value type (all
+ * fp16 or all 8-bit) on one device, K <= USP_MAX_K_Q. An expert may occur more than once and
+ * in several groups. The handles stay the caller's; while a group holds one, usp_free refuses
+ * it. Blocking. 1 <= E <= 65536.
+ */
+usp_status usp_group_create(const usp_matrix *const *experts, int64_t E, usp_group **out);
+
+/* usp_group_free -- releases the group (not its experts). NULL is accepted. */
+usp_status usp_group_free(usp_group *G);
+
+/* usp_group_workspace_size -- bytes of device workspace usp_spmm_grouped needs for T rows (0 when none, or for no
+ * valid group or T). */
+size_t usp_group_workspace_size(const usp_group *G, int64_t T);
+
+/*
+ * usp_spmm_grouped -- for each expert e and each row t of its range offsets[e] <= t < offsets[e + 1]:
+ *     Y[t] = row_weight[t] * act(W_e X[rows[t]] + bias[e])
+ *   X        device pointer, x_rows rows with stride ldx >= K: fp16, or int8 for experts of
+ *            8-bit weights
+ *   x_scale  device fp32 [x_rows], the scales of the 8-bit rows (NULL for fp16 experts)
+ *   rows     device int32 [T], the row of X that row t multiplies (a row may occur several
+ *            times, as for tokens that go to several experts), or NULL: row t itself, and then
+ *            x_rows >= T. An index outside [0, x_rows) stands for a row of zeros.
+ *   E        the group's number of experts (any other is refused)
+ *   offsets  device int32 [E + 1], not decreasing, within [0, T]. They are read on the device, so
+ *            the call needs no host knowledge of the counts and may be captured; values outside
+ *            [0, T] count as the nearer end and a decreasing value as the one before it. Rows of Y
+ *            that no expert has are left as they were.
+ *   Y        device fp16, row t at Y + t * ldy, ldy >= M; must not overlap X
+ *   bias     device fp16, expert e's at bias + e * ldb (ldb >= M), or NULL
+ *   row_weight  device fp32 [T], the router's weights, or NULL for ones
+ *   activation  a usp_activation
+ *   T        0 <= T <= 2^20 (0: nothing is done)
+ *   workspace  as usp_spmm_q, of usp_group_workspace_size(G, T) bytes
+ * Accumulation and rounding as in usp_spmm (fp16 experts) and usp_spmm_q; an offset or a row index
+ * never makes the call read or write outside the operands.
+ */
+usp_status usp_spmm_grouped(const usp_group *G, const void *X, int64_t ldx, int64_t x_rows, const float *x_scale,
+                            const int32_t *rows, const int32_t *offsets, int64_t E, void *Y, int64_t ldy, int64_t T,
+                            const void *bias, int64_t ldb, const float *row_weight, int activation,
+                            void *workspace, size_t ws_bytes, void *stream);
+
+/* ---- Norms around a block ------------------------------------------------------ */
+
+typedef enum {
+    USP_NORM_NONE = 0,
+    USP_NORM_RMS = 1,  /* v / sqrt(mean(v^2) + eps) * weight + bias */
+    USP_NORM_LAYER = 2 /* (v - mean(v)) / sqrt(var(v) + eps) * weight + bias */
+} usp_norm_kind;
+
+typedef enum {
+    USP_GATE_NONE = 0, /* g */
+    USP_GATE_SIGMOID = 1,
+    USP_GATE_TANH = 2,
+    USP_GATE_SILU = 3
+} usp_gate_activation;
+
+/*
+ * One token's update, all in fp32:
+ *     r = residual + scale * gate_act(gate) * post(y)        (y NULL: r = residual)
+ *     h = pre(r)
+ * residual_out takes r and out takes h, each rounded to fp16 once (h is computed from r before
+ * its rounding); out_q and out_scale take the fp16 h in 8 bits, as usp_quantize(h) does. Pointers
+ * are device pointers; strides count elements.
+ */
+typedef struct {
+    const void *residual;      /* fp16 [N, K], stride ld_residual */
+    const void *y;             /* fp16 [N, K], stride ld_y: the block's output; or NULL */
+    const void *gate;          /* fp16 [N, K] with stride ld_gate, or [K] with ld_gate = 0; or NULL: 1 */
+    const void *post_weight;   /* fp16 [K], or NULL: 1 */
+    const void *post_bias;     /* fp16 [K], or NULL: 0 */
+    const void *pre_weight;
+    const void *pre_bias;
+    void *residual_out;        /* fp16, stride ld_residual_out; may be residual or y; or NULL */
+    void *out;                 /* fp16, stride ld_out; may be y; or NULL */
+    void *out_q;               /* int8, stride ld_out_q; or NULL */
+    float *out_scale;          /* fp32 [N]; needed with out_q */
+    int64_t ld_residual, ld_y, ld_gate, ld_residual_out, ld_out, ld_out_q;
+    float scale;               /* residual scale */
+    float eps;                 /* >= 0 */
+    int post_kind, pre_kind;   /* usp_norm_kind; post_kind needs y */
+    int gate_activation;       /* usp_gate_activation */
+} usp_norm_args;
+
+/*
+ * usp_norm -- the update above for N >= 1 tokens of K >= 1 channels. At least one output. An output
+ * that is an input has its stride and base; other overlaps are not allowed. A gate needs y.
+ * Asynchronous on `stream` (of `device`); no allocation, capturable, bitwise reproducible.
+ */
+usp_status usp_norm(const usp_norm_args *args, int64_t N, int64_t K, int device, void *stream);
+
+/* usp_free -- releases the handle and its device memory. NULL is accepted. A handle that a
+ * group holds is refused (USP_ERR_INVALID_ARG).
+ * The caller guarantees no product or usp_densify on it is still in flight.
  * Handles are looked up among the live ones before use, never dereferenced
  * blindly: passing a freed handle (or any pointer usp_encode did not return)
  * to any entry point gives USP_ERR_INVALID_ARG, unless a later usp_encode

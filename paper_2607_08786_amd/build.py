@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libusp.so")
-SOURCES = ["usp_abi.cpp", "usp_encode.cpp", "usp_kernels.hip", "usp_wide.hip"]
+SOURCES = ["usp_abi.cpp", "usp_encode.cpp", "usp_kernels.hip", "usp_wide.hip", "usp_norm.hip",
+           "usp_product.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # Packed fp32 VALU forms are disabled for all device code.

@@ -49,10 +49,28 @@ inline uint8_t nonzero_bits(const uint8_t *p, int64_t n) {
     return (uint8_t)(((t >> 7) * 0x0102040810204080ull) >> 56);
 }
 
-}  // namespace
+// Records of fp16 values (V = uint16_t) and of 8-bit values (V = int8_t) differ in
+// the columns of a lane's mask byte y and in the size of a value, nothing else.
+template <class V>
+inline int byte_col(int g, int y) {
+    return sizeof(V) == 2 ? tile_col(g, y, 0) : tile_col_q(g, y, 0);
+}
 
-void encode_host(const uint16_t *W, int64_t ldw, const uint8_t *mask, int64_t ldm,
-                 int64_t M, int64_t K, HostEncoding &out) {
+// Lane group g and mask byte y of the tile's columns 8 c .. 8 c + 7.
+template <class V>
+inline void place8(int c, int &g, int &y) {
+    if (sizeof(V) == 2) {
+        g = c % 4;
+        y = c / 4;
+    } else {
+        g = c / 2 % 4;
+        y = 2 * (c / 8) + c % 2;
+    }
+}
+
+template <class V>
+void encode_records(const V *W, int64_t ldw, const uint8_t *mask, int64_t ldm, int64_t M, int64_t K,
+                    HostEncoding &out) {
     out.M = M;
     out.K = K;
     out.RB = ceil_div(M, kTileRows);
@@ -76,17 +94,19 @@ void encode_host(const uint16_t *W, int64_t ldw, const uint8_t *mask, int64_t ld
                     for (int i = 0; i < kTileK / 16; ++i) {
                         const __m128i x = _mm_loadu_si128(reinterpret_cast<const __m128i *>(mr + kt * kTileK + 16 * i));
                         const int z = _mm_movemask_epi8(_mm_cmpeq_epi8(x, _mm_setzero_si128()));
-                        const int s = i / 2, g = 2 * (i % 2);
-                        m[8 * (g * kTileRows + r) + s] = (uint8_t)~z;
-                        m[8 * ((g + 1) * kTileRows + r) + s] = (uint8_t)(~z >> 8);
+                        int g, y;
+                        place8<V>(2 * i, g, y);
+                        m[8 * (g * kTileRows + r) + y] = (uint8_t)~z;
+                        place8<V>(2 * i + 1, g, y);
+                        m[8 * (g * kTileRows + r) + y] = (uint8_t)(~z >> 8);
                     }
                     continue;
                 }
 #endif
-                for (int s = 0; s < kSteps; ++s)
+                for (int y = 0; y < kMaskBytes / kLanes; ++y)
                     for (int g = 0; g < kLanes / kTileRows; ++g) {
-                        const int64_t c = kt * kTileK + tile_col(g, s, 0);
-                        m[8 * (g * kTileRows + r) + s] = row < M && c < K ? nonzero_bits(mr + c, K - c) : 0;
+                        const int64_t c = kt * kTileK + byte_col<V>(g, y);
+                        m[8 * (g * kTileRows + r) + y] = row < M && c < K ? nonzero_bits(mr + c, K - c) : 0;
                     }
             }
             int64_t cnt = 0;
@@ -102,7 +122,7 @@ void encode_host(const uint16_t *W, int64_t ldw, const uint8_t *mask, int64_t ld
     int64_t total = 0, nnz = 0, max_chunks = 0;
     for (int64_t t = 0; t < T; ++t) {
         out.off[t] = (uint32_t)total;
-        const int64_t chunks = ceil_div(2 * tile_nnz[t], 16);
+        const int64_t chunks = ceil_div((int64_t)sizeof(V) * tile_nnz[t], 16);
         total += kMaskChunks + chunks;
         max_chunks = std::max(max_chunks, chunks);
         nnz += tile_nnz[t];
@@ -116,21 +136,20 @@ void encode_host(const uint16_t *W, int64_t ldw, const uint8_t *mask, int64_t ld
     // Pass 2: fill records. Each position writes its value at the record's current
     // end and advances it if it is kept: no branch on the mask.
     parallel_rows(out.RB, [&](int64_t rb) {
-        uint16_t vals[kMaxValBytes / 2 + 8];
+        V vals[kTileRows * kTileK + 8];
         for (int64_t kt = 0; kt < out.KT; ++kt) {
             const int64_t t = rb * out.KT + kt;
             const uint8_t *m = masks.data() + (size_t)t * kMaskBytes;
             const bool inside = (rb + 1) * kTileRows <= M && (kt + 1) * kTileK <= K;
             int64_t v = 0;
-            for (int s = 0; s < kSteps; ++s) {
-                // Values of step s: block (s, low nibble), then block (s, high nibble);
-                // within a block lane 0's values first, in column order.
+            for (int y = 0; y < kMaskBytes / kLanes; ++y) {
+                // Values of mask byte y: the block of its low nibble, then that of its high
+                // nibble; within a block lane 0's values first, in column order.
                 for (int h = 0; h < 2; ++h) {
                     for (int l = 0; l < kLanes; ++l) {
                         const int r = l % kTileRows, g = l / kTileRows;
-                        const uint32_t n = (uint32_t)(m[8 * l + s] >> (4 * h)) & 15u;
-                        const uint16_t *w =
-                            W + (rb * kTileRows + r) * ldw + kt * kTileK + tile_col(g, s, 0) + 4 * h;
+                        const uint32_t n = (uint32_t)(m[8 * l + y] >> (4 * h)) & 15u;
+                        const V *w = W + (rb * kTileRows + r) * ldw + kt * kTileK + byte_col<V>(g, y) + 4 * h;
                         if (inside) {
                             vals[v] = w[0];
                             v += n & 1;
@@ -148,7 +167,7 @@ void encode_host(const uint16_t *W, int64_t ldw, const uint8_t *mask, int64_t ld
                 }
             }
             uint8_t *rec = out.stream.data() + (size_t)out.off[t] * 16;
-            const size_t bytes = (size_t)v * 2, room = (size_t)(out.off[t + 1] - out.off[t]) * 16 - kMaskBytes;
+            const size_t bytes = (size_t)v * sizeof(V), room = (size_t)(out.off[t + 1] - out.off[t]) * 16 - kMaskBytes;
             std::memcpy(rec, m, kMaskBytes);
             std::memcpy(rec + kMaskBytes, vals, bytes);
             std::memset(rec + kMaskBytes + bytes, 0, room - bytes);
@@ -156,30 +175,31 @@ void encode_host(const uint16_t *W, int64_t ldw, const uint8_t *mask, int64_t ld
     });
 }
 
-bool decode_host(const HostEncoding &enc, uint16_t *W_out, uint8_t *mask_out) {
+template <class V>
+bool decode_records(const HostEncoding &enc, V *W_out, uint8_t *mask_out) {
     const int64_t M = enc.M, K = enc.K;
     const int64_t T = enc.RB * enc.KT;
     if ((int64_t)enc.off.size() != T + 1) return false;
     if ((size_t)enc.off[T] * 16 != enc.stream.size()) return false;
-    std::memset(W_out, 0, sizeof(uint16_t) * (size_t)(M * K));
+    std::memset(W_out, 0, sizeof(V) * (size_t)(M * K));
     std::memset(mask_out, 0, (size_t)(M * K));
     bool ok = true;
     for (int64_t rb = 0; rb < enc.RB && ok; ++rb) {
         for (int64_t kt = 0; kt < enc.KT && ok; ++kt) {
             const int64_t t = rb * enc.KT + kt;
             const uint8_t *rec = enc.stream.data() + (size_t)enc.off[t] * 16;
-            const int64_t cap = ((int64_t)enc.off[t + 1] - enc.off[t] - kMaskChunks) * 8;  // halfs
-            const uint16_t *vals = reinterpret_cast<const uint16_t *>(rec + kMaskBytes);
+            const int64_t cap = ((int64_t)enc.off[t + 1] - enc.off[t] - kMaskChunks) * 16 / (int64_t)sizeof(V);
+            const V *vals = reinterpret_cast<const V *>(rec + kMaskBytes);
             int64_t v = 0;
-            for (int sh = 0; sh < 2 * kSteps && ok; ++sh) {
-                const int s = sh / 2, h = sh % 2;  // block (step s, nibble half h)
+            for (int yh = 0; yh < 2 * kMaskBytes / kLanes && ok; ++yh) {
+                const int y = yh / 2, h = yh % 2;  // block (mask byte y, nibble half h)
                 for (int l = 0; l < kLanes; ++l) {
                     const int r = l % kTileRows, g = l / kTileRows;
                     const int64_t row = rb * kTileRows + r;
-                    const uint8_t b = rec[8 * l + s];
+                    const uint8_t b = rec[8 * l + y];
                     for (int j = 4 * h; j < 4 * h + 4; ++j) {
                         if (!(b & (1u << j))) continue;
-                        const int64_t col = kt * kTileK + tile_col(g, s, j);
+                        const int64_t col = kt * kTileK + byte_col<V>(g, y) + j;
                         if (row >= M || col >= K || v >= cap) { ok = false; break; }
                         W_out[row * K + col] = vals[v++];
                         mask_out[row * K + col] = 1;
@@ -189,6 +209,26 @@ bool decode_host(const HostEncoding &enc, uint16_t *W_out, uint8_t *mask_out) {
         }
     }
     return ok;
+}
+
+}  // namespace
+
+void encode_host(const uint16_t *W, int64_t ldw, const uint8_t *mask, int64_t ldm,
+                 int64_t M, int64_t K, HostEncoding &out) {
+    encode_records(W, ldw, mask, ldm, M, K, out);
+}
+
+void encode_host_q(const int8_t *W, int64_t ldw, const uint8_t *mask, int64_t ldm, int64_t M, int64_t K,
+                   HostEncoding &out) {
+    encode_records(W, ldw, mask, ldm, M, K, out);
+}
+
+bool decode_host(const HostEncoding &enc, uint16_t *W_out, uint8_t *mask_out) {
+    return decode_records(enc, W_out, mask_out);
+}
+
+bool decode_host_q(const HostEncoding &enc, int8_t *W_out, uint8_t *mask_out) {
+    return decode_records(enc, W_out, mask_out);
 }
 
 }  // namespace usp

@@ -29,6 +29,12 @@
 //                       apart (32 lanes span about the 32 LDS banks).
 //   zero padding to a multiple of 16 bytes.
 // off[] holds T + 1 uint32 entries in 16-byte units; off[T] is the total size.
+//
+// Records of 8-bit values (format version 3) have the same tiles, mask words and
+// blocks; a value takes one byte, and a lane's slice is that of a 16 x 64 MFMA
+// operand: at step s (0..3) lane (r, g) owns columns 256 kt + 64 s + 16 g + j,
+// j = 0..15. Its mask byte y = 2 s + j / 8 holds positions j of step s, so block
+// b = 4 s + j / 4 holds nibble b of the lane's 64 mask bits, as for fp16.
 #pragma once
 #include <stdint.h>
 
@@ -46,6 +52,7 @@ constexpr int kLanes = 64;
 constexpr int kSteps = 8;                    // k-steps of 32 columns per tile
 constexpr int kMaskBytes = kLanes * kSteps;  // 512
 constexpr int kMaskChunks = kMaskBytes / 16; // 32 sixteen-byte units
+constexpr int kStepsQ = 4;                   // k-steps of 64 columns per tile of 8-bit values
 constexpr int kMaxValBytes = kTileRows * kTileK * 2;  // 8192 (a fully dense tile)
 constexpr int kStreamPad = 1024;  // device bytes after the last record (read, never used)
 
@@ -53,5 +60,7 @@ USP_HD inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Column of position (g, s, j) inside a tile.
 USP_HD inline int tile_col(int g, int s, int j) { return 32 * s + 8 * g + j; }
+// The same for 8-bit values: column of bit j of mask byte y of lane group g.
+USP_HD inline int tile_col_q(int g, int y, int j) { return 64 * (y / 2) + 16 * g + 8 * (y % 2) + j; }
 
 }  // namespace usp

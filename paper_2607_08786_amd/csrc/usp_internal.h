@@ -22,6 +22,20 @@ struct usp_matrix {
     void *d_stream;          // device: tile records
     uint32_t *d_off;         // device: RB*KT + 1 offsets in 16-byte units
     int num_cus;             // compute units of the device
+    int value_bytes;         // 2: fp16 values; 1: 8-bit values
+    float *d_scale;          // device: scale of each row (8-bit values), or null
+    int groups;              // live groups that hold this matrix (under the handles' lock)
+};
+
+// Experts of one shape and value type on one device (usp_group_create).
+struct usp_group {
+    int device;
+    int64_t E, M, K, RB, KT;
+    int64_t max_chunks;      // most 16-byte value chunks in one tile record of any expert
+    int num_cus;
+    int value_bytes;
+    void *d_experts;         // device: E usp::ExpertRef
+    std::vector<usp_matrix *> experts;
 };
 
 namespace usp {
@@ -62,6 +76,11 @@ void encode_host(const uint16_t *W, int64_t ldw, const uint8_t *mask, int64_t ld
                  int64_t M, int64_t K, HostEncoding &out);
 // Returns false when the records are inconsistent with the shape.
 bool decode_host(const HostEncoding &enc, uint16_t *W_out, uint8_t *mask_out);
+
+// The same for 8-bit values.
+void encode_host_q(const int8_t *W, int64_t ldw, const uint8_t *mask, int64_t ldm, int64_t M, int64_t K,
+                   HostEncoding &out);
+bool decode_host_q(const HostEncoding &enc, int8_t *W_out, uint8_t *mask_out);
 
 // Error reporting (usp_abi.cpp).
 usp_status fail(usp_status st, const std::string &msg);
@@ -122,6 +141,46 @@ WidePlan plan_wide(const usp_matrix *A, int64_t N, size_t max_bytes, size_t min_
 int launch_wide(const usp_matrix *A, const WidePlan &plan, const void *X, int64_t ldx, void *Y, int64_t ldy,
                 int64_t N, const Epilogue &ep, void *workspace, size_t ws_bytes, void *stream);
 int launch_densify(const usp_matrix *A, void *Wd, int64_t ldw, void *stream);
+
+// Norms, and tokens in 8 bits (usp_norm.hip).
+int launch_norm(const usp_norm_args &p, int64_t N, int64_t K, void *stream);
+
+// Products on 8-bit values and products grouped by expert (usp_product.hip).
+struct ExpertRef {             // one encoded matrix, as the kernels see it
+    const uint8_t *stream;
+    const uint32_t *off;
+    const float *scale;        // scale of each row, whole row blocks; null for fp16
+};
+struct ProductShape {
+    const usp_matrix *A;       // the matrix, or
+    const usp_group *G;        // the group
+    int64_t M, K, RB, KT, max_chunks;
+    int value_bytes, num_cus;
+};
+inline ProductShape product_shape(const usp_matrix *A) {
+    return {A, nullptr, A->M, A->K, A->RB, A->KT, A->max_chunks, A->value_bytes, A->num_cus};
+}
+inline ProductShape product_shape(const usp_group *G) {
+    return {nullptr, G, G->M, G->K, G->RB, G->KT, G->max_chunks, G->value_bytes, G->num_cus};
+}
+struct ProductCall {
+    const void *X;
+    int64_t ldx, x_rows;       // elements
+    const float *x_scale;
+    const int32_t *rows, *offsets;
+    void *Y;
+    int64_t ldy, N;
+    Epilogue ep;
+    int64_t ldb;
+    const float *weight;
+};
+bool product_fits(const ProductShape &s, int64_t N);  // its jobs are counted in 31 bits
+size_t product_workspace_bytes(const ProductShape &s, int64_t N);
+std::string describe_product(const ProductShape &s, int64_t N);
+int launch_densify_q(const usp_matrix *A, void *Wd, int64_t ldw, void *stream);
+int launch_product(const ProductShape &s, const ProductCall &c, void *workspace, void *stream);
+// Most columns that a group's or an 8-bit matrix's kernels serve.
+constexpr int64_t kMaxProductK = USP_MAX_K_Q;
 // Device scratch of usp_spmm_noalloc: noalloc_setup looks up and clears the
 // calling thread's current device's copy once (returns a HIP error code);
 // noalloc_scratch returns its device address, or null before the set-up.

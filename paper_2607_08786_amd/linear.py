@@ -5,10 +5,16 @@ steps: the pruned weight is encoded once and every call is one ``usp_spmm_ex``
 ``torch.ops.usp.sparse_linear`` is the custom operator; ``SparseLinear`` is the
 module around it. Inputs are fp16 CUDA (HIP) tensors whose last dimension is
 ``in_features``; leading dimensions are flattened into the token count N.
+
+``SparseLinearQ`` is the same with 8-bit weights and tokens, ``SparseExperts`` a linear
+layer with a weight for each expert on rows sorted by expert, and ``BlockNorm`` the norms
+around a block with its gate and residual scale, whose output may be the 8-bit tokens that
+the two read (operators ``usp::sparse_linear_q``, ``usp::sparse_experts``, ``usp::block_norm``).
+All of it is for inference: nothing here has a backward pass.
 """
 from __future__ import annotations
 
-from typing import Optional
+from typing import Optional, Tuple, Union
 
 import numpy as np
 import torch
@@ -55,7 +61,10 @@ class SparseLinear(torch.nn.Module):
         if m.shape != w.shape:
             raise ValueError("mask must have the weight's shape")
         self.matrix = usp.SparseMatrix(w, m, dev)
-        self.out_features, self.in_features = w.shape
+        self._set_up(w.shape, bias, activation, dev)
+
+    def _set_up(self, shape, bias, activation, dev) -> None:
+        self.out_features, self.in_features = shape
         self.activation = activation
         self.register_buffer(
             "bias", None if bias is None else bias.detach().to(device=f"cuda:{dev}", dtype=torch.float16).contiguous())
@@ -115,3 +124,250 @@ class SparseLinear(torch.nn.Module):
     def extra_repr(self) -> str:
         return (f"in_features={self.in_features}, out_features={self.out_features}, "
                 f"nnz={self.matrix.nnz}, bias={self.bias is not None}, activation={self.activation}")
+
+
+# ---- 8-bit layers, experts and the norms around a block
+
+
+def quantize_rows(weight: torch.Tensor, mask) -> Tuple[torch.Tensor, torch.Tensor]:
+    """A weight in 8 bits, symmetric per row over the kept entries: (codes int8, scale fp32 [rows])."""
+    m = torch.as_tensor(mask, device=weight.device) != 0
+    w = torch.where(m, weight.detach().float(), torch.zeros((), device=weight.device))
+    scale = w.abs().amax(1) / 127
+    safe = torch.where(scale > 0, scale, torch.ones_like(scale))
+    return (w / safe[:, None]).round().clamp(-127, 127).to(torch.int8), scale
+
+
+def _int8_tokens(N: int, K: int, device) -> torch.Tensor:
+    """An [N, K] int8 tensor whose rows start at multiples of 16 bytes, as the products read them in place."""
+    return torch.empty((N, (K + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :K]
+
+
+def _tokens(x: torch.Tensor, x_scale: Optional[torch.Tensor]) -> Tuple[torch.Tensor, torch.Tensor]:
+    """8-bit tokens and scales: x and x_scale themselves, or fp16 x quantised."""
+    if x_scale is not None:
+        return x, x_scale
+    xq = _int8_tokens(*x.shape, x.device)
+    x_scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    usp.usp_quantize(x, xq, x_scale)
+    return xq, x_scale
+
+
+def _linear_q(x: torch.Tensor, x_scale: Optional[torch.Tensor], handle: int, out_features: int,
+              bias: Optional[torch.Tensor], residual: Optional[torch.Tensor], activation: int,
+              workspace: Optional[torch.Tensor]) -> torch.Tensor:
+    """act(x @ W^T + bias) + residual for the 8-bit weight behind ``handle``; x is [N, in_features], fp16, or int8
+    with the tokens' scales."""
+    xq, x_scale = _tokens(x, x_scale)
+    y = torch.empty((x.shape[0], out_features), dtype=torch.float16, device=x.device)
+    usp.usp_spmm_q(handle, xq, x_scale, y, workspace, bias, residual, activation)
+    return y
+
+
+def _experts(x: torch.Tensor, x_scale: Optional[torch.Tensor], offsets: torch.Tensor, rows: Optional[torch.Tensor],
+             row_weight: Optional[torch.Tensor], group: int, out_features: int, eight_bit: bool,
+             bias: Optional[torch.Tensor], activation: int, workspace: Optional[torch.Tensor]) -> torch.Tensor:
+    """usp_spmm_grouped into a new tensor; zeros in the rows that no expert has."""
+    if eight_bit:
+        x, x_scale = _tokens(x, x_scale)
+    T = x.shape[0] if rows is None else rows.shape[0]
+    y = torch.zeros((T, out_features), dtype=torch.float16, device=x.device)
+    usp.usp_spmm_grouped(group, x, offsets, y, workspace, x_scale, rows, bias, row_weight, activation)
+    return y
+
+
+def _block_norm(residual: torch.Tensor, y: Optional[torch.Tensor], gate: Optional[torch.Tensor], scale: float,
+                post: str, post_weight: Optional[torch.Tensor], post_bias: Optional[torch.Tensor], pre: str,
+                pre_weight: Optional[torch.Tensor], pre_bias: Optional[torch.Tensor], eps: float, gate_activation: str,
+                quantize: bool) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """The residual's update, the norm of it (int8 if quantize) and the tokens' scales (empty if not)."""
+    N, K = residual.shape
+    r = torch.empty((N, K), dtype=torch.float16, device=residual.device)
+    h = _int8_tokens(N, K, r.device) if quantize else torch.empty_like(r)
+    h_scale = torch.empty(N if quantize else 0, dtype=torch.float32, device=r.device)
+    usp.usp_norm(residual, y, gate, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, gate_activation,
+                 residual_out=r, **(dict(out_q=h, out_scale=h_scale) if quantize else dict(out=h)))
+    return r, h, h_scale
+
+
+sparse_linear_q = torch.library.custom_op("usp::sparse_linear_q", _linear_q, mutates_args=("workspace",))
+sparse_experts = torch.library.custom_op("usp::sparse_experts", _experts, mutates_args=("workspace",))
+block_norm = torch.library.custom_op("usp::block_norm", _block_norm, mutates_args=())
+
+
+@sparse_linear_q.register_fake
+def _(x, x_scale, handle, out_features, bias, residual, activation, workspace):
+    return x.new_empty((x.shape[0], out_features), dtype=torch.float16)
+
+
+@sparse_experts.register_fake
+def _(x, x_scale, offsets, rows, row_weight, group, out_features, eight_bit, bias, activation, workspace):
+    return x.new_empty(((x if rows is None else rows).shape[0], out_features), dtype=torch.float16)
+
+
+@block_norm.register_fake
+def _(residual, y, gate, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, gate_activation, quantize):
+    N, K = residual.shape
+    h = residual.new_empty((N, (K + 15) // 16 * 16), dtype=torch.int8)[:, :K] if quantize else torch.empty_like(residual)
+    return residual.new_empty((N, K)), h, residual.new_empty(N if quantize else 0, dtype=torch.float32)
+
+
+def _call(op, plain, *args):
+    """The operator where a compiler or autograd has to see it; else the function itself, which spares an eager
+    decode step the dispatcher (a small layer's kernels take less time than it)."""
+    if torch.compiler.is_compiling() or (torch.is_grad_enabled() and
+                                         any(isinstance(a, torch.Tensor) and a.requires_grad for a in args)):
+        return op(*args)
+    return plain(*args)
+
+
+def _rows_of(x: torch.Tensor, width: int) -> torch.Tensor:
+    """x as fp16 [N, width] with unit inner stride."""
+    x = x.reshape(-1, width)
+    if x.dtype != torch.float16 or x.stride(1) != 1:
+        x = x.to(torch.float16).contiguous()
+    return x
+
+
+Tokens = Union[torch.Tensor, Tuple[torch.Tensor, torch.Tensor]]
+
+
+class SparseLinearQ(SparseLinear):
+    """``act(x W^T + b) (+ residual)`` with W pruned by ``mask`` and held in 8 bits with a scale per output feature,
+    x quantised to 8 bits with a scale per token.
+
+    weight: int8 [out_features, in_features]; scale: fp32 [out_features]; the rest as SparseLinear. The input is an
+    fp16 tensor, or the pair of int8 tokens [N, in_features] and their scales [N] that BlockNorm gives. Calls and
+    captured graphs may overlap as SparseLinear's may."""
+
+    def __init__(self, weight: torch.Tensor, mask, scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                 activation: str = "none", device: Optional[int] = None):
+        torch.nn.Module.__init__(self)
+        if activation not in usp.ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(usp.ACTIVATIONS)}")
+        if weight.dtype != torch.int8:
+            raise TypeError("weight must be int8 (quantize_rows makes it from a float weight)")
+        dev = torch.cuda.current_device() if device is None else int(device)
+        m = mask.detach().cpu().numpy() if isinstance(mask, torch.Tensor) else np.asarray(mask)
+        self.matrix = usp.SparseMatrixQ(weight.detach().cpu().contiguous().numpy(), np.ascontiguousarray(m != 0),
+                                        scale.detach().float().cpu().numpy(), dev)
+        self._set_up(weight.shape, bias, activation, dev)
+
+    @classmethod
+    def from_linear(cls, linear: torch.nn.Linear, mask, activation: str = "none") -> "SparseLinearQ":
+        dev = linear.weight.device.index if linear.weight.is_cuda else None
+        codes, scale = quantize_rows(linear.weight, mask)
+        return cls(codes, mask, scale, linear.bias, activation, dev)
+
+    def forward(self, x: Tokens, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        x, x_scale = x if isinstance(x, tuple) else (x, None)
+        lead = x.shape[:-1]
+        x2 = _rows_of(x, self.in_features) if x_scale is None else x
+        N = x2.shape[0]
+        if N == 0:
+            return x.new_empty((*lead, self.out_features), dtype=torch.float16)
+        r2 = None if residual is None else _rows_of(residual, self.out_features)
+        y = _call(sparse_linear_q, _linear_q, x2, x_scale, self.matrix.handle, self.out_features, self.bias, r2,
+                  usp.ACTIVATIONS[self.activation], self.workspace(N))
+        return y.reshape(*lead, self.out_features)
+
+
+class SparseExperts(SparseLinear):
+    """A linear layer with a pruned weight for each expert, on rows that are sorted by expert.
+
+    weights: E tensors [out_features, in_features], fp16, or int8 with ``scales`` (E fp32 vectors [out_features]);
+    masks: E arrays of that shape; bias: [E, out_features] or None; activation as SparseLinear."""
+
+    def __init__(self, weights, masks, scales=None, bias: Optional[torch.Tensor] = None, activation: str = "none",
+                 device: Optional[int] = None):
+        torch.nn.Module.__init__(self)
+        if activation not in usp.ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(usp.ACTIVATIONS)}")
+        if len(masks) != len(weights) or (scales is not None and len(scales) != len(weights)):
+            raise ValueError("weights, masks and scales must have one entry per expert")
+        if bias is not None and tuple(bias.shape) != (len(weights), weights[0].shape[0]):
+            raise ValueError("bias must be [experts, out_features]")
+        dev = torch.cuda.current_device() if device is None else int(device)
+        experts = []
+        for e, w in enumerate(weights):
+            m = masks[e].detach().cpu().numpy() if isinstance(masks[e], torch.Tensor) else np.asarray(masks[e])
+            m = np.ascontiguousarray(m != 0)
+            if scales is None:
+                w16 = w.detach().to(torch.float16).cpu().contiguous().numpy().view(np.uint16)
+                experts.append(usp.SparseMatrix(w16, m, dev))
+            else:
+                if w.dtype != torch.int8:
+                    raise TypeError("weights with scales must be int8 (quantize_rows makes them from float weights)")
+                experts.append(usp.SparseMatrixQ(w.detach().cpu().contiguous().numpy(), m,
+                                                 scales[e].detach().float().cpu().numpy(), dev))
+        self.matrix = usp.ExpertGroup(experts)
+        self.eight_bit = scales is not None
+        self._set_up(weights[0].shape, bias, activation, dev)
+
+    @classmethod
+    def from_linear(cls, linear, mask, activation: str = "none"):
+        raise TypeError("SparseExperts is made from the experts' weights")
+
+    def forward(self, x: Tokens, offsets: torch.Tensor, rows: Optional[torch.Tensor] = None,
+                row_weight: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x: [*, in_features] fp16 (or 8-bit tokens and scales, for 8-bit experts); offsets: int32 [E + 1] on the
+        GPU; rows: int32 [T], x's row for each row of the result (default: its own); row_weight: fp32 [T]. Rows
+        outside the offsets' range are zeros."""
+        x, x_scale = x if isinstance(x, tuple) else (x, None)
+        if x_scale is not None and not self.eight_bit:
+            raise TypeError("8-bit tokens need 8-bit experts")
+        if offsets.shape[0] != len(self.matrix.experts) + 1:
+            raise ValueError("offsets must have one entry more than there are experts")
+        x2 = _rows_of(x, self.in_features) if x_scale is None else x
+        T = x2.shape[0] if rows is None else rows.shape[0]
+        if T == 0 or x2.shape[0] == 0:
+            return x2.new_zeros((T, self.out_features), dtype=torch.float16)
+        return _call(sparse_experts, _experts, x2, x_scale, offsets, rows, row_weight, self.matrix.handle,
+                     self.out_features, self.eight_bit, self.bias, usp.ACTIVATIONS[self.activation], self.workspace(T))
+
+    def extra_repr(self) -> str:
+        return (f"experts={len(self.matrix.experts)}, in_features={self.in_features}, "
+                f"out_features={self.out_features}, eight_bit={self.eight_bit}, bias={self.bias is not None}, "
+                f"activation={self.activation}")
+
+
+class BlockNorm(torch.nn.Module):
+    """The norms around a block: ``r = residual + scale * act(gate) * post(y)`` and ``h = pre(r)``.
+
+    post, pre: "none", "rms" or "layer"; weights and biases are fp16 buffers of ``features`` entries (ones and zeros
+    until loaded; biases for "layer" only); gate_activation: "none", "sigmoid", "tanh" or "silu"."""
+
+    def __init__(self, features: int, post: str = "none", pre: str = "rms", scale: float = 1.0, eps: float = 1e-5,
+                 gate_activation: str = "none", device=None):
+        super().__init__()
+        if post not in usp.NORMS or pre not in usp.NORMS:
+            raise ValueError(f"post and pre must be one of {sorted(usp.NORMS)}")
+        if gate_activation not in usp.GATES:
+            raise ValueError(f"gate_activation must be one of {sorted(usp.GATES)}")
+        self.features, self.post, self.pre = features, post, pre
+        self.scale, self.eps, self.gate_activation = scale, eps, gate_activation
+        dev = "cuda" if device is None else f"cuda:{device}" if isinstance(device, int) else device
+        for side, kind in (("post", post), ("pre", pre)):
+            make = lambda on, fill: torch.full((features,), fill, dtype=torch.float16, device=dev) if on else None  # noqa: E731
+            self.register_buffer(side + "_weight", make(kind != "none", 1.0))
+            self.register_buffer(side + "_bias", make(kind == "layer", 0.0))
+
+    def forward(self, residual: torch.Tensor, y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                quantize: bool = False):
+        """(r, h): both as residual, or with quantize h as the pair of int8 tokens [N, features] and scales [N].
+        Without y (the first block's norm) r is residual and post is not applied."""
+        shape = residual.shape
+        r2 = _rows_of(residual, self.features)
+        y2 = None if y is None else _rows_of(y, self.features)
+        g2 = gate if gate is None or gate.dim() == 1 else _rows_of(gate, self.features)
+        if r2.shape[0] == 0:
+            h = (r2.to(torch.int8), r2.new_empty(0, dtype=torch.float32)) if quantize else r2.reshape(shape)
+            return r2.reshape(shape), h
+        r, h, h_scale = _call(block_norm, _block_norm, r2, y2, g2, self.scale, "none" if y is None else self.post,
+                              self.post_weight, self.post_bias, self.pre, self.pre_weight, self.pre_bias, self.eps,
+                              self.gate_activation, quantize)
+        return r.reshape(shape), (h, h_scale) if quantize else h.reshape(shape)
+
+    def extra_repr(self) -> str:
+        return (f"{self.features}, post={self.post}, pre={self.pre}, scale={self.scale}, eps={self.eps}, "
+                f"gate_activation={self.gate_activation}")

@@ -20,11 +20,19 @@ USP_OK = 0
 _STATUS = {0: "USP_OK", 1: "USP_ERR_INVALID_ARG", 2: "USP_ERR_UNSUPPORTED", 3: "USP_ERR_OOM",
            4: "USP_ERR_HIP", 5: "USP_ERR_INTERNAL"}
 
-EXPORTED = ("usp_encode", "usp_workspace_size", "usp_spmm", "usp_spmm_ex", "usp_spmm_noalloc", "usp_plan",
+EXPORTED = ("usp_encode_q", "usp_decode_q", "usp_quantize", "usp_spmm_q", "usp_group_create", "usp_group_free",
+            "usp_group_workspace_size", "usp_spmm_grouped", "usp_norm", "usp_encode", "usp_workspace_size", "usp_spmm", "usp_spmm_ex", "usp_spmm_noalloc", "usp_plan",
             "usp_densify", "usp_decode", "usp_info", "usp_free", "usp_last_error")
 
 # Bytes of the per-GPU device scratch usp_spmm_noalloc uses (USP_NOALLOC_SCRATCH_BYTES).
 NOALLOC_SCRATCH_BYTES = 32 << 20
+
+# Most columns of an 8-bit weight and of a group's experts (USP_MAX_K_Q).
+MAX_K_Q = 129024
+
+# usp_norm_kind and usp_gate_activation
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+GATES = {"none": 0, "sigmoid": 1, "tanh": 2, "silu": 3}
 
 # usp_activation
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu_tanh": 2, "silu": 3}
@@ -41,6 +49,14 @@ class usp_info_t(ctypes.Structure):
                 ("device_bytes", ctypes.c_size_t), ("table_bytes", ctypes.c_size_t),
                 ("format_version", ctypes.c_int32), ("tile_rows", ctypes.c_int32),
                 ("tile_k", ctypes.c_int32), ("device", ctypes.c_int32)]
+
+
+class usp_norm_args(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_void_p) for f in ("residual", "y", "gate", "post_weight", "post_bias", "pre_weight",
+                                                "pre_bias", "residual_out", "out", "out_q", "out_scale")] +
+                [(f, ctypes.c_int64) for f in ("ld_residual", "ld_y", "ld_gate", "ld_residual_out", "ld_out", "ld_out_q")] +
+                [("scale", ctypes.c_float), ("eps", ctypes.c_float), ("post_kind", ctypes.c_int),
+                 ("pre_kind", ctypes.c_int), ("gate_activation", ctypes.c_int)])
 
 
 _lib = None
@@ -77,6 +93,19 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.usp_info.restype = st
     lib.usp_free.argtypes = [p]
     lib.usp_free.restype = st
+    lib.usp_encode_q.argtypes = [p, i64, p, i64, p, i64, i64, ctypes.c_int, ctypes.POINTER(p)]
+    lib.usp_decode_q.argtypes = [p, p, p, p]
+    lib.usp_quantize.argtypes = [p, i64, i64, i64, p, i64, p, ctypes.c_int, p]
+    lib.usp_spmm_q.argtypes = [p, p, i64, p, p, i64, i64, p, p, i64, ctypes.c_int, p, sz, p]
+    lib.usp_group_create.argtypes = [ctypes.POINTER(p), i64, ctypes.POINTER(p)]
+    lib.usp_group_free.argtypes = [p]
+    lib.usp_spmm_grouped.argtypes = [p, p, i64, i64, p, p, p, i64, p, i64, i64, p, i64, p, ctypes.c_int, p, sz, p]
+    lib.usp_norm.argtypes = [ctypes.POINTER(usp_norm_args), i64, i64, ctypes.c_int, p]
+    for name in ("usp_encode_q", "usp_decode_q", "usp_quantize", "usp_spmm_q", "usp_group_create", "usp_group_free",
+                 "usp_spmm_grouped", "usp_norm"):
+        getattr(lib, name).restype = st
+    lib.usp_group_workspace_size.argtypes = [p, i64]
+    lib.usp_group_workspace_size.restype = sz
     lib.usp_last_error.argtypes = []
     lib.usp_last_error.restype = ctypes.c_char_p
     if path == LIB_PATH:
@@ -233,11 +262,198 @@ def usp_free(handle: int) -> None:
     _check(load_library().usp_free(handle))
 
 
+def usp_encode_q(W: np.ndarray, mask: np.ndarray, scale: np.ndarray, device: int = 0) -> int:
+    """W: (M, K) int8; mask: (M, K), nonzero = kept; scale: (M,) float32, one per row."""
+    W = np.ascontiguousarray(W)
+    if W.dtype != np.int8 or W.ndim != 2:
+        raise TypeError("W must be a 2-D int8 array")
+    mask = np.ascontiguousarray(mask)
+    if mask.dtype == np.bool_:
+        mask = mask.view(np.uint8)
+    if mask.dtype != np.uint8 or mask.shape != W.shape:
+        raise TypeError("mask must be a uint8/bool array of W's shape")
+    scale = np.ascontiguousarray(scale)
+    if scale.dtype != np.float32 or scale.shape != W.shape[:1]:
+        raise TypeError("scale must be a float32 array of one value per row of W")
+    M, K = W.shape
+    h = ctypes.c_void_p()
+    _check(load_library().usp_encode_q(W.ctypes.data, K, mask.ctypes.data, K, scale.ctypes.data, M, K, device,
+                                       ctypes.byref(h)))
+    return h.value
+
+
+def usp_decode_q(handle: int):
+    info = usp_info(handle)
+    M, K = info["M"], info["K"]
+    W, mask, scale = np.empty((M, K), np.int8), np.empty((M, K), np.uint8), np.empty(M, np.float32)
+    _check(load_library().usp_decode_q(handle, W.ctypes.data, mask.ctypes.data, scale.ctypes.data))
+    return W, mask, scale
+
+
+def _matrix_ptr(t: torch.Tensor, dtype: torch.dtype, shape, device: torch.device, name: str) -> int:
+    """The address of a 2-D operand after its checks."""
+    if t.dtype != dtype or t.dim() != 2 or t.stride(1) != 1 and t.shape[1] > 1:
+        raise TypeError(f"{name} must be a 2-D {dtype} tensor with unit inner stride")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _vector_ptr(t: torch.Tensor | None, dtype: torch.dtype, n: int, device: torch.device, name: str) -> int | None:
+    """The address of a contiguous vector of n values after its checks; None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or t.stride(0) != 1 and n > 1:
+        raise TypeError(f"{name} must be a contiguous {dtype} vector of {n} values")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    return t.data_ptr()
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Row stride of a 2-D operand: with one row its stride is not looked at."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _stream_of(stream, device: torch.device) -> int:
+    """The stream of a call on `device`: its current one, unless one is given."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    return _stream_handle(stream)
+
+
+def _workspace(ws: torch.Tensor | None):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def _cuda(t: torch.Tensor, name: str) -> torch.device:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a GPU")
+    return t.device
+
+
+def usp_quantize(X: torch.Tensor, Xq: torch.Tensor, x_scale: torch.Tensor, stream=None) -> None:
+    """Tokens in 8 bits: X [N, K] fp16 into Xq [N, K] int8 and x_scale [N] fp32."""
+    dev = _cuda(X, "X")
+    N, K = X.shape
+    _check(load_library().usp_quantize(_matrix_ptr(X, torch.float16, X.shape, dev, "X"), _ld(X), N, K,
+                                       _matrix_ptr(Xq, torch.int8, X.shape, dev, "Xq"), _ld(Xq),
+                                       _vector_ptr(x_scale, torch.float32, N, dev, "x_scale"), dev.index,
+                                       _stream_of(stream, dev)))
+
+
+def usp_spmm_q(handle: int, Xq: torch.Tensor, x_scale: torch.Tensor, Y: torch.Tensor,
+               workspace: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+               residual: torch.Tensor | None = None, activation: str | int = "none", stream=None) -> None:
+    """Y = act(W X + bias) + residual with 8-bit weights and tokens (Xq [N, K] int8, x_scale [N]
+    fp32; Y, bias, residual as usp_spmm_ex)."""
+    dev = _cuda(Xq, "Xq")
+    N, M = Y.shape
+    act = ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
+    r_ptr, ldr = None, 0
+    if residual is not None:
+        r_ptr, ldr = _matrix_ptr(residual, torch.float16, Y.shape, dev, "residual"), _ld(residual)
+    ws_ptr, ws_bytes = _workspace(workspace)
+    _check(load_library().usp_spmm_q(
+        handle, _matrix_ptr(Xq, torch.int8, (N, Xq.shape[1]), dev, "Xq"), _ld(Xq),
+        _vector_ptr(x_scale, torch.float32, N, dev, "x_scale"), _matrix_ptr(Y, torch.float16, Y.shape, dev, "Y"), _ld(Y),
+        N, _vector_ptr(bias, torch.float16, M, dev, "bias"), r_ptr, ldr, act, ws_ptr, ws_bytes, _stream_of(stream, dev)))
+
+
+def usp_group_create(handles) -> int:
+    arr = (ctypes.c_void_p * len(handles))(*handles)
+    g = ctypes.c_void_p()
+    _check(load_library().usp_group_create(arr, len(handles), ctypes.byref(g)))
+    return g.value
+
+
+def usp_group_free(group: int) -> None:
+    _check(load_library().usp_group_free(group))
+
+
+def usp_group_workspace_size(group: int, T: int) -> int:
+    return int(load_library().usp_group_workspace_size(group, T))
+
+
+def usp_spmm_grouped(group: int, X: torch.Tensor, offsets: torch.Tensor, Y: torch.Tensor,
+                     workspace: torch.Tensor | None = None, x_scale: torch.Tensor | None = None,
+                     rows: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                     row_weight: torch.Tensor | None = None, activation: str | int = "none", stream=None) -> None:
+    """Y[t] = row_weight[t] * act(W_e X[rows[t]] + bias[e]) for the rows offsets[e] <= t < offsets[e + 1] of
+    expert e. X [*, K] fp16, or int8 with x_scale; offsets [E + 1] and rows [T] int32; bias [E, M] fp16;
+    row_weight [T] fp32; Y [T, M] fp16."""
+    dev = _cuda(X, "X")
+    T, M = Y.shape
+    act = ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
+    x_type = torch.float16 if x_scale is None else torch.int8
+    E = offsets.shape[0] - 1
+    b_ptr, ldb = None, 0
+    if bias is not None:
+        b_ptr, ldb = _matrix_ptr(bias, torch.float16, (E, M), dev, "bias"), _ld(bias)
+    ws_ptr, ws_bytes = _workspace(workspace)
+    _check(load_library().usp_spmm_grouped(
+        group, _matrix_ptr(X, x_type, X.shape, dev, "X"), _ld(X), X.shape[0],
+        _vector_ptr(x_scale, torch.float32, X.shape[0], dev, "x_scale"), _vector_ptr(rows, torch.int32, T, dev, "rows"),
+        _vector_ptr(offsets, torch.int32, E + 1, dev, "offsets"), E, _matrix_ptr(Y, torch.float16, Y.shape, dev, "Y"),
+        _ld(Y), T, b_ptr, ldb, _vector_ptr(row_weight, torch.float32, T, dev, "row_weight"), act, ws_ptr, ws_bytes,
+        _stream_of(stream, dev)))
+
+
+def usp_norm(residual: torch.Tensor, y: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+             scale: float = 1.0, post: str = "none", post_weight: torch.Tensor | None = None,
+             post_bias: torch.Tensor | None = None, pre: str = "none", pre_weight: torch.Tensor | None = None,
+             pre_bias: torch.Tensor | None = None, eps: float = 1e-5, gate_activation: str = "none",
+             residual_out: torch.Tensor | None = None, out: torch.Tensor | None = None,
+             out_q: torch.Tensor | None = None, out_scale: torch.Tensor | None = None, stream=None) -> None:
+    """r = residual + scale * act(gate) * post(y) into residual_out and h = pre(r) into out (fp16) and / or
+    out_q, out_scale (8-bit tokens). All [N, K] fp16 but out_q (int8); gate [N, K], or [K] for all tokens; weights
+    and biases [K]; out_scale [N] fp32. residual_out may be residual or y, out may be y."""
+    dev = _cuda(residual, "residual")
+    N, K = residual.shape
+    f16 = torch.float16
+    a = usp_norm_args(scale=scale, eps=eps, post_kind=NORMS[post], pre_kind=NORMS[pre],
+                      gate_activation=GATES[gate_activation])
+    a.residual, a.ld_residual = _matrix_ptr(residual, f16, residual.shape, dev, "residual"), _ld(residual)
+    if y is not None:
+        a.y, a.ld_y = _matrix_ptr(y, f16, residual.shape, dev, "y"), _ld(y)
+    if gate is not None:
+        if gate.dim() == 1:
+            a.gate = _vector_ptr(gate, f16, K, dev, "gate")
+        else:
+            a.gate, a.ld_gate = _matrix_ptr(gate, f16, residual.shape, dev, "gate"), _ld(gate)
+    a.post_weight = _vector_ptr(post_weight, f16, K, dev, "post_weight")
+    a.post_bias = _vector_ptr(post_bias, f16, K, dev, "post_bias")
+    a.pre_weight = _vector_ptr(pre_weight, f16, K, dev, "pre_weight")
+    a.pre_bias = _vector_ptr(pre_bias, f16, K, dev, "pre_bias")
+    if residual_out is not None:
+        a.residual_out = _matrix_ptr(residual_out, f16, residual.shape, dev, "residual_out")
+        a.ld_residual_out = _ld(residual_out)
+    if out is not None:
+        a.out, a.ld_out = _matrix_ptr(out, f16, residual.shape, dev, "out"), _ld(out)
+    if out_q is not None:
+        a.out_q, a.ld_out_q = _matrix_ptr(out_q, torch.int8, residual.shape, dev, "out_q"), _ld(out_q)
+    a.out_scale = _vector_ptr(out_scale, torch.float32, N, dev, "out_scale")
+    _check(load_library().usp_norm(ctypes.byref(a), N, K, dev.index, _stream_of(stream, dev)))
+
+
+def _zeros(n: int, device: int, stream) -> torch.Tensor | None:
+    """n zero bytes, allocated and cleared on `stream`; None for none."""
+    if n == 0:
+        return None
+    with torch.cuda.stream(_torch_stream(stream)):
+        return torch.zeros(n, dtype=torch.uint8, device=f"cuda:{device}")
+
+
 class SparseMatrix:
     """Owns one encoded weight matrix (a usp_matrix handle)."""
 
     def __init__(self, W: np.ndarray, mask: np.ndarray, device: int = 0):
-        self.handle = usp_encode(W, mask, device)
+        self._own(usp_encode(W, mask, device), device)
+
+    def _own(self, handle: int, device: int) -> None:
+        self.handle = handle
         info = usp_info(self.handle)
         self.M, self.K, self.nnz = info["M"], info["K"], info["nnz"]
         self.device = device
@@ -252,11 +468,7 @@ class SparseMatrix:
     def make_workspace(self, N: int, stream=None) -> torch.Tensor | None:
         """A zero-filled workspace for N tokens, allocated and cleared on `stream` (default: the
         current stream), so calls enqueued on that stream are ordered after the clear."""
-        n = self.workspace_size(N)
-        if n == 0:
-            return None
-        with torch.cuda.stream(_torch_stream(stream)):
-            return torch.zeros(n, dtype=torch.uint8, device=f"cuda:{self.device}")  # zeroed once
+        return _zeros(self.workspace_size(N), self.device, stream)
 
     def spmm(self, X: torch.Tensor, Y: torch.Tensor | None = None, workspace=None, stream=None,
              bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
@@ -292,6 +504,73 @@ class SparseMatrix:
     def free(self) -> None:
         if self.handle:
             usp_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+class SparseMatrixQ(SparseMatrix):
+    """Owns one encoded weight matrix of 8-bit values with a scale per row."""
+
+    def __init__(self, W: np.ndarray, mask: np.ndarray, scale: np.ndarray, device: int = 0):
+        self._own(usp_encode_q(W, mask, scale, device), device)
+
+    def spmm(self, Xq: torch.Tensor, x_scale: torch.Tensor, Y: torch.Tensor | None = None, workspace=None, stream=None,
+             bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+             activation: str | int = "none") -> torch.Tensor:
+        """act(W X + bias) + residual of 8-bit tokens (usp_quantize); what the call creates is allocated as in
+        SparseMatrix.spmm."""
+        N = Xq.shape[0]
+        if Y is None or workspace is None:
+            with torch.cuda.stream(_torch_stream(stream)):
+                if Y is None:
+                    Y = torch.empty((N, self.M), dtype=torch.float16, device=Xq.device)
+                if workspace is None:
+                    workspace = self.make_workspace(N)
+        usp_spmm_q(self.handle, Xq, x_scale, Y, workspace, bias, residual, activation, stream)
+        return Y
+
+    def decode(self):
+        return usp_decode_q(self.handle)
+
+
+class ExpertGroup:
+    """Encoded experts of one shape and value type (a usp_group handle); keeps them alive."""
+
+    def __init__(self, experts):
+        self.experts = list(experts)
+        self.handle = None
+        self.handle = usp_group_create([m.handle for m in self.experts])
+        self.M, self.K, self.device = self.experts[0].M, self.experts[0].K, self.experts[0].device
+
+    def workspace_size(self, T: int) -> int:
+        return usp_group_workspace_size(self.handle, T)
+
+    def make_workspace(self, T: int, stream=None) -> torch.Tensor | None:
+        """A workspace for T rows, allocated and cleared on `stream` (default: the current one)."""
+        return _zeros(self.workspace_size(T), self.device, stream)
+
+    def spmm(self, X: torch.Tensor, offsets: torch.Tensor, T: int | None = None, Y: torch.Tensor | None = None,
+             workspace=None, stream=None, **operands) -> torch.Tensor:
+        """usp_spmm_grouped into Y, or into a new tensor of T rows (default: those of `rows`, or of X), of which
+        the rows that no expert has are zeros."""
+        with torch.cuda.stream(_torch_stream(stream)):
+            if Y is None:
+                rows = operands.get("rows")
+                T = (X if rows is None else rows).shape[0] if T is None else T
+                Y = torch.zeros((T, self.M), dtype=torch.float16, device=X.device)
+            if workspace is None:
+                workspace = self.make_workspace(Y.shape[0])
+        usp_spmm_grouped(self.handle, X, offsets, Y, workspace, stream=stream, **operands)
+        return Y
+
+    def free(self) -> None:
+        if self.handle:
+            usp_group_free(self.handle)
             self.handle = None
 
     def __del__(self):
