@@ -280,6 +280,9 @@ usp_status usp_group_free(usp_group *G);
  * valid group or T). */
 size_t usp_group_workspace_size(const usp_group *G, int64_t T);
 
+/* usp_group_plan -- which kernel usp_spmm_grouped runs for T >= 1 rows when X is dword-aligned, as usp_plan. */
+usp_status usp_group_plan(const usp_group *G, int64_t T, char *buf, size_t len);
+
 /*
  * usp_spmm_grouped -- for each expert e and each row t of its range offsets[e] <= t < offsets[e + 1]:
  *     Y[t] = row_weight[t] * act(W_e X[rows[t]] + bias[e])

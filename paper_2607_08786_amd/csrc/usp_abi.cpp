@@ -262,6 +262,13 @@ size_t usp_workspace_size(const usp_matrix *A, int64_t N) {
     return usp::spmm_workspace_bytes(A, N);
 }
 
+static usp_status copy_text(const std::string &d, char *buf, size_t len) {
+    const size_t n = d.size() < len - 1 ? d.size() : len - 1;
+    std::memcpy(buf, d.data(), n);
+    buf[n] = '\0';
+    return USP_OK;
+}
+
 usp_status usp_plan(const usp_matrix *A, int64_t N, char *buf, size_t len) {
     if (!alive(A)) return usp::fail(USP_ERR_INVALID_ARG, "usp_plan: invalid or freed handle");
     if (N < 1 || !buf || len == 0) return usp::fail(USP_ERR_INVALID_ARG, "usp_plan: need N >= 1 and a buffer");
@@ -269,10 +276,7 @@ usp_status usp_plan(const usp_matrix *A, int64_t N, char *buf, size_t len) {
     if (!g.ok) return usp::fail(USP_ERR_HIP, "usp_plan: cannot select device");
     const std::string d =
         A->value_bytes == 1 ? usp::describe_product(usp::product_shape(A), N) : usp::describe_plan(A, N);
-    const size_t n = d.size() < len - 1 ? d.size() : len - 1;
-    std::memcpy(buf, d.data(), n);
-    buf[n] = '\0';
-    return USP_OK;
+    return copy_text(d, buf, len);
 }
 
 // The text of usp_spmm's refusal of a handle of the other value type, or null.
@@ -561,6 +565,12 @@ usp_status usp_group_free(usp_group *G) {
 size_t usp_group_workspace_size(const usp_group *G, int64_t T) {
     if (!alive(G) || T < 1) return 0;
     return usp::product_workspace_bytes(usp::product_shape(G), T);
+}
+
+usp_status usp_group_plan(const usp_group *G, int64_t T, char *buf, size_t len) {
+    if (!alive(G)) return usp::fail(USP_ERR_INVALID_ARG, "usp_group_plan: invalid or freed group");
+    if (T < 1 || !buf || len == 0) return usp::fail(USP_ERR_INVALID_ARG, "usp_group_plan: need T >= 1 and a buffer");
+    return copy_text(usp::describe_product(usp::product_shape(G), T), buf, len);
 }
 
 usp_status usp_spmm_grouped(const usp_group *G, const void *X, int64_t ldx, int64_t x_rows, const float *x_scale,

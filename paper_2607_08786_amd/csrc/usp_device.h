@@ -209,9 +209,7 @@ struct RecState {
 };
 
 // start: LDS byte offset of the record's values from the region that read_step
-// is given (a multiple of 4). VB: bytes of a value. For 8-bit values s is the mask
-// byte (usp_format.h) and the selector table's entries take 4 bytes.
-template <int VB = 2>
+// is given (a multiple of 4).
 __device__ inline RecState rec_state(uint2 msk, uint32_t start = 0) {
     const uint32_t nx = nibble_popcounts(msk.x), ny = nibble_popcounts(msk.y);
     const uint32_t w[4] = {nx & 0x0F0F0F0Fu, (nx >> 4) & 0x0F0F0F0Fu, ny & 0x0F0F0F0Fu, (ny >> 4) & 0x0F0F0F0Fu};
@@ -235,14 +233,12 @@ __device__ inline RecState rec_state(uint2 msk, uint32_t start = 0) {
     for (int st = 0; st < kSteps; ++st) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            o.base2[2 * st + h] = start + VB * run;
+            o.base2[2 * st + h] = start + 2 * run;
             run += tot[2 * (st >> 2) + h][st & 3];
         }
     }
-    constexpr int up = VB == 2 ? 3 : 2;
-    constexpr uint32_t index = 0x0F0F0F0Fu << up;
-    uint32_t t0 = (msk.x << up) & index, t1 = (msk.x >> (4 - up)) & index;
-    uint32_t t2 = (msk.y << up) & index, t3 = (msk.y >> (4 - up)) & index;
+    uint32_t t0 = (msk.x << 3) & 0x78787878u, t1 = (msk.x >> 1) & 0x78787878u;
+    uint32_t t2 = (msk.y << 3) & 0x78787878u, t3 = (msk.y >> 1) & 0x78787878u;
     // Opaque to the optimizer: a step's selector index is then one bit-field
     // extract of these words instead of a shift and a mask of the raw mask.
     asm("" : "+v"(t0), "+v"(t1), "+v"(t2), "+v"(t3));
@@ -274,52 +270,6 @@ __device__ inline half8 finish_step(const StepWords &w) {
 
 __device__ inline half8 decode_step(lds_u32 *region, const uint8_t *lut, const RecState &rs, int s) {
     return finish_step(read_step(region, lut, rs, s));
-}
-
-// The same for records of 8-bit values. A step is 64 columns, a lane's 16 of them
-// four nibbles: blocks 4 s .. 4 s + 3. A nibble's up to 4 bytes lie in two dwords
-// whatever its alignment, one funnel shift aligns them and one byte permute places
-// them (or zeros): about 6 VALU and 12 LDS bytes per 4 positions, where fp16 takes
-// 8 and 20.
-__device__ inline uint32_t nibble_selector_q(uint32_t n) {
-    uint32_t sel = 0x0c0c0c0cu, r = 0;
-    for (int j = 0; j < 4; ++j)
-        if (n & (1u << j)) sel = (sel & ~(0xFFu << (8 * j))) | (r++ << (8 * j));
-    return sel;
-}
-
-struct StepWordsQ {
-    uint32_t e[8];
-    uint32_t sel[4];
-    uint32_t hb[4];
-};
-
-__device__ inline StepWordsQ read_step_q(lds_u32 *region, const uint8_t *lut, const RecState &rs, int s) {
-    typedef const __attribute__((address_space(3))) uint8_t lds_u8;
-    typedef volatile const __attribute__((address_space(3))) uint32_t lds_vu32;
-    StepWordsQ w;
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        const int b = 4 * s + h, y = b / 2;  // block; mask byte
-        const int q = 2 * (y / 4) + b % 2, f = 8 * (y % 4);
-        w.hb[h] = ((rs.excl[q] >> f) & 0xFFu) + rs.base2[b];
-        lds_vu32 *d = (lds_vu32 *)((lds_u8 *)region + (w.hb[h] & ~3u));
-        w.e[2 * h] = d[0];
-        w.e[2 * h + 1] = d[1];
-        w.sel[h] = *reinterpret_cast<const uint32_t *>(lut + ((rs.t[q] >> f) & 0xFFu));
-    }
-    return w;
-}
-
-// The A operand (16 bytes) of a step from its LDS words.
-__device__ inline v4u32 finish_step_q(const StepWordsQ &w) {
-    v4u32 a;
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        const uint32_t x = __builtin_amdgcn_alignbyte(w.e[2 * h + 1], w.e[2 * h], w.hb[h]);  // uses hb & 3
-        a[h] = __builtin_amdgcn_perm(0u, x, w.sel[h]);
-    }
-    return a;
 }
 
 // X[0 .. 7] of a token row at any 2-byte alignment, zeros from element `left` on

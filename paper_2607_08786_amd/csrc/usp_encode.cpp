@@ -50,7 +50,9 @@ inline uint8_t nonzero_bits(const uint8_t *p, int64_t n) {
 }
 
 // Records of fp16 values (V = uint16_t) and of 8-bit values (V = int8_t) differ in
-// the columns of a lane's mask byte y and in the size of a value, nothing else.
+// the columns of a lane's mask byte y, in the size of a value, and in the blocks:
+// of a nibble (4 bits of mask), or of a whole mask byte with the blocks' starts
+// between the mask and the values.
 template <class V>
 inline int byte_col(int g, int y) {
     return sizeof(V) == 2 ? tile_col(g, y, 0) : tile_col_q(g, y, 0);
@@ -67,6 +69,13 @@ inline void place8(int c, int &g, int &y) {
         y = 2 * (c / 8) + c % 2;
     }
 }
+
+template <class V>
+constexpr int kBlockBits = sizeof(V) == 2 ? 4 : 8;
+template <class V>
+constexpr int kHeadBytes = kMaskBytes + (sizeof(V) == 2 ? 0 : kStartBytesQ);
+// Block y's place among the starts.
+inline int start_place(int y) { return (y & 4) | (y & 1) << 1 | (y & 2) >> 1; }
 
 template <class V>
 void encode_records(const V *W, int64_t ldw, const uint8_t *mask, int64_t ldm, int64_t M, int64_t K,
@@ -122,7 +131,8 @@ void encode_records(const V *W, int64_t ldw, const uint8_t *mask, int64_t ldm, i
     int64_t total = 0, nnz = 0, max_chunks = 0;
     for (int64_t t = 0; t < T; ++t) {
         out.off[t] = (uint32_t)total;
-        const int64_t chunks = ceil_div((int64_t)sizeof(V) * tile_nnz[t], 16);
+        const int64_t chunks =
+            ceil_div((int64_t)sizeof(V) * tile_nnz[t] + kHeadBytes<V> - kMaskBytes, 16);
         total += kMaskChunks + chunks;
         max_chunks = std::max(max_chunks, chunks);
         nnz += tile_nnz[t];
@@ -142,35 +152,35 @@ void encode_records(const V *W, int64_t ldw, const uint8_t *mask, int64_t ldm, i
             const uint8_t *m = masks.data() + (size_t)t * kMaskBytes;
             const bool inside = (rb + 1) * kTileRows <= M && (kt + 1) * kTileK <= K;
             int64_t v = 0;
+            uint16_t starts[kStartBytesQ / 2] = {};
+            constexpr int B = kBlockBits<V>;
             for (int y = 0; y < kMaskBytes / kLanes; ++y) {
-                // Values of mask byte y: the block of its low nibble, then that of its high
-                // nibble; within a block lane 0's values first, in column order.
-                for (int h = 0; h < 2; ++h) {
+                starts[start_place(y)] = (uint16_t)(kHeadBytes<V> + v * (int64_t)sizeof(V));
+                // Values of mask byte y: of its low and then its high nibble, or of all of it;
+                // within a block lane 0's values first, in column order.
+                for (int h = 0; h < 8 / B; ++h) {
                     for (int l = 0; l < kLanes; ++l) {
                         const int r = l % kTileRows, g = l / kTileRows;
-                        const uint32_t n = (uint32_t)(m[8 * l + y] >> (4 * h)) & 15u;
-                        const V *w = W + (rb * kTileRows + r) * ldw + kt * kTileK + byte_col<V>(g, y) + 4 * h;
+                        const uint32_t n = (uint32_t)(m[8 * l + y] >> (B * h)) & ((1u << B) - 1);
+                        const V *w = W + (rb * kTileRows + r) * ldw + kt * kTileK + byte_col<V>(g, y) + B * h;
                         if (inside) {
-                            vals[v] = w[0];
-                            v += n & 1;
-                            vals[v] = w[1];
-                            v += (n >> 1) & 1;
-                            vals[v] = w[2];
-                            v += (n >> 2) & 1;
-                            vals[v] = w[3];
-                            v += n >> 3;
+                            for (int j = 0; j < B; ++j) {
+                                vals[v] = w[j];
+                                v += (n >> j) & 1;
+                            }
                         } else {  // positions outside W are never kept
-                            for (int j = 0; j < 4; ++j)
+                            for (int j = 0; j < B; ++j)
                                 if (n & (1u << j)) vals[v++] = w[j];
                         }
                     }
                 }
             }
             uint8_t *rec = out.stream.data() + (size_t)out.off[t] * 16;
-            const size_t bytes = (size_t)v * sizeof(V), room = (size_t)(out.off[t + 1] - out.off[t]) * 16 - kMaskBytes;
+            const size_t bytes = (size_t)v * sizeof(V), room = (size_t)(out.off[t + 1] - out.off[t]) * 16 - kHeadBytes<V>;
             std::memcpy(rec, m, kMaskBytes);
-            std::memcpy(rec + kMaskBytes, vals, bytes);
-            std::memset(rec + kMaskBytes + bytes, 0, room - bytes);
+            if (sizeof(V) == 1) std::memcpy(rec + kMaskBytes, starts, kStartBytesQ);
+            std::memcpy(rec + kHeadBytes<V>, vals, bytes);
+            std::memset(rec + kHeadBytes<V> + bytes, 0, room - bytes);
         }
     });
 }
@@ -188,16 +198,17 @@ bool decode_records(const HostEncoding &enc, V *W_out, uint8_t *mask_out) {
         for (int64_t kt = 0; kt < enc.KT && ok; ++kt) {
             const int64_t t = rb * enc.KT + kt;
             const uint8_t *rec = enc.stream.data() + (size_t)enc.off[t] * 16;
-            const int64_t cap = ((int64_t)enc.off[t + 1] - enc.off[t] - kMaskChunks) * 16 / (int64_t)sizeof(V);
-            const V *vals = reinterpret_cast<const V *>(rec + kMaskBytes);
+            const int64_t cap = (((int64_t)enc.off[t + 1] - enc.off[t]) * 16 - kHeadBytes<V>) / (int64_t)sizeof(V);
+            const V *vals = reinterpret_cast<const V *>(rec + kHeadBytes<V>);
             int64_t v = 0;
-            for (int yh = 0; yh < 2 * kMaskBytes / kLanes && ok; ++yh) {
-                const int y = yh / 2, h = yh % 2;  // block (mask byte y, nibble half h)
+            constexpr int B = kBlockBits<V>;
+            for (int yh = 0; yh < kMaskBytes / kLanes * (8 / B) && ok; ++yh) {
+                const int y = yh / (8 / B), h = yh % (8 / B);  // block (mask byte y, its part h)
                 for (int l = 0; l < kLanes; ++l) {
                     const int r = l % kTileRows, g = l / kTileRows;
                     const int64_t row = rb * kTileRows + r;
                     const uint8_t b = rec[8 * l + y];
-                    for (int j = 4 * h; j < 4 * h + 4; ++j) {
+                    for (int j = B * h; j < B * h + B; ++j) {
                         if (!(b & (1u << j))) continue;
                         const int64_t col = kt * kTileK + byte_col<V>(g, y) + j;
                         if (row >= M || col >= K || v >= cap) { ok = false; break; }

@@ -2,13 +2,12 @@
 // expert share: arguments, the two value formats, and the search for a workgroup's
 // part of a ragged batch.
 #pragma once
+#include <algorithm>
+
 #include "usp_device.h"
 #include "usp_internal.h"
 
 namespace usp {
-namespace {
-
-typedef int intx4 __attribute__((ext_vector_type(4)));
 
 struct ProductArgs {
     ExpertRef one;             // the matrix, when there is no group
@@ -21,6 +20,7 @@ struct ProductArgs {
     int job0;                  // the launch's first job
     const uint8_t *X;
     int64_t ldx;               // bytes
+    const uint8_t *xp;         // X packed (pack_kernel)
     int64_t x_rows;
     const int32_t *rows;       // row of X for each row of Y, or null
     const float *xs;           // scales of 8-bit rows, or null
@@ -30,21 +30,113 @@ struct ProductArgs {
     uint16_t *Y;
     int64_t ldy;
     int N;                     // rows of Y
-    int y_vec;
+    int y_vec, y_wide;         // rows 4 (8) a multiple of 4 (8) apart may be stored as one 8-byte (16-byte) vector
     const uint16_t *bias, *res;
     int64_t ldb, ldr;
     int act, e_flags;
 };
 
+namespace {
+
+typedef int intx4 __attribute__((ext_vector_type(4)));
+
+// ---- Records of 8-bit values (usp_format.h)
+//
+// Four prefix scans over pairs of 16-bit fields give every lane the start of its
+// values in all 8 blocks, the blocks' own starts coming with the record. Per mask
+// byte (8 positions): three LDS dwords hold its up to 8 values whatever their
+// alignment, two funnel shifts align them, and two byte permutes place them (or
+// zeros) by the selectors of a table of all 256 masks. About 110 VALU and 34 LDS
+// instructions per record; with nibble blocks as in fp16 records (twice the
+// offsets, a selector of 16 entries per nibble, block sums in scalar code) it was
+// 175, 49 and 97 scalar ones, and what bounds a decode is its instructions: 70B
+// FFN at 16 tokens 32.4 us.
+
+// Selectors of mask byte n: output byte j takes the value of its rank when bit j is
+// set and zero (0x0c) otherwise.
+__device__ inline uint2 byte_selectors(uint32_t n) {
+    uint32_t sel[2] = {0x0c0c0c0cu, 0x0c0c0c0cu}, r = 0;
+    for (int j = 0; j < 8; ++j)
+        if (n & (1u << j)) sel[j / 4] = (sel[j / 4] & ~(0xFFu << (8 * (j % 4)))) | (r++ << (8 * (j % 4)));
+    return make_uint2(sel[0], sel[1]);
+}
+
+struct RecStateQ {
+    uint32_t at[4];  // LDS byte offsets of the lane's values: blocks (0, 2), (1, 3), (4, 6), (5, 7) in 16-bit halves
+    uint2 msk;
+};
+
+// start: LDS byte offset of the record from the region that read_step_q is given,
+// below 2^16 - 8192.
+__device__ inline RecStateQ rec_state_q(uint2 msk, v4u32 starts, uint32_t start) {
+    RecStateQ o;
+    o.msk = msk;
+    const uint32_t m[2] = {msk.x, msk.y};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t n = nibble_popcounts(m[i]);
+        const uint32_t b = (n + (n >> 4)) & 0x0F0F0F0Fu;
+        const uint32_t w[2] = {b & 0x00FF00FFu, (b >> 8) & 0x00FF00FFu};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t inc = wave_inclusive_scan(w[h]);
+            asm("" : "+v"(inc));  // keeps the scan's last add a DPP add
+            o.at[2 * i + h] = inc + starts[2 * i + h] + (start * 0x00010001u - w[h]);
+        }
+    }
+    return o;
+}
+
+struct StepWordsQ {
+    uint32_t e[6];
+    uint2 sel[2];
+    uint32_t hb[2];
+};
+
+// Issues the LDS reads of step s of the staged record.
+__device__ inline StepWordsQ read_step_q(lds_u32 *region, const uint8_t *lut, const RecStateQ &rs, int s) {
+    typedef const __attribute__((address_space(3))) uint8_t lds_u8;
+    typedef volatile const __attribute__((address_space(3))) uint32_t lds_vu32;
+    StepWordsQ w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int y = 2 * s + h;
+        const uint32_t at = rs.at[2 * (y / 4) + y % 2], m = y < 4 ? rs.msk.x : rs.msk.y;
+        w.hb[h] = (y & 2) ? at >> 16 : at;  // the low half's other bits are not looked at
+        lds_vu32 *d = (lds_vu32 *)((lds_u8 *)region + (w.hb[h] & 0xFFFCu));
+        w.e[3 * h] = d[0];
+        w.e[3 * h + 1] = d[1];
+        w.e[3 * h + 2] = d[2];
+        w.sel[h] = *reinterpret_cast<const uint2 *>(lut + 8 * ((m >> (8 * (y % 4))) & 0xFFu));
+    }
+    return w;
+}
+
+// The A operand (16 bytes) of a step from its LDS words.
+__device__ inline v4u32 finish_step_q(const StepWordsQ &w) {
+    v4u32 a;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t x0 = __builtin_amdgcn_alignbyte(w.e[3 * h + 1], w.e[3 * h], w.hb[h]);  // uses hb & 3
+        const uint32_t x1 = __builtin_amdgcn_alignbyte(w.e[3 * h + 2], w.e[3 * h + 1], w.hb[h]);
+        a[2 * h] = __builtin_amdgcn_perm(x1, x0, w.sel[h].x);
+        a[2 * h + 1] = __builtin_amdgcn_perm(x1, x0, w.sel[h].y);
+    }
+    return a;
+}
+
 // fp16 values: products of 16 rows x 32 columns with fp32 sums.
 struct ValuesF16 {
-    static constexpr int kBytes = 2, kStepsPerTile = kSteps, kLutBytes = 16 * 8;
+    static constexpr int kBytes = 2, kStepsPerTile = kSteps, kLutEntries = 16;
     typedef StepWords Words;
+    typedef RecState State;
     typedef floatx4 Acc;
-    __device__ static void fill_lut(uint8_t *lut, int i) {
-        reinterpret_cast<uint2 *>(lut)[i] = nibble_selectors((uint32_t)i);
+    __device__ static uint2 selectors(int i) { return nibble_selectors((uint32_t)i); }
+    // The record at `slot`, `start` bytes into the region.
+    __device__ static State state(const uint8_t *slot, int lane, uint32_t start) {
+        return rec_state(slot_mask(slot, lane), start + kMaskBytes);
     }
-    __device__ static Words read(lds_u32 *region, const uint8_t *lut, const RecState &rs, int s) {
+    __device__ static Words read(lds_u32 *region, const uint8_t *lut, const State &rs, int s) {
         return read_step(region, lut, rs, s);
     }
     __device__ static v4u32 finish(const Words &w) { return __builtin_bit_cast(v4u32, finish_step(w)); }
@@ -56,13 +148,17 @@ struct ValuesF16 {
 
 // 8-bit values: 16 rows x 64 columns with exact 32-bit integer sums.
 struct ValuesQ {
-    static constexpr int kBytes = 1, kStepsPerTile = kStepsQ, kLutBytes = 16 * 4;
+    static constexpr int kBytes = 1, kStepsPerTile = kStepsQ, kLutEntries = 256;
     typedef StepWordsQ Words;
+    typedef RecStateQ State;
     typedef intx4 Acc;
-    __device__ static void fill_lut(uint8_t *lut, int i) {
-        reinterpret_cast<uint32_t *>(lut)[i] = nibble_selector_q((uint32_t)i);
+    __device__ static uint2 selectors(int i) { return byte_selectors((uint32_t)i); }
+    __device__ static State state(const uint8_t *slot, int lane, uint32_t start) {
+        typedef const __attribute__((address_space(3))) v4u32 lds_v4;
+        const v4u32 starts = *(lds_v4 *)(const __attribute__((address_space(3))) void *)(slot + kMaskBytes);
+        return rec_state_q(slot_mask(slot, lane), starts, start);
     }
-    __device__ static Words read(lds_u32 *region, const uint8_t *lut, const RecState &rs, int s) {
+    __device__ static Words read(lds_u32 *region, const uint8_t *lut, const State &rs, int s) {
         return read_step_q(region, lut, rs, s);
     }
     __device__ static v4u32 finish(const Words &w) { return finish_step_q(w); }
@@ -72,10 +168,26 @@ struct ValuesQ {
     __device__ static floatx4 sum(Acc v) { return floatx4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]}; }
 };
 
-// A workgroup's part: row set `set` of expert e for rows [row0, row0 + n).
+// Waits until at most n loads are outstanding (they complete in order). Stated where a
+// record's transfer must have ended: the compiler's own waits for transfers into LDS
+// go by what it knows of each read, and it has left one out.
+template <int N>
+__device__ inline void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N < 63 ? N : 63) : "memory");
+}
+
+// Fills the selector table with `threads` threads.
+template <class V>
+__device__ inline void fill_lut(uint8_t *lut, int thread, int threads) {
+    for (int i = thread; i < V::kLutEntries; i += threads) reinterpret_cast<uint2 *>(lut)[i] = V::selectors(i);
+}
+
+// A workgroup's part: row set `set` of expert e for rows [row0, row0 + n), whose X
+// packed in blocks of 16 rows (pack_kernel) starts at block tb.
 struct Job {
-    int e, set, row0, n;
+    int e, set, row0, n, tb;
 };
+constexpr int kBlock = 16;  // tokens of an MFMA operand
 
 // Inclusive scans over the wavefront's lanes.
 __device__ inline int scan_max(int v, int lane) {
@@ -118,21 +230,22 @@ __device__ inline int first_row(const ProductArgs &a) {
 // An expert with n rows has ceil(n / TB) groups of at most TB rows, and sets x
 // groups jobs, the groups of a row set next to each other.
 template <int TB>
-__device__ inline bool find_job(const ProductArgs &a, int b, int lane, Job &j) {
+__device__ inline bool find_job(const ProductArgs &a, int b, int sets, int lane, Job &j) {
     if (!a.experts) {
         const int groups = (a.N + TB - 1) / TB;
         j.e = 0;
         j.set = b / groups;
         j.row0 = b % groups * TB;
         j.n = a.N - j.row0 < TB ? a.N - j.row0 : TB;
-        return j.set < a.sets;
+        j.tb = j.row0 / kBlock;
+        return j.set < sets;
     }
-    int run = first_row(a);
+    int run = first_row(a), blocks = 0;
     for (int c0 = 0; c0 < a.E; c0 += kLanes) {
         int lo, hi;
         expert_rows(a, c0, lane, run, lo, hi);
-        const int jobs = (hi - lo + TB - 1) / TB * a.sets;
-        const int end = scan_sum(jobs, lane);
+        const int jobs = (hi - lo + TB - 1) / TB * sets, mine = (hi - lo + kBlock - 1) / kBlock;
+        const int end = scan_sum(jobs, lane), tb = scan_sum(mine, lane);
         const uint64_t past = __ballot(b < end);
         if (past) {
             const int l = __builtin_ctzll(past);
@@ -141,39 +254,91 @@ __device__ inline bool find_job(const ProductArgs &a, int b, int lane, Job &j) {
             const int groups = (r1 - r0 + TB - 1) / TB;
             j.e = c0 + l;
             j.set = at / groups;
-            j.row0 = r0 + at % groups * TB;
+            const int first = at % groups * TB;
+            j.row0 = r0 + first;
             j.n = r1 - j.row0 < TB ? r1 - j.row0 : TB;
+            j.tb = blocks + __builtin_amdgcn_readlane(tb, l) - __builtin_amdgcn_readlane(mine, l) + first / kBlock;
             return true;
         }
         b -= __builtin_amdgcn_readlane(end, kLanes - 1);
+        blocks += __builtin_amdgcn_readlane(tb, kLanes - 1);
     }
     return false;
 }
 
-// The fused epilogue and store of rows m .. m + 3 of row n of Y from their sums.
-// e: the expert (its scales w_scale, its bias).
+// The job's matrix, in scalar registers: buffer resources are made of its pointers,
+// and a resource that is not known to be uniform costs a loop at every load.
+__device__ inline ExpertRef job_matrix(const ProductArgs &a, const Job &j) {
+    if (!a.experts) return a.one;
+    const uint32_t *p = reinterpret_cast<const uint32_t *>(a.experts + j.e);
+    auto word = [&](int i) -> uint64_t { return (uint32_t)__builtin_amdgcn_readfirstlane((int)p[i]); };
+    ExpertRef r;
+    r.stream = reinterpret_cast<const uint8_t *>(word(0) | word(1) << 32);
+    r.off = reinterpret_cast<const uint32_t *>(word(2) | word(3) << 32);
+    r.scale = reinterpret_cast<const float *>(word(4) | word(5) << 32);
+    return r;
+}
+
+// Scale of the 8-bit row of X that row n of Y multiplies; 0 for a row of zeros.
+__device__ inline float token_scale(const ProductArgs &a, int n) {
+    const int64_t x = a.xs_rows ? a.xs_rows[n] : n;
+    return x >= 0 && x < a.xs_count ? a.xs[x] : 0.f;
+}
+
+// Four outputs from their sums, rounded to fp16: scales, the fused epilogue and the
+// row's factor, the operands at hand.
 template <class V>
-__device__ inline void finish_quad(const ProductArgs &a, const float *w_scale, int e, int n, int64_t m,
-                                   typename V::Acc acc) {
+__device__ inline uint2 finished_quad(const ProductArgs &a, typename V::Acc acc, floatx4 ws, float xs, uint2 bias,
+                                      uint2 res, float weight) {
+    typedef _Float16 half4 __attribute__((ext_vector_type(4)));
     floatx4 v = V::sum(acc);
-    if (V::kBytes == 1) {  // w_scale holds whole row blocks
-        const int64_t x = a.xs_rows ? a.xs_rows[n] : n;
-        const float xs = x >= 0 && x < a.xs_count ? a.xs[x] : 0.f;  // a row of zeros
-        const floatx4 ws = *reinterpret_cast<const floatx4 *>(w_scale + m);
+    if (V::kBytes == 1) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] *= xs * ws[i];
     }
-    if (a.e_flags & kEpiAny) {
-        const uint2 bq = load_quad(a.bias ? a.bias + e * a.ldb : nullptr, m, a.M, a.e_flags & kEpiBiasVec);
-        v = epilogue(a, v, bq, residual_quad(a, n, m));
-    }
+    if (a.e_flags & kEpiAny) v = epilogue(a, v, bias, res);
     if (a.weight) {
-        const float w = a.weight[n];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] *= w;
+        for (int i = 0; i < 4; ++i) v[i] *= weight;
     }
-    store_rounded4(a, n, m, v);
+    return __builtin_bit_cast(uint2, half4{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]});
+}
+
+// Stores rows m .. m + 3 of row n of Y, those < M.
+__device__ inline void store_quad(const ProductArgs &a, int n, int64_t m, uint2 q) {
+    uint16_t *const dst = a.Y + (int64_t)n * a.ldy + m;
+    if (a.y_vec && m + 4 <= a.M) {
+        *reinterpret_cast<uint2 *>(dst) = q;
+    } else {
+        if (m < a.M) dst[0] = (uint16_t)q.x;
+        if (m + 1 < a.M) dst[1] = (uint16_t)(q.x >> 16);
+        if (m + 2 < a.M) dst[2] = (uint16_t)q.y;
+        if (m + 3 < a.M) dst[3] = (uint16_t)(q.y >> 16);
+    }
+}
+
+// Rows m .. m + 3 of row n of Y from their sums (w_scale: the expert's scales, of
+// whole row blocks).
+template <class V>
+__device__ inline void finish_quad(const ProductArgs &a, const float *w_scale, int e, int n, int64_t m,
+                                   typename V::Acc acc) {
+    const floatx4 ws = V::kBytes == 1 ? *reinterpret_cast<const floatx4 *>(w_scale + m) : floatx4{};
+    const float xs = V::kBytes == 1 ? token_scale(a, n) : 0.f, weight = a.weight ? a.weight[n] : 1.f;
+    const uint2 bias = load_quad(a.bias ? a.bias + e * a.ldb : nullptr, m, a.M, a.e_flags & kEpiBiasVec);
+    store_quad(a, n, m, finished_quad<V>(a, acc, ws, xs, bias, residual_quad(a, n, m), weight));
 }
 
 }  // namespace
+
+typedef void (*ProductKernelFn)(ProductArgs);
+
+// The wide kernel (usp_product_wide.hip): column tiles whose records are in LDS; whether
+// it is built for records of L KB, R row blocks and NB token blocks per wavefront (of
+// 2 and 4; what fits 160 KB of LDS and 256 registers); and the kernel.
+constexpr int wide_ring(int L) { return L <= 3 ? 3 : 2; }
+constexpr bool wide_serves_rows(int value_bytes, int L, int R, int NB) {
+    return 2048 + 8192 * R + wide_ring(L) * (1024 * L * R + 16) <= 160 * 1024 && (R == 4 || NB == 2 || value_bytes == 1);
+}
+ProductKernelFn wide_product_kernel_of(int value_bytes, int loads, int rows, int nb);
+
 }  // namespace usp

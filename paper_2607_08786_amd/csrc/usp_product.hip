@@ -3,115 +3,225 @@
 #include "usp_product.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace usp {
 namespace {
 
 // ---------------------------------------------------------------------------
-// X copied to rows of whole column tiles, zeros past K (and gathered, where it is
-// to be): for X whose rows the products cannot load in place. One thread per 16
-// bytes of a row; elements of ES bytes at any alignment.
+// X packed in the order of the products' B operands: block (tb KT + kt) S + s of
+// 1 KB, lane 16 g + n, holds bytes 64 s + 16 g .. + 15 of column tile kt of row
+// 16 tb + n (of an expert's rows, gathered; zeros past them and past K). A load of
+// X in place touches 16 rows' segments of 64 bytes, which the memory pipeline takes
+// several times as long for as for 1 KB in one piece, and each column tile is
+// loaded once per row set. One wavefront per block of rows and column tile.
 // ---------------------------------------------------------------------------
-template <class E>
-__global__ __launch_bounds__(256) void copy_x_kernel(const E *__restrict__ X, int64_t ldx, int64_t x_rows,
-                                                     const int32_t *__restrict__ rows, int64_t K, int64_t row_chunks,
-                                                     int64_t chunks, E *__restrict__ out) {
-    constexpr int V = 16 / sizeof(E);
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= chunks) return;
-    const int64_t t = i / row_chunks, k = i % row_chunks * V, r = rows ? rows[t] : t;
-    const bool real = r >= 0 && r < x_rows;
-    E v[V];
+template <class V>
+__global__ __launch_bounds__(kLanes) void pack_kernel(ProductArgs a, uint8_t *__restrict__ xp) {
+    constexpr int S = V::kStepsPerTile, E = 16 / V::kBytes;  // elements of a chunk
+    const int lane = threadIdx.x;
+    const int kt = blockIdx.x % a.KT;
+    Job j;
+    if (!find_job<kBlock>(a, a.job0 + (int)(blockIdx.x / a.KT), 1, lane, j)) return;
+    const int n = lane & 15;
+    int64_t x = j.row0 + n;
+    if (a.rows && n < j.n) x = a.rows[j.row0 + n];
+    const bool real = n < j.n && x >= 0 && x < a.x_rows;
+    const uint8_t *const row = a.X + (real ? x * a.ldx : 0);
+    const bool aligned = ((reinterpret_cast<uintptr_t>(a.X) | (uintptr_t)a.ldx) & 3) == 0;
+    v4u32 v[S];
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = real && k + j < K ? X[r * ldx + k + j] : (E)0;
+    for (int s = 0; s < S; ++s) {
+        typedef v4u32 __attribute__((aligned(4))) v4u32_a4;
+        const int k = kt * kTileK + (64 * s + 16 * (lane >> 4)) / V::kBytes;
+        const uint8_t *const p = row + (int64_t)k * V::kBytes;
+        v[s] = v4u32{0u, 0u, 0u, 0u};
+        if (!real || k >= a.K) continue;
+        if (aligned && k + E <= a.K) {
+            v[s] = *reinterpret_cast<const v4u32_a4 *>(p);
+        } else if (aligned) {  // dwords that hold some of the row, their bytes past it cleared
+            const int left = (a.K - k) * V::kBytes;
 #pragma unroll
-    for (int j = 0; j < V; ++j) out[i * V + j] = v[j];
+            for (int i = 0; i < 4; ++i)
+                if (4 * i < left) {
+                    const uint32_t d = reinterpret_cast<const uint32_t *>(p)[i];
+                    v[s][i] = 4 * i + 4 <= left ? d : d & ((1u << (8 * (left - 4 * i))) - 1);
+                }
+        } else if (V::kBytes == 2) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < a.K) v[s][i / 2] |= (uint32_t) reinterpret_cast<const uint16_t *>(p)[i] << (16 * (i % 2));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (k + i < a.K) v[s][i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+        }
+    }
+    v4u32 *const out = reinterpret_cast<v4u32 *>(xp + (((int64_t)j.tb * a.KT + kt) * S << 10));
+#pragma unroll
+    for (int s = 0; s < S; ++s) out[s * kLanes + lane] = v[s];
 }
 
 // ---------------------------------------------------------------------------
 // Product kernel: a workgroup of W wavefronts takes R row blocks and NB blocks of
 // 16 tokens; its wavefronts split the column tiles and sum their parts in LDS.
 // ---------------------------------------------------------------------------
-template <class V, int L, int R, int W, int NB>
+
+// Requests the whole record at 16-byte units [o0, o1) into an LDS slot: L transfers
+// of 16 bytes per lane; past the record's end they read nothing and write zeros.
+template <int L>
+__device__ inline void request_record(const uint8_t *stream, uint32_t o0, uint32_t o1, int lane, uint8_t *slot) {
+    const __amdgpu_buffer_rsrc_t rec = __builtin_amdgcn_make_buffer_rsrc(
+        (void *)(stream + (uint64_t)o0 * 16), (short)0, (int)((o1 - o0) * 16), kBufferRsrcWord3);
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rec, (__attribute__((address_space(3))) void *)(slot + 1024 * i), 16,
+                                                 1024 * i + lane * 16, 0, 0, kCachePolicyStream);
+}
+
+template <class V, int L, int R, int W, int NB, bool PACKED>
 __global__ __launch_bounds__(W *kLanes) void product_kernel(ProductArgs a) {
     constexpr int S = V::kStepsPerTile, TB = 16 * NB;
+    constexpr int kSlots = 2;  // records of a wavefront in LDS: one being decoded, one in flight
+    constexpr int U = 2;       // column tiles per round of the loop, buffers of X
+    constexpr int XD = 1;      // how many tiles ahead X is requested
     constexpr int kSlot = 1024 * L;
-    constexpr int kSum = R * NB * 1024;  // a wavefront's sums
-    constexpr int kWave = kSlot > kSum ? kSlot : kSum;
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[W * kWave + 16];
-    __shared__ __attribute__((aligned(16))) uint8_t lut[V::kLutBytes];
+    // One array per slot (the compiler then waits for the transfers into the one that
+    // a decode reads, and no others), each with a part for every wavefront.
+    __shared__ __attribute__((aligned(16))) uint8_t slot0[W * kSlot + 16], slot1[W * kSlot + 16];
+    __shared__ __attribute__((aligned(16))) uint8_t lut[V::kLutEntries * 8];
     const int lane = threadIdx.x & (kLanes - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    uint8_t *const slots[kSlots] = {slot0 + wave * kSlot, slot1 + wave * kSlot};
     Job job;
-    if (!find_job<TB>(a, a.job0 + (int)blockIdx.x, lane, job)) return;  // the whole workgroup
-    const ExpertRef ref = a.experts ? a.experts[job.e] : a.one;
-    if (threadIdx.x < 16) V::fill_lut(lut, threadIdx.x);
-    __syncthreads();
+    if (!find_job<TB>(a, a.job0 + (int)blockIdx.x, a.sets, lane, job)) return;  // the whole workgroup
+    const ExpertRef ref = job_matrix(a, job);
+    fill_lut<V>(lut, threadIdx.x, W * kLanes);
 
-    // Rows of X: a resource over the job's rows, or over all of X where rows are
-    // gathered; lanes of tokens past the job's end read past its end (zeros).
-    const int64_t x0 = a.rows ? 0 : (int64_t)job.row0 * a.ldx;
-    const int64_t x_rows = a.rows ? a.x_rows : job.n;
-    const uint32_t x_bytes = (uint32_t)(((x_rows - 1) * a.ldx + (int64_t)a.K * V::kBytes + 3) & ~(int64_t)3);
-    const __amdgpu_buffer_rsrc_t xr =
-        __builtin_amdgcn_make_buffer_rsrc((void *)(a.X + x0), (short)0, (int)x_bytes, kBufferRsrcWord3);
-    uint32_t xoff[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int t = 16 * nb + (lane & 15);
-        int64_t x = t;
-        if (a.rows && t < job.n) x = a.rows[job.row0 + t];
-        xoff[nb] = t < job.n && x >= 0 && x < x_rows ? (uint32_t)(x * a.ldx) + 16 * (lane >> 4) : x_bytes;
-    }
+    const int kt0 = wave * a.KT / W, kt1 = (wave + 1) * a.KT / W;
+    // Lane l: the offset of tile kt0 + l of each row block (0, an empty record, past
+    // the matrix and past the next wavefront's first).
     const __amdgpu_buffer_rsrc_t offr = __builtin_amdgcn_make_buffer_rsrc(
         (void *)ref.off, (short)0, (a.RB * a.KT + 1) * 4, kBufferRsrcWord3);
-    const int slot = wave * kWave;
-    const uint32_t lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)smem) + slot;
-
-    typename V::Acc acc[R][NB] = {};
-    const int kt0 = wave * a.KT / W, kt1 = (wave + 1) * a.KT / W;
-    for (int kt = kt0; kt < kt1; ++kt) {
-        v4u32 xb[NB][S];
+    uint32_t off[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int rb = job.set * R + r;
+        const bool ok = rb < a.RB && lane <= kt1 - kt0;
+        off[r] = __builtin_amdgcn_raw_buffer_load_b32(offr, ok ? (rb * a.KT + kt0 + lane) * 4 : 0x7FFFFFF0, 0, 0);
+    }
+    // X: the packed blocks of the job's rows; or in place, from a resource over the
+    // job's rows (over all of X where rows are gathered), which lanes of tokens past
+    // the job's end read past the end of (zeros).
+    __amdgpu_buffer_rsrc_t xr;
+    uint32_t x_bytes, xoff[NB];
+    if (PACKED) {
+        const int64_t block = (int64_t)a.KT * S << 10;
+        x_bytes = (uint32_t)(NB * block);
+        xr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.xp + job.tb * block), (short)0, (int)x_bytes, kBufferRsrcWord3);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) xoff[nb] = (uint32_t)(nb * block) + 16 * lane;
+    } else {
+        const int64_t x0 = a.rows ? 0 : (int64_t)job.row0 * a.ldx;
+        const int64_t x_rows = a.rows ? a.x_rows : job.n;
+        x_bytes = (uint32_t)(((x_rows - 1) * a.ldx + (int64_t)a.K * V::kBytes + 3) & ~(int64_t)3);
+        xr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.X + x0), (short)0, (int)x_bytes, kBufferRsrcWord3);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int t = kBlock * nb + (lane & 15);
+            int64_t x = t;
+            if (a.rows && t < job.n) x = a.rows[job.row0 + t];
+            xoff[nb] = t < job.n && x >= 0 && x < x_rows ? (uint32_t)(x * a.ldx) + 16 * (lane >> 4) : x_bytes;
+        }
+    }
+    auto request_x = [&](int kt, v4u32(&xb)[NB][S]) __attribute__((always_inline)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                uint32_t at = xoff[nb] + (uint32_t)(kt * kTileK * V::kBytes + 64 * s);
-                // fp16 past a row's end could be a NaN, which zeros in W do not undo.
-                if (V::kBytes == 2 && kt * kTileK + 32 * s + 8 * (lane >> 4) >= a.K) at = x_bytes;
-                xb[nb][s] = __builtin_amdgcn_raw_buffer_load_b128(xr, (int)at, 0, 0);
+                uint32_t at = xoff[nb];
+                if (PACKED) {
+                    xb[nb][s] = __builtin_amdgcn_raw_buffer_load_b128(xr, (int)at, (kt * S + s) << 10, 0);
+                } else {
+                    at += (uint32_t)(kt * kTileK * V::kBytes + 64 * s);
+                    // fp16 past a row's end could be a NaN, which zeros in W do not undo.
+                    if (V::kBytes == 2 && kt * kTileK + 32 * s + 8 * (lane >> 4) >= a.K) at = x_bytes;
+                    xb[nb][s] = __builtin_amdgcn_raw_buffer_load_b128(xr, (int)at, 0, 0);
+                }
             }
+    };
+    // Record `rec` (0 .. U R + 2, a constant) of the round that starts at tile kt.
+    auto request = [&](int kt, int rec) __attribute__((always_inline)) {
+        const int r = rec % R, u = kt - kt0 + rec / R;
+        const bool real = kt0 + u < kt1;
+        const uint32_t o0 = real ? __builtin_amdgcn_readlane(off[r], u) : 0;
+        const uint32_t o1 = real ? __builtin_amdgcn_readlane(off[r], u + 1) : 0;
+        request_record<L>(ref.stream, o0, o1, lane, slots[rec % kSlots]);
+    };
+    __syncthreads();  // the selector table
+    typename V::Acc acc[R][NB] = {};
+    v4u32 xb[U][NB][S];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int rb = job.set * R + r;
-            const bool ok = rb < a.RB && lane < 2;
-            const uint32_t o = __builtin_amdgcn_raw_buffer_load_b32(offr, ok ? (rb * a.KT + kt + lane) * 4 : 0x7FFFFFF0, 0, 0);
-            dma_rec_asm<L>(ref.stream, __builtin_amdgcn_readlane(o, 0), __builtin_amdgcn_readlane(o, 1), lane, lds);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            const RecState rs = rec_state<V::kBytes>(slot_mask(smem + slot, lane), (uint32_t)(slot + kMaskBytes));
+    for (int u = 0; u < XD; ++u) request_x(kt0 + u, xb[u]);
 #pragma unroll
-            for (int s = 0; s < S; ++s) {
-                const v4u32 av = V::finish(V::read(as_lds(smem), lut, rs, s));
+    for (int i = 0; i < kSlots - 1; ++i) request(kt0, i);
+    for (int kt = kt0; kt < kt1; kt += U) {
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) acc[r][nb] = V::multiply(av, xb[nb][s], acc[r][nb]);
+        for (int u = 0; u < U; ++u) {
+            if (u && kt + u >= kt1) break;
+            request_x(kt + u + XD, xb[(u + XD) % U]);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int rec = u * R + r;
+                request(kt, rec + kSlots - 1);
+                uint8_t *const slot = slots[rec % kSlots];
+                // The record is there once at most the loads issued after it are outstanding:
+                // the next tile's X, at a tile's first record, and the next record's.
+                if (r == 0)
+                    wait_loads<L + NB * S>();
+                else
+                    wait_loads<L>();
+                const typename V::State rs = V::state(slot, lane, (uint32_t)(wave * kSlot));
+                lds_u32 *const region = as_lds(rec % kSlots == 0 ? slot0 : slot1);
+                typename V::Words w = V::read(region, lut, rs, 0);
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    typename V::Words next;
+                    if (s + 1 < S) next = V::read(region, lut, rs, s + 1);
+                    const v4u32 av = V::finish(w);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) acc[r][nb] = V::multiply(av, xb[u][nb][s], acc[r][nb]);
+                    if (s + 1 < S) w = next;
+                }
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot's reads, before its next record
         }
     }
-    __syncthreads();
-    typename V::Acc *const part = reinterpret_cast<typename V::Acc *>(smem + slot);
+    __builtin_amdgcn_s_waitcnt(0);  // the transfers past the range's end
+    // Item i of the R x NB products is finished by wavefront i % W, parts in wavefront
+    // order; they pass through the slots, as many at a time as those hold. One copy of
+    // the code that finishes an item: with one for each, its instructions came from
+    // memory for every item.
+    constexpr int kItems = R * NB, kRound = kSlots * L;
+    uint8_t *const area[kSlots] = {slot0, slot1};
+    typedef typename V::Acc Acc;
+    static_assert(kSlots == 2 && kRound * W * 1024 <= kSlots * W * kSlot, "the slots hold a round's sums");
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int i0 = 0; i0 < kItems; i0 += kRound) {
+        __syncthreads();
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) part[(r * NB + nb) * kLanes + lane] = acc[r][nb];
-    __syncthreads();
-    for (int i = wave; i < R * NB; i += W) {
-        typename V::Acc sum = reinterpret_cast<typename V::Acc *>(smem)[i * kLanes + lane];
+        for (int i = i0; i < i0 + kRound && i < kItems; ++i)
+            reinterpret_cast<Acc *>(area[i % 2])[((i - i0) / 2 * W + wave) * kLanes + lane] = acc[i / NB][i % NB];
+        __syncthreads();
+#pragma unroll 1
+        for (int i = i0 + (wave + W - i0 % W) % W; i < i0 + kRound && i < kItems; i += W) {
+            const Acc *const p = reinterpret_cast<const Acc *>(i % 2 ? slot1 : slot0) + (i - i0) / 2 * W * kLanes + lane;
+            Acc sum = {};
 #pragma unroll
-        for (int w = 1; w < W; ++w) sum += reinterpret_cast<typename V::Acc *>(smem + w * kWave)[i * kLanes + lane];
-        const int t = 16 * (i % NB) + (lane & 15);
-        const int64_t m = ((int64_t)job.set * R + i / NB) * kTileRows + 4 * (lane >> 4);
-        if (t < job.n && m < a.M) finish_quad<V>(a, ref.scale, job.e, job.row0 + t, m, sum);
+            for (int w = 0; w < W; ++w) sum += p[w * kLanes];
+            const int t = kBlock * (i % NB) + (lane & 15);
+            const int64_t m = ((int64_t)job.set * R + i / NB) * kTileRows + 4 * (lane >> 4);
+            if (t < job.n && m < a.M) finish_quad<V>(a, ref.scale, job.e, job.row0 + t, m, sum);
+        }
     }
 }
 
@@ -119,19 +229,16 @@ __global__ __launch_bounds__(W *kLanes) void product_kernel(ProductArgs a) {
 // scale, rounded to fp16.
 __global__ __launch_bounds__(kLanes) void densify_q_kernel(ExpertRef ref, int64_t M, int64_t K, int64_t KT,
                                                            uint16_t *Wd, int64_t ldw) {
-    __shared__ __attribute__((aligned(16))) uint8_t region[kTileRows * kTileK + 16];
-    __shared__ __attribute__((aligned(16))) uint8_t lut[ValuesQ::kLutBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t region[kMaskBytes + kStartBytesQ + kTileRows * kTileK + 16];
+    __shared__ __attribute__((aligned(16))) uint8_t lut[ValuesQ::kLutEntries * 8];
     const int lane = threadIdx.x;
     const int64_t t = blockIdx.x, rb = t / KT, kt = t % KT;
-    if (lane < 16) ValuesQ::fill_lut(lut, lane);
+    fill_lut<ValuesQ>(lut, lane, kLanes);
     const uint32_t o0 = ref.off[t], o1 = ref.off[t + 1];
-    const uint8_t *rec = ref.stream + (size_t)o0 * 16;
-    const uint2 msk = reinterpret_cast<const uint2 *>(rec)[lane];
-    const int nch = (int)(o1 - o0) - kMaskChunks;
-    const uint4 *vp = reinterpret_cast<const uint4 *>(rec + kMaskBytes);
-    for (int c = lane; c < nch; c += kLanes) reinterpret_cast<uint4 *>(region)[c] = vp[c];
+    const uint4 *rec = reinterpret_cast<const uint4 *>(ref.stream + (size_t)o0 * 16);
+    for (int c = lane; c < (int)(o1 - o0); c += kLanes) reinterpret_cast<uint4 *>(region)[c] = rec[c];
     __syncthreads();
-    const RecState rs = rec_state<1>(msk);
+    const RecStateQ rs = ValuesQ::state(region, lane, 0);
     const int64_t row = rb * kTileRows + (lane & 15);
     if (row >= M) return;
     const float scale = ref.scale[row];
@@ -145,61 +252,141 @@ __global__ __launch_bounds__(kLanes) void densify_q_kernel(ExpertRef ref, int64_
     }
 }
 
-typedef void (*ProductKernelFn)(ProductArgs);
-
-constexpr int kRows = 1, kWaves = 4;
-
-template <class V, int L>
-ProductKernelFn product_kernel_of(int nb) {
-    return nb == 1 ? product_kernel<V, L, kRows, kWaves, 1> : product_kernel<V, L, kRows, kWaves, 2>;
+template <class V, int L, int NB, bool PACKED>
+ProductKernelFn product_kernel_of(int rows, int waves) {
+    if (rows == 1) return waves == 4 ? product_kernel<V, L, 1, 4, NB, PACKED> : product_kernel<V, L, 1, 8, NB, PACKED>;
+    if (rows == 2) return waves == 4 ? product_kernel<V, L, 2, 4, NB, PACKED> : product_kernel<V, L, 2, 8, NB, PACKED>;
+    return waves == 4 ? product_kernel<V, L, 4, 4, NB, PACKED> : product_kernel<V, L, 4, 8, NB, PACKED>;
 }
 
-// 1 KB transfers that cover every record.
-int record_loads(const ProductShape &s) { return (int)ceil_div(kMaskChunks + s.max_chunks, kLanes); }
+// The smallest built count of 1 KB transfers that covers every record, the decode's
+// reads past its values included.
+int record_loads(const ProductShape &s) {
+    const int64_t kb = ceil_div(16 * (kMaskChunks + s.max_chunks) + 12, (int64_t)1024);
+    return s.value_bytes == 1 ? kb <= 3 ? 3 : 5 : kb <= 5 ? 5 : 9;
+}
 
 struct ProductPlan {
-    ProductKernelFn fn;
-    int nb, rows, waves;
+    bool wide, packed;
+    int rows, waves, nb;  // wide: waves = rows
     int64_t sets, grid;
 };
 
-ProductPlan plan_product(const ProductShape &s, int64_t N) {
-    ProductPlan p;
-    const int64_t E = s.G ? s.G->E : 1;
-    p.nb = N > 16 * E ? 2 : 1;
-    p.rows = kRows;
-    p.waves = kWaves;
-    const int l = record_loads(s);
-    if (s.value_bytes == 1)
-        p.fn = l <= 3 ? product_kernel_of<ValuesQ, 3>(p.nb) : product_kernel_of<ValuesQ, 5>(p.nb);
-    else
-        p.fn = l <= 5 ? product_kernel_of<ValuesF16, 5>(p.nb) : product_kernel_of<ValuesF16, 9>(p.nb);
-    p.sets = ceil_div(s.RB, p.rows);
-    // A group's counts are known on the device alone: at most one group of tokens
-    // beyond N / TB for every expert with rows.
-    const int64_t tb = 16 * p.nb;
-    p.grid = p.sets * (s.G ? N / tb + std::min(E, N) : ceil_div(N, tb));
-    return p;
+// Groups of at most tb tokens that a call has, at most and as expected. A group's counts
+// are known on the device alone: at most one group beyond N / tb for every expert with
+// rows; expected, half of one for every expert that random rows reach.
+int64_t most_groups(const ProductShape &s, int64_t N, int64_t tb) {
+    return s.G ? N / tb + std::min(s.G->E, N) : ceil_div(N, tb);
+}
+double expected_groups(const ProductShape &s, int64_t N, int64_t tb) {
+    if (!s.G) return (double)ceil_div(N, tb);
+    const double E = (double)s.G->E, active = 0.9 * E * (1.0 - std::exp(-(double)N / E));
+    return std::max(1.0, std::max(active, (double)N / (double)tb + 0.5 * active));
 }
 
-// Bytes that a resource over rows of X may span: offsets past its end, for rows and
-// columns that are to read zeros, stay below 2^32.
+// The kernel that costs least by a model of what was measured (us; 8-bit values at 50%,
+// fp16 records scaled; layers of 1024 x 1024 to 28672 x 8192 and groups of 7 to 64
+// experts). Product kernel: a launch, a wavefront's start, and the longer of a
+// wavefront's chain of records and the records of a CU, whose time has a part for X
+// that R row blocks share. At 16 tokens (R W): 13B attention 1 4 10.3, 2 8 9.6, 4 8
+// 13.3; 13B FFN up 1 4 18.6, 2 4 13.9, 4 8 14.1; 70B FFN 1 8 43.4, 2 4 34.3, 4 4 30.5;
+// at 64: 70B FFN 2 4 57.2, 4 8 51.2. Wide kernel: rounds of workgroups of KT tiles and an
+// epilogue; two of 4 row blocks share a CU. It wins from about 128 tokens on large
+// layers (70B FFN at 128 63.3 against 99.0) and 256 on small ones (13B attention at 128
+// 31.5 against 22.6, at 256 33.0 against 34.0).
+ProductPlan plan_product(const ProductShape &s, int64_t N) {
+    const double cus = s.num_cus > 0 ? s.num_cus : 256;
+    const int loads = record_loads(s);
+    const double value = s.value_bytes == 1 ? 1.0 : 1.8, size = value * (loads > 5 || (loads > 3 && s.value_bytes == 1) ? 1.5 : 1.0);
+    ProductPlan best = {};
+    double least = 0;
+    auto consider = [&](const ProductPlan &p, double cost) {
+        if (best.grid && cost >= least) return;
+        best = p;
+        least = cost;
+    };
+    static const struct {
+        int rows, waves, nb;
+        double record;  // us of a CU
+    } kernels[] = {{1, 4, 1, .15}, {1, 8, 1, .15}, {2, 4, 1, .118}, {2, 8, 1, .118}, {4, 4, 1, .107}, {4, 8, 1, .107},
+                   {1, 4, 2, .16}, {1, 8, 2, .16}, {2, 4, 2, .13},  {2, 8, 2, .13},  {4, 4, 2, .121}, {4, 8, 2, .121},
+                   {1, 4, 4, .27}, {2, 4, 4, .19}, {2, 8, 4, .21},  {4, 8, 4, .167}};
+    for (const auto &k : kernels) {
+        if (k.nb == 4 && s.value_bytes != 1) continue;  // registers
+        const int64_t tb = kBlock * k.nb, sets = ceil_div(s.RB, (int64_t)k.rows);
+        const double wgs = std::ceil((double)sets * expected_groups(s, N, tb) / cus);
+        const double chain = 0.75 * size * k.rows * (double)ceil_div(s.KT, (int64_t)k.waves);
+        const double cost = 2.6 + (k.nb > 1 ? 2.5 : 0.0) + 0.24 * std::min(16.0, wgs * k.waves) +
+                            std::max(chain, wgs * k.rows * (double)s.KT * k.record * size * (k.nb > 1 && value > 1 ? 1.2 : 1.0));
+        consider({false, k.nb > 1, k.rows, k.waves, k.nb, sets, sets * most_groups(s, N, tb)}, cost);
+    }
+    static const struct {
+        int rows, nb;
+        double alone[2], shared[2];  // us of a tile of fp16 and 8-bit values, for one workgroup on a CU and for two
+    } wides[] = {{4, 2, {1.65, 1.22}, {2.3, 1.7}}, {4, 4, {2.2, 1.5}, {3.3, 2.15}}, {8, 2, {4.2, 2.1}, {0, 0}}, {8, 4, {0, 3.25}, {0, 0}}};
+    for (const auto &k : wides) {
+        if (!wide_serves_rows(s.value_bytes, loads, k.rows, k.nb)) continue;
+        const int q = s.value_bytes == 1;
+        const int64_t tb = (int64_t)kBlock * k.nb * k.rows, sets = ceil_div(s.RB, (int64_t)k.rows);
+        const bool two = k.rows == 4 && loads <= 5;
+        const double wgs = (double)sets * expected_groups(s, N, tb), slots = two ? 2 * cus : cus;
+        const double full = std::floor(wgs / slots), rest = wgs - full * slots;
+        const double tile = two ? k.shared[q] : k.alone[q];
+        // A group's last round is as full as its counts make it.
+        const double tiles = s.G ? std::max(k.alone[q], wgs / slots * tile + 0.5 * k.alone[q])
+                                 : full * tile + (rest <= 0 ? 0 : rest > cus ? tile : k.alone[q]);
+        const double cost = 7.5 + std::ceil(wgs / slots) * (1.0 + k.nb) + tiles * (double)s.KT;
+        consider({true, true, k.rows, k.rows, k.nb, sets, sets * most_groups(s, N, tb)}, cost);
+    }
+    return best;
+}
+
+template <class V, int L>
+ProductKernelFn kernel_for(const ProductPlan &p) {
+    if (p.nb == 1)
+        return p.packed ? product_kernel_of<V, L, 1, true>(p.rows, p.waves) : product_kernel_of<V, L, 1, false>(p.rows, p.waves);
+    if constexpr (V::kBytes == 1) {
+        if (p.nb == 4)
+            return p.rows == 1   ? product_kernel<V, L, 1, 4, 4, true>
+                   : p.rows == 4 ? product_kernel<V, L, 4, 8, 4, true>
+                   : p.waves == 4 ? product_kernel<V, L, 2, 4, 4, true>
+                                  : product_kernel<V, L, 2, 8, 4, true>;
+    }
+    return product_kernel_of<V, L, 2, true>(p.rows, p.waves);
+}
+
+ProductKernelFn plan_kernel(const ProductShape &s, const ProductPlan &p) {
+    const int l = record_loads(s);
+    if (p.wide) return wide_product_kernel_of(s.value_bytes, l, p.rows, p.nb);
+    if (s.value_bytes == 1) return l == 3 ? kernel_for<ValuesQ, 3>(p) : kernel_for<ValuesQ, 5>(p);
+    return l == 5 ? kernel_for<ValuesF16, 5>(p) : kernel_for<ValuesF16, 9>(p);
+}
+
+// X in place: dword-aligned rows, whole 16-byte chunks of fp16 (what follows a row
+// of 8-bit values meets zeros in W), rows of a resource within 32-bit offsets.
 constexpr int64_t kMaxSpan = ((int64_t)1 << 32) - ((int64_t)1 << 20);
 // Workgroups of one launch (a grid has fewer than 2^32 threads).
 constexpr int64_t kMaxGrid = (int64_t)1 << 21;
 
-size_t copied_x_bytes(const ProductShape &s, int64_t N) { return (size_t)N * s.KT * kTileK * s.value_bytes; }
+// Blocks of 16 rows of X packed, at most, and what a job may read past its last one.
+int64_t packed_blocks(const ProductShape &s, int64_t N) { return most_groups(s, N, kBlock); }
+constexpr int64_t kMoreBlocks = 32;
+
+size_t packed_bytes(const ProductShape &s, int64_t N) {
+    return (size_t)(packed_blocks(s, N) + kMoreBlocks) * s.KT * kTileK * s.value_bytes * kBlock;
+}
 
 }  // namespace
 
 bool product_fits(const ProductShape &s, int64_t N) { return plan_product(s, N).grid < ((int64_t)1 << 31); }
 
-// The copy of X follows the region that other products keep cleared.
-size_t product_workspace_bytes(const ProductShape &s, int64_t N) { return kCounterRegionBytes + copied_x_bytes(s, N); }
+// X packed follows the region that other products keep cleared.
+size_t product_workspace_bytes(const ProductShape &s, int64_t N) { return kCounterRegionBytes + packed_bytes(s, N); }
 
 std::string describe_product(const ProductShape &s, int64_t N) {
     const ProductPlan p = plan_product(s, N);
-    return "product R=" + std::to_string(p.rows) + " W=" + std::to_string(p.waves) + " nb=" + std::to_string(p.nb) +
+    return std::string(p.wide ? "wide-product" : "product") + " R=" + std::to_string(p.rows) +
+           (p.wide ? "" : " W=" + std::to_string(p.waves)) + " nb=" + std::to_string(p.nb) +
            " grid=" + std::to_string(p.grid);
 }
 
@@ -213,7 +400,7 @@ int launch_densify_q(const usp_matrix *A, void *Wd, int64_t ldw, void *stream) {
 
 int launch_product(const ProductShape &s, const ProductCall &c, void *workspace, void *stream) {
     const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const ProductPlan p = plan_product(s, c.N);
+    ProductPlan p = plan_product(s, c.N);
     const int vb = s.value_bytes;
     ProductArgs a = {};
     if (s.G) {
@@ -240,6 +427,7 @@ int launch_product(const ProductShape &s, const ProductCall &c, void *workspace,
     a.ldy = c.ldy;
     a.N = (int)c.N;
     a.y_vec = (reinterpret_cast<uintptr_t>(c.Y) & 7) == 0 && c.ldy % 4 == 0;
+    a.y_wide = (reinterpret_cast<uintptr_t>(c.Y) & 15) == 0 && c.ldy % 8 == 0;
     a.bias = c.ep.bias;
     a.ldb = c.ldb;
     a.res = c.ep.res;
@@ -247,29 +435,23 @@ int launch_product(const ProductShape &s, const ProductCall &c, void *workspace,
     a.act = c.ep.act;
     a.e_flags = epilogue_flags(c.ep);
     if (c.ldb % 4 != 0) a.e_flags &= ~kEpiBiasVec;
-    // In place: dword-aligned rows, whole 16-byte chunks of fp16 (what follows a row
-    // of 8-bit values meets zeros in W), rows of a resource within 32-bit offsets.
-    const int64_t span = c.rows ? c.x_rows : std::min<int64_t>(c.N, 16 * p.nb);
-    if ((reinterpret_cast<uintptr_t>(c.X) & 3) || a.ldx % 4 != 0 || (vb == 2 && s.K % 8 != 0) ||
-        span > kMaxSpan / a.ldx) {
-        uint8_t *const x = reinterpret_cast<uint8_t *>(workspace) + kCounterRegionBytes;
-        const int64_t row_chunks = s.KT * kTileK * vb / 16, chunks = row_chunks * c.N;
-        const dim3 grid((unsigned)ceil_div(chunks, 256));
-        if (vb == 1)
-            hipLaunchKernelGGL(copy_x_kernel<uint8_t>, grid, dim3(256), 0, st, reinterpret_cast<const uint8_t *>(c.X),
-                               c.ldx, c.x_rows, c.rows, s.K, row_chunks, chunks, x);
-        else
-            hipLaunchKernelGGL(copy_x_kernel<uint16_t>, grid, dim3(256), 0, st, reinterpret_cast<const uint16_t *>(c.X),
-                               c.ldx, c.x_rows, c.rows, s.K, row_chunks, chunks, reinterpret_cast<uint16_t *>(x));
-        a.X = x;
-        a.K = (int)(s.KT * kTileK);
-        a.ldx = a.K * vb;
-        a.x_rows = c.N;
-        a.rows = nullptr;
+    const int64_t span = c.rows ? c.x_rows : std::min<int64_t>(c.N, kBlock * p.nb);
+    p.packed = p.packed || (reinterpret_cast<uintptr_t>(c.X) & 3) || a.ldx % 4 != 0 || (vb == 2 && s.K % 8 != 0) ||
+               span > kMaxSpan / a.ldx;
+    if (p.packed) {
+        uint8_t *const xp = reinterpret_cast<uint8_t *>(workspace) + kCounterRegionBytes;
+        const int64_t blocks = packed_blocks(s, c.N), most = kMaxGrid / s.KT;
+        a.xp = xp;
+        for (int64_t b0 = 0; b0 < blocks; b0 += most) {
+            a.job0 = (int)b0;
+            hipLaunchKernelGGL(vb == 1 ? pack_kernel<ValuesQ> : pack_kernel<ValuesF16>,
+                               dim3((unsigned)(std::min(most, blocks - b0) * s.KT)), dim3(kLanes), 0, st, a, xp);
+        }
     }
+    const ProductKernelFn fn = plan_kernel(s, p);
     for (int64_t j0 = 0; j0 < p.grid; j0 += kMaxGrid) {
         a.job0 = (int)j0;
-        hipLaunchKernelGGL(p.fn, dim3((unsigned)std::min(kMaxGrid, p.grid - j0)), dim3(p.waves * kLanes), 0, st, a);
+        hipLaunchKernelGGL(fn, dim3((unsigned)std::min(kMaxGrid, p.grid - j0)), dim3(p.waves * kLanes), 0, st, a);
     }
     return (int)hipGetLastError();
 }

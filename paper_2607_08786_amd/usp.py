@@ -21,7 +21,7 @@ _STATUS = {0: "USP_OK", 1: "USP_ERR_INVALID_ARG", 2: "USP_ERR_UNSUPPORTED", 3: "
            4: "USP_ERR_HIP", 5: "USP_ERR_INTERNAL"}
 
 EXPORTED = ("usp_encode_q", "usp_decode_q", "usp_quantize", "usp_spmm_q", "usp_group_create", "usp_group_free",
-            "usp_group_workspace_size", "usp_spmm_grouped", "usp_norm", "usp_encode", "usp_workspace_size", "usp_spmm", "usp_spmm_ex", "usp_spmm_noalloc", "usp_plan",
+            "usp_group_workspace_size", "usp_group_plan", "usp_spmm_grouped", "usp_norm", "usp_encode", "usp_workspace_size", "usp_spmm", "usp_spmm_ex", "usp_spmm_noalloc", "usp_plan",
             "usp_densify", "usp_decode", "usp_info", "usp_free", "usp_last_error")
 
 # Bytes of the per-GPU device scratch usp_spmm_noalloc uses (USP_NOALLOC_SCRATCH_BYTES).
@@ -102,9 +102,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.usp_spmm_grouped.argtypes = [p, p, i64, i64, p, p, p, i64, p, i64, i64, p, i64, p, ctypes.c_int, p, sz, p]
     lib.usp_norm.argtypes = [ctypes.POINTER(usp_norm_args), i64, i64, ctypes.c_int, p]
     for name in ("usp_encode_q", "usp_decode_q", "usp_quantize", "usp_spmm_q", "usp_group_create", "usp_group_free",
-                 "usp_spmm_grouped", "usp_norm"):
+                 "usp_spmm_grouped", "usp_norm", "usp_group_plan"):
         getattr(lib, name).restype = st
     lib.usp_group_workspace_size.argtypes = [p, i64]
+    lib.usp_group_plan.argtypes = [p, i64, ctypes.c_char_p, sz]
     lib.usp_group_workspace_size.restype = sz
     lib.usp_last_error.argtypes = []
     lib.usp_last_error.restype = ctypes.c_char_p
@@ -377,6 +378,13 @@ def usp_group_workspace_size(group: int, T: int) -> int:
     return int(load_library().usp_group_workspace_size(group, T))
 
 
+def usp_group_plan(group: int, T: int) -> str:
+    """The kernel usp_spmm_grouped runs for this group and T rows, as text."""
+    buf = ctypes.create_string_buffer(128)
+    _check(load_library().usp_group_plan(group, T, buf, len(buf)))
+    return buf.value.decode()
+
+
 def usp_spmm_grouped(group: int, X: torch.Tensor, offsets: torch.Tensor, Y: torch.Tensor,
                      workspace: torch.Tensor | None = None, x_scale: torch.Tensor | None = None,
                      rows: torch.Tensor | None = None, bias: torch.Tensor | None = None,
@@ -549,6 +557,9 @@ class ExpertGroup:
 
     def workspace_size(self, T: int) -> int:
         return usp_group_workspace_size(self.handle, T)
+
+    def plan(self, T: int) -> str:
+        return usp_group_plan(self.handle, T)
 
     def make_workspace(self, T: int, stream=None) -> torch.Tensor | None:
         """A workspace for T rows, allocated and cleared on `stream` (default: the current one)."""

@@ -30,7 +30,7 @@ def encode(lib, W, mask, pad=0):
     Wl[:, :K], ml[:, :K] = W, mask
     tiles = -(-M // 16) * -(-K // 256)
     Wo, mo, nnz = np.empty_like(W), np.empty((M, K), np.uint8), ctypes.c_int64()
-    stream, off = np.zeros(tiles * (512 + 4096), np.uint8), np.zeros(tiles + 1, np.uint32)
+    stream, off = np.zeros(tiles * (528 + 4096), np.uint8), np.zeros(tiles + 1, np.uint32)
     rc = lib.usp_test_q(Wl.ctypes.data, K + pad, ml.ctypes.data, K + pad, M, K, Wo.ctypes.data, mo.ctypes.data,
                         ctypes.byref(nnz), stream.ctypes.data, stream.size, off.ctypes.data)
     assert rc == 0, rc
@@ -51,28 +51,30 @@ def test_round_trip(hlib, M, K, keep, pad):
     padded = np.zeros((RB * 16, KT * 256), bool)
     padded[:M, :K] = kept
     per_tile = padded.reshape(RB, 16, KT, 256).sum(axis=(1, 3)).reshape(-1)
-    assert np.array_equal(np.diff(off.astype(np.int64)) * 16, 512 + (per_tile + 15) // 16 * 16)
+    assert np.array_equal(np.diff(off.astype(np.int64)) * 16, 528 + (per_tile + 15) // 16 * 16)
 
 
 def test_layout(hlib):
-    """Position (r, 64 s + 16 g + j) is bit 16 s + j of lane 16 g + r; its value lies in block (16 s + j) / 4 behind
-    those of the lanes before and of the nibble's bits before."""
+    """Position (r, 64 s + 16 g + j) is bit 16 s + j of lane 16 g + r; its value lies in the block of its mask byte behind
+    those of the lanes before and of the byte's bits before; the blocks' starts stand between mask and values."""
     rng = np.random.default_rng(5)
     W = rng.integers(-128, 128, (16, 256)).astype(np.int8)
     mask = (rng.random((16, 256)) < 0.5).astype(np.uint8)
     _, _, _, stream, _ = encode(hlib, W, mask)
     lanes = stream[:512].reshape(64, 8).copy().view(np.uint64)[:, 0]
-    values = []
-    for b in range(16):
+    values, starts = [], []
+    for y in range(8):
+        starts.append(528 + len(values))
         for lane in range(64):
             r, g = lane % 16, lane // 16
-            for j in range(4):
-                bit = 4 * b + j
+            for j in range(8):
+                bit = 8 * y + j
                 col = 64 * (bit // 16) + 16 * g + bit % 16
                 assert (int(lanes[lane]) >> bit & 1) == mask[r, col]
                 if mask[r, col]:
                     values.append(W[r, col])
-    assert np.array_equal(stream[512:512 + len(values)].view(np.int8), np.array(values, np.int8))
+    assert np.array_equal(stream[528:528 + len(values)].view(np.int8), np.array(values, np.int8))
+    assert stream[512:528].view(np.uint16).tolist() == [starts[y] for y in (0, 2, 1, 3, 4, 6, 5, 7)]
 
 
 def test_refusals_without_device():
