@@ -250,12 +250,13 @@ usp_status usp_quantize(const void *X, int64_t ldx, int64_t N, int64_t K, void *
 /*
  * usp_spmm_q -- Y = act(W X + bias) + residual with 8-bit W and X, on the handle's device.
  *   Xq       device pointer, int8, token n at Xq + n * ldx, ldx >= K
- *   x_scale  device pointer, fp32 [N], 4-byte aligned
+ *   x_scale  device pointer, fp32 [N], 4-byte aligned; or NULL: Xq then points to fp16
+ *            tokens, which are brought to 8 bits first, as usp_quantize does
  *   workspace  16-byte aligned, to >= usp_workspace_size(A, N) bytes (may be NULL when that is
  *       0); must not be used by another in-flight call. It needs no clearing, and the region that
  *       usp_spmm expects cleared is left alone, so that one workspace can serve both.
- * Xq with a base or stride that is no multiple of 4 bytes is copied first. Everything else --
- * Y, bias, residual, activation, asynchrony, capture, reproducibility -- as usp_spmm_ex.
+ * X is packed for the products first where many tokens or its alignment ask for it. Everything
+ * else -- Y, bias, residual, activation, asynchrony, capture, reproducibility -- as usp_spmm_ex.
  */
 usp_status usp_spmm_q(const usp_matrix *A, const void *Xq, int64_t ldx, const float *x_scale, void *Y, int64_t ldy,
                       int64_t N, const void *bias, const void *residual, int64_t ldr, int activation,

@@ -80,7 +80,7 @@ static usp_status product_common(const std::string &f, const usp::ProductShape &
     if (c.N > (int64_t)1 << 20 || !usp::product_fits(s, c.N)) return usp::fail(USP_ERR_UNSUPPORTED, f + ": too many tokens");
     if (c.ldx < s.K) return usp::fail(USP_ERR_INVALID_ARG, f + ": ldx must be >= K");
     if (c.ldy < s.M) return usp::fail(USP_ERR_INVALID_ARG, f + ": ldy must be >= M");
-    if ((reinterpret_cast<uintptr_t>(c.X) & (s.value_bytes - 1)) || (reinterpret_cast<uintptr_t>(c.Y) & 1))
+    if ((reinterpret_cast<uintptr_t>(c.X) & (c.quantize ? 1 : s.value_bytes - 1)) || (reinterpret_cast<uintptr_t>(c.Y) & 1))
         return usp::fail(USP_ERR_INVALID_ARG, f + ": X and Y must be aligned to their elements");
     if (reinterpret_cast<uintptr_t>(c.x_scale) & 3)
         return usp::fail(USP_ERR_INVALID_ARG, f + ": x_scale must be 4-byte aligned");
@@ -464,7 +464,6 @@ usp_status usp_spmm_q(const usp_matrix *A, const void *Xq, int64_t ldx, const fl
     if (!alive(A)) return usp::fail(USP_ERR_INVALID_ARG, f + ": invalid or freed handle");
     if (const char *why = wrong_values(A, 1)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
     if (N < 1) return usp::fail(USP_ERR_INVALID_ARG, f + ": N must be >= 1");
-    if (!x_scale) return usp::fail(USP_ERR_INVALID_ARG, f + ": null x_scale");
     if (residual && ((reinterpret_cast<uintptr_t>(residual) & 1) || ldr < A->M))
         return usp::fail(USP_ERR_INVALID_ARG, f + ": residual must be 2-byte aligned with ldr >= M");
     usp::ProductCall c = {};
@@ -472,6 +471,7 @@ usp_status usp_spmm_q(const usp_matrix *A, const void *Xq, int64_t ldx, const fl
     c.ldx = ldx;
     c.x_rows = N;
     c.x_scale = x_scale;
+    c.quantize = !x_scale;
     c.Y = Y;
     c.ldy = ldy;
     c.N = N;

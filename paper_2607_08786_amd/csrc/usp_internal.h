@@ -173,6 +173,7 @@ struct ProductCall {
     Epilogue ep;
     int64_t ldb;
     const float *weight;
+    bool quantize;             // X is fp16, for 8-bit weights
 };
 bool product_fits(const ProductShape &s, int64_t N);  // its jobs are counted in 31 bits
 size_t product_workspace_bytes(const ProductShape &s, int64_t N);

@@ -63,17 +63,24 @@ typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 // Channels k .. k + 7 of a row of fp16, those < K (the others 0). VEC: 16-byte
 // aligned and K a multiple of 8.
 template <bool VEC>
-__device__ inline void load8(const void *row, int k, int K, float (&v)[kVec]) {
+__device__ inline half8v load8h(const void *row, int k, int K) {
     const _Float16 *p = reinterpret_cast<const _Float16 *>(row);
+    half8v h = {};
     if (VEC) {
-        half8v h = {};
         if (k < K) h = *reinterpret_cast<const half8v *>(p + k);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = (float)h[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = k + i < K ? (float)p[k + i] : 0.f;
+        for (int i = 0; i < kVec; ++i)
+            if (k + i < K) h[i] = p[k + i];
     }
+    return h;
+}
+
+template <bool VEC>
+__device__ inline void load8(const void *row, int k, int K, float (&v)[kVec]) {
+    const half8v h = load8h<VEC>(row, k, K);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = (float)h[i];
 }
 
 template <bool VEC>
@@ -177,6 +184,17 @@ __device__ inline void moments(const float (&v)[C][kVec], int kind, float eps, i
     inv = 1.f / sqrtf(reduce<Sum, THREADS>(s, part + THREADS / kLanes) / (float)K + eps);
 }
 
+// v <- (v - shift) * inv * w + b, with w and b at hand where there are any.
+__device__ inline void scale8h(float (&v)[kVec], float shift, float inv, bool weight, half8v w, bool bias, half8v b) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        float x = (v[i] - shift) * inv;
+        if (weight) x *= (float)w[i];
+        if (bias) x += (float)b[i];
+        v[i] = x;
+    }
+}
+
 template <int THREADS, int C, bool VEC>
 __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
     // Every reduction has its own values: no barrier between the end of one and the
@@ -185,23 +203,52 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
     __shared__ uint32_t top_part[THREADS / kLanes];
     const int64_t n = blockIdx.x;
     const int K = a.K, t = threadIdx.x;
+    auto at = [&](int c) -> int { return (c * THREADS + t) * kVec; };
+    // Everything that comes from HBM is requested first, the vectors of a norm before
+    // its reductions: one round trip to memory instead of one behind each reduction
+    // (2048 tokens of 5120 channels, layer norms on both sides, a gate: 35.0 us before).
+    half8v yh[C], rh[C], gh[C], pw[C], pb[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        if (a.p.y) yh[c] = load8h<VEC>(reinterpret_cast<const _Float16 *>(a.p.y) + n * a.p.ld_y, at(c), K);
+        rh[c] = load8h<VEC>(reinterpret_cast<const _Float16 *>(a.p.residual) + n * a.p.ld_residual, at(c), K);
+        if (a.p.gate) gh[c] = load8h<VEC>(reinterpret_cast<const _Float16 *>(a.p.gate) + n * a.p.ld_gate, at(c), K);
+        if (a.p.post_kind && a.p.post_weight) pw[c] = load8h<VEC>(a.p.post_weight, at(c), K);
+        if (a.p.post_kind && a.p.post_bias) pb[c] = load8h<VEC>(a.p.post_bias, at(c), K);
+    }
     float r[C][kVec];
-    {
-        float y[C][kVec] = {};
-        if (a.p.y) {
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-                load8<VEC>(reinterpret_cast<const _Float16 *>(a.p.y) + n * a.p.ld_y, (c * THREADS + t) * kVec, K, y[c]);
-            if (a.p.post_kind) {
-                float shift, inv;
-                moments<THREADS, C>(y, a.p.post_kind, a.p.eps, K, part[0], shift, inv);
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int c = 0; c < C; ++c)
-                    scale8<VEC>(y[c], shift, inv, a.p.post_weight, a.p.post_bias, (c * THREADS + t) * kVec, K);
-            }
+        for (int i = 0; i < kVec; ++i) r[c][i] = (float)rh[c][i];
+    if (a.p.y) {
+        float y[C][kVec];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) y[c][i] = (float)yh[c][i];
+        if (a.p.post_kind) {
+            float shift, inv;
+            moments<THREADS, C>(y, a.p.post_kind, a.p.eps, K, part[0], shift, inv);
+#pragma unroll
+            for (int c = 0; c < C; ++c) scale8h(y[c], shift, inv, a.p.post_weight, pw[c], a.p.post_bias, pb[c]);
         }
 #pragma unroll
-        for (int c = 0; c < C; ++c) update8<VEC>(a, n, (c * THREADS + t) * kVec, y[c], r[c]);
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                // Channels past the token's end stay 0 (a bias would make them otherwise).
+                float v = at(c) + i < K ? y[c][i] : 0.f;
+                if (a.p.gate) v *= gate_act((float)gh[c][i], a.p.gate_activation);
+                r[c][i] += a.p.scale * v;
+            }
+    }
+    if (a.p.pre_kind) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (a.p.pre_weight) pw[c] = load8h<VEC>(a.p.pre_weight, at(c), K);
+            if (a.p.pre_bias) pb[c] = load8h<VEC>(a.p.pre_bias, at(c), K);
+        }
     }
     if (a.p.residual_out) {
         _Float16 *row = reinterpret_cast<_Float16 *>(a.p.residual_out) + n * a.p.ld_residual_out;
@@ -218,8 +265,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
         float shift, inv;
         moments<THREADS, C>(r, a.p.pre_kind, a.p.eps, K, part[2], shift, inv);
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            scale8<VEC>(r[c], shift, inv, a.p.pre_weight, a.p.pre_bias, (c * THREADS + t) * kVec, K);
+        for (int c = 0; c < C; ++c) scale8h(r[c], shift, inv, a.p.pre_weight, pw[c], a.p.pre_bias, pb[c]);
     }
     half8v h[C];
     uint32_t top = 0;
@@ -345,7 +391,8 @@ int launch_norm(const usp_norm_args &p, int64_t N, int64_t K, void *stream) {
     const int64_t chunks = ceil_div(K, kVec);
     NormKernelFn fn;
     int threads;
-    if (chunks <= 256 * kMaxChunks) {
+    // Few tokens leave CUs idle: more threads with fewer chunks each then.
+    if (chunks <= 256 * (N <= 512 ? 1 : kMaxChunks)) {
         threads = 256;
         const int c = (int)ceil_div(chunks, threads);
         fn = vec ? norm_kernel_of<256, true>(c) : norm_kernel_of<256, false>(c);

@@ -18,7 +18,7 @@ namespace {
 // ---------------------------------------------------------------------------
 template <class V>
 __global__ __launch_bounds__(kLanes) void pack_kernel(ProductArgs a, uint8_t *__restrict__ xp) {
-    constexpr int S = V::kStepsPerTile, E = 16 / V::kBytes;  // elements of a chunk
+    constexpr int S = V::kStepsPerTile;
     const int lane = threadIdx.x;
     const int kt = blockIdx.x % a.KT;
     Job j;
@@ -28,33 +28,34 @@ __global__ __launch_bounds__(kLanes) void pack_kernel(ProductArgs a, uint8_t *__
     if (a.rows && n < j.n) x = a.rows[j.row0 + n];
     const bool real = n < j.n && x >= 0 && x < a.x_rows;
     const uint8_t *const row = a.X + (real ? x * a.ldx : 0);
-    const bool aligned = ((reinterpret_cast<uintptr_t>(a.X) | (uintptr_t)a.ldx) & 3) == 0;
     v4u32 v[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         typedef v4u32 __attribute__((aligned(4))) v4u32_a4;
         const int k = kt * kTileK + (64 * s + 16 * (lane >> 4)) / V::kBytes;
-        const uint8_t *const p = row + (int64_t)k * V::kBytes;
         v[s] = v4u32{0u, 0u, 0u, 0u};
         if (!real || k >= a.K) continue;
-        if (aligned && k + E <= a.K) {
-            v[s] = *reinterpret_cast<const v4u32_a4 *>(p);
-        } else if (aligned) {  // dwords that hold some of the row, their bytes past it cleared
-            const int left = (a.K - k) * V::kBytes;
+        // Five dwords hold the chunk whatever its alignment; only those that hold some of
+        // the row are read, and the bytes past it cleared.
+        const uint8_t *const p = row + (int64_t)k * V::kBytes;
+        const uint32_t sh = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
+        const uint32_t *const q = reinterpret_cast<const uint32_t *>(p - sh);
+        const int left = (a.K - k) * V::kBytes;  // of the row, from p
+        if (left >= 16) {
+            const v4u32 d = *reinterpret_cast<const v4u32_a4 *>(q);
+            const uint32_t e = q[sh ? 4 : 3];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (4 * i < left) {
-                    const uint32_t d = reinterpret_cast<const uint32_t *>(p)[i];
-                    v[s][i] = 4 * i + 4 <= left ? d : d & ((1u << (8 * (left - 4 * i))) - 1);
-                }
-        } else if (V::kBytes == 2) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + i < a.K) v[s][i / 2] |= (uint32_t) reinterpret_cast<const uint16_t *>(p)[i] << (16 * (i % 2));
+            for (int i = 0; i < 4; ++i) v[s][i] = __builtin_amdgcn_alignbyte(i < 3 ? d[i < 3 ? i + 1 : 3] : e, d[i], sh);
         } else {
+            uint32_t d[5];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (k + i < a.K) v[s][i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+            for (int i = 0; i < 5; ++i) d[i] = 4 * i < left + (int)sh ? q[i] : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = __builtin_amdgcn_alignbyte(d[i + 1], d[i], sh);
+                const int bytes = left - 4 * i;
+                v[s][i] = bytes >= 4 ? x : bytes > 0 ? x & ((1u << (8 * bytes)) - 1) : 0;
+            }
         }
     }
     v4u32 *const out = reinterpret_cast<v4u32 *>(xp + (((int64_t)j.tb * a.KT + kt) * S << 10));
@@ -316,7 +317,7 @@ ProductPlan plan_product(const ProductShape &s, int64_t N) {
         const int64_t tb = kBlock * k.nb, sets = ceil_div(s.RB, (int64_t)k.rows);
         const double wgs = std::ceil((double)sets * expected_groups(s, N, tb) / cus);
         const double chain = 0.75 * size * k.rows * (double)ceil_div(s.KT, (int64_t)k.waves);
-        const double cost = 2.6 + (k.nb > 1 ? 2.5 : 0.0) + 0.24 * std::min(16.0, wgs * k.waves) +
+        const double cost = 2.6 + (k.nb > 1 ? 3.5 : 0.0) + 0.24 * std::min(16.0, wgs * k.waves) +
                             std::max(chain, wgs * k.rows * (double)s.KT * k.record * size * (k.nb > 1 && value > 1 ? 1.2 : 1.0));
         consider({false, k.nb > 1, k.rows, k.waves, k.nb, sets, sets * most_groups(s, N, tb)}, cost);
     }
@@ -378,10 +379,26 @@ size_t packed_bytes(const ProductShape &s, int64_t N) {
 
 }  // namespace
 
+// Where in the workspace what lies: X packed, after the region that other products keep
+// cleared, then (8-bit matrices) fp16 tokens quantised, in rows that are read in place,
+// and their scales.
+struct ProductSpace {
+    size_t packed, codes, scales, end;
+    int64_t ld_codes;
+};
+static ProductSpace product_space(const ProductShape &s, int64_t N) {
+    ProductSpace w;
+    w.ld_codes = ceil_div(s.K, (int64_t)16) * 16;
+    w.packed = kCounterRegionBytes;
+    w.codes = w.packed + packed_bytes(s, N);
+    w.scales = w.codes + (s.A && s.value_bytes == 1 ? (size_t)(N * w.ld_codes) : 0);
+    w.end = w.scales + (s.A && s.value_bytes == 1 ? (size_t)(4 * N) : 0);
+    return w;
+}
+
 bool product_fits(const ProductShape &s, int64_t N) { return plan_product(s, N).grid < ((int64_t)1 << 31); }
 
-// X packed follows the region that other products keep cleared.
-size_t product_workspace_bytes(const ProductShape &s, int64_t N) { return kCounterRegionBytes + packed_bytes(s, N); }
+size_t product_workspace_bytes(const ProductShape &s, int64_t N) { return product_space(s, N).end; }
 
 std::string describe_product(const ProductShape &s, int64_t N) {
     const ProductPlan p = plan_product(s, N);
@@ -398,8 +415,23 @@ int launch_densify_q(const usp_matrix *A, void *Wd, int64_t ldw, void *stream) {
     return (int)hipGetLastError();
 }
 
-int launch_product(const ProductShape &s, const ProductCall &c, void *workspace, void *stream) {
+int launch_product(const ProductShape &s, const ProductCall &call, void *workspace, void *stream) {
     const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    const ProductSpace space = product_space(s, call.N);
+    uint8_t *const ws = reinterpret_cast<uint8_t *>(workspace);
+    ProductCall c = call;
+    if (c.quantize) {
+        usp_norm_args q = {};
+        q.residual = c.X;
+        q.ld_residual = c.ldx;
+        q.out_q = ws + space.codes;
+        q.ld_out_q = space.ld_codes;
+        q.out_scale = reinterpret_cast<float *>(ws + space.scales);
+        if (const int rc = launch_norm(q, c.N, s.K, stream)) return rc;
+        c.X = q.out_q;
+        c.ldx = q.ld_out_q;
+        c.x_scale = q.out_scale;
+    }
     ProductPlan p = plan_product(s, c.N);
     const int vb = s.value_bytes;
     ProductArgs a = {};
@@ -439,7 +471,7 @@ int launch_product(const ProductShape &s, const ProductCall &c, void *workspace,
     p.packed = p.packed || (reinterpret_cast<uintptr_t>(c.X) & 3) || a.ldx % 4 != 0 || (vb == 2 && s.K % 8 != 0) ||
                span > kMaxSpan / a.ldx;
     if (p.packed) {
-        uint8_t *const xp = reinterpret_cast<uint8_t *>(workspace) + kCounterRegionBytes;
+        uint8_t *const xp = ws + space.packed;
         const int64_t blocks = packed_blocks(s, c.N), most = kMaxGrid / s.KT;
         a.xp = xp;
         for (int64_t b0 = 0; b0 < blocks; b0 += most) {

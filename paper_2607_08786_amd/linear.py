@@ -158,9 +158,8 @@ def _linear_q(x: torch.Tensor, x_scale: Optional[torch.Tensor], handle: int, out
               workspace: Optional[torch.Tensor]) -> torch.Tensor:
     """act(x @ W^T + bias) + residual for the 8-bit weight behind ``handle``; x is [N, in_features], fp16, or int8
     with the tokens' scales."""
-    xq, x_scale = _tokens(x, x_scale)
     y = torch.empty((x.shape[0], out_features), dtype=torch.float16, device=x.device)
-    usp.usp_spmm_q(handle, xq, x_scale, y, workspace, bias, residual, activation)
+    usp.usp_spmm_q(handle, x, x_scale, y, workspace, bias, residual, activation)
     return y
 
 
@@ -267,6 +266,8 @@ class SparseLinearQ(SparseLinear):
         if N == 0:
             return x.new_empty((*lead, self.out_features), dtype=torch.float16)
         r2 = None if residual is None else _rows_of(residual, self.out_features)
+        if r2 is not None and r2.shape[0] != N:
+            raise ValueError("residual must have one row per token")
         y = _call(sparse_linear_q, _linear_q, x2, x_scale, self.matrix.handle, self.out_features, self.bias, r2,
                   usp.ACTIVATIONS[self.activation], self.workspace(N))
         return y.reshape(*lead, self.out_features)

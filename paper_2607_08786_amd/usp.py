@@ -345,11 +345,11 @@ def usp_quantize(X: torch.Tensor, Xq: torch.Tensor, x_scale: torch.Tensor, strea
                                        _stream_of(stream, dev)))
 
 
-def usp_spmm_q(handle: int, Xq: torch.Tensor, x_scale: torch.Tensor, Y: torch.Tensor,
+def usp_spmm_q(handle: int, Xq: torch.Tensor, x_scale: torch.Tensor | None, Y: torch.Tensor,
                workspace: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                residual: torch.Tensor | None = None, activation: str | int = "none", stream=None) -> None:
-    """Y = act(W X + bias) + residual with 8-bit weights and tokens (Xq [N, K] int8, x_scale [N]
-    fp32; Y, bias, residual as usp_spmm_ex)."""
+    """Y = act(W X + bias) + residual with 8-bit weights and tokens (Xq [N, K] int8 and x_scale [N] fp32, or fp16
+    Xq and None, which is quantised first; Y, bias, residual as usp_spmm_ex)."""
     dev = _cuda(Xq, "Xq")
     N, M = Y.shape
     act = ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
@@ -358,7 +358,7 @@ def usp_spmm_q(handle: int, Xq: torch.Tensor, x_scale: torch.Tensor, Y: torch.Te
         r_ptr, ldr = _matrix_ptr(residual, torch.float16, Y.shape, dev, "residual"), _ld(residual)
     ws_ptr, ws_bytes = _workspace(workspace)
     _check(load_library().usp_spmm_q(
-        handle, _matrix_ptr(Xq, torch.int8, (N, Xq.shape[1]), dev, "Xq"), _ld(Xq),
+        handle, _matrix_ptr(Xq, torch.float16 if x_scale is None else torch.int8, (N, Xq.shape[-1]), dev, "Xq"), _ld(Xq),
         _vector_ptr(x_scale, torch.float32, N, dev, "x_scale"), _matrix_ptr(Y, torch.float16, Y.shape, dev, "Y"), _ld(Y),
         N, _vector_ptr(bias, torch.float16, M, dev, "bias"), r_ptr, ldr, act, ws_ptr, ws_bytes, _stream_of(stream, dev)))
 
@@ -419,30 +419,26 @@ def usp_norm(residual: torch.Tensor, y: torch.Tensor | None = None, gate: torch.
     out_q, out_scale (8-bit tokens). All [N, K] fp16 but out_q (int8); gate [N, K], or [K] for all tokens; weights
     and biases [K]; out_scale [N] fp32. residual_out may be residual or y, out may be y."""
     dev = _cuda(residual, "residual")
-    N, K = residual.shape
+    N, K = shape = residual.shape
     f16 = torch.float16
-    a = usp_norm_args(scale=scale, eps=eps, post_kind=NORMS[post], pre_kind=NORMS[pre],
-                      gate_activation=GATES[gate_activation])
-    a.residual, a.ld_residual = _matrix_ptr(residual, f16, residual.shape, dev, "residual"), _ld(residual)
-    if y is not None:
-        a.y, a.ld_y = _matrix_ptr(y, f16, residual.shape, dev, "y"), _ld(y)
-    if gate is not None:
-        if gate.dim() == 1:
-            a.gate = _vector_ptr(gate, f16, K, dev, "gate")
-        else:
-            a.gate, a.ld_gate = _matrix_ptr(gate, f16, residual.shape, dev, "gate"), _ld(gate)
-    a.post_weight = _vector_ptr(post_weight, f16, K, dev, "post_weight")
-    a.post_bias = _vector_ptr(post_bias, f16, K, dev, "post_bias")
-    a.pre_weight = _vector_ptr(pre_weight, f16, K, dev, "pre_weight")
-    a.pre_bias = _vector_ptr(pre_bias, f16, K, dev, "pre_bias")
-    if residual_out is not None:
-        a.residual_out = _matrix_ptr(residual_out, f16, residual.shape, dev, "residual_out")
-        a.ld_residual_out = _ld(residual_out)
-    if out is not None:
-        a.out, a.ld_out = _matrix_ptr(out, f16, residual.shape, dev, "out"), _ld(out)
-    if out_q is not None:
-        a.out_q, a.ld_out_q = _matrix_ptr(out_q, torch.int8, residual.shape, dev, "out_q"), _ld(out_q)
-    a.out_scale = _vector_ptr(out_scale, torch.float32, N, dev, "out_scale")
+
+    def matrix(t, dtype, name):
+        return (None, 0) if t is None else (_matrix_ptr(t, dtype, shape, dev, name), _ld(t))
+
+    r_ptr, ld_r = matrix(residual, f16, "residual")
+    y_ptr, ld_y = matrix(y, f16, "y")
+    if gate is not None and gate.dim() == 1:
+        g_ptr, ld_g = _vector_ptr(gate, f16, K, dev, "gate"), 0
+    else:
+        g_ptr, ld_g = matrix(gate, f16, "gate")
+    ro_ptr, ld_ro = matrix(residual_out, f16, "residual_out")
+    o_ptr, ld_o = matrix(out, f16, "out")
+    q_ptr, ld_q = matrix(out_q, torch.int8, "out_q")
+    a = usp_norm_args(r_ptr, y_ptr, g_ptr, _vector_ptr(post_weight, f16, K, dev, "post_weight"),
+                      _vector_ptr(post_bias, f16, K, dev, "post_bias"), _vector_ptr(pre_weight, f16, K, dev, "pre_weight"),
+                      _vector_ptr(pre_bias, f16, K, dev, "pre_bias"), ro_ptr, o_ptr, q_ptr,
+                      _vector_ptr(out_scale, torch.float32, N, dev, "out_scale"), ld_r, ld_y, ld_g, ld_ro, ld_o, ld_q,
+                      scale, eps, NORMS[post], NORMS[pre], GATES[gate_activation])
     _check(load_library().usp_norm(ctypes.byref(a), N, K, dev.index, _stream_of(stream, dev)))
 
 
@@ -527,10 +523,10 @@ class SparseMatrixQ(SparseMatrix):
     def __init__(self, W: np.ndarray, mask: np.ndarray, scale: np.ndarray, device: int = 0):
         self._own(usp_encode_q(W, mask, scale, device), device)
 
-    def spmm(self, Xq: torch.Tensor, x_scale: torch.Tensor, Y: torch.Tensor | None = None, workspace=None, stream=None,
+    def spmm(self, Xq: torch.Tensor, x_scale: torch.Tensor | None = None, Y: torch.Tensor | None = None, workspace=None, stream=None,
              bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
              activation: str | int = "none") -> torch.Tensor:
-        """act(W X + bias) + residual of 8-bit tokens (usp_quantize); what the call creates is allocated as in
+        """act(W X + bias) + residual of 8-bit tokens (usp_quantize), or of fp16 tokens without x_scale; what the call creates is allocated as in
         SparseMatrix.spmm."""
         N = Xq.shape[0]
         if Y is None or workspace is None:
