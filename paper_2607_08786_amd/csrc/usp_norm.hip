@@ -24,6 +24,7 @@ struct NormArgs {
     int K;
 };
 
+constexpr int kMaxWaves = 16;  // wavefronts of a workgroup
 constexpr int kVec = 8;  // channels of a chunk: one 16-byte load of fp16
 
 struct Sum {
@@ -33,65 +34,75 @@ struct Max {
     __device__ static uint32_t apply(uint32_t a, uint32_t b) { return a > b ? a : b; }
 };
 
-// The reduction of v over the workgroup's THREADS threads, in every thread (the
+// One step of a wavefront's reduction: v with what the lanes that DPP control CTRL
+// names hold (0, the identity of both operations, where it names none).
+template <class Op, int CTRL, int ROWS, class T>
+__device__ inline T dpp_step(T v) {
+    const uint32_t u = __builtin_amdgcn_update_dpp(0u, __builtin_bit_cast(uint32_t, v), CTRL, ROWS, 0xF, ROWS == 0xF);
+    return Op::apply(v, __builtin_bit_cast(T, u));
+}
+
+// The reduction of v over the workgroup's threads, in every thread (the
 // same bits whatever the wavefronts' timing: fixed pairing, then wavefront order).
-// `part` holds one value per wavefront and is not in use on entry.
-template <class Op, int THREADS, class T>
+// Within a wavefront by DPP row shifts and broadcasts, whose last lane holds the
+// result. `part` holds one value per wavefront and is not in use on entry.
+template <class Op, class T>
 __device__ inline T reduce(T v, T *part) {
-#pragma unroll
-    for (int o = kLanes / 2; o > 0; o >>= 1) v = Op::apply(v, __shfl_xor(v, o, kLanes));
-    if (THREADS == kLanes) return v;
+    v = dpp_step<Op, 0x111, 0xF>(v);  // row_shr:1
+    v = dpp_step<Op, 0x112, 0xF>(v);  // row_shr:2
+    v = dpp_step<Op, 0x114, 0xF>(v);  // row_shr:4
+    v = dpp_step<Op, 0x118, 0xF>(v);  // row_shr:8
+    v = dpp_step<Op, 0x142, 0xA>(v);  // row_bcast:15
+    v = dpp_step<Op, 0x143, 0xC>(v);  // row_bcast:31
+    v = __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kLanes - 1));
     if ((threadIdx.x & (kLanes - 1)) == 0) part[threadIdx.x / kLanes] = v;
     __syncthreads();
     v = part[0];
-#pragma unroll
-    for (int w = 1; w < THREADS / kLanes; ++w) v = Op::apply(v, part[w]);
+    for (int w = 1; w < (int)blockDim.x / kLanes; ++w) v = Op::apply(v, part[w]);
     return v;
-}
-
-__device__ inline float gate_act(float g, int act) {
-    switch (act) {  // uniform
-        case USP_GATE_SIGMOID: return 1.f / (1.f + expf(-g));
-        case USP_GATE_TANH: return tanhf(g);
-        case USP_GATE_SILU: return g / (1.f + expf(-g));
-        default: return g;
-    }
 }
 
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 
-// Channels k .. k + 7 of a row of fp16, those < K (the others 0). VEC: 16-byte
-// aligned and K a multiple of 8.
+// A row of K elements of ES bytes as a buffer resource, empty where there is none:
+// loads past its end give zeros and stores there do nothing, so neither needs a
+// branch. (Behind branches the compiler waited for each of a norm's vectors before
+// it requested the next: 28.9 us for 2048 x 5120 with RMS norms and a gate.)
+// A resource's base is a multiple of 4 bytes; `sh` is how far the row starts behind it.
+struct Row {
+    __amdgpu_buffer_rsrc_t rsrc;
+    int sh;
+};
+template <int ES>
+__device__ inline Row row_of(const void *base, int64_t offset, int K, bool there = true) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(base) + offset * ES;
+    Row r;
+    r.sh = (int)(at & 3);
+    r.rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(at - r.sh), (short)0, base && there ? K * ES + r.sh : 0,
+                                               kBufferRsrcWord3);
+    return r;
+}
+
+// Channels k .. k + 7 of a row of fp16 (zeros past its end). VEC: 16-byte aligned
+// and K a multiple of 8.
 template <bool VEC>
-__device__ inline half8v load8h(const void *row, int k, int K) {
-    const _Float16 *p = reinterpret_cast<const _Float16 *>(row);
-    half8v h = {};
-    if (VEC) {
-        if (k < K) h = *reinterpret_cast<const half8v *>(p + k);
-    } else {
+__device__ inline half8v load8h(Row row, int k) {
+    if (VEC) return __builtin_bit_cast(half8v, __builtin_amdgcn_raw_buffer_load_b128(row.rsrc, 2 * k, 0, 0));
+    half8v h;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (k + i < K) h[i] = p[k + i];
-    }
+    for (int i = 0; i < kVec; ++i)
+        h[i] = __builtin_bit_cast(_Float16, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(row.rsrc, row.sh + 2 * (k + i), 0, 0));
     return h;
 }
 
 template <bool VEC>
-__device__ inline void load8(const void *row, int k, int K, float (&v)[kVec]) {
-    const half8v h = load8h<VEC>(row, k, K);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) v[i] = (float)h[i];
-}
-
-template <bool VEC>
-__device__ inline void store8(void *row, int k, int K, const half8v &h) {
-    _Float16 *p = reinterpret_cast<_Float16 *>(row);
+__device__ inline void store8(Row row, int k, const half8v &h) {
     if (VEC) {
-        if (k < K) *reinterpret_cast<half8v *>(p + k) = h;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, h), row.rsrc, 2 * k, 0, 0);
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
-            if (k + i < K) p[k + i] = h[i];
+            __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (_Float16)h[i]), row.rsrc, row.sh + 2 * (k + i), 0, 0);
     }
 }
 
@@ -99,9 +110,9 @@ __device__ inline uint32_t abs_bits(_Float16 h) { return __builtin_bit_cast(uint
 
 // 8-bit codes of 8 channels; inv is 0 for tokens whose codes are all 0.
 template <bool VEC>
-__device__ inline void store_codes(void *row, int k, int K, const half8v &h, float inv) {
-    int8_t *p = reinterpret_cast<int8_t *>(row);
-    uint32_t w[2] = {0, 0};
+__device__ inline void store_codes(Row row, int k, const half8v &h, float inv) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    u32x2 w = {0, 0};
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
         // inv 0 may meet a NaN or an infinity, whose product must not be converted.
@@ -109,11 +120,11 @@ __device__ inline void store_codes(void *row, int k, int K, const half8v &h, flo
         w[i / 4] |= (uint32_t)(uint8_t)c << (8 * (i % 4));
     }
     if (VEC) {
-        if (k < K) *reinterpret_cast<uint2 *>(p + k) = make_uint2(w[0], w[1]);
+        __builtin_amdgcn_raw_buffer_store_b64(w, row.rsrc, k, 0, 0);
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
-            if (k + i < K) p[k + i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+            __builtin_amdgcn_raw_buffer_store_b8((uint8_t)(w[i / 4] >> (8 * (i % 4))), row.rsrc, row.sh + k + i, 0, 0);
     }
 }
 
@@ -126,66 +137,8 @@ __device__ inline void code_scale(uint32_t top, float &scale, float &inv) {
     inv = finite && top ? 127.f / a : 0.f;
 }
 
-// v <- (v - shift) * inv * weight + bias
-template <bool VEC>
-__device__ inline void scale8(float (&v)[kVec], float shift, float inv, const void *weight, const void *bias, int k,
-                              int K) {
-    float w[kVec], b[kVec];
-    if (weight) load8<VEC>(weight, k, K, w);
-    if (bias) load8<VEC>(bias, k, K, b);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        float x = (v[i] - shift) * inv;
-        if (weight) x *= w[i];
-        if (bias) x += b[i];
-        v[i] = x;
-    }
-}
-
-// r of 8 channels from y's (normed already if a norm is asked for).
-template <bool VEC>
-__device__ inline void update8(const NormArgs &a, int64_t n, int k, const float (&y)[kVec], float (&r)[kVec]) {
-    load8<VEC>(reinterpret_cast<const _Float16 *>(a.p.residual) + n * a.p.ld_residual, k, a.K, r);
-    if (!a.p.y) return;
-    float g[kVec];
-    if (a.p.gate) load8<VEC>(reinterpret_cast<const _Float16 *>(a.p.gate) + n * a.p.ld_gate, k, a.K, g);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        float v = y[i];
-        if (a.p.gate) v *= gate_act(g[i], a.p.gate_activation);
-        r[i] += a.p.scale * v;
-    }
-}
-
-// Mean (layer norm) and 1 / sqrt(mean square of v - mean + eps) of the token whose
-// channels thread t holds in v[c] (from channel (c THREADS + t) 8); part: 2 areas.
-template <int THREADS, int C>
-__device__ inline void moments(const float (&v)[C][kVec], int kind, float eps, int K, float *part, float &shift,
-                               float &inv) {
-    shift = 0.f;
-    if (kind == USP_NORM_LAYER) {
-        float s = 0.f;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) s += v[c][i];
-        shift = reduce<Sum, THREADS>(s, part) / (float)K;
-    }
-    float s = 0.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int k = (c * THREADS + (int)threadIdx.x) * kVec;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            const float d = v[c][i] - shift;
-            if (k + i < K) s += d * d;  // channels past the token's end are 0, not the mean
-        }
-    }
-    inv = 1.f / sqrtf(reduce<Sum, THREADS>(s, part + THREADS / kLanes) / (float)K + eps);
-}
-
-// v <- (v - shift) * inv * w + b, with w and b at hand where there are any.
-__device__ inline void scale8h(float (&v)[kVec], float shift, float inv, bool weight, half8v w, bool bias, half8v b) {
+// v <- (v - shift) * inv * w + b, with w and b where there are any.
+__device__ inline void scale8(float (&v)[kVec], float shift, float inv, bool weight, half8v w, bool bias, half8v b) {
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
         float x = (v[i] - shift) * inv;
@@ -195,98 +148,167 @@ __device__ inline void scale8h(float (&v)[kVec], float shift, float inv, bool we
     }
 }
 
-template <int THREADS, int C, bool VEC>
-__global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
+// act(gate) of 8 channels. One branch for all of them.
+__device__ inline void gate8(float (&g)[kVec], int act) {
+    if (act == USP_GATE_NONE) return;
+    if (act == USP_GATE_TANH) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) g[i] = tanhf(g[i]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        const float s = 1.f / (1.f + expf(-g[i]));
+        g[i] = act == USP_GATE_SILU ? g[i] * s : s;
+    }
+}
+
+__device__ inline void to_float(half8v h, float (&v)[kVec]) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = (float)h[i];
+}
+
+// r += scale * act(gate) * y for the channels < K (past the token's end r stays 0,
+// which y after a norm's bias would change).
+__device__ inline void update8(const NormArgs &a, int k, const float (&y)[kVec], half8v gate, float (&r)[kVec]) {
+    float g[kVec];
+    to_float(gate, g);
+    gate8(g, a.p.gate ? a.p.gate_activation : USP_GATE_NONE);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        float v = k + i < a.K ? y[i] : 0.f;
+        if (a.p.gate) v *= g[i];
+        r[i] += a.p.scale * v;
+    }
+}
+
+// The rows of a token.
+struct Rows {
+    Row y, residual, gate, post_weight, post_bias, pre_weight, pre_bias;
+    __device__ Rows(const NormArgs &a, int64_t n)
+        : y(row_of<2>(a.p.y, n * a.p.ld_y, a.K)),
+          residual(row_of<2>(a.p.residual, n * a.p.ld_residual, a.K)),
+          gate(row_of<2>(a.p.gate, n * a.p.ld_gate, a.K)),
+          post_weight(row_of<2>(a.p.post_weight, 0, a.K, a.p.post_kind)),
+          post_bias(row_of<2>(a.p.post_bias, 0, a.K, a.p.post_kind)),
+          pre_weight(row_of<2>(a.p.pre_weight, 0, a.K, a.p.pre_kind)),
+          pre_bias(row_of<2>(a.p.pre_bias, 0, a.K, a.p.pre_kind)) {}
+};
+
+// Mean (layer norm) and 1 / sqrt(mean square of v - mean + eps) of the token whose
+// channels thread t holds in v[c] (from channel (c threads + t) 8); part: 2 areas.
+template <int C>
+__device__ inline void moments(const float (&v)[C][kVec], int kind, float eps, int K, float *part, float &shift,
+                               float &inv) {
+    shift = 0.f;
+    if (kind == USP_NORM_LAYER) {
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) s += v[c][i];
+        shift = reduce<Sum>(s, part) / (float)K;
+    }
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int k = (c * (int)blockDim.x + (int)threadIdx.x) * kVec;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float d = v[c][i] - shift;
+            if (k + i < K) s += d * d;  // channels past the token's end are 0, not the mean
+        }
+    }
+    inv = 1.f / sqrtf(reduce<Sum>(s, part + kMaxWaves) / (float)K + eps);
+}
+
+template <int MOST, int C, bool VEC>
+__global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a) {
     // Every reduction has its own values: no barrier between the end of one and the
     // start of the next.
-    __shared__ float part[4][THREADS / kLanes];
-    __shared__ uint32_t top_part[THREADS / kLanes];
+    __shared__ float part[4][kMaxWaves];
+    __shared__ uint32_t top_part[kMaxWaves];
     const int64_t n = blockIdx.x;
-    const int K = a.K, t = threadIdx.x;
-    auto at = [&](int c) -> int { return (c * THREADS + t) * kVec; };
+    const int K = a.K, t = threadIdx.x, threads = blockDim.x;
+    auto at = [&](int c) -> int { return (c * threads + t) * kVec; };
     // Everything that comes from HBM is requested first, the vectors of a norm before
-    // its reductions: one round trip to memory instead of one behind each reduction
-    // (2048 tokens of 5120 channels, layer norms on both sides, a gate: 35.0 us before).
+    // its reductions: one round trip to memory instead of one behind each reduction.
+    const Rows rows(a, n);
     half8v yh[C], rh[C], gh[C], pw[C], pb[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        if (a.p.y) yh[c] = load8h<VEC>(reinterpret_cast<const _Float16 *>(a.p.y) + n * a.p.ld_y, at(c), K);
-        rh[c] = load8h<VEC>(reinterpret_cast<const _Float16 *>(a.p.residual) + n * a.p.ld_residual, at(c), K);
-        if (a.p.gate) gh[c] = load8h<VEC>(reinterpret_cast<const _Float16 *>(a.p.gate) + n * a.p.ld_gate, at(c), K);
-        if (a.p.post_kind && a.p.post_weight) pw[c] = load8h<VEC>(a.p.post_weight, at(c), K);
-        if (a.p.post_kind && a.p.post_bias) pb[c] = load8h<VEC>(a.p.post_bias, at(c), K);
+        yh[c] = load8h<VEC>(rows.y, at(c));
+        rh[c] = load8h<VEC>(rows.residual, at(c));
+        gh[c] = load8h<VEC>(rows.gate, at(c));
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        pw[c] = load8h<VEC>(rows.post_weight, at(c));
+        pb[c] = load8h<VEC>(rows.post_bias, at(c));
     }
     float r[C][kVec];
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) r[c][i] = (float)rh[c][i];
     if (a.p.y) {
         float y[C][kVec];
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) y[c][i] = (float)yh[c][i];
+        for (int c = 0; c < C; ++c) to_float(yh[c], y[c]);
         if (a.p.post_kind) {
             float shift, inv;
-            moments<THREADS, C>(y, a.p.post_kind, a.p.eps, K, part[0], shift, inv);
+            moments<C>(y, a.p.post_kind, a.p.eps, K, part[0], shift, inv);
 #pragma unroll
-            for (int c = 0; c < C; ++c) scale8h(y[c], shift, inv, a.p.post_weight, pw[c], a.p.post_bias, pb[c]);
+            for (int c = 0; c < C; ++c) scale8(y[c], shift, inv, a.p.post_weight, pw[c], a.p.post_bias, pb[c]);
         }
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                // Channels past the token's end stay 0 (a bias would make them otherwise).
-                float v = at(c) + i < K ? y[c][i] : 0.f;
-                if (a.p.gate) v *= gate_act((float)gh[c][i], a.p.gate_activation);
-                r[c][i] += a.p.scale * v;
-            }
-    }
-    if (a.p.pre_kind) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (a.p.pre_weight) pw[c] = load8h<VEC>(a.p.pre_weight, at(c), K);
-            if (a.p.pre_bias) pb[c] = load8h<VEC>(a.p.pre_bias, at(c), K);
+            to_float(rh[c], r[c]);
+            update8(a, at(c), y[c], gh[c], r[c]);
         }
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c) to_float(rh[c], r[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        pw[c] = load8h<VEC>(rows.pre_weight, at(c));
+        pb[c] = load8h<VEC>(rows.pre_bias, at(c));
     }
     if (a.p.residual_out) {
-        _Float16 *row = reinterpret_cast<_Float16 *>(a.p.residual_out) + n * a.p.ld_residual_out;
+        const Row row = row_of<2>(a.p.residual_out, n * a.p.ld_residual_out, K);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             half8v h;
 #pragma unroll
             for (int i = 0; i < kVec; ++i) h[i] = (_Float16)r[c][i];
-            store8<VEC>(row, (c * THREADS + t) * kVec, K, h);
+            store8<VEC>(row, at(c), h);
         }
     }
     if (!a.p.out && !a.p.out_q) return;
     if (a.p.pre_kind) {
         float shift, inv;
-        moments<THREADS, C>(r, a.p.pre_kind, a.p.eps, K, part[2], shift, inv);
+        moments<C>(r, a.p.pre_kind, a.p.eps, K, part[2], shift, inv);
 #pragma unroll
-        for (int c = 0; c < C; ++c) scale8h(r[c], shift, inv, a.p.pre_weight, pw[c], a.p.pre_bias, pb[c]);
+        for (int c = 0; c < C; ++c) scale8(r[c], shift, inv, a.p.pre_weight, pw[c], a.p.pre_bias, pb[c]);
     }
     half8v h[C];
+    const Row out = row_of<2>(a.p.out, n * a.p.ld_out, K);
     uint32_t top = 0;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int k = (c * THREADS + t) * kVec;
+        const int k = at(c);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             h[c][i] = (_Float16)r[c][i];
             if (k + i < K) top = Max::apply(top, abs_bits(h[c][i]));
         }
-        if (a.p.out) store8<VEC>(reinterpret_cast<_Float16 *>(a.p.out) + n * a.p.ld_out, k, K, h[c]);
+        store8<VEC>(out, k, h[c]);
     }
     if (!a.p.out_q) return;
-    top = reduce<Max, THREADS>(top, top_part);
+    top = reduce<Max>(top, top_part);
     float scale, inv;
     code_scale(top, scale, inv);
     if (t == 0) a.p.out_scale[n] = scale;
+    const Row codes = row_of<1>(a.p.out_q, n * a.p.ld_out_q, K);
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-        store_codes<VEC>(reinterpret_cast<int8_t *>(a.p.out_q) + n * a.p.ld_out_q, (c * THREADS + t) * kVec, K, h[c], inv);
+    for (int c = 0; c < C; ++c) store_codes<VEC>(codes, at(c), h[c], inv);
 }
 
 // Tokens that do not fit the registers: every reduction reads its inputs again and
@@ -295,19 +317,22 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
 constexpr int kLoopThreads = 1024;
 
 __global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
-    __shared__ float part[4][kLoopThreads / kLanes];
-    __shared__ uint32_t top_part[kLoopThreads / kLanes];
+    __shared__ float part[4][kMaxWaves];
+    __shared__ uint32_t top_part[kMaxWaves];
     const int64_t n = blockIdx.x;
     const int K = a.K, k0 = threadIdx.x * kVec, step = kLoopThreads * kVec;
     float ys = 0.f, yi = 1.f, rs = 0.f, ri = 1.f;  // shift and factor of y and of r
-    auto load_y = [&](int k, float(&y)[kVec]) {
-        if (a.p.y) load8<false>(reinterpret_cast<const _Float16 *>(a.p.y) + n * a.p.ld_y, k, K, y);
-    };
+    const Rows rows(a, n);
+    auto load_y = [&](int k, float(&y)[kVec]) { to_float(load8h<false>(rows.y, k), y); };
     auto load_r = [&](int k, float(&r)[kVec]) {
-        float y[kVec] = {};
+        to_float(load8h<false>(rows.residual, k), r);
+        if (!a.p.y) return;
+        float y[kVec];
         load_y(k, y);
-        if (a.p.y && a.p.post_kind) scale8<false>(y, ys, yi, a.p.post_weight, a.p.post_bias, k, K);
-        update8<false>(a, n, k, y, r);
+        if (a.p.post_kind)
+            scale8(y, ys, yi, a.p.post_weight, load8h<false>(rows.post_weight, k), a.p.post_bias,
+                   load8h<false>(rows.post_bias, k));
+        update8(a, k, y, load8h<false>(rows.gate, k), r);
     };
     auto loop_moments = [&](auto load, int kind, float *area, float &shift, float &inv) {
         float m = 0.f;
@@ -318,7 +343,7 @@ __global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
                 load(k, v);
                 for (int i = 0; i < kVec; ++i) s += k + i < K ? v[i] : 0.f;
             }
-            m = reduce<Sum, kLoopThreads>(s, area) / (float)K;
+            m = reduce<Sum>(s, area) / (float)K;
         }
         float s = 0.f;
         for (int k = k0; k < K; k += step) {
@@ -326,7 +351,7 @@ __global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
             load(k, v);
             for (int i = 0; i < kVec; ++i) s += k + i < K ? (v[i] - m) * (v[i] - m) : 0.f;
         }
-        inv = 1.f / sqrtf(reduce<Sum, kLoopThreads>(s, area + kLoopThreads / kLanes) / (float)K + a.p.eps);
+        inv = 1.f / sqrtf(reduce<Sum>(s, area + kMaxWaves) / (float)K + a.p.eps);
         shift = m;
     };
     if (a.p.y && a.p.post_kind) loop_moments(load_y, a.p.post_kind, part[0], ys, yi);
@@ -335,7 +360,8 @@ __global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
     auto load_h = [&](int k, float(&r)[kVec], half8v &h) {  // h from r
         float v[kVec];
         for (int i = 0; i < kVec; ++i) v[i] = r[i];
-        if (a.p.pre_kind) scale8<false>(v, rs, ri, a.p.pre_weight, a.p.pre_bias, k, K);
+        if (a.p.pre_kind)
+            scale8(v, rs, ri, a.p.pre_weight, load8h<false>(rows.pre_weight, k), a.p.pre_bias, load8h<false>(rows.pre_bias, k));
         for (int i = 0; i < kVec; ++i) h[i] = (_Float16)v[i];
     };
     float scale = 0.f, inv = 0.f;
@@ -348,7 +374,7 @@ __global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
             load_h(k, r, h);
             for (int i = 0; i < kVec; ++i) top = k + i < K ? Max::apply(top, abs_bits(h[i])) : top;
         }
-        code_scale(reduce<Max, kLoopThreads>(top, top_part), scale, inv);
+        code_scale(reduce<Max>(top, top_part), scale, inv);
         if (threadIdx.x == 0) a.p.out_scale[n] = scale;
     }
     for (int k = k0; k < K; k += step) {
@@ -357,21 +383,20 @@ __global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
         load_r(k, r);
         for (int i = 0; i < kVec; ++i) r16[i] = (_Float16)r[i];
         if (normed) load_h(k, r, h);
-        if (a.p.residual_out)
-            store8<false>(reinterpret_cast<_Float16 *>(a.p.residual_out) + n * a.p.ld_residual_out, k, K, r16);
-        if (a.p.out) store8<false>(reinterpret_cast<_Float16 *>(a.p.out) + n * a.p.ld_out, k, K, h);
-        if (a.p.out_q) store_codes<false>(reinterpret_cast<int8_t *>(a.p.out_q) + n * a.p.ld_out_q, k, K, h, inv);
+        store8<false>(row_of<2>(a.p.residual_out, n * a.p.ld_residual_out, K), k, r16);
+        if (a.p.out) store8<false>(row_of<2>(a.p.out, n * a.p.ld_out, K), k, h);
+        if (a.p.out_q) store_codes<false>(row_of<1>(a.p.out_q, n * a.p.ld_out_q, K), k, h, inv);
     }
 }
 
 typedef void (*NormKernelFn)(NormArgs);
 
-template <int THREADS, bool VEC>
+template <int MOST, bool VEC>
 NormKernelFn norm_kernel_of(int chunks) {
-    return chunks <= 1 ? norm_kernel<THREADS, 1, VEC>
-         : chunks == 2 ? norm_kernel<THREADS, 2, VEC>
-         : chunks == 3 ? norm_kernel<THREADS, 3, VEC>
-                       : norm_kernel<THREADS, 4, VEC>;
+    return chunks <= 1 ? norm_kernel<MOST, 1, VEC>
+         : chunks == 2 ? norm_kernel<MOST, 2, VEC>
+         : chunks == 3 ? norm_kernel<MOST, 3, VEC>
+                       : norm_kernel<MOST, 4, VEC>;
 }
 
 constexpr int kMaxChunks = 4;
@@ -389,22 +414,20 @@ int launch_norm(const usp_norm_args &p, int64_t N, int64_t K, void *stream) {
                      aligned(p.out, p.ld_out, 2) && aligned(p.out_q, p.ld_out_q, 1) && aligned(p.post_weight, 0, 2) &&
                      aligned(p.post_bias, 0, 2) && aligned(p.pre_weight, 0, 2) && aligned(p.pre_bias, 0, 2);
     const int64_t chunks = ceil_div(K, kVec);
-    NormKernelFn fn;
-    int threads;
-    // Few tokens leave CUs idle: more threads with fewer chunks each then.
-    if (chunks <= 256 * (N <= 512 ? 1 : kMaxChunks)) {
-        threads = 256;
-        const int c = (int)ceil_div(chunks, threads);
-        fn = vec ? norm_kernel_of<256, true>(c) : norm_kernel_of<256, false>(c);
-    } else if (chunks <= 1024 * kMaxChunks) {
-        threads = 1024;
-        const int c = (int)ceil_div(chunks, threads);
-        fn = vec ? norm_kernel_of<1024, true>(c) : norm_kernel_of<1024, false>(c);
-    } else {
-        threads = kLoopThreads;
-        fn = norm_loop_kernel;
+    // Chunks per thread, then as many whole wavefronts as they need. Many tokens: about
+    // five wavefronts each; few leave CUs idle, so one chunk per thread.
+    constexpr int kMost = 512;
+    NormKernelFn fn = norm_loop_kernel;
+    int64_t threads = kLoopThreads;
+    if (chunks <= (int64_t)kLoopThreads * kMaxChunks) {
+        const int64_t c = std::max(ceil_div(chunks, (int64_t)kLoopThreads),
+                                   N > 512 ? std::min<int64_t>(kMaxChunks, ceil_div(chunks, (int64_t)320)) : 1);
+        threads = ceil_div(ceil_div(chunks, c), (int64_t)kLanes) * kLanes;
+        fn = threads <= kMost ? vec ? norm_kernel_of<kMost, true>((int)c) : norm_kernel_of<kMost, false>((int)c)
+             : vec            ? norm_kernel_of<kLoopThreads, true>((int)c)
+                              : norm_kernel_of<kLoopThreads, false>((int)c);
     }
-    hipLaunchKernelGGL(fn, dim3((unsigned)N), dim3(threads), 0, st, a);
+    hipLaunchKernelGGL(fn, dim3((unsigned)N), dim3((unsigned)threads), 0, st, a);
     return (int)hipGetLastError();
 }
 

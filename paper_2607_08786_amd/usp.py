@@ -20,9 +20,9 @@ USP_OK = 0
 _STATUS = {0: "USP_OK", 1: "USP_ERR_INVALID_ARG", 2: "USP_ERR_UNSUPPORTED", 3: "USP_ERR_OOM",
            4: "USP_ERR_HIP", 5: "USP_ERR_INTERNAL"}
 
-EXPORTED = ("usp_encode_q", "usp_decode_q", "usp_quantize", "usp_spmm_q", "usp_group_create", "usp_group_free",
-            "usp_group_workspace_size", "usp_group_plan", "usp_spmm_grouped", "usp_norm", "usp_encode", "usp_workspace_size", "usp_spmm", "usp_spmm_ex", "usp_spmm_noalloc", "usp_plan",
-            "usp_densify", "usp_decode", "usp_info", "usp_free", "usp_last_error")
+EXPORTED = ("usp_encode", "usp_encode_q", "usp_workspace_size", "usp_spmm", "usp_spmm_ex", "usp_spmm_noalloc", "usp_spmm_q",
+            "usp_quantize", "usp_plan", "usp_group_create", "usp_group_free", "usp_group_workspace_size", "usp_group_plan",
+            "usp_spmm_grouped", "usp_norm", "usp_decode_q", "usp_densify", "usp_decode", "usp_info", "usp_free", "usp_last_error")
 
 # Bytes of the per-GPU device scratch usp_spmm_noalloc uses (USP_NOALLOC_SCRATCH_BYTES).
 NOALLOC_SCRATCH_BYTES = 32 << 20
@@ -291,58 +291,60 @@ def usp_decode_q(handle: int):
     return W, mask, scale
 
 
-def _matrix_ptr(t: torch.Tensor, dtype: torch.dtype, shape, device: torch.device, name: str) -> int:
-    """The address of a 2-D operand after its checks."""
-    if t.dtype != dtype or t.dim() != 2 or t.stride(1) != 1 and t.shape[1] > 1:
-        raise TypeError(f"{name} must be a 2-D {dtype} tensor with unit inner stride")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
+def _matrix(t: torch.Tensor, dtype: torch.dtype, shape, dev: int, name: str):
+    """(address, row stride) of a 2-D operand after its checks. The stride of a single row is not looked at."""
+    if t.dtype is not dtype or len(shape) != 2 or t.dim() != 2:
+        raise TypeError(f"{name} must be a 2-D {dtype} tensor")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on GPU {dev}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}")
-    return t.data_ptr()
+    ld, inner = t.stride()
+    if inner != 1 and shape[1] > 1:
+        raise TypeError(f"{name} must have unit inner stride")
+    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])
 
 
-def _vector_ptr(t: torch.Tensor | None, dtype: torch.dtype, n: int, device: torch.device, name: str) -> int | None:
+def _vector(t: torch.Tensor | None, dtype: torch.dtype, n: int, dev: int, name: str) -> int | None:
     """The address of a contiguous vector of n values after its checks; None for None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or t.stride(0) != 1 and n > 1:
+    if t.dtype is not dtype or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise TypeError(f"{name} must be a contiguous {dtype} vector of {n} values")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on GPU {dev}")
     return t.data_ptr()
 
 
-def _ld(t: torch.Tensor) -> int:
-    """Row stride of a 2-D operand: with one row its stride is not looked at."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _stream_of(stream, dev: int) -> int:
+    """The stream of a call on GPU `dev`: its current one, unless one is given."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream_handle(stream)
 
 
-def _stream_of(stream, device: torch.device) -> int:
-    """The stream of a call on `device`: its current one, unless one is given."""
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index)
-    return _stream_handle(stream)
+def _workspace(ws: torch.Tensor | None, dev: int):
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"the workspace must be a contiguous tensor on GPU {dev}")
+    return ws.data_ptr(), ws.nbytes
 
 
-def _workspace(ws: torch.Tensor | None):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
-
-
-def _cuda(t: torch.Tensor, name: str) -> torch.device:
-    if not t.is_cuda:
+def _gpu(t: torch.Tensor, name: str) -> int:
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError(f"{name} must be on a GPU")
-    return t.device
+    return dev
 
 
 def usp_quantize(X: torch.Tensor, Xq: torch.Tensor, x_scale: torch.Tensor, stream=None) -> None:
     """Tokens in 8 bits: X [N, K] fp16 into Xq [N, K] int8 and x_scale [N] fp32."""
-    dev = _cuda(X, "X")
-    N, K = X.shape
-    _check(load_library().usp_quantize(_matrix_ptr(X, torch.float16, X.shape, dev, "X"), _ld(X), N, K,
-                                       _matrix_ptr(Xq, torch.int8, X.shape, dev, "Xq"), _ld(Xq),
-                                       _vector_ptr(x_scale, torch.float32, N, dev, "x_scale"), dev.index,
-                                       _stream_of(stream, dev)))
+    dev = _gpu(X, "X")
+    shape = X.shape
+    x, ldx = _matrix(X, torch.float16, shape, dev, "X")
+    q, ldq = _matrix(Xq, torch.int8, shape, dev, "Xq")
+    _check((_lib or load_library()).usp_quantize(x, ldx, shape[0], shape[1], q, ldq,
+                                                 _vector(x_scale, torch.float32, shape[0], dev, "x_scale"), dev,
+                                                 _stream_of(stream, dev)))
 
 
 def usp_spmm_q(handle: int, Xq: torch.Tensor, x_scale: torch.Tensor | None, Y: torch.Tensor,
@@ -350,17 +352,18 @@ def usp_spmm_q(handle: int, Xq: torch.Tensor, x_scale: torch.Tensor | None, Y: t
                residual: torch.Tensor | None = None, activation: str | int = "none", stream=None) -> None:
     """Y = act(W X + bias) + residual with 8-bit weights and tokens (Xq [N, K] int8 and x_scale [N] fp32, or fp16
     Xq and None, which is quantised first; Y, bias, residual as usp_spmm_ex)."""
-    dev = _cuda(Xq, "Xq")
+    dev = _gpu(Xq, "Xq")
+    y, ldy = _matrix(Y, torch.float16, Y.shape, dev, "Y")
     N, M = Y.shape
+    if Xq.dim() != 2 or Xq.shape[0] != N:
+        raise ValueError("Xq and Y must have the same number of tokens")
     act = ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
-    r_ptr, ldr = None, 0
-    if residual is not None:
-        r_ptr, ldr = _matrix_ptr(residual, torch.float16, Y.shape, dev, "residual"), _ld(residual)
-    ws_ptr, ws_bytes = _workspace(workspace)
-    _check(load_library().usp_spmm_q(
-        handle, _matrix_ptr(Xq, torch.float16 if x_scale is None else torch.int8, (N, Xq.shape[-1]), dev, "Xq"), _ld(Xq),
-        _vector_ptr(x_scale, torch.float32, N, dev, "x_scale"), _matrix_ptr(Y, torch.float16, Y.shape, dev, "Y"), _ld(Y),
-        N, _vector_ptr(bias, torch.float16, M, dev, "bias"), r_ptr, ldr, act, ws_ptr, ws_bytes, _stream_of(stream, dev)))
+    x, ldx = _matrix(Xq, torch.float16 if x_scale is None else torch.int8, Xq.shape, dev, "Xq")
+    r, ldr = (None, 0) if residual is None else _matrix(residual, torch.float16, Y.shape, dev, "residual")
+    ws, ws_bytes = _workspace(workspace, dev)
+    _check((_lib or load_library()).usp_spmm_q(
+        handle, x, ldx, _vector(x_scale, torch.float32, N, dev, "x_scale"), y, ldy, N,
+        _vector(bias, torch.float16, M, dev, "bias"), r, ldr, act, ws, ws_bytes, _stream_of(stream, dev)))
 
 
 def usp_group_create(handles) -> int:
@@ -392,21 +395,18 @@ def usp_spmm_grouped(group: int, X: torch.Tensor, offsets: torch.Tensor, Y: torc
     """Y[t] = row_weight[t] * act(W_e X[rows[t]] + bias[e]) for the rows offsets[e] <= t < offsets[e + 1] of
     expert e. X [*, K] fp16, or int8 with x_scale; offsets [E + 1] and rows [T] int32; bias [E, M] fp16;
     row_weight [T] fp32; Y [T, M] fp16."""
-    dev = _cuda(X, "X")
+    dev = _gpu(X, "X")
+    y, ldy = _matrix(Y, torch.float16, Y.shape, dev, "Y")
     T, M = Y.shape
     act = ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
-    x_type = torch.float16 if x_scale is None else torch.int8
+    x, ldx = _matrix(X, torch.float16 if x_scale is None else torch.int8, X.shape, dev, "X")
     E = offsets.shape[0] - 1
-    b_ptr, ldb = None, 0
-    if bias is not None:
-        b_ptr, ldb = _matrix_ptr(bias, torch.float16, (E, M), dev, "bias"), _ld(bias)
-    ws_ptr, ws_bytes = _workspace(workspace)
-    _check(load_library().usp_spmm_grouped(
-        group, _matrix_ptr(X, x_type, X.shape, dev, "X"), _ld(X), X.shape[0],
-        _vector_ptr(x_scale, torch.float32, X.shape[0], dev, "x_scale"), _vector_ptr(rows, torch.int32, T, dev, "rows"),
-        _vector_ptr(offsets, torch.int32, E + 1, dev, "offsets"), E, _matrix_ptr(Y, torch.float16, Y.shape, dev, "Y"),
-        _ld(Y), T, b_ptr, ldb, _vector_ptr(row_weight, torch.float32, T, dev, "row_weight"), act, ws_ptr, ws_bytes,
-        _stream_of(stream, dev)))
+    b, ldb = (None, 0) if bias is None else _matrix(bias, torch.float16, (E, M), dev, "bias")
+    ws, ws_bytes = _workspace(workspace, dev)
+    _check((_lib or load_library()).usp_spmm_grouped(
+        group, x, ldx, X.shape[0], _vector(x_scale, torch.float32, X.shape[0], dev, "x_scale"),
+        _vector(rows, torch.int32, T, dev, "rows"), _vector(offsets, torch.int32, E + 1, dev, "offsets"), E, y, ldy, T, b,
+        ldb, _vector(row_weight, torch.float32, T, dev, "row_weight"), act, ws, ws_bytes, _stream_of(stream, dev)))
 
 
 def usp_norm(residual: torch.Tensor, y: torch.Tensor | None = None, gate: torch.Tensor | None = None,
@@ -418,28 +418,28 @@ def usp_norm(residual: torch.Tensor, y: torch.Tensor | None = None, gate: torch.
     """r = residual + scale * act(gate) * post(y) into residual_out and h = pre(r) into out (fp16) and / or
     out_q, out_scale (8-bit tokens). All [N, K] fp16 but out_q (int8); gate [N, K], or [K] for all tokens; weights
     and biases [K]; out_scale [N] fp32. residual_out may be residual or y, out may be y."""
-    dev = _cuda(residual, "residual")
-    N, K = shape = residual.shape
+    dev = _gpu(residual, "residual")
+    shape = residual.shape
     f16 = torch.float16
-
-    def matrix(t, dtype, name):
-        return (None, 0) if t is None else (_matrix_ptr(t, dtype, shape, dev, name), _ld(t))
-
-    r_ptr, ld_r = matrix(residual, f16, "residual")
-    y_ptr, ld_y = matrix(y, f16, "y")
-    if gate is not None and gate.dim() == 1:
-        g_ptr, ld_g = _vector_ptr(gate, f16, K, dev, "gate"), 0
+    none = (None, 0)
+    res, ld_res = _matrix(residual, f16, shape, dev, "residual")
+    N, K = shape
+    yp, ld_y = none if y is None else _matrix(y, f16, shape, dev, "y")
+    if gate is None:
+        gp, ld_g = none
+    elif gate.dim() == 1:
+        gp, ld_g = _vector(gate, f16, K, dev, "gate"), 0
     else:
-        g_ptr, ld_g = matrix(gate, f16, "gate")
-    ro_ptr, ld_ro = matrix(residual_out, f16, "residual_out")
-    o_ptr, ld_o = matrix(out, f16, "out")
-    q_ptr, ld_q = matrix(out_q, torch.int8, "out_q")
-    a = usp_norm_args(r_ptr, y_ptr, g_ptr, _vector_ptr(post_weight, f16, K, dev, "post_weight"),
-                      _vector_ptr(post_bias, f16, K, dev, "post_bias"), _vector_ptr(pre_weight, f16, K, dev, "pre_weight"),
-                      _vector_ptr(pre_bias, f16, K, dev, "pre_bias"), ro_ptr, o_ptr, q_ptr,
-                      _vector_ptr(out_scale, torch.float32, N, dev, "out_scale"), ld_r, ld_y, ld_g, ld_ro, ld_o, ld_q,
+        gp, ld_g = _matrix(gate, f16, shape, dev, "gate")
+    ro, ld_ro = none if residual_out is None else _matrix(residual_out, f16, shape, dev, "residual_out")
+    op, ld_o = none if out is None else _matrix(out, f16, shape, dev, "out")
+    qp, ld_q = none if out_q is None else _matrix(out_q, torch.int8, shape, dev, "out_q")
+    a = usp_norm_args(res, yp, gp, _vector(post_weight, f16, K, dev, "post_weight"),
+                      _vector(post_bias, f16, K, dev, "post_bias"), _vector(pre_weight, f16, K, dev, "pre_weight"),
+                      _vector(pre_bias, f16, K, dev, "pre_bias"), ro, op, qp,
+                      _vector(out_scale, torch.float32, N, dev, "out_scale"), ld_res, ld_y, ld_g, ld_ro, ld_o, ld_q,
                       scale, eps, NORMS[post], NORMS[pre], GATES[gate_activation])
-    _check(load_library().usp_norm(ctypes.byref(a), N, K, dev.index, _stream_of(stream, dev)))
+    _check((_lib or load_library()).usp_norm(ctypes.byref(a), N, K, dev, _stream_of(stream, dev)))
 
 
 def _zeros(n: int, device: int, stream) -> torch.Tensor | None:
