@@ -69,9 +69,9 @@ usp_status usp_encode(const uint16_t *W, int64_t ldw, const uint8_t *mask, int64
                       int64_t M, int64_t K, int device, usp_matrix **out);
 
 /*
- * usp_workspace_size -- bytes of device workspace usp_spmm needs for this
- * handle and this N (0 when none). Returns 0 for a NULL handle. The
- * workspace holds the split rows' arrival counters and fp32 partials and,
+ * usp_workspace_size -- bytes of device workspace usp_spmm (of an 8-bit handle:
+ * usp_spmm_q) needs for this handle and this N (0 when none). Returns 0 for a NULL
+ * handle. The workspace of usp_spmm holds the split rows' arrival counters and fp32 partials and,
  * where the shared-decode or the wide kernel serves the call (33 to 256 tokens
  * on large layers, 320 and more on all), a copy of X rearranged into the order
  * its products read it (512 KT bytes per token, KT = ceil(K / 256), of at most
@@ -270,11 +270,12 @@ typedef struct usp_group usp_group; /* opaque; a list of encoded experts */
  * usp_group_create -- a group of E experts: handles of the same shape and value type (all
  * fp16 or all 8-bit) on one device, K <= USP_MAX_K_Q. An expert may occur more than once and
  * in several groups. The handles stay the caller's; while a group holds one, usp_free refuses
- * it. Blocking. 1 <= E <= 65536.
+ * it. Blocking. 1 <= E <= 4096.
  */
 usp_status usp_group_create(const usp_matrix *const *experts, int64_t E, usp_group **out);
 
-/* usp_group_free -- releases the group (not its experts). NULL is accepted. */
+/* usp_group_free -- releases the group (not its experts). NULL is accepted. The caller
+ * guarantees that no product on it is still in flight. */
 usp_status usp_group_free(usp_group *G);
 
 /* usp_group_workspace_size -- bytes of device workspace usp_spmm_grouped needs for T rows (0 when none, or for no

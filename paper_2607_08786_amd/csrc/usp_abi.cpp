@@ -486,7 +486,7 @@ usp_status usp_group_create(const usp_matrix *const *experts, int64_t E, usp_gro
     const std::string f("usp_group_create");
     if (out) *out = nullptr;
     if (!out || !experts) return usp::fail(USP_ERR_INVALID_ARG, f + ": null pointer");
-    if (E < 1 || E > 65536) return usp::fail(USP_ERR_INVALID_ARG, f + ": E must be 1 to 65536");
+    if (E < 1 || E > 4096) return usp::fail(USP_ERR_INVALID_ARG, f + ": E must be 1 to 4096");
     usp_group *G = new (std::nothrow) usp_group();
     if (!G) return usp::fail(USP_ERR_OOM, f + ": host allocation failed");
     std::vector<usp::ExpertRef> refs;

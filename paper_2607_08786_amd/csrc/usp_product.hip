@@ -311,9 +311,10 @@ ProductPlan plan_product(const ProductShape &s, int64_t N) {
         double record;  // us of a CU
     } kernels[] = {{1, 4, 1, .15}, {1, 8, 1, .15}, {2, 4, 1, .118}, {2, 8, 1, .118}, {4, 4, 1, .107}, {4, 8, 1, .107},
                    {1, 4, 2, .16}, {1, 8, 2, .16}, {2, 4, 2, .13},  {2, 8, 2, .13},  {4, 4, 2, .121}, {4, 8, 2, .121},
-                   {1, 4, 4, .27}, {2, 4, 4, .19}, {2, 8, 4, .21},  {4, 8, 4, .167}};
+                   {1, 4, 4, .27}, {2, 4, 4, .19}, {4, 8, 4, .167}};
     for (const auto &k : kernels) {
         if (k.nb == 4 && s.value_bytes != 1) continue;  // registers
+        if (ceil_div(s.KT, (int64_t)k.waves) >= kLanes) continue;  // a lane per tile's offset and one for the end
         const int64_t tb = kBlock * k.nb, sets = ceil_div(s.RB, (int64_t)k.rows);
         const double wgs = std::ceil((double)sets * expected_groups(s, N, tb) / cus);
         const double chain = 0.75 * size * k.rows * (double)ceil_div(s.KT, (int64_t)k.waves);
@@ -350,8 +351,7 @@ ProductKernelFn kernel_for(const ProductPlan &p) {
         if (p.nb == 4)
             return p.rows == 1   ? product_kernel<V, L, 1, 4, 4, true>
                    : p.rows == 4 ? product_kernel<V, L, 4, 8, 4, true>
-                   : p.waves == 4 ? product_kernel<V, L, 2, 4, 4, true>
-                                  : product_kernel<V, L, 2, 8, 4, true>;
+                                 : product_kernel<V, L, 2, 4, 4, true>;
     }
     return product_kernel_of<V, L, 2, true>(p.rows, p.waves);
 }

@@ -90,8 +90,8 @@ __global__ __launch_bounds__(R *kLanes, 2) void wide_product_kernel(ProductArgs 
     // with the tile's last steps its slot is free for tile kt + kRing.
     auto decode = [&](int kt, int g, uint8_t *slot, int buf) __attribute__((always_inline)) {
         if (g == 0) {
-            // At most a group's X and the next record have been requested since this one
-            // on every path.
+            // Since this record at least the other slots' records and a group's X have been
+            // requested, on every path.
             wait_loads<(kRing - 1) * L + kGroup * NB>();
             rs = V::state(slot + wave * kSlot, lane, (uint32_t)(wave * kSlot));
         }
@@ -134,6 +134,7 @@ __global__ __launch_bounds__(R *kLanes, 2) void wide_product_kernel(ProductArgs 
     };
 #pragma unroll
     for (int i = 0; i < kRing; ++i) request(i, slots[i]);
+    asm volatile("" ::: "memory");  // X after the records, as decode()'s wait counts them
 #pragma unroll
     for (int s = 0; s < kGroup; ++s) load_x(s, xb[s]);
     lds_barrier();  // the selector table

@@ -279,3 +279,94 @@ def test_module_of_a_routed_block(q):
     blocks64.close(r.cpu().numpy(), want[0], want[1])
     want, tol = blocks64.product(stands(h2), (codes * out_mask).double().cpu().numpy() * scale.double().cpu().numpy()[:, None])
     blocks64.close(z.cpu().numpy(), want, tol)
+
+
+@pytest.mark.parametrize("q", [False, True])
+@pytest.mark.parametrize("keep", [0.5, 1.0])
+def test_prefill(q, keep):
+    """Many ragged rows on the wide kernel, gathered, weighted, with a bias per expert; dense records too."""
+    E, M, K = 4, 700, 776
+    counts = [700, 0, 33, 515]
+    ends = np.cumsum([0] + counts)
+    T = int(ends[-1])
+    G, dense = group(101, E, M, K, q, keep)
+    assert G.plan(8192).startswith("wide-product")
+    X, s, x = inputs(102, 900, K, q)
+    rng = np.random.default_rng(103)
+    rows, w = rng.integers(0, 900, T), rng.random(T).astype(np.float32)
+    b = rng.standard_normal((E, M)).astype(np.float16)
+    for total in (T, 8192):  # the second with rows behind the last expert's
+        Y = torch.full((total, M), 7.0, dtype=torch.float16, device="cuda")
+        index = np.zeros(total, np.int64)
+        index[:T] = rows
+        weight = np.ones(total, np.float32)
+        weight[:T] = w
+        usp.usp_spmm_grouped(G.handle, X, i32(ends), Y, G.make_workspace(total), x_scale=s, rows=i32(index),
+                             bias=torch.from_numpy(b).cuda(), row_weight=torch.from_numpy(weight).cuda(), activation="silu")
+        want, tol = plain(dense, x, list(zip(ends[:-1], ends[1:])), K, q, index, b.astype(np.float64), "silu",
+                          weight.astype(np.float64), untouched=7.0)
+        blocks64.close(Y.cpu().numpy(), want, tol)
+
+
+
+# Every fp16 kernel of the planner at a small shape that takes it: (plan, M, K, T, experts), for records of up to 5 KB and
+# larger ones.
+KERNELS = [
+    ("product R=1 W=4 nb=1", 16, 206, 1, 1),
+    ("product R=1 W=4 nb=2", 37, 8860, 1432, 1),
+    ("product R=1 W=8 nb=1", 16, 1038, 2, 1),
+    ("product R=2 W=4 nb=1", 22, 814, 2041, 2),
+    ("product R=2 W=4 nb=2", 197, 747, 2045, 2),
+    ("product R=2 W=8 nb=1", 22, 1554, 2035, 2),
+    ("product R=2 W=8 nb=2", 68, 4491, 1979, 1),
+    ("product R=4 W=4 nb=1", 262, 635, 1363, 1),
+    ("product R=4 W=4 nb=2", 391, 520, 1906, 1),
+    ("product R=4 W=8 nb=1", 76, 1689, 1757, 1),
+    ("product R=4 W=8 nb=2", 141, 2892, 1955, 1),
+    ("wide-product R=4 nb=2", 434, 1085, 1759, 1),
+    ("wide-product R=4 nb=4", 2068, 365, 1978, 1),
+    ("wide-product R=8 nb=2", 2648, 246, 1510, 1),
+]
+KERNELS_DENSE = [
+    ("product R=1 W=4 nb=1", 16, 205, 1, 1),
+    ("product R=1 W=4 nb=2", 38, 6019, 1545, 1),
+    ("product R=1 W=8 nb=1", 16, 1053, 4, 1),
+    ("product R=1 W=8 nb=2", 38, 7405, 2042, 1),
+    ("product R=2 W=4 nb=1", 20, 815, 2043, 3),
+    ("product R=2 W=4 nb=2", 271, 670, 1655, 1),
+    ("product R=2 W=8 nb=1", 23, 1419, 2046, 1),
+    ("product R=2 W=8 nb=2", 56, 3078, 2041, 1),
+    ("product R=4 W=4 nb=1", 204, 604, 1816, 1),
+    ("product R=4 W=4 nb=2", 2622, 270, 476, 6),
+    ("product R=4 W=8 nb=1", 70, 1788, 1788, 1),
+    ("product R=4 W=8 nb=2", 132, 2371, 1838, 1),
+    ("wide-product R=4 nb=2", 306, 561, 1679, 1),
+    ("wide-product R=4 nb=4", 1095, 208, 1706, 2),
+]
+
+
+@pytest.mark.parametrize("keep,plan,M,K,T,E", [(0.5, *k) for k in KERNELS] + [(0.95, *k) for k in KERNELS_DENSE])
+def test_every_kernel(keep, plan, M, K, T, E):
+    G, dense = group(M + T, E, M, K, False, keep)
+    assert G.plan(T).startswith(plan + " "), G.plan(T)
+    ends = np.linspace(0, T, E + 1).astype(np.int64)
+    X, _, x = inputs(T, T, K, False)
+    Y = G.spmm(X, i32(ends))
+    want, tol = plain(dense, x, list(zip(ends[:-1], ends[1:])), K, False)
+    blocks64.close(Y.cpu().numpy(), want, tol)
+    assert torch.equal(G.spmm(X, i32(ends)), Y)  # bitwise reproducible
+
+
+def test_many_experts():
+    """More experts than a wavefront has lanes, several times over, nearly all without rows."""
+    G, dense = group(111, 3, 20, 256, False)
+    E = 1000
+    H = usp.ExpertGroup([G.experts[e % 3] for e in range(E)])
+    counts = np.zeros(E, np.int64)
+    counts[[0, 63, 64, 500, 999]] = [3, 20, 1, 40, 5]
+    ends = np.cumsum(np.concatenate([[0], counts]))
+    X, _, x = inputs(112, int(ends[-1]), 256, False)
+    want, tol = plain([dense[e % 3] for e in range(E)], x, list(zip(ends[:-1], ends[1:])), 256, False)
+    blocks64.close(H.spmm(X, i32(ends)).cpu().numpy(), want, tol)
+    with pytest.raises(usp.UspError):
+        usp.ExpertGroup([G.experts[0]] * 4097)

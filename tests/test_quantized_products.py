@@ -236,3 +236,124 @@ def test_module_captured():
         mod(half(70, 900, 515))
         assert torch.equal(mod(x), got)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("K", [64512, 65000, 129024])
+@pytest.mark.parametrize("N", [1, 50, 300])
+def test_most_columns(K, N):
+    """A wavefront's share of the column tiles up to what its offsets' lanes hold, and the limit itself."""
+    rng = np.random.default_rng(K)
+    W, mask = rng.integers(-3, 4, (20, K)).astype(np.int8), (rng.random((20, K)) < 0.5).astype(np.uint8)
+    A = usp.SparseMatrixQ(W, mask, np.full(20, 0.01, np.float32))
+    xq = torch.from_numpy(rng.integers(-3, 4, (N, K)).astype(np.int8)).cuda()
+    want, tol = blocks64.product(f64(xq), np.where(mask != 0, W, 0).astype(np.float64) * np.float64(np.float32(0.01)))
+    blocks64.close(A.spmm(xq, torch.ones(N, device="cuda")).cpu().numpy(), want, tol)
+
+
+def test_too_many_columns():
+    one = np.ones((1, usp.MAX_K_Q + 1), np.int8)
+    with pytest.raises(usp.UspError) as e:
+        usp.SparseMatrixQ(one, one.astype(np.uint8), np.ones(1, np.float32))
+    assert e.value.status == 2
+
+
+def test_fp16_tokens_are_quantised():
+    """Without scales the tokens are fp16: the bits of usp_quantize and the product after it."""
+    A, _ = matrix(80, 130, 701, 0.5)
+    for N in (1, 30, 500):
+        x = half(81 + N, N, 703)[:, 1:702]
+        xq, s = torch.empty(N, 701, dtype=torch.int8, device="cuda"), torch.empty(N, device="cuda")
+        usp.usp_quantize(x, xq, s)
+        assert torch.equal(A.spmm(x), A.spmm(xq, s))
+
+
+# Every kernel of the planner at a small shape that takes it: (plan, M, K, N), for records of up to 3 KB and larger ones.
+KERNELS = [
+    ("product R=1 W=4 nb=1", 16, 203, 1),
+    ("product R=1 W=4 nb=2", 76, 6750, 1371),
+    ("product R=1 W=4 nb=4", 68, 4185, 1992),
+    ("product R=1 W=8 nb=1", 16, 3101, 3),
+    ("product R=1 W=8 nb=2", 36, 12276, 1462),
+    ("product R=2 W=4 nb=1", 37, 370, 1365),
+    ("product R=2 W=4 nb=2", 390, 960, 1221),
+    ("product R=2 W=4 nb=4", 135, 1636, 1923),
+    ("product R=2 W=8 nb=1", 39, 1343, 1364),
+    ("product R=2 W=8 nb=2", 152, 8618, 1623),
+    ("product R=4 W=4 nb=1", 133, 629, 1654),
+    ("product R=4 W=4 nb=2", 1258, 620, 794),
+    ("product R=4 W=8 nb=1", 70, 1908, 1726),
+    ("product R=4 W=8 nb=2", 292, 2857, 1606),
+    ("product R=4 W=8 nb=4", 261, 1280, 1928),
+    ("wide-product R=4 nb=2", 941, 1144, 1652),
+    ("wide-product R=4 nb=4", 1058, 2886, 2004),
+    ("wide-product R=8 nb=2", 16605, 292, 130),
+    ("wide-product R=8 nb=4", 11706, 280, 518),
+]
+KERNELS_DENSE = [
+    ("product R=1 W=4 nb=1", 16, 200, 3),
+    ("product R=1 W=4 nb=2", 71, 4017, 1373),
+    ("product R=1 W=4 nb=4", 69, 2102, 1651),
+    ("product R=1 W=8 nb=1", 16, 1036, 2),
+    ("product R=1 W=8 nb=2", 36, 8044, 1381),
+    ("product R=2 W=4 nb=1", 36, 595, 1393),
+    ("product R=2 W=4 nb=2", 403, 660, 1231),
+    ("product R=2 W=4 nb=4", 137, 787, 1820),
+    ("product R=2 W=8 nb=1", 36, 1359, 1407),
+    ("product R=2 W=8 nb=2", 152, 3871, 1618),
+    ("product R=4 W=4 nb=1", 196, 603, 1765),
+    ("product R=4 W=4 nb=2", 1654, 608, 594),
+    ("product R=4 W=8 nb=1", 69, 1746, 1659),
+    ("product R=4 W=8 nb=2", 304, 1349, 1617),
+    ("product R=4 W=8 nb=4", 280, 850, 1816),
+    ("wide-product R=4 nb=2", 590, 770, 1739),
+    ("wide-product R=4 nb=4", 1201, 2678, 1738),
+    ("wide-product R=8 nb=2", 16822, 204, 129),
+    ("wide-product R=8 nb=4", 16545, 213, 277),
+]
+
+
+@pytest.mark.parametrize("keep,plan,M,K,N", [(0.5, *k) for k in KERNELS] + [(0.9, *k) for k in KERNELS_DENSE])
+def test_every_kernel(keep, plan, M, K, N):
+    A, w = matrix(M + N, M, K, keep, low=-128)
+    assert A.plan(N).startswith(plan + " "), A.plan(N)
+    xq, s, x = tokens(M, N, K)
+    b = half(3, M)
+    want, tol = blocks64.product(x, w, f64(b), "relu")
+    y = A.spmm(xq, s, bias=b, activation="relu")
+    blocks64.close(y.cpu().numpy(), want, tol)
+    assert torch.equal(A.spmm(xq, s, bias=b, activation="relu"), y)  # bitwise reproducible
+
+
+@pytest.mark.parametrize("N", [200, 900, 2048])
+@pytest.mark.parametrize("keep", [0.5, 0.9])
+def test_wide_kernels(N, keep):
+    """Many tokens on enough rows for every form of the wide kernel, with the whole epilogue."""
+    M, K = 2500, 515
+    A, w = matrix(95, M, K, keep)
+    xq, s, x = tokens(96, N, K)
+    b, r = half(97, M), half(98, N, M)
+    want, tol = blocks64.product(x, w, f64(b), "silu", f64(r))
+    blocks64.close(A.spmm(xq, s, bias=b, residual=r, activation="silu").cpu().numpy(), want, tol)
+    wide = torch.full((N, M + 7), 3.0, dtype=torch.float16, device="cuda")  # no vector stores
+    usp.usp_spmm_q(A.handle, xq, s, wide[:, 1:1 + M], A.make_workspace(N), b, r, "silu")
+    assert torch.equal(wide[:, 1:1 + M], A.spmm(xq, s, bias=b, residual=r, activation="silu"))
+    assert (wide[:, 0] == 3).all() and (wide[:, 1 + M:] == 3).all()
+
+
+def test_two_streams():
+    """Two modules' calls on two streams at once, and one module's."""
+    w = torch.randn(1500, 2000).half().cuda()
+    mask = torch.rand(1500, 2000) < 0.5
+    codes, scale = linear.quantize_rows(w, mask)
+    mod = linear.SparseLinearQ(codes, mask, scale)
+    xs = [half(100 + i, 64 + 200 * i, 2000) for i in range(2)]
+    want = [mod(x) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [[], []]
+    for _ in range(10):
+        for i, x in enumerate(xs):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(mod(x))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i]) for i in range(2) for g in got[i])
