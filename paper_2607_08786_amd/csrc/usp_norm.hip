@@ -11,6 +11,7 @@
 // the centred sum of squares (a one-pass variance would cancel where the mean is
 // large), the maximum. Tokens of more channels than the registers hold are read
 // again for every reduction instead.
+#include "usp_codes.h"
 #include "usp_device.h"
 #include "usp_internal.h"
 
@@ -106,8 +107,6 @@ __device__ inline void store8(Row row, int k, const half8v &h) {
     }
 }
 
-__device__ inline uint32_t abs_bits(_Float16 h) { return __builtin_bit_cast(uint16_t, h) & 0x7FFFu; }
-
 // 8-bit codes of 8 channels; inv is 0 for tokens whose codes are all 0.
 template <bool VEC>
 __device__ inline void store_codes(Row row, int k, const half8v &h, float inv) {
@@ -115,9 +114,7 @@ __device__ inline void store_codes(Row row, int k, const half8v &h, float inv) {
     u32x2 w = {0, 0};
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-        // inv 0 may meet a NaN or an infinity, whose product must not be converted.
-        const int c = inv == 0.f ? 0 : (int)rintf((float)h[i] * inv);
-        w[i / 4] |= (uint32_t)(uint8_t)c << (8 * (i % 4));
+        w[i / 4] |= code_bits(h[i], inv) << (8 * (i % 4));
     }
     if (VEC) {
         __builtin_amdgcn_raw_buffer_store_b64(w, row.rsrc, k, 0, 0);
@@ -126,15 +123,6 @@ __device__ inline void store_codes(Row row, int k, const half8v &h, float inv) {
         for (int i = 0; i < kVec; ++i)
             __builtin_amdgcn_raw_buffer_store_b8((uint8_t)(w[i / 4] >> (8 * (i % 4))), row.rsrc, row.sh + k + i, 0, 0);
     }
-}
-
-// Scale and reciprocal of a token's codes from the bits of its largest magnitude.
-// fp16 magnitudes order as their bits do, NaN above infinity above all others.
-__device__ inline void code_scale(uint32_t top, float &scale, float &inv) {
-    const float a = (float)__builtin_bit_cast(_Float16, (uint16_t)top);
-    const bool finite = top < 0x7C00u;
-    scale = finite ? a / 127.f : __builtin_nanf("");
-    inv = finite && top ? 127.f / a : 0.f;
 }
 
 // v <- (v - shift) * inv * w + b, with w and b where there are any.
@@ -297,7 +285,7 @@ __global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             h[c][i] = (_Float16)r[c][i];
-            if (k + i < K) top = Max::apply(top, abs_bits(h[c][i]));
+            if (k + i < K) top = Max::apply(top, magnitude_bits(h[c][i]));
         }
         store8<VEC>(out, k, h[c]);
     }
@@ -372,7 +360,7 @@ __global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
             half8v h;
             load_r(k, r);
             load_h(k, r, h);
-            for (int i = 0; i < kVec; ++i) top = k + i < K ? Max::apply(top, abs_bits(h[i])) : top;
+            for (int i = 0; i < kVec; ++i) top = k + i < K ? Max::apply(top, magnitude_bits(h[i])) : top;
         }
         code_scale(reduce<Max>(top, top_part), scale, inv);
         if (threadIdx.x == 0) a.p.out_scale[n] = scale;

@@ -2,6 +2,8 @@
 // fp16 and 8-bit values (include/usp.h, usp_spmm_q and usp_spmm_grouped).
 #include "usp_product.h"
 
+#include "usp_codes.h"
+
 #include <algorithm>
 #include <cmath>
 
@@ -61,6 +63,84 @@ __global__ __launch_bounds__(kLanes) void pack_kernel(ProductArgs a, uint8_t *__
     v4u32 *const out = reinterpret_cast<v4u32 *>(xp + (((int64_t)j.tb * a.KT + kt) * S << 10));
 #pragma unroll
     for (int s = 0; s < S; ++s) out[s * kLanes + lane] = v[s];
+}
+
+// ---------------------------------------------------------------------------
+// fp16 tokens in 8 bits, packed as pack_kernel<ValuesQ> packs usp_quantize's codes and
+// with the same bits, in one launch instead of two and without the codes in between.
+// A workgroup takes 4 tokens, a quarter of a block of 16, lane by lane, so that a
+// wavefront reads 512 bytes of each row and writes pieces of 64 bytes; whole blocks, a
+// wavefront to a token, left three quarters of the chip idle at 1024 tokens. Threads keep
+// the values of their first kKept chunks of 16 channels between the maximum and the
+// codes and read what follows again. VEC: rows of whole 16-byte vectors.
+// ---------------------------------------------------------------------------
+constexpr int kPackTokens = 4, kPackThreads = 1024, kKept = 2;
+
+template <bool VEC>
+__global__ __launch_bounds__(kPackThreads) void quantize_pack_kernel(const _Float16 *__restrict__ X, int64_t ldx, int N,
+                                                                     int K, int chunks, uint8_t *__restrict__ xp,
+                                                                     float *__restrict__ scales) {
+    constexpr int kStride = kPackThreads / kPackTokens, kWaves = kPackThreads / kLanes;
+    __shared__ uint32_t tops[kWaves][kPackTokens];
+    const int t = threadIdx.x % kPackTokens, first = threadIdx.x / kPackTokens;
+    const int64_t n = (int64_t)blockIdx.x * kPackTokens + t;
+    const _Float16 *const row = X + (n < N ? n : 0) * ldx;
+    const int cols = n < N ? K : 0;
+    // Channels 16 c .. 16 c + 15, zeros past the row.
+    auto load = [&](int c, half8 (&h)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int k = 16 * c + 8 * i;
+            h[i] = half8{};
+            if (VEC) {
+                if (k < cols) h[i] = *reinterpret_cast<const half8 *>(row + k);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (k + j < cols) h[i][j] = row[k + j];
+            }
+        }
+    };
+    half8 kept[kKept][2];
+    uint32_t top = 0;
+    auto larger = [&](const half8 (&h)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = max(top, magnitude_bits(h[i / 8][i % 8]));
+    };
+#pragma unroll
+    for (int i = 0; i < kKept; ++i) load(first + i * kStride, kept[i]);
+#pragma unroll
+    for (int i = 0; i < kKept; ++i) larger(kept[i]);
+    for (int c = first + kKept * kStride; c < chunks; c += kStride) {
+        half8 h[2];
+        load(c, h);
+        larger(h);
+    }
+#pragma unroll
+    for (int o = kPackTokens; o < kLanes; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, kLanes));
+    if (threadIdx.x % kLanes < kPackTokens) tops[threadIdx.x / kLanes][t] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = max(top, tops[w][t]);
+    float scale, inv;
+    code_scale(top, scale, inv);
+    if (threadIdx.x < kPackTokens && n < N) scales[n] = scale;
+    // Chunk c of a block's token: step c / 4, lane 16 (c % 4) + the token.
+    v4u32 *const out = reinterpret_cast<v4u32 *>(xp) + n / kBlock * kBlock * chunks + n % kBlock;
+    auto store = [&](int c, const half8 (&h)[2]) __attribute__((always_inline)) {
+        v4u32 v = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i / 4] |= code_bits(h[i / 8][i % 8], inv) << (8 * (i % 4));
+        out[(int64_t)c * kBlock] = v;
+    };
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+        if (first + i * kStride < chunks) store(first + i * kStride, kept[i]);
+    for (int c = first + kKept * kStride; c < chunks; c += kStride) {
+        half8 h[2];
+        load(c, h);
+        store(c, h);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -420,7 +500,16 @@ int launch_product(const ProductShape &s, const ProductCall &call, void *workspa
     const ProductSpace space = product_space(s, call.N);
     uint8_t *const ws = reinterpret_cast<uint8_t *>(workspace);
     ProductCall c = call;
-    if (c.quantize) {
+    ProductPlan p = plan_product(s, c.N);
+    const bool fused = c.quantize && p.packed;
+    if (fused) {
+        const bool vec = (reinterpret_cast<uintptr_t>(c.X) & 15) == 0 && c.ldx % 8 == 0 && s.K % 8 == 0;
+        c.x_scale = reinterpret_cast<const float *>(ws + space.scales);
+        hipLaunchKernelGGL(vec ? quantize_pack_kernel<true> : quantize_pack_kernel<false>,
+                           dim3((unsigned)(ceil_div(c.N, (int64_t)kBlock) * (kBlock / kPackTokens))), dim3(kPackThreads), 0, st,
+                           reinterpret_cast<const _Float16 *>(c.X), c.ldx, (int)c.N, (int)s.K,
+                           (int)(s.KT * kTileK / 16), ws + space.packed, reinterpret_cast<float *>(ws + space.scales));
+    } else if (c.quantize) {
         usp_norm_args q = {};
         q.residual = c.X;
         q.ld_residual = c.ldx;
@@ -432,7 +521,6 @@ int launch_product(const ProductShape &s, const ProductCall &call, void *workspa
         c.ldx = q.ld_out_q;
         c.x_scale = q.out_scale;
     }
-    ProductPlan p = plan_product(s, c.N);
     const int vb = s.value_bytes;
     ProductArgs a = {};
     if (s.G) {
@@ -474,7 +562,7 @@ int launch_product(const ProductShape &s, const ProductCall &call, void *workspa
         uint8_t *const xp = ws + space.packed;
         const int64_t blocks = packed_blocks(s, c.N), most = kMaxGrid / s.KT;
         a.xp = xp;
-        for (int64_t b0 = 0; b0 < blocks; b0 += most) {
+        for (int64_t b0 = 0; !fused && b0 < blocks; b0 += most) {
             a.job0 = (int)b0;
             hipLaunchKernelGGL(vb == 1 ? pack_kernel<ValuesQ> : pack_kernel<ValuesF16>,
                                dim3((unsigned)(std::min(most, blocks - b0) * s.KT)), dim3(kLanes), 0, st, a, xp);

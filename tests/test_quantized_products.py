@@ -357,3 +357,25 @@ def test_two_streams():
                 got[i].append(mod(x))
     torch.cuda.synchronize()
     assert all(torch.equal(g, want[i]) for i in range(2) for g in got[i])
+
+
+@pytest.mark.parametrize("K,ld,offset", [(8, 8, 0), (16, 24, 8), (100, 104, 0), (2056, 2056, 0), (8191, 8200, 0), (8200, 8208, 0),
+                                         (8200, 8201, 0), (8448, 8448, 4), (20000, 20008, 0), (33001, 33001, 1)])
+@pytest.mark.parametrize("N", [17, 35, 300])
+def test_fp16_tokens_at_every_width(K, ld, offset, N):
+    """Rows shorter and longer than what a thread keeps, aligned and not, in a buffer of NaN,
+    with tokens of zeros, of a NaN and of an infinity: the bits of the two calls."""
+    A, _ = matrix(90, 40, K, 0.5)
+    buf = torch.full((N * ld + offset + 64,), float("nan"), dtype=torch.float16, device="cuda")
+    x = torch.as_strided(buf, (N, K), (ld, 1), offset)
+    x.copy_(half(91, N, K))
+    x[2] = 0
+    x[5, K // 2] = float("nan")
+    x[N - 1, K - 1] = float("-inf")
+    xq, s = torch.empty(N, K, dtype=torch.int8, device="cuda"), torch.empty(N, device="cuda")
+    usp.usp_quantize(x, xq, s)
+    got, want = A.spmm(x), A.spmm(xq, s)
+    bad = torch.isnan(want).all(1).nonzero().flatten().tolist()
+    assert bad == [5, N - 1] and torch.isnan(got[bad]).all()
+    keep = [n for n in range(N) if n not in bad]
+    assert torch.equal(got[keep], want[keep])
