@@ -113,9 +113,7 @@ __device__ inline void store_codes(Row row, int k, const half8v &h, float inv) {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     u32x2 w = {0, 0};
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        w[i / 4] |= code_bits(h[i], inv) << (8 * (i % 4));
-    }
+    for (int i = 0; i < kVec; ++i) w[i / 4] |= code_bits(h[i], inv) << (8 * (i % 4));
     if (VEC) {
         __builtin_amdgcn_raw_buffer_store_b64(w, row.rsrc, k, 0, 0);
     } else {
@@ -125,18 +123,21 @@ __device__ inline void store_codes(Row row, int k, const half8v &h, float inv) {
     }
 }
 
-// v <- (v - shift) * inv * w + b, with w and b where there are any.
-__device__ inline void scale8(float (&v)[kVec], float shift, float inv, bool weight, half8v w, bool bias, half8v b) {
+// v <- (v - shift) * inv * w + b.
+__device__ inline void scale8(float (&v)[kVec], float shift, float inv, half8v w, half8v b) {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        float x = (v[i] - shift) * inv;
-        if (weight) x *= (float)w[i];
-        if (bias) x += (float)b[i];
-        v[i] = x;
-    }
+    for (int i = 0; i < kVec; ++i) v[i] = fmaf((v[i] - shift) * inv, (float)w[i], (float)b[i]);
+}
+
+// A weight or a gate that is not there is 1 (a bias that is not there reads as 0): a
+// select for a vector instead of a branch for a channel.
+__device__ inline half8v or_ones(bool there, half8v w) {
+    const v4u32 one = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
+    return there ? w : __builtin_bit_cast(half8v, one);
 }
 
 // act(gate) of 8 channels. One branch for all of them.
+// The reciprocal instruction's error is one unit in the last place.
 __device__ inline void gate8(float (&g)[kVec], int act) {
     if (act == USP_GATE_NONE) return;
     if (act == USP_GATE_TANH) {
@@ -146,7 +147,7 @@ __device__ inline void gate8(float (&g)[kVec], int act) {
     }
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-        const float s = 1.f / (1.f + expf(-g[i]));
+        const float s = __builtin_amdgcn_rcpf(1.f + expf(-g[i]));
         g[i] = act == USP_GATE_SILU ? g[i] * s : s;
     }
 }
@@ -158,16 +159,15 @@ __device__ inline void to_float(half8v h, float (&v)[kVec]) {
 
 // r += scale * act(gate) * y for the channels < K (past the token's end r stays 0,
 // which y after a norm's bias would change).
+template <bool VEC>
 __device__ inline void update8(const NormArgs &a, int k, const float (&y)[kVec], half8v gate, float (&r)[kVec]) {
     float g[kVec];
-    to_float(gate, g);
+    to_float(or_ones(a.p.gate, gate), g);
     gate8(g, a.p.gate ? a.p.gate_activation : USP_GATE_NONE);
+    if (VEC && k >= a.K) return;
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        float v = k + i < a.K ? y[i] : 0.f;
-        if (a.p.gate) v *= g[i];
-        r[i] += a.p.scale * v;
-    }
+    for (int i = 0; i < kVec; ++i)
+        if (VEC || k + i < a.K) r[i] = fmaf(a.p.scale, y[i] * g[i], r[i]);
 }
 
 // The rows of a token.
@@ -185,7 +185,7 @@ struct Rows {
 
 // Mean (layer norm) and 1 / sqrt(mean square of v - mean + eps) of the token whose
 // channels thread t holds in v[c] (from channel (c threads + t) 8); part: 2 areas.
-template <int C>
+template <int C, bool VEC>
 __device__ inline void moments(const float (&v)[C][kVec], int kind, float eps, int K, float *part, float &shift,
                                float &inv) {
     shift = 0.f;
@@ -201,11 +201,13 @@ __device__ inline void moments(const float (&v)[C][kVec], int kind, float eps, i
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int k = (c * (int)blockDim.x + (int)threadIdx.x) * kVec;
+        float q = 0.f;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             const float d = v[c][i] - shift;
-            if (k + i < K) s += d * d;  // channels past the token's end are 0, not the mean
+            if (VEC || k + i < K) q = fmaf(d, d, q);  // channels past the token's end are 0, not the mean
         }
+        s += !VEC || k < K ? q : 0.f;
     }
     inv = 1.f / sqrtf(reduce<Sum>(s, part + kMaxWaves) / (float)K + eps);
 }
@@ -241,14 +243,14 @@ __global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a) {
         for (int c = 0; c < C; ++c) to_float(yh[c], y[c]);
         if (a.p.post_kind) {
             float shift, inv;
-            moments<C>(y, a.p.post_kind, a.p.eps, K, part[0], shift, inv);
+            moments<C, VEC>(y, a.p.post_kind, a.p.eps, K, part[0], shift, inv);
 #pragma unroll
-            for (int c = 0; c < C; ++c) scale8(y[c], shift, inv, a.p.post_weight, pw[c], a.p.post_bias, pb[c]);
+            for (int c = 0; c < C; ++c) scale8(y[c], shift, inv, or_ones(a.p.post_weight, pw[c]), pb[c]);
         }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             to_float(rh[c], r[c]);
-            update8(a, at(c), y[c], gh[c], r[c]);
+            update8<VEC>(a, at(c), y[c], gh[c], r[c]);
         }
     } else {
 #pragma unroll
@@ -272,24 +274,28 @@ __global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a) {
     if (!a.p.out && !a.p.out_q) return;
     if (a.p.pre_kind) {
         float shift, inv;
-        moments<C>(r, a.p.pre_kind, a.p.eps, K, part[2], shift, inv);
+        moments<C, VEC>(r, a.p.pre_kind, a.p.eps, K, part[2], shift, inv);
 #pragma unroll
-        for (int c = 0; c < C; ++c) scale8(r[c], shift, inv, a.p.pre_weight, pw[c], a.p.pre_bias, pb[c]);
+        for (int c = 0; c < C; ++c) scale8(r[c], shift, inv, or_ones(a.p.pre_weight, pw[c]), pb[c]);
     }
     half8v h[C];
     const Row out = row_of<2>(a.p.out, n * a.p.ld_out, K);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) h[c][i] = (_Float16)r[c][i];
+        store8<VEC>(out, at(c), h[c]);
+    }
+    if (!a.p.out_q) return;
     uint32_t top = 0;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int k = at(c);
+        uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            h[c][i] = (_Float16)r[c][i];
-            if (k + i < K) top = Max::apply(top, magnitude_bits(h[c][i]));
-        }
-        store8<VEC>(out, k, h[c]);
+        for (int i = 0; i < kVec; ++i)
+            if (VEC || at(c) + i < K) m = Max::apply(m, magnitude_bits(h[c][i]));
+        top = Max::apply(top, !VEC || at(c) < K ? m : 0);
     }
-    if (!a.p.out_q) return;
     top = reduce<Max>(top, top_part);
     float scale, inv;
     code_scale(top, scale, inv);
@@ -318,9 +324,8 @@ __global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
         float y[kVec];
         load_y(k, y);
         if (a.p.post_kind)
-            scale8(y, ys, yi, a.p.post_weight, load8h<false>(rows.post_weight, k), a.p.post_bias,
-                   load8h<false>(rows.post_bias, k));
-        update8(a, k, y, load8h<false>(rows.gate, k), r);
+            scale8(y, ys, yi, or_ones(a.p.post_weight, load8h<false>(rows.post_weight, k)), load8h<false>(rows.post_bias, k));
+        update8<false>(a, k, y, load8h<false>(rows.gate, k), r);
     };
     auto loop_moments = [&](auto load, int kind, float *area, float &shift, float &inv) {
         float m = 0.f;
@@ -349,7 +354,7 @@ __global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
         float v[kVec];
         for (int i = 0; i < kVec; ++i) v[i] = r[i];
         if (a.p.pre_kind)
-            scale8(v, rs, ri, a.p.pre_weight, load8h<false>(rows.pre_weight, k), a.p.pre_bias, load8h<false>(rows.pre_bias, k));
+            scale8(v, rs, ri, or_ones(a.p.pre_weight, load8h<false>(rows.pre_weight, k)), load8h<false>(rows.pre_bias, k));
         for (int i = 0; i < kVec; ++i) h[i] = (_Float16)v[i];
     };
     float scale = 0.f, inv = 0.f;

@@ -76,6 +76,10 @@ class SparseLinear(torch.nn.Module):
         dev = linear.weight.device.index if linear.weight.is_cuda else None
         return cls(linear.weight, mask, linear.bias, activation, dev)
 
+    def _stream(self) -> int:
+        """The stream that forward enqueues its calls on."""
+        return usp.current_stream_handle()
+
     def workspace(self, N: int) -> Optional[torch.Tensor]:
         """A zero-filled workspace of at least usp_workspace_size(N) bytes for a call enqueued on the
         current stream.
@@ -100,7 +104,7 @@ class SparseLinear(torch.nn.Module):
                     self._graph_ws.append(ws)
                     return ws
             return self.matrix.make_workspace(N)
-        stream = usp.current_stream_handle()
+        stream = self._stream()
         ws = self._ws.get(stream)
         if ws is None or ws.numel() < need:
             ws = self._ws[stream] = self.matrix.make_workspace(N)
@@ -258,6 +262,9 @@ class SparseLinearQ(SparseLinear):
         codes, scale = quantize_rows(linear.weight, mask)
         return cls(codes, mask, scale, linear.bias, activation, dev)
 
+    def _stream(self) -> int:
+        return usp.current_stream_handle(self.matrix.device)
+
     def forward(self, x: Tokens, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         x, x_scale = x if isinstance(x, tuple) else (x, None)
         lead = x.shape[:-1]
@@ -308,6 +315,9 @@ class SparseExperts(SparseLinear):
     @classmethod
     def from_linear(cls, linear, mask, activation: str = "none"):
         raise TypeError("SparseExperts is made from the experts' weights")
+
+    def _stream(self) -> int:
+        return usp.current_stream_handle(self.matrix.device)
 
     def forward(self, x: Tokens, offsets: torch.Tensor, rows: Optional[torch.Tensor] = None,
                 row_weight: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -133,10 +133,10 @@ def _torch_stream(stream):
     return torch.cuda.ExternalStream(int(stream))
 
 
-def current_stream_handle() -> int:
-    """The hipStream_t of torch's current stream, without the Stream object of
-    torch.cuda.current_stream()."""
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+def current_stream_handle(device: int | None = None) -> int:
+    """The hipStream_t of torch's current stream (of the current device, or of `device`), without
+    the Stream object of torch.cuda.current_stream()."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
 
 
 def _stream_handle(stream) -> int | None:
@@ -318,7 +318,7 @@ def _vector(t: torch.Tensor | None, dtype: torch.dtype, n: int, dev: int, name: 
 
 def _stream_of(stream, dev: int) -> int:
     """The stream of a call on GPU `dev`: its current one, unless one is given."""
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream_handle(stream)
+    return current_stream_handle(dev) if stream is None else _stream_handle(stream)
 
 
 def _workspace(ws: torch.Tensor | None, dev: int):
