@@ -162,7 +162,7 @@ def _linear_q(x: torch.Tensor, x_scale: Optional[torch.Tensor], handle: int, out
               workspace: Optional[torch.Tensor]) -> torch.Tensor:
     """act(x @ W^T + bias) + residual for the 8-bit weight behind ``handle``; x is [N, in_features], fp16, or int8
     with the tokens' scales."""
-    y = torch.empty((x.shape[0], out_features), dtype=torch.float16, device=x.device)
+    y = x.new_empty((x.shape[0], out_features), dtype=torch.float16)
     usp.usp_spmm_q(handle, x, x_scale, y, workspace, bias, residual, activation)
     return y
 
@@ -185,9 +185,9 @@ def _block_norm(residual: torch.Tensor, y: Optional[torch.Tensor], gate: Optiona
                 quantize: bool) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """The residual's update, the norm of it (int8 if quantize) and the tokens' scales (empty if not)."""
     N, K = residual.shape
-    r = torch.empty((N, K), dtype=torch.float16, device=residual.device)
+    r = residual.new_empty((N, K))
     h = _int8_tokens(N, K, r.device) if quantize else torch.empty_like(r)
-    h_scale = torch.empty(N if quantize else 0, dtype=torch.float32, device=r.device)
+    h_scale = r.new_empty(N if quantize else 0, dtype=torch.float32)
     usp.usp_norm(residual, y, gate, scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, gate_activation,
                  residual_out=r, **(dict(out_q=h, out_scale=h_scale) if quantize else dict(out=h)))
     return r, h, h_scale
@@ -218,16 +218,19 @@ def _(residual, y, gate, scale, post, post_weight, post_bias, pre, pre_weight, p
 def _call(op, plain, *args):
     """The operator where a compiler or autograd has to see it; else the function itself, which spares an eager
     decode step the dispatcher (a small layer's kernels take less time than it)."""
-    if torch.compiler.is_compiling() or (torch.is_grad_enabled() and
-                                         any(isinstance(a, torch.Tensor) and a.requires_grad for a in args)):
+    if torch.compiler.is_compiling() or (torch.is_grad_enabled() and any(
+            [a.requires_grad for a in args if isinstance(a, torch.Tensor)])):
         return op(*args)
     return plain(*args)
 
 
 def _rows_of(x: torch.Tensor, width: int) -> torch.Tensor:
-    """x as fp16 [N, width] with unit inner stride."""
-    x = x.reshape(-1, width)
-    if x.dtype != torch.float16 or x.stride(1) != 1:
+    """x [*, width] as fp16 [N, width] with unit inner stride."""
+    if x.shape[-1] != width:
+        raise ValueError(f"expected {width} features, got {x.shape[-1]}")
+    if x.dim() != 2:
+        x = x.reshape(-1, width)
+    if x.dtype is not torch.float16 or x.stride(1) != 1:
         x = x.to(torch.float16).contiguous()
     return x
 
@@ -267,17 +270,16 @@ class SparseLinearQ(SparseLinear):
 
     def forward(self, x: Tokens, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         x, x_scale = x if isinstance(x, tuple) else (x, None)
-        lead = x.shape[:-1]
         x2 = _rows_of(x, self.in_features) if x_scale is None else x
         N = x2.shape[0]
         if N == 0:
-            return x.new_empty((*lead, self.out_features), dtype=torch.float16)
+            return x.new_empty((*x.shape[:-1], self.out_features), dtype=torch.float16)
         r2 = None if residual is None else _rows_of(residual, self.out_features)
         if r2 is not None and r2.shape[0] != N:
             raise ValueError("residual must have one row per token")
-        y = _call(sparse_linear_q, _linear_q, x2, x_scale, self.matrix.handle, self.out_features, self.bias, r2,
-                  usp.ACTIVATIONS[self.activation], self.workspace(N))
-        return y.reshape(*lead, self.out_features)
+        y = _call(sparse_linear_q, _linear_q, x2, x_scale, self.matrix.handle, self.out_features, self._buffers["bias"],
+                  r2, usp.ACTIVATIONS[self.activation], self.workspace(N))
+        return y if x.dim() == 2 else y.reshape(*x.shape[:-1], self.out_features)
 
 
 class SparseExperts(SparseLinear):
@@ -334,7 +336,7 @@ class SparseExperts(SparseLinear):
         if T == 0 or x2.shape[0] == 0:
             return x2.new_zeros((T, self.out_features), dtype=torch.float16)
         return _call(sparse_experts, _experts, x2, x_scale, offsets, rows, row_weight, self.matrix.handle,
-                     self.out_features, self.eight_bit, self.bias, usp.ACTIVATIONS[self.activation], self.workspace(T))
+                     self.out_features, self.eight_bit, self._buffers["bias"], usp.ACTIVATIONS[self.activation], self.workspace(T))
 
     def extra_repr(self) -> str:
         return (f"experts={len(self.matrix.experts)}, in_features={self.in_features}, "
@@ -374,10 +376,13 @@ class BlockNorm(torch.nn.Module):
         if r2.shape[0] == 0:
             h = (r2.to(torch.int8), r2.new_empty(0, dtype=torch.float32)) if quantize else r2.reshape(shape)
             return r2.reshape(shape), h
+        v = self._buffers  # each attribute of a module costs a search
         r, h, h_scale = _call(block_norm, _block_norm, r2, y2, g2, self.scale, "none" if y is None else self.post,
-                              self.post_weight, self.post_bias, self.pre, self.pre_weight, self.pre_bias, self.eps,
+                              v["post_weight"], v["post_bias"], self.pre, v["pre_weight"], v["pre_bias"], self.eps,
                               self.gate_activation, quantize)
-        return r.reshape(shape), (h, h_scale) if quantize else h.reshape(shape)
+        if len(shape) != 2:
+            r, h = r.reshape(shape), h if quantize else h.reshape(shape)
+        return r, (h, h_scale) if quantize else h
 
     def extra_repr(self) -> str:
         return (f"{self.features}, post={self.post}, pre={self.pre}, scale={self.scale}, eps={self.eps}, "

@@ -164,3 +164,47 @@ def test_quantize_rows():
     assert ((codes * scale[:, None] - kept).abs() <= scale[:, None] * (0.5 + 1e-4)).all()
     full = mask.any(1)
     assert (codes.abs().amax(1)[full] == 127).all()
+
+
+def test_workspaces_go_by_the_stream_of_the_layers_device(monkeypatch):
+    """A layer on another GPU than the current one enqueues on that GPU's current stream, and its workspaces are
+    told apart by it: two streams there must not share one."""
+    import types
+
+    import torch
+
+    from paper_2607_08786_amd import linear
+
+    current = {0: 5, 1: 100}
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: current[device], raising=False)
+    for cls in (linear.SparseLinearQ, linear.SparseExperts):
+        layer = cls.__new__(cls)
+        torch.nn.Module.__init__(layer)
+        layer.matrix = types.SimpleNamespace(device=1, workspace_size=lambda N: 16,
+                                             make_workspace=lambda N: torch.zeros(16, dtype=torch.uint8))
+        layer._ws, layer._graph_ws = {}, []
+        current[1] = 100
+        first = layer.workspace(1)
+        current[1] = 101
+        assert layer.workspace(1) is not first
+        current[1] = 100
+        assert layer.workspace(1) is first
+
+
+def test_width_of_the_input_is_checked():
+    import types
+
+    import torch
+
+    from paper_2607_08786_amd import linear
+
+    layer = linear.SparseLinearQ.__new__(linear.SparseLinearQ)
+    torch.nn.Module.__init__(layer)
+    layer.in_features, layer.out_features, layer.matrix = 8, 4, types.SimpleNamespace(device=0)
+    with pytest.raises(ValueError, match="features"):
+        layer(torch.zeros(2, 16, dtype=torch.float16))
+    norm = linear.BlockNorm(8, device="cpu")
+    with pytest.raises(ValueError, match="features"):
+        norm(torch.zeros(2, 16, dtype=torch.float16))
