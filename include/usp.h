@@ -166,10 +166,11 @@ usp_status usp_spmm_noalloc(const usp_matrix *A, const void *X, int64_t ldx, voi
                             int64_t N, void *stream);
 
 /*
- * usp_plan -- which kernel usp_spmm runs for this handle and N when X is 16-byte
- * aligned with ldx = K, as a short text ("row W=8", "chunk S=5 W=8 nb=1 grid=200",
- * "dma nb=4 tg=1 grid=1024", "fourwave passes=1 nt=2 grid=768",
- * "wide passes=1 nb=2 grid=216"), written to
+ * usp_plan -- which kernel usp_spmm (usp_spmm_q, of an 8-bit handle) runs for this
+ * handle and N when X is 16-byte aligned with ldx = K, as a short text ("row W=8",
+ * "chunk S=5 W=8 nb=1 grid=200", "dma nb=4 tg=1 grid=1024", "fourwave passes=1 nt=2
+ * grid=768", "wide passes=1 nb=2 grid=216"; of 8-bit handles and groups "product R=4
+ * W=4 nb=1 grid=448", "wide-product R=4 nb=4 grid=216"), written to
  * buf (at most len bytes with the terminating NUL, truncated if longer). For
  * tests and tuning; enqueues nothing. USP_ERR_INVALID_ARG for a NULL handle,
  * N < 1, or no buffer.
