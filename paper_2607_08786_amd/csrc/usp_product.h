@@ -285,6 +285,28 @@ __device__ inline float token_scale(const ProductArgs &a, int n) {
     return x >= 0 && x < a.xs_count ? a.xs[x] : 0.f;
 }
 
+// bias, activation, residual. The activations by the exponential and reciprocal
+// instructions: gelu(v) = v / (1 + exp(-2 u)), the tanh form's 0.5 (1 + tanh(u)), and
+// silu(v) = v / (1 + exp(-v)). An exponent's rounding moves the result by at most
+// 2^-23 |v| (x exp(-x) < 0.37). With the library's tanhf the activations of 13B FFN up
+// at 1024 tokens took 7.6 us more (93.2 against 85.6): all workgroups of a round come to them at once.
+__device__ inline floatx4 product_epilogue(const ProductArgs &a, floatx4 v, uint2 bias, uint2 res) {
+    if (a.bias) v = add_quad(v, bias);
+    if (a.act == USP_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = v[i] > 0.f ? v[i] : 0.f;
+    } else if (a.act != USP_ACT_NONE) {
+        constexpr float kLog2e = 1.4426950408889634f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float e = a.act == USP_ACT_SILU ? v[i] : 1.5957691216057308f * (v[i] + 0.044715f * v[i] * v[i] * v[i]);
+            v[i] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * e));
+        }
+    }
+    if (a.res) v = add_quad(v, res);
+    return v;
+}
+
 // Four outputs from their sums, rounded to fp16: scales, the fused epilogue and the
 // row's factor, the operands at hand.
 template <class V>
@@ -296,7 +318,7 @@ __device__ inline uint2 finished_quad(const ProductArgs &a, typename V::Acc acc,
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] *= xs * ws[i];
     }
-    if (a.e_flags & kEpiAny) v = epilogue(a, v, bias, res);
+    if (a.e_flags & kEpiAny) v = product_epilogue(a, v, bias, res);
     if (a.weight) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] *= weight;

@@ -165,3 +165,36 @@ def test_binding_refusals():
         usp.usp_norm(R, pre="rms")
     with pytest.raises(usp.UspError):
         usp.usp_norm(R, gate=R, out=out)
+
+
+@pytest.mark.parametrize("offset,gap", [(0, 0), (1, 0), (2, 3), (3, 1), (5, 2)])
+@pytest.mark.parametrize("K", [1, 7, 8, 33, 510, 1000, 5123, 8191, 32776, 33001])
+def test_every_alignment(K, offset, gap):
+    """Rows that start at any element, between NaN: the bits of aligned copies, and nothing written beside them."""
+    N = 3
+    g = torch.Generator(device="cuda").manual_seed(K)
+    rows = [torch.randn(N, K, device="cuda", generator=g).half() for _ in range(3)]
+    vectors = [torch.randn(K, device="cuda", generator=g).half() for _ in range(4)]
+
+    def placed(t, fill):
+        buf = torch.full((offset + t.numel() + N * gap + 16,), fill, dtype=t.dtype, device="cuda")
+        at = torch.as_strided(buf, t.shape, (t.shape[-1] + gap, 1)[-t.dim():], offset)
+        at.copy_(t)
+        return buf, at
+
+    def call(residual, y, gate, vec, r, h, q, s):
+        usp.usp_norm(residual, y, gate, 0.5, "layer", vec[0], vec[1], "rms", vec[2], vec[3], residual_out=r, out=h,
+                     out_q=q, out_scale=s, gate_activation="sigmoid")
+
+    want = [torch.empty(N, K, dtype=d, device="cuda") for d in (torch.float16, torch.float16, torch.int8)]
+    want_s = torch.empty(N, device="cuda")
+    call(*rows, vectors, *want, want_s)
+    outs = [placed(torch.zeros(N, K, dtype=d, device="cuda"), 9) for d in (torch.float16, torch.float16, torch.int8)]
+    s = torch.empty(N, device="cuda")
+    nan = float("nan")
+    call(*[placed(t, nan)[1] for t in rows], [placed(t, nan)[1] for t in vectors], *[o[1] for o in outs], s)
+    assert torch.equal(s, want_s) and torch.isfinite(s).all()
+    for (buf, at), w in zip(outs, want):
+        assert torch.equal(at, w)
+        at.fill_(9)
+        assert (buf == 9).all()
