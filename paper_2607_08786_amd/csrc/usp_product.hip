@@ -16,9 +16,12 @@ namespace {
 // 16 tb + n (of an expert's rows, gathered; zeros past them and past K). A load of
 // X in place touches 16 rows' segments of 64 bytes, which the memory pipeline takes
 // several times as long for as for 1 KB in one piece, and each column tile is
-// loaded once per row set. One wavefront per block of rows and column tile.
+// loaded once per row set. One wavefront per block of rows and column tile. ALIGNED: rows
+// at multiples of 4 bytes, without the fifth dword of every chunk (4096 gathered rows of
+// 2048 fp16 channels: 10.6 against 12.8 us; 32 x 5120 in 8 bits: 2.7 against 3.4). What
+// remains is a chain of latencies: offsets, row indices, X, the store.
 // ---------------------------------------------------------------------------
-template <class V>
+template <class V, bool ALIGNED>
 __global__ __launch_bounds__(kLanes) void pack_kernel(ProductArgs a, uint8_t *__restrict__ xp) {
     constexpr int S = V::kStepsPerTile;
     const int lane = threadIdx.x;
@@ -37,14 +40,16 @@ __global__ __launch_bounds__(kLanes) void pack_kernel(ProductArgs a, uint8_t *__
         const int k = kt * kTileK + (64 * s + 16 * (lane >> 4)) / V::kBytes;
         v[s] = v4u32{0u, 0u, 0u, 0u};
         if (!real || k >= a.K) continue;
-        // Five dwords hold the chunk whatever its alignment; only those that hold some of
-        // the row are read, and the bytes past it cleared.
+        // Five dwords hold the chunk whatever its alignment (four, ALIGNED); only those that
+        // hold some of the row are read, and the bytes past it cleared.
         const uint8_t *const p = row + (int64_t)k * V::kBytes;
-        const uint32_t sh = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
+        const uint32_t sh = ALIGNED ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
         const uint32_t *const q = reinterpret_cast<const uint32_t *>(p - sh);
         const int left = (a.K - k) * V::kBytes;  // of the row, from p
         if (left >= 16) {
             const v4u32 d = *reinterpret_cast<const v4u32_a4 *>(q);
+            v[s] = d;
+            if (ALIGNED) continue;
             const uint32_t e = q[sh ? 4 : 3];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[s][i] = __builtin_amdgcn_alignbyte(i < 3 ? d[i < 3 ? i + 1 : 3] : e, d[i], sh);
@@ -355,6 +360,12 @@ ProductKernelFn product_kernel_of(int rows, int waves) {
     return waves == 4 ? product_kernel<V, L, 4, 4, NB, PACKED> : product_kernel<V, L, 4, 8, NB, PACKED>;
 }
 
+typedef void (*PackKernelFn)(ProductArgs, uint8_t *);
+template <class V>
+PackKernelFn pack_kernel_of(bool aligned) {
+    return aligned ? pack_kernel<V, true> : pack_kernel<V, false>;
+}
+
 // The smallest built count of 1 KB transfers that covers every record, the decode's
 // reads past its values included.
 int record_loads(const ProductShape &s) {
@@ -573,7 +584,8 @@ int launch_product(const ProductShape &s, const ProductCall &call, void *workspa
     a.e_flags = epilogue_flags(c.ep);
     if (c.ldb % 4 != 0) a.e_flags &= ~kEpiBiasVec;
     const int64_t span = c.rows ? c.x_rows : std::min<int64_t>(c.N, kBlock * p.nb);
-    p.packed = p.packed || (reinterpret_cast<uintptr_t>(c.X) & 3) || a.ldx % 4 != 0 || (vb == 2 && s.K % 8 != 0) ||
+    const bool aligned = (reinterpret_cast<uintptr_t>(c.X) & 3) == 0 && a.ldx % 4 == 0;
+    p.packed = p.packed || !aligned || (vb == 2 && s.K % 8 != 0) ||
                span > kMaxSpan / a.ldx;
     if (p.packed) {
         uint8_t *const xp = ws + space.packed;
@@ -581,7 +593,7 @@ int launch_product(const ProductShape &s, const ProductCall &call, void *workspa
         a.xp = xp;
         for (int64_t b0 = 0; !fused && b0 < blocks; b0 += most) {
             a.job0 = (int)b0;
-            hipLaunchKernelGGL(vb == 1 ? pack_kernel<ValuesQ> : pack_kernel<ValuesF16>,
+            hipLaunchKernelGGL(vb == 1 ? pack_kernel_of<ValuesQ>(aligned) : pack_kernel_of<ValuesF16>(aligned),
                                dim3((unsigned)(std::min(most, blocks - b0) * s.KT)), dim3(kLanes), 0, st, a, xp);
         }
     }
