@@ -400,8 +400,10 @@ double expected_groups(const ProductShape &s, int64_t N, int64_t tb) {
 // at 64: 70B FFN 2 4 57.2, 4 8 51.2. Wide kernel: rounds of workgroups of KT tiles and an
 // epilogue; two of 4 row blocks share a CU. It wins from about 128 tokens on large
 // layers (70B FFN at 128 63.3 against 99.0) and 256 on small ones (13B attention at 128
-// 31.5 against 22.6, at 256 33.0 against 34.0).
-ProductPlan plan_product(const ProductShape &s, int64_t N) {
+// 31.5 against 22.6, at 256 33.0 against 34.0). Packing is a launch more, but not for fp16
+// tokens of 8-bit products (`quantize`), which take one either way (4999 x 4096, 21 tokens:
+// 12.4 us, 13.9 planned as packed at a cost; 3584 x 8192, 24: 14.5 and 16.1).
+ProductPlan plan_product(const ProductShape &s, int64_t N, bool quantize = false) {
     const double cus = s.num_cus > 0 ? s.num_cus : 256;
     const int loads = record_loads(s);
     const double value = s.value_bytes == 1 ? 1.0 : 1.8, size = value * (loads > 5 || (loads > 3 && s.value_bytes == 1) ? 1.5 : 1.0);
@@ -424,7 +426,7 @@ ProductPlan plan_product(const ProductShape &s, int64_t N) {
         const int64_t tb = kBlock * k.nb, sets = ceil_div(s.RB, (int64_t)k.rows);
         const double wgs = std::ceil((double)sets * expected_groups(s, N, tb) / cus);
         const double chain = 0.75 * size * k.rows * (double)ceil_div(s.KT, (int64_t)k.waves);
-        const double cost = 2.6 + (k.nb > 1 ? 3.5 : 0.0) + 0.24 * std::min(16.0, wgs * k.waves) +
+        const double cost = 2.6 + (k.nb > 1 && !quantize ? 3.5 : 0.0) + 0.24 * std::min(16.0, wgs * k.waves) +
                             std::max(chain, wgs * k.rows * (double)s.KT * k.record * size * (k.nb > 1 && value > 1 ? 1.2 : 1.0));
         consider({false, k.nb > 1, k.rows, k.waves, k.nb, sets, sets * most_groups(s, N, tb)}, cost);
     }
@@ -443,7 +445,7 @@ ProductPlan plan_product(const ProductShape &s, int64_t N) {
         // A group's last round is as full as its counts make it.
         const double tiles = s.G ? std::max(k.alone[q], wgs / slots * tile + 0.5 * k.alone[q])
                                  : full * tile + (rest <= 0 ? 0 : rest > cus ? tile : k.alone[q]);
-        const double cost = 7.5 + std::ceil(wgs / slots) * (1.0 + k.nb) + tiles * (double)s.KT;
+        const double cost = (quantize ? 4.0 : 7.5) + std::ceil(wgs / slots) * (1.0 + k.nb) + tiles * (double)s.KT;
         consider({true, true, k.rows, k.rows, k.nb, sets, sets * most_groups(s, N, tb)}, cost);
     }
     return best;
@@ -528,7 +530,7 @@ int launch_product(const ProductShape &s, const ProductCall &call, void *workspa
     const ProductSpace space = product_space(s, call.N);
     uint8_t *const ws = reinterpret_cast<uint8_t *>(workspace);
     ProductCall c = call;
-    ProductPlan p = plan_product(s, c.N);
+    ProductPlan p = plan_product(s, c.N, c.quantize);
     const bool fused = c.quantize && p.packed;
     if (fused) {
         const bool vec = (reinterpret_cast<uintptr_t>(c.X) & 15) == 0 && c.ldx % 8 == 0 && s.K % 8 == 0;
