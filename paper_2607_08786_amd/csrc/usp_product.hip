@@ -10,6 +10,35 @@
 namespace usp {
 namespace {
 
+// 16 bytes of a row from p, of which `left` >= 1 bytes remain; zeros past those. Five
+// dwords hold them whatever p's alignment (four, ALIGNED: p a multiple of 4); only those
+// that hold some of the row are read, and the bytes past it cleared.
+template <bool ALIGNED>
+__device__ inline v4u32 load_chunk(const uint8_t *p, int left) {
+    typedef v4u32 __attribute__((aligned(4))) v4u32_a4;
+    const uint32_t sh = ALIGNED ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
+    const uint32_t *const q = reinterpret_cast<const uint32_t *>(p - sh);
+    v4u32 v;
+    if (left >= 16) {
+        const v4u32 d = *reinterpret_cast<const v4u32_a4 *>(q);
+        if (ALIGNED) return d;
+        const uint32_t e = q[sh ? 4 : 3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbyte(i < 3 ? d[i < 3 ? i + 1 : 3] : e, d[i], sh);
+    } else {
+        uint32_t d[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) d[i] = 4 * i < left + (int)sh ? q[i] : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = __builtin_amdgcn_alignbyte(d[i + 1], d[i], sh);
+            const int bytes = left - 4 * i;
+            v[i] = bytes >= 4 ? x : bytes > 0 ? x & ((1u << (8 * bytes)) - 1) : 0;
+        }
+    }
+    return v;
+}
+
 // ---------------------------------------------------------------------------
 // X packed in the order of the products' B operands: block (tb KT + kt) S + s of
 // 1 KB, lane 16 g + n, holds bytes 64 s + 16 g .. + 15 of column tile kt of row
@@ -36,34 +65,10 @@ __global__ __launch_bounds__(kLanes) void pack_kernel(ProductArgs a, uint8_t *__
     v4u32 v[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        typedef v4u32 __attribute__((aligned(4))) v4u32_a4;
         const int k = kt * kTileK + (64 * s + 16 * (lane >> 4)) / V::kBytes;
         v[s] = v4u32{0u, 0u, 0u, 0u};
         if (!real || k >= a.K) continue;
-        // Five dwords hold the chunk whatever its alignment (four, ALIGNED); only those that
-        // hold some of the row are read, and the bytes past it cleared.
-        const uint8_t *const p = row + (int64_t)k * V::kBytes;
-        const uint32_t sh = ALIGNED ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
-        const uint32_t *const q = reinterpret_cast<const uint32_t *>(p - sh);
-        const int left = (a.K - k) * V::kBytes;  // of the row, from p
-        if (left >= 16) {
-            const v4u32 d = *reinterpret_cast<const v4u32_a4 *>(q);
-            v[s] = d;
-            if (ALIGNED) continue;
-            const uint32_t e = q[sh ? 4 : 3];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[s][i] = __builtin_amdgcn_alignbyte(i < 3 ? d[i < 3 ? i + 1 : 3] : e, d[i], sh);
-        } else {
-            uint32_t d[5];
-#pragma unroll
-            for (int i = 0; i < 5; ++i) d[i] = 4 * i < left + (int)sh ? q[i] : 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t x = __builtin_amdgcn_alignbyte(d[i + 1], d[i], sh);
-                const int bytes = left - 4 * i;
-                v[s][i] = bytes >= 4 ? x : bytes > 0 ? x & ((1u << (8 * bytes)) - 1) : 0;
-            }
-        }
+        v[s] = load_chunk<ALIGNED>(row + (int64_t)k * V::kBytes, (a.K - k) * V::kBytes);
     }
     v4u32 *const out = reinterpret_cast<v4u32 *>(xp + (((int64_t)j.tb * a.KT + kt) * S << 10));
 #pragma unroll
@@ -77,7 +82,8 @@ __global__ __launch_bounds__(kLanes) void pack_kernel(ProductArgs a, uint8_t *__
 // wavefront reads 512 bytes of each row and writes pieces of 64 bytes; whole blocks, a
 // wavefront to a token, left three quarters of the chip idle at 1024 tokens. Threads keep
 // the values of their first kKept chunks of 16 channels between the maximum and the
-// codes and read what follows again. VEC: rows of whole 16-byte vectors.
+// codes and read what follows again. VEC: rows of whole 16-byte vectors; others by
+// load_chunk (21 tokens of 4093 channels: 4.8 us, 6.2 channel by channel).
 // ---------------------------------------------------------------------------
 constexpr int kPackTokens = 4, kPackThreads = 1024, kKept = 2;
 
@@ -97,13 +103,11 @@ __global__ __launch_bounds__(kPackThreads) void quantize_pack_kernel(const _Floa
         for (int i = 0; i < 2; ++i) {
             const int k = 16 * c + 8 * i;
             h[i] = half8{};
-            if (VEC) {
-                if (k < cols) h[i] = *reinterpret_cast<const half8 *>(row + k);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (k + j < cols) h[i][j] = row[k + j];
-            }
+            if (k >= cols) continue;
+            if (VEC)
+                h[i] = *reinterpret_cast<const half8 *>(row + k);
+            else
+                h[i] = __builtin_bit_cast(half8, load_chunk<false>(reinterpret_cast<const uint8_t *>(row + k), 2 * (cols - k)));
         }
     };
     half8 kept[kKept][2];
