@@ -235,6 +235,13 @@ def _rows_of(x: torch.Tensor, width: int) -> torch.Tensor:
     return x
 
 
+def _codes_of(x: torch.Tensor, width: int) -> torch.Tensor:
+    """8-bit tokens [N, width]: rows are padded in memory, so a wrong width would not show by their stride."""
+    if x.dim() != 2 or x.shape[1] != width:
+        raise ValueError(f"expected 8-bit tokens [N, {width}], got {tuple(x.shape)}")
+    return x
+
+
 Tokens = Union[torch.Tensor, Tuple[torch.Tensor, torch.Tensor]]
 
 
@@ -270,7 +277,7 @@ class SparseLinearQ(SparseLinear):
 
     def forward(self, x: Tokens, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         x, x_scale = x if isinstance(x, tuple) else (x, None)
-        x2 = _rows_of(x, self.in_features) if x_scale is None else x
+        x2 = _rows_of(x, self.in_features) if x_scale is None else _codes_of(x, self.in_features)
         N = x2.shape[0]
         if N == 0:
             return x.new_empty((*x.shape[:-1], self.out_features), dtype=torch.float16)
@@ -331,7 +338,7 @@ class SparseExperts(SparseLinear):
             raise TypeError("8-bit tokens need 8-bit experts")
         if offsets.shape[0] != len(self.matrix.experts) + 1:
             raise ValueError("offsets must have one entry more than there are experts")
-        x2 = _rows_of(x, self.in_features) if x_scale is None else x
+        x2 = _rows_of(x, self.in_features) if x_scale is None else _codes_of(x, self.in_features)
         T = x2.shape[0] if rows is None else rows.shape[0]
         if T == 0 or x2.shape[0] == 0:
             return x2.new_zeros((T, self.out_features), dtype=torch.float16)

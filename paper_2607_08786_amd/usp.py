@@ -61,6 +61,10 @@ class usp_norm_args(ctypes.Structure):
 
 _lib = None
 
+# (M, K) of the live handles and groups made here. The C calls are given row strides alone: a product whose operands are
+# narrower than that would read or write beside them.
+_shapes: dict[int, tuple[int, int]] = {}
+
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     """Loads libusp.so (raises when it has not been built)."""
@@ -162,6 +166,7 @@ def usp_encode(W: np.ndarray, mask: np.ndarray, device: int = 0) -> int:
     M, K = W.shape
     h = ctypes.c_void_p()
     _check(load_library().usp_encode(W.ctypes.data, K, mask.ctypes.data, K, M, K, device, ctypes.byref(h)))
+    _shapes[h.value] = (M, K)
     return h.value
 
 
@@ -260,7 +265,12 @@ def usp_decode(handle: int):
 
 
 def usp_free(handle: int) -> None:
-    _check(load_library().usp_free(handle))
+    shape = _shapes.pop(handle, None)  # before the address can be another handle's
+    status = load_library().usp_free(handle)
+    if status != USP_OK:
+        if shape is not None:
+            _shapes[handle] = shape
+        _check(status)
 
 
 def usp_encode_q(W: np.ndarray, mask: np.ndarray, scale: np.ndarray, device: int = 0) -> int:
@@ -280,6 +290,7 @@ def usp_encode_q(W: np.ndarray, mask: np.ndarray, scale: np.ndarray, device: int
     h = ctypes.c_void_p()
     _check(load_library().usp_encode_q(W.ctypes.data, K, mask.ctypes.data, K, scale.ctypes.data, M, K, device,
                                        ctypes.byref(h)))
+    _shapes[h.value] = (M, K)
     return h.value
 
 
@@ -314,6 +325,20 @@ def _vector(t: torch.Tensor | None, dtype: torch.dtype, n: int, dev: int, name: 
     if t.get_device() != dev:
         raise ValueError(f"{name} must be on GPU {dev}")
     return t.data_ptr()
+
+
+def _shape_of(handle: int) -> tuple[int, int]:
+    """(M, K) of a matrix; an error for one that is not alive."""
+    shape = _shapes.get(handle)
+    if shape is None:
+        info = usp_info(handle)
+        shape = info["M"], info["K"]
+    return shape
+
+
+def _check_widths(shape, M: int, K: int) -> None:
+    if shape != (M, K):
+        raise UspError(1, f"the weight is {shape[0]} x {shape[1]}: X must have {shape[1]} columns (has {K}) and Y {shape[0]} (has {M})")
 
 
 def _stream_of(stream, dev: int) -> int:
@@ -351,12 +376,13 @@ def usp_spmm_q(handle: int, Xq: torch.Tensor, x_scale: torch.Tensor | None, Y: t
                workspace: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                residual: torch.Tensor | None = None, activation: str | int = "none", stream=None) -> None:
     """Y = act(W X + bias) + residual with 8-bit weights and tokens (Xq [N, K] int8 and x_scale [N] fp32, or fp16
-    Xq and None, which is quantised first; Y, bias, residual as usp_spmm_ex)."""
+    Xq and None, which is quantised first; Y, bias, residual as usp_spmm_ex). Xq and Y must have the weight's widths."""
     dev = _gpu(Xq, "Xq")
     y, ldy = _matrix(Y, torch.float16, Y.shape, dev, "Y")
     N, M = Y.shape
     if Xq.dim() != 2 or Xq.shape[0] != N:
         raise ValueError("Xq and Y must have the same number of tokens")
+    _check_widths(_shapes.get(handle) or _shape_of(handle), M, Xq.shape[1])
     act = ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
     x, ldx = _matrix(Xq, torch.float16 if x_scale is None else torch.int8, Xq.shape, dev, "Xq")
     r, ldr = (None, 0) if residual is None else _matrix(residual, torch.float16, Y.shape, dev, "residual")
@@ -370,10 +396,12 @@ def usp_group_create(handles) -> int:
     arr = (ctypes.c_void_p * len(handles))(*handles)
     g = ctypes.c_void_p()
     _check(load_library().usp_group_create(arr, len(handles), ctypes.byref(g)))
+    _shapes[g.value] = _shape_of(handles[0])
     return g.value
 
 
 def usp_group_free(group: int) -> None:
+    _shapes.pop(group, None)
     _check(load_library().usp_group_free(group))
 
 
@@ -394,12 +422,15 @@ def usp_spmm_grouped(group: int, X: torch.Tensor, offsets: torch.Tensor, Y: torc
                      row_weight: torch.Tensor | None = None, activation: str | int = "none", stream=None) -> None:
     """Y[t] = row_weight[t] * act(W_e X[rows[t]] + bias[e]) for the rows offsets[e] <= t < offsets[e + 1] of
     expert e. X [*, K] fp16, or int8 with x_scale; offsets [E + 1] and rows [T] int32; bias [E, M] fp16;
-    row_weight [T] fp32; Y [T, M] fp16."""
+    row_weight [T] fp32; Y [T, M] fp16. X and Y must have the experts' widths."""
     dev = _gpu(X, "X")
     y, ldy = _matrix(Y, torch.float16, Y.shape, dev, "Y")
     T, M = Y.shape
     act = ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
     x, ldx = _matrix(X, torch.float16 if x_scale is None else torch.int8, X.shape, dev, "X")
+    shape = _shapes.get(group)
+    if shape is not None:  # else the call refuses the group, or it was made without this binding
+        _check_widths(shape, M, X.shape[1])
     E = offsets.shape[0] - 1
     b, ldb = (None, 0) if bias is None else _matrix(bias, torch.float16, (E, M), dev, "bias")
     ws, ws_bytes = _workspace(workspace, dev)
