@@ -215,13 +215,35 @@ def _(residual, y, gate, scale, post, post_weight, post_bias, pre, pre_weight, p
     return residual.new_empty((N, K)), h, residual.new_empty(N if quantize else 0, dtype=torch.float32)
 
 
+# What a thread's dispatch keys are where nothing stands between a call and its kernel (the second under inference_mode):
+# tracers, dispatch modes and function transforms each add theirs.
+_NOTHING_BETWEEN = {
+    torch._C.DispatchKeySet(torch._C.DispatchKey.BackendSelect).raw_repr(),
+    (torch._C.DispatchKeySet(torch._C.DispatchKey.BackendSelect) |
+     torch._C.DispatchKeySet(torch._C.DispatchKey.ADInplaceOrView)).raw_repr(),
+}
+_PLAIN_VALUES = {type(None), bool, int, float, str}
+_PLAIN_TENSORS = {torch.Tensor, torch.nn.Parameter}
+
+
+def _seen(args) -> bool:
+    """Whether anything has to see the call as an operator: a compiler, a tracer, a mode, a transform, a tensor subclass,
+    autograd, or a view that only the dispatcher resolves. The function itself writes memory that none of them knows of."""
+    if (torch.compiler.is_compiling() or torch._C._dispatch_tls_local_include_set().raw_repr() not in _NOTHING_BETWEEN
+            or torch._C._len_torch_function_stack()):
+        return True
+    grad = torch.is_grad_enabled()
+    for a in args:
+        t = type(a)
+        if t not in _PLAIN_VALUES and (t not in _PLAIN_TENSORS or a.is_neg() or (grad and a.requires_grad)):
+            return True
+    return False
+
+
 def _call(op, plain, *args):
-    """The operator where a compiler or autograd has to see it; else the function itself, which spares an eager
-    decode step the dispatcher (a small layer's kernels take less time than it)."""
-    if torch.compiler.is_compiling() or (torch.is_grad_enabled() and any(
-            [a.requires_grad for a in args if isinstance(a, torch.Tensor)])):
-        return op(*args)
-    return plain(*args)
+    """The operator where anything has to see it; else the function itself, which spares an eager decode step the
+    dispatcher (a small layer's kernels take less time than it)."""
+    return op(*args) if _seen(args) else plain(*args)
 
 
 def _rows_of(x: torch.Tensor, width: int) -> torch.Tensor:
