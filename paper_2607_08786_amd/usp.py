@@ -65,6 +65,9 @@ _lib = None
 # narrower than that would read or write beside them.
 _shapes: dict[int, tuple[int, int]] = {}
 
+# Live handles whose owners are gone while a group held them: freed with the last of their groups.
+_ownerless: set[int] = set()
+
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     """Loads libusp.so (raises when it has not been built)."""
@@ -271,6 +274,7 @@ def usp_free(handle: int) -> None:
         if shape is not None:
             _shapes[handle] = shape
         _check(status)
+    _ownerless.discard(handle)
 
 
 def usp_encode_q(W: np.ndarray, mask: np.ndarray, scale: np.ndarray, device: int = 0) -> int:
@@ -403,6 +407,36 @@ def usp_group_create(handles) -> int:
 def usp_group_free(group: int) -> None:
     _shapes.pop(group, None)
     _check(load_library().usp_group_free(group))
+    _free_ownerless(list(_ownerless))
+
+
+def _free_ownerless(handles) -> None:
+    """Frees those of the ownerless handles that no group holds any more."""
+    for h in handles:
+        try:
+            _ownerless.remove(h)
+        except KeyError:  # another thread has it
+            continue
+        try:
+            usp_free(h)
+        except UspError:
+            if _alive(h):
+                _ownerless.add(h)
+
+
+def _alive(handle: int) -> bool:
+    try:
+        usp_info(handle)
+    except UspError:
+        return False
+    return True
+
+
+def _owner_gone(handle: int) -> None:
+    """For a handle that could not be freed at its owner's end: the collector takes an owner and the group in any order."""
+    if _alive(handle):
+        _ownerless.add(handle)
+        _free_ownerless([handle])  # the group may be gone by now
 
 
 def usp_group_workspace_size(group: int, T: int) -> int:
@@ -543,7 +577,10 @@ class SparseMatrix:
 
     def __del__(self):
         try:
-            self.free()
+            try:
+                self.free()
+            except UspError:
+                _owner_gone(self.handle)
         except Exception:
             pass
 
