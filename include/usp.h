@@ -113,7 +113,7 @@ usp_status usp_spmm(const usp_matrix *A, const void *X, int64_t ldx, void *Y, in
 /* Activation of usp_spmm_ex, applied after the bias. */
 typedef enum {
     USP_ACT_NONE = 0,
-    USP_ACT_RELU = 1,      /* max(v, 0) */
+    USP_ACT_RELU = 1,      /* max(v, 0); of a NaN: 0 in usp_spmm_ex, NaN in usp_spmm_q and usp_spmm_grouped */
     USP_ACT_GELU_TANH = 2, /* 0.5 v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) */
     USP_ACT_SILU = 3       /* v / (1 + exp(-v)) */
 } usp_activation;
@@ -237,7 +237,7 @@ usp_status usp_decode_q(const usp_matrix *A, int8_t *W_out, uint8_t *mask_out, f
  * usp_quantize -- tokens in 8 bits: per token n, a = max_k |X[n, k]|, x_scale[n] = a / 127
  * and Xq[n, k] = X[n, k] * (127 / a) rounded to the nearest integer, ties to even (all in
  * fp32; a = 0 gives zeros and scale 0). A token that holds a NaN or an infinity gets zeros
- * and the scale NaN, so its products are NaN.
+ * and the scale NaN, so its products are NaN, whatever the activation.
  *   X        device pointer, fp16, token n at X + n * ldx, ldx >= K
  *   Xq       device pointer, int8, token n at Xq + n * ldq, ldq >= K
  *   x_scale  device pointer, fp32 [N]

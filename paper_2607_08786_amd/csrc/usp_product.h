@@ -294,7 +294,7 @@ __device__ inline floatx4 product_epilogue(const ProductArgs &a, floatx4 v, uint
     if (a.bias) v = add_quad(v, bias);
     if (a.act == USP_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = v[i] > 0.f ? v[i] : 0.f;
+        for (int i = 0; i < 4; ++i) v[i] = v[i] <= 0.f ? 0.f : v[i];  // a NaN stays
     } else if (a.act != USP_ACT_NONE) {
         constexpr float kLog2e = 1.4426950408889634f;
 #pragma unroll
