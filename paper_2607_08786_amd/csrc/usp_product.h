@@ -315,8 +315,10 @@ __device__ inline uint2 finished_quad(const ProductArgs &a, typename V::Acc acc,
     typedef _Float16 half4 __attribute__((ext_vector_type(4)));
     floatx4 v = V::sum(acc);
     if (V::kBytes == 1) {
+        // A sum of zero meets the token's scale alone, which may be NaN: the two scales' product can overflow, and
+        // zero times that is no zero. (Of any other sum an overflow is fp16's too.)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] *= xs * ws[i];
+        for (int i = 0; i < 4; ++i) v[i] *= v[i] == 0.f ? xs : xs * ws[i];
     }
     if (a.e_flags & kEpiAny) v = product_epilogue(a, v, bias, res);
     if (a.weight) {
