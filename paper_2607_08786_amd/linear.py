@@ -247,12 +247,13 @@ def _call(op, plain, *args):
 
 
 def _rows_of(x: torch.Tensor, width: int) -> torch.Tensor:
-    """x [*, width] as fp16 [N, width] with unit inner stride."""
+    """x [*, width] as fp16 [N, width] with unit inner stride and rows apart from each other."""
     if x.shape[-1] != width:
         raise ValueError(f"expected {width} features, got {x.shape[-1]}")
     if x.dim() != 2:
         x = x.reshape(-1, width)
-    if x.dtype is not torch.float16 or x.stride(1) != 1:
+    ld, inner = x.stride()
+    if x.dtype is not torch.float16 or inner != 1 or (ld < width and x.shape[0] > 1):
         x = x.to(torch.float16).contiguous()
     return x
 
