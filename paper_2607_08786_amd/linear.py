@@ -398,11 +398,18 @@ class BlockNorm(torch.nn.Module):
     def forward(self, residual: torch.Tensor, y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
                 quantize: bool = False):
         """(r, h): both as residual, or with quantize h as the pair of int8 tokens [N, features] and scales [N].
-        Without y (the first block's norm) r is residual and post is not applied."""
+        Without y (the first block's norm) r is residual and post is not applied. gate: [features], or a row for each of
+        residual's."""
         shape = residual.shape
         r2 = _rows_of(residual, self.features)
         y2 = None if y is None else _rows_of(y, self.features)
-        g2 = gate if gate is None or gate.dim() == 1 else _rows_of(gate, self.features)
+        g2 = gate
+        if gate is not None and gate.dim() != 1:
+            g2 = _rows_of(gate, self.features)
+        elif gate is not None and (gate.dtype is not torch.float16 or gate.stride(0) != 1):
+            g2 = gate.to(torch.float16).contiguous()
+        if g2 is not None and g2.shape[-1] != self.features:
+            raise ValueError(f"expected a gate of {self.features} features, got {g2.shape[-1]}")
         if r2.shape[0] == 0:
             h = (r2.to(torch.int8), r2.new_empty(0, dtype=torch.float32)) if quantize else r2.reshape(shape)
             return r2.reshape(shape), h

@@ -3,7 +3,7 @@ copies, as SparseLinear gives them."""
 import pytest
 import torch
 
-from paper_2607_08786_amd import linear
+from paper_2607_08786_amd import linear, usp
 
 K, M, N = 32, 24, 6
 
@@ -36,6 +36,25 @@ def test_rows_apart_are_not_copied():
     wide = torch.zeros(N, K + 5, dtype=torch.float16)
     for x in (wide[:, :K], wide[:, 3:3 + K], wide[:1, :K], wide[:1, :K].expand(1, K), wide[::2, :K]):
         assert linear._rows_of(x, K).data_ptr() == x.data_ptr()
+
+
+def test_gate_of_a_channel(monkeypatch):
+    """A gate [features] of any type and stride, as one for each token may be."""
+    seen = []
+
+    def norm(residual, y, gate, *args, **kw):
+        seen.append(gate)
+
+    monkeypatch.setattr(usp, "usp_norm", norm)
+    mod = linear.BlockNorm(K, device="cpu")
+    x = torch.zeros(N, K, dtype=torch.float16)
+    values = torch.randn(2 * K)
+    for gate in (values[:K], values[::2].half(), values[:1].half().expand(K), values[:K].half()):
+        mod(x, x, gate)
+        assert seen[-1].dtype == torch.float16 and seen[-1].is_contiguous() and torch.equal(seen[-1], gate.half())
+    assert seen[-1] is gate
+    with pytest.raises(ValueError):
+        mod(x, x, values[:K - 1].half())
 
 
 @pytest.mark.gpu
