@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <exception>
 #include <mutex>
 #include <new>
 #include <string>
@@ -175,7 +176,7 @@ static usp_status encode_common(const char *fn, const void *W, int64_t ldw, cons
             scales.assign((size_t)enc.RB * usp::kTileRows, 0.f);
             std::copy(scale, scale + M, scales.begin());
         }
-    } catch (const std::bad_alloc &) {
+    } catch (const std::exception &) {  // bad_alloc, or length_error of sizes that no vector has
         return usp::fail(USP_ERR_OOM, f + ": host allocation failed (or encoding exceeds 64 GiB)");
     }
     DeviceGuard g(device);

@@ -4,6 +4,7 @@
 // format described in usp_format.h.
 #include <algorithm>
 #include <cstring>
+#include <exception>
 #include <thread>
 
 #if defined(__SSE2__)
@@ -24,13 +25,19 @@ void parallel_rows(int64_t n, F &&fn) {
         for (int64_t i = 0; i < n; ++i) fn(i);
         return;
     }
+    auto part = [&fn, n, nt](int64_t t) {
+        for (int64_t i = t; i < n; i += nt) fn(i);
+    };
     std::vector<std::thread> th;
     th.reserve(nt);
-    for (int64_t t = 0; t < nt; ++t) {
-        th.emplace_back([&, t] {
-            for (int64_t i = t; i < n; i += nt) fn(i);
-        });
+    int64_t started = 0;
+    try {
+        for (; started < nt; ++started) th.emplace_back(part, started);
+    } catch (const std::exception &) {
+        // The system has no more threads: an exception past the running ones would end
+        // the process, so the calling thread takes the parts that are left.
     }
+    for (int64_t t = started; t < nt; ++t) part(t);
     for (auto &x : th) x.join();
 }
 
