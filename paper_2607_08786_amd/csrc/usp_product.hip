@@ -395,6 +395,10 @@ double expected_groups(const ProductShape &s, int64_t N, int64_t tb) {
     return std::max(1.0, std::max(active, (double)N / (double)tb + 0.5 * active));
 }
 
+// Up to so many tokens no wide kernel is considered (the model below took none up to 18 in
+// 3 million random shapes), so that few tokens need little behind X packed.
+constexpr int64_t kFewTokens = kBlock;
+
 // The kernel that costs least by a model of what was measured (us; 8-bit values at 50%,
 // fp16 records scaled; layers of 1024 x 1024 to 28672 x 8192 and groups of 7 to 64
 // experts). Product kernel: a launch, a wavefront's start, and the longer of a
@@ -439,6 +443,7 @@ ProductPlan plan_product(const ProductShape &s, int64_t N, bool quantize = false
         double alone[2], shared[2];  // us of a tile of fp16 and 8-bit values, for one workgroup on a CU and for two
     } wides[] = {{4, 2, {1.65, 1.22}, {2.3, 1.7}}, {4, 4, {2.2, 1.5}, {3.3, 2.15}}, {8, 2, {4.2, 2.1}, {0, 0}}, {8, 4, {0, 3.25}, {0, 0}}};
     for (const auto &k : wides) {
+        if (N <= kFewTokens) break;
         if (!wide_serves_rows(s.value_bytes, loads, k.rows, k.nb)) continue;
         const int q = s.value_bytes == 1;
         const int64_t tb = (int64_t)kBlock * k.nb * k.rows, sets = ceil_div(s.RB, (int64_t)k.rows);
@@ -481,19 +486,21 @@ constexpr int64_t kMaxSpan = ((int64_t)1 << 32) - ((int64_t)1 << 20);
 // Workgroups of one launch (a grid has fewer than 2^32 threads).
 constexpr int64_t kMaxGrid = (int64_t)1 << 21;
 
-// Blocks of 16 rows of X packed, at most, and what a job may read past its last one.
+// Blocks of 16 rows of X packed, at most, and what a job may read past its last one: a
+// job has at least one block of its own and reads as many as its workgroup takes (4 at most
+// of the product kernel, 8 x 4 of the wide one), and a column tile past those.
 int64_t packed_blocks(const ProductShape &s, int64_t N) { return most_groups(s, N, kBlock); }
-constexpr int64_t kMoreBlocks = 32;
+constexpr int64_t more_blocks(int64_t N) { return N <= kFewTokens ? 4 : 32; }
 
 size_t packed_bytes(const ProductShape &s, int64_t N) {
-    return (size_t)(packed_blocks(s, N) + kMoreBlocks) * s.KT * kTileK * s.value_bytes * kBlock;
+    return (size_t)(packed_blocks(s, N) + more_blocks(N)) * s.KT * kTileK * s.value_bytes * kBlock;
 }
 
 }  // namespace
 
 // Where in the workspace what lies: X packed, after the region that other products keep
-// cleared, then (8-bit matrices) fp16 tokens quantised, in rows that are read in place,
-// and their scales.
+// cleared, or in its place (8-bit matrices) the codes of fp16 tokens, in rows that are read
+// in place and are no longer than packed ones; then the scales of those tokens.
 struct ProductSpace {
     size_t packed, codes, scales, end;
     int64_t ld_codes;
@@ -502,8 +509,8 @@ static ProductSpace product_space(const ProductShape &s, int64_t N) {
     ProductSpace w;
     w.ld_codes = ceil_div(s.K, (int64_t)16) * 16;
     w.packed = kCounterRegionBytes;
-    w.codes = w.packed + packed_bytes(s, N);
-    w.scales = w.codes + (s.A && s.value_bytes == 1 ? (size_t)(N * w.ld_codes) : 0);
+    w.codes = w.packed;
+    w.scales = w.packed + packed_bytes(s, N);
     w.end = w.scales + (s.A && s.value_bytes == 1 ? (size_t)(4 * N) : 0);
     return w;
 }
@@ -551,6 +558,9 @@ int launch_product(const ProductShape &s, const ProductCall &call, void *workspa
         q.ld_out_q = space.ld_codes;
         q.out_scale = reinterpret_cast<float *>(ws + space.scales);
         if (const int rc = launch_norm(q, c.N, s.K, stream)) return rc;
+        // Read where they are, which is where X would be packed: their rows are aligned, and
+        // a job's (64 of at most USP_MAX_K_Q bytes) are within a resource's offsets.
+        static_assert(64 * (int64_t)(USP_MAX_K_Q + 16) <= kMaxSpan, "");
         c.X = q.out_q;
         c.ldx = q.ld_out_q;
         c.x_scale = q.out_scale;

@@ -515,6 +515,21 @@ def _zeros(n: int, device: int, stream) -> torch.Tensor | None:
         return torch.zeros(n, dtype=torch.uint8, device=f"cuda:{device}")
 
 
+# The part of a workspace that usp_spmm expects cleared; usp_spmm_q and usp_spmm_grouped leave it alone and need nothing
+# cleared.
+_COUNTER_BYTES = 256 << 10
+
+
+def _space(n: int, device: int, stream) -> torch.Tensor | None:
+    """n bytes for the products that need nothing cleared, allocated on `stream`, the counters' part cleared; None for none."""
+    if n == 0:
+        return None
+    with torch.cuda.stream(_torch_stream(stream)):
+        ws = torch.empty(n, dtype=torch.uint8, device=f"cuda:{device}")
+        ws[:_COUNTER_BYTES].zero_()
+        return ws
+
+
 class SparseMatrix:
     """Owns one encoded weight matrix (a usp_matrix handle)."""
 
@@ -591,6 +606,11 @@ class SparseMatrixQ(SparseMatrix):
     def __init__(self, W: np.ndarray, mask: np.ndarray, scale: np.ndarray, device: int = 0):
         self._own(usp_encode_q(W, mask, scale, device), device)
 
+    def make_workspace(self, N: int, stream=None) -> torch.Tensor | None:
+        """A workspace for N tokens, allocated on `stream` (default: the current one). Only the part that usp_spmm expects
+        cleared is."""
+        return _space(self.workspace_size(N), self.device, stream)
+
     def spmm(self, Xq: torch.Tensor, x_scale: torch.Tensor | None = None, Y: torch.Tensor | None = None, workspace=None, stream=None,
              bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
              activation: str | int = "none") -> torch.Tensor:
@@ -626,8 +646,8 @@ class ExpertGroup:
         return usp_group_plan(self.handle, T)
 
     def make_workspace(self, T: int, stream=None) -> torch.Tensor | None:
-        """A workspace for T rows, allocated and cleared on `stream` (default: the current one)."""
-        return _zeros(self.workspace_size(T), self.device, stream)
+        """A workspace for T rows, allocated on `stream` (default: the current one), cleared as SparseMatrixQ's."""
+        return _space(self.workspace_size(T), self.device, stream)
 
     def spmm(self, X: torch.Tensor, offsets: torch.Tensor, T: int | None = None, Y: torch.Tensor | None = None,
              workspace=None, stream=None, **operands) -> torch.Tensor:
