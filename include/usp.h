@@ -167,7 +167,8 @@ usp_status usp_spmm_noalloc(const usp_matrix *A, const void *X, int64_t ldx, voi
 
 /*
  * usp_plan -- which kernel usp_spmm (usp_spmm_q, of an 8-bit handle) runs for this
- * handle and N when X is 16-byte aligned with ldx = K, as a short text ("row W=8",
+ * handle and N when X is 16-byte aligned with ldx = K (of an 8-bit handle: 8-bit tokens;
+ * fp16 tokens, which a kernel brings to 8 bits first, may take another), as a short text ("row W=8",
  * "chunk S=5 W=8 nb=1 grid=200", "dma nb=4 tg=1 grid=1024", "fourwave passes=1 nt=2
  * grid=768", "wide passes=1 nb=2 grid=216"; of 8-bit handles and groups "product R=4
  * W=4 nb=1 grid=448", "wide-product R=4 nb=4 grid=216"), written to
@@ -241,7 +242,7 @@ usp_status usp_decode_q(const usp_matrix *A, int8_t *W_out, uint8_t *mask_out, f
  *   X        device pointer, fp16, token n at X + n * ldx, ldx >= K
  *   Xq       device pointer, int8, token n at Xq + n * ldq, ldq >= K
  *   x_scale  device pointer, fp32 [N]
- *   N, K     >= 1
+ *   N, K     >= 1 (N up to 2^20, K up to 2^28)
  *   device   the HIP device of the pointers and of `stream`
  * Asynchronous on `stream`; no allocation, capturable.
  */
@@ -256,8 +257,8 @@ usp_status usp_quantize(const void *X, int64_t ldx, int64_t N, int64_t K, void *
  *   workspace  16-byte aligned, to >= usp_workspace_size(A, N) bytes (may be NULL when that is
  *       0); must not be used by another in-flight call. It needs no clearing, and the region that
  *       usp_spmm expects cleared is left alone, so that one workspace can serve both.
- * X is packed for the products first where many tokens or its alignment ask for it. Everything
- * else -- Y, bias, residual, activation, asynchrony, capture, reproducibility -- as usp_spmm_ex.
+ * X is packed for the products first where many tokens or its alignment ask for it. N up to 2^20, and
+ * ceil(M / 16) ceil(N / 16) below 2^31. Everything else -- Y, bias, residual, activation, asynchrony, capture, reproducibility -- as usp_spmm_ex.
  */
 usp_status usp_spmm_q(const usp_matrix *A, const void *Xq, int64_t ldx, const float *x_scale, void *Y, int64_t ldy,
                       int64_t N, const void *bias, const void *residual, int64_t ldr, int activation,
@@ -357,7 +358,7 @@ typedef struct {
 } usp_norm_args;
 
 /*
- * usp_norm -- the update above for N >= 1 tokens of K >= 1 channels. At least one output. An output
+ * usp_norm -- the update above for 1 to 2^20 tokens of 1 to 2^28 channels. At least one output. An output
  * that is an input has its stride and base; other overlaps are not allowed. A gate needs y.
  * Asynchronous on `stream` (of `device`); no allocation, capturable, bitwise reproducible.
  */

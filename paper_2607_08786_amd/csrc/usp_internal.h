@@ -180,8 +180,6 @@ size_t product_workspace_bytes(const ProductShape &s, int64_t N);
 std::string describe_product(const ProductShape &s, int64_t N);
 int launch_densify_q(const usp_matrix *A, void *Wd, int64_t ldw, void *stream);
 int launch_product(const ProductShape &s, const ProductCall &c, void *workspace, void *stream);
-// Most columns that a group's or an 8-bit matrix's kernels serve.
-constexpr int64_t kMaxProductK = USP_MAX_K_Q;
 // Device scratch of usp_spmm_noalloc: noalloc_setup looks up and clears the
 // calling thread's current device's copy once (returns a HIP error code);
 // noalloc_scratch returns its device address, or null before the set-up.

@@ -7,11 +7,13 @@
 // Every input is read once and every output written once, so the call is bound by HBM
 // at many tokens and by its launch and one round trip to memory at few. The vector
 // units come close behind HBM (a wavefront's fp32 instruction takes 4 cycles: 20 for a
-// channel of 10 bytes are 8 us of 2048 x 5120 tokens), so what a channel costs is kept
-// low: selects for a vector, conversions in the products (v_fma_mix). Back to back, in
-// graphs: 2048 x 5120, layer norms and a gate, 105 MB: 26.7 us (3.9 TB/s; 32.2 with
-// selects for each channel); no norms 19.8 (5.3 TB/s); RMS before and no gate 15.7;
-// 1 x 8192, RMS: 3.6 us.
+// channel of 10 bytes are 5 us of 2048 x 5120 tokens), so what a channel costs is kept
+// low: selects for a vector, conversions in the products (v_fma_mix). In graphs over
+// buffers of 1 GB together, so that all comes from HBM: 2048 x 5120, 105 MB, layer norms
+// and a gate 28.2 us (3.7 TB/s), RMS norms and a gate 26.3, a gate alone 22.0 (4.8 TB/s, where
+// a copy of as many bytes takes 20.5); RMS before and no gate, 84 MB, 20.3 (4.1). Over one set
+// of buffers, much of which the 256 MB cache keeps: 22.5, 20.7, 16.8 and 16.1. There selects
+// for each channel cost 5.5 us more. 1 x 8192, RMS: 3.5 us.
 //
 // One workgroup per token keeps the token in registers (C chunks of 8 channels per
 // thread) between the reductions: the mean and then the centred sum of squares (a

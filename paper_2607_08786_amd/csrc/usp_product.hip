@@ -46,8 +46,8 @@ __device__ inline v4u32 load_chunk(const uint8_t *p, int left) {
 // X in place touches 16 rows' segments of 64 bytes, which the memory pipeline takes
 // several times as long for as for 1 KB in one piece, and each column tile is
 // loaded once per row set. One wavefront per block of rows and column tile. ALIGNED: rows
-// at multiples of 4 bytes, without the fifth dword of every chunk (4096 gathered rows of
-// 2048 fp16 channels: 10.6 against 12.8 us; 32 x 5120 in 8 bits: 2.7 against 3.4). What
+// at multiples of 4 bytes, without the fifth dword of every chunk (traced, 4096 gathered rows
+// of 2048 fp16 channels: 16.2 against 18.1 us; 32 x 5120 in 8 bits: 3.6 against 3.8). What
 // remains is a chain of latencies: offsets, row indices, X, the store.
 // ---------------------------------------------------------------------------
 template <class V, bool ALIGNED>
@@ -163,8 +163,9 @@ __global__ __launch_bounds__(kPackThreads) void quantize_pack_kernel(const _Floa
 // 8-bit, 148 MB), 16 tokens, R = 4, W = 4: 30.5 us, 4.85 TB/s, where a copy of 2 GB runs
 // at 4.94. Every record is read once and decoded in registers, each lane's mask bits into
 // the A operand of its products; the next record of a wavefront is in flight into LDS
-// meanwhile. Three or four slots a wavefront gain nothing over two (a record takes 2-3 us
-// to come, and 16 wavefronts of a CU keep 32 in flight), and cost wavefronts. More row
+// meanwhile. Three or four slots a wavefront gain nothing over two there (a record takes 2-3 us
+// to come, and 16 wavefronts of a CU keep 32 in flight), and cost wavefronts; on layers of one
+// workgroup a CU, with 8 records in flight, they were not measured. More row
 // blocks share a load of X; more wavefronts shorten the chain of records where there are
 // few row blocks. At 32 and more tokens what bounds it is the decode, 2050-2200 cycles a
 // record of a wavefront, so that a decoded operand serves NB blocks of tokens: 70B FFN at

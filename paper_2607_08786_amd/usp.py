@@ -178,7 +178,7 @@ def usp_workspace_size(handle: int, N: int) -> int:
 
 
 def usp_plan(handle: int, N: int) -> str:
-    """The kernel usp_spmm runs for this handle and N (X aligned, ldx = K), as text."""
+    """The kernel usp_spmm (usp_spmm_q on 8-bit tokens) runs for this handle and N (X aligned, ldx = K), as text."""
     buf = ctypes.create_string_buffer(128)
     _check(load_library().usp_plan(handle, N, buf, len(buf)))
     return buf.value.decode()
