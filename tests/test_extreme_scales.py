@@ -46,3 +46,20 @@ def test_sums_that_are_not_zero(x_scale, w_scale):
     # One rounding to fp16 and four in fp32: the sum's conversion, the two scales' product, the product with the sum, none lost.
     tol = 2.0 ** -11 * np.abs(want) + 2.0 ** -25 + 4 * 2.0 ** -24 * np.abs(want)
     assert (np.abs(y - want)[~big] <= tol[~big]).all()
+
+
+@pytest.mark.parametrize("kernel,M,K,N", [("product", 40, 300, 5), ("wide-product", 941, 1144, 1652)])
+def test_infinite_token_scale(kernel, M, K, N):
+    """As of a token with an infinity, whose codes are then zero: NaN, and infinities where codes are not."""
+    rng = np.random.default_rng(3)
+    W = rng.integers(1, 9, (M, K)).astype(np.int8)
+    A = usp.SparseMatrixQ(W, np.ones((M, K), np.uint8), np.full(M, 1e-3, np.float32))
+    assert A.plan(N).startswith(kernel + " ")
+    x = torch.from_numpy(rng.integers(1, 9, (N, K)).astype(np.int8)).cuda()
+    s = torch.full((N,), 1e-3, device="cuda")
+    clean = A.spmm(x, s)
+    x[2], s[2], s[4] = 0, float("inf"), float("-inf")
+    y = A.spmm(x, s)
+    assert torch.isnan(y[2]).all() and (y[4] == float("-inf")).all()
+    keep = [n for n in range(N) if n not in (2, 4)]
+    assert torch.equal(y[keep], clean[keep])
