@@ -268,13 +268,15 @@ def usp_decode(handle: int):
 
 
 def usp_free(handle: int) -> None:
-    shape = _shapes.pop(handle, None)  # before the address can be another handle's
+    shape, ownerless = _shapes.pop(handle, None), handle in _ownerless
+    _ownerless.discard(handle)  # all before the number can be another handle's
     status = load_library().usp_free(handle)
     if status != USP_OK:
         if shape is not None:
             _shapes[handle] = shape
+        if ownerless:
+            _ownerless.add(handle)
         _check(status)
-    _ownerless.discard(handle)
 
 
 def usp_encode_q(W: np.ndarray, mask: np.ndarray, scale: np.ndarray, device: int = 0) -> int:

@@ -146,6 +146,23 @@ def test_freed_by_number(lib):
     assert h in lib.live
 
 
+def test_number_taken_meanwhile(lib):
+    """Between a handle's end and the return of the call another thread may get its number, and lose the owner."""
+    m = matrix()
+    free = lib.usp_free
+
+    def free_and_reuse(handle):
+        status = free(handle)
+        usp._shapes[handle] = (5, 5)
+        usp._ownerless.add(handle)
+        return status
+
+    lib.usp_free = free_and_reuse
+    h = m.handle
+    m.free()
+    assert usp._ownerless == {h} and usp._shapes == {h: (5, 5)}
+
+
 @pytest.mark.gpu
 def test_device_memory_of_a_cycle():
     """An expert group that dies in a cycle gives its experts' device memory back."""
