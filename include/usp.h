@@ -258,7 +258,8 @@ usp_status usp_quantize(const void *X, int64_t ldx, int64_t N, int64_t K, void *
  *       0); must not be used by another in-flight call. It needs no clearing, and the region that
  *       usp_spmm expects cleared is left alone, so that one workspace can serve both.
  * X is packed for the products first where many tokens or its alignment ask for it. N up to 2^20, and
- * ceil(M / 16) ceil(N / 16) below 2^31. Everything else -- Y, bias, residual, activation, asynchrony, capture, reproducibility -- as usp_spmm_ex.
+ * ceil(M / 16) ceil(N / 16) below 2^31. Everything else -- Y, bias, residual, activation, asynchrony,
+ * capture, reproducibility -- as usp_spmm_ex.
  */
 usp_status usp_spmm_q(const usp_matrix *A, const void *Xq, int64_t ldx, const float *x_scale, void *Y, int64_t ldy,
                       int64_t N, const void *bias, const void *residual, int64_t ldr, int activation,
