@@ -77,3 +77,28 @@ def test_only_the_counters_are_cleared(group):
     torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")  # its memory is the next tensor's
     ws = A.make_workspace(N)
     assert (ws[:COUNTERS] == 0).all() and (ws[COUNTERS:] == 0xFF).any()
+
+
+@pytest.mark.parametrize("N", [3, 40, 700])
+def test_capture_without_a_warm_up(N):
+    """The graph allocates its workspaces itself; replays between eager calls give the eager bits."""
+    from paper_2607_08786_amd import linear
+    g = torch.Generator().manual_seed(N)
+    codes, mask = torch.randint(-9, 9, (3, 300, 515), generator=g).to(torch.int8), torch.rand(3, 300, 515, generator=g) < 0.5
+    scale = torch.full((300,), 0.01)
+    layer = linear.SparseLinearQ(codes[0], mask[0], scale)
+    routed = linear.SparseExperts(list(codes[1:]), list(mask[1:]), [scale, scale])
+    offsets = experts.i32([0, N // 3, N])
+    x = quantized.half(1, N, 515)
+    usp.usp_quantize(x, torch.empty(N, 515, dtype=torch.int8, device="cuda"), torch.empty(N, device="cuda"))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, z = layer(x), routed(x, offsets)
+    for k in range(4):
+        x.copy_(quantized.half(2 + k, N, 515))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone(), z.clone()
+        assert torch.equal(layer(x), got[0]) and torch.equal(routed(x, offsets), got[1])
+        torch.cuda.synchronize()
