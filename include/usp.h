@@ -365,6 +365,132 @@ typedef struct {
  */
 usp_status usp_norm(const usp_norm_args *args, int64_t N, int64_t K, int device, void *stream);
 
+/* ---- Attention over a paged cache ------------------------------------------------
+ *
+ * A cache holds the keys and values of tokens that a decoder's layers have seen, in pages that
+ * sequences own in any order. Its memory is the caller's: `layers` pools of `pages` pages of
+ * usp_cache_page_bytes bytes each, page p of layer l at data + (l * pages + p) * page bytes. A page
+ * holds page_tokens tokens of every head, in the order the matrix products read them:
+ *
+ *   page    kv_heads x (page_tokens / 32) blocks, a head's blocks one after the other
+ *   block   32 tokens of one head: keys, then values, then for 8-bit values 32 fp32 scales of the
+ *           keys and 32 of the values. W = head_dim rounded up to 32, 64, 96, 128, 192 or 256.
+ *   keys    W / 8 x 32 x 8: channel d of token j at ((d / 8) * 32 + place(j)) * 8 + d % 8, place(j)
+ *           being j with its bits 2 and 3 exchanged; channels from head_dim on are zeros
+ *   values  4 x W x 8: channel d of token j at ((j / 8) * W + d) * 8 + j % 8; channels from head_dim on
+ *           are not defined
+ *
+ * 8-bit keys and values are what usp_quantize makes of a head's fp16 channels: codes, and one scale a
+ * token. A pool need not be cleared: nothing is read of tokens that were never written.
+ */
+typedef struct {
+    void *data;          /* device pointer, 16-byte aligned */
+    int64_t layers;      /* >= 1 */
+    int64_t pages;       /* of a layer, 1 to 2^31 - 1 */
+    int32_t kv_heads;    /* 1 to 4096 */
+    int32_t head_dim;    /* a multiple of 8, 8 to 256 */
+    int32_t page_tokens; /* a multiple of 32, 32 to 4096 */
+    int32_t value_bytes; /* 2: fp16; 1: 8 bits */
+    int32_t device;      /* the HIP device of every pointer of a call, and of its stream */
+} usp_cache;
+
+/* usp_cache_page_bytes -- bytes of a page of one layer (0 for a NULL or invalid description; data, pages and layers are
+ * not looked at). */
+size_t usp_cache_page_bytes(const usp_cache *cache);
+
+/*
+ * The rows of a step: new tokens of some sequences, sequence after sequence. Sequence s has
+ * lengths[s] tokens in the cache, those of the step included, and the rows offsets[s] <= t <
+ * offsets[s + 1]: row t is its token lengths[s] - offsets[s + 1] + t. Token j of it lies in page
+ * table[s * ld_table + j / page_tokens]. All are read on the device, so a captured call takes what they
+ * hold when it is replayed, and none makes a call read or write outside its operands: lengths count as at
+ * most table_pages * page_tokens and at least 0, offsets as within [0, rows] and not below an earlier
+ * one, a token before the sequence's start is not there, and neither is one in a page outside [0, pages).
+ */
+typedef struct {
+    const int32_t *table;    /* device int32, sequences rows of table_pages entries with stride ld_table */
+    int64_t ld_table;        /* >= table_pages */
+    int64_t table_pages;     /* >= 1; table_pages * page_tokens below 2^31 - 4096 */
+    const int32_t *lengths;  /* device int32 [sequences] */
+    const int32_t *offsets;  /* device int32 [sequences + 1]; or NULL: row s is sequence s's only one */
+    int64_t sequences;       /* 1 to 2^20; without offsets: rows */
+    int64_t rows;            /* T, 0 to 2^20 (0: nothing is done) */
+} usp_cache_rows;
+
+/*
+ * usp_cache_append -- writes the step's keys and values into their pages of one layer (fp16 ones in 8 bits first, as
+ * usp_quantize does for each head, where the cache holds 8-bit values).
+ *   K, V        device fp16: channel d of head h of row t at t * ld + h * head_stride + d
+ *   ld, heads   strides in elements, >= 0 (rows and heads may overlap)
+ * Two rows of a step for one place of one page (a page that two sequences of the step have) leave one of them or a
+ * mixture. Asynchronous on `stream`; no allocation, capturable.
+ */
+usp_status usp_cache_append(const usp_cache *cache, const usp_cache_rows *rows, int64_t layer, const void *K,
+                            int64_t ld_k, int64_t head_k, const void *V, int64_t ld_v, int64_t head_v, void *stream);
+
+/*
+ * usp_cache_read -- the reverse: the step's keys and values (8-bit ones as code * scale, rounded to fp16) from their
+ * pages into K and V, laid out as above with strides that keep rows and heads apart (heads at least head_dim, rows at
+ * least one head, either one inside the other). Rows that are not there are left as they were.
+ */
+usp_status usp_cache_read(const usp_cache *cache, const usp_cache_rows *rows, int64_t layer, void *K, int64_t ld_k,
+                          int64_t head_k, void *V, int64_t ld_v, int64_t head_v, void *stream);
+
+/*
+ * usp_cache_copy -- copies page src[i] to page dst[i] in every layer, for i < n: for forks whose last page the next token
+ * changes, and to move pages together. src and dst are HOST pointers, read before the call returns (a captured call
+ * keeps what they held). Pages outside [0, pages), a destination named twice, and a page that is a source of one pair and
+ * the destination of another are USP_ERR_INVALID_ARG, and nothing is done; a pair of equal pages is left out.
+ * Asynchronous on `stream`; no device allocation, capturable. 0 <= n <= pages.
+ */
+usp_status usp_cache_copy(const usp_cache *cache, const int32_t *src, const int32_t *dst, int64_t n, void *stream);
+
+/*
+ * Attention of each row over the tokens of its sequence. Row t, the token p of its sequence s, sees the tokens
+ *     max(first[t], p - window + 1, 0) <= k < min(last[t], lengths[s])
+ * where a missing `first` is 0, a missing `last` is p + 1 (causal) and window 0 is none. Packed documents: first[t] =
+ * the start of t's document. A prefix that all rows see: last[t] = max(p + 1, prefix). Head h of q reads head
+ * h / (heads / kv_heads) of the cache:
+ *     x[k] = scale * q . K[k];   x[k] <- cap * tanh(x[k] / cap)  (cap > 0);   x[k] <- x[k] - slopes[h] * |p - k|
+ *     out  = sum_k exp(x[k]) V[k] / sum_k exp(x[k]),   zeros for a row that sees nothing
+ * in fp32, the weights exp(x - max) rounded to fp16 for the product with V (relative 2^-11 each; the sum below the
+ * line takes them unrounded), one rounding to fp16 at the end. What a row does not see has no influence on
+ * it, NaN and infinities included. A row that sees a NaN, or a score of +infinity, is NaN.
+ */
+typedef struct {
+    const void *q;          /* device fp16: channel d of head h of row t at q + t * ld_q + h * head_q + d */
+    void *out;              /* device fp16, laid out by ld_out and head_out; must not overlap q or the cache */
+    const int32_t *first;   /* device int32 [rows], or NULL */
+    const int32_t *last;    /* device int32 [rows], or NULL */
+    const float *slopes;    /* device fp32 [heads], or NULL */
+    int64_t ld_q, head_q;   /* strides in elements, >= 0 */
+    int64_t ld_out, head_out; /* as usp_cache_read's */
+    int64_t layer;
+    int64_t window;         /* >= 0 */
+    int32_t heads;          /* a multiple of kv_heads, up to 65536 */
+    float scale;            /* finite */
+    float cap;              /* >= 0, finite; 0: none */
+} usp_attention_args;
+
+/* usp_attention_workspace_size -- bytes of device workspace usp_attention needs for such a step (sequences, rows and
+ * whether there are offsets are looked at; no pointer is read); 0 for an invalid description. */
+size_t usp_attention_workspace_size(const usp_cache *cache, const usp_cache_rows *rows, int32_t heads);
+
+/* usp_attention_plan -- which kernel usp_attention runs for such a step, as usp_plan. */
+usp_status usp_attention_plan(const usp_cache *cache, const usp_cache_rows *rows, int32_t heads, char *buf, size_t len);
+
+/*
+ * usp_attention -- the attention above, of the rows' own tokens too once usp_cache_append has written them (on the same
+ * stream, or waited for). Rows that no sequence has are left as they were.
+ *   workspace  as usp_spmm's: 16-byte aligned, zero-filled before its first use, left ready for the next call of any
+ *              operator; not used by another call in flight
+ * The kernel is chosen by the number of rows for each sequence, so a step that mixes single tokens with
+ * prompts is faster as two calls. Asynchronous on `stream`; no allocation, capturable; the same bits for the same
+ * operands (which other sequences a step has may move a result by roundings of its fp32 sums).
+ */
+usp_status usp_attention(const usp_cache *cache, const usp_cache_rows *rows, const usp_attention_args *args,
+                         void *workspace, size_t ws_bytes, void *stream);
+
 /* usp_free -- releases the handle and its device memory. NULL is accepted. A handle that a
  * group holds is refused (USP_ERR_INVALID_ARG).
  * The caller guarantees no product or usp_densify on it is still in flight.

@@ -6,11 +6,17 @@ and raises if it has not been built.
 """
 from . import usp  # noqa: F401
 from .usp import (  # noqa: F401
+    CacheRows,
     ExpertGroup,
+    KVCache,
     SparseMatrix,
     SparseMatrixQ,
     UspError,
     load_library,
+    usp_attention,
+    usp_cache_append,
+    usp_cache_copy,
+    usp_cache_read,
     usp_decode,
     usp_decode_q,
     usp_densify,

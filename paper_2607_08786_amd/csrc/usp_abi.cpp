@@ -11,6 +11,7 @@
 #include <string>
 #include <unordered_set>
 
+#include "usp_cache.h"
 #include "usp_internal.h"
 
 namespace {
@@ -139,6 +140,73 @@ static usp_status norm_common(const char *fn, const usp_norm_args &p, int64_t N,
     DeviceGuard g(device);
     if (!g.ok) return usp::fail(USP_ERR_HIP, f + ": cannot select device");
     const int rc = usp::launch_norm(p, N, K, stream);
+    if (rc != 0) return hip_fail((hipError_t)rc, (f + ": launch").c_str());
+    return USP_OK;
+}
+
+// Why a cache's description is none; null where it is one. `memory`: its pool too.
+static const char *wrong_cache(const usp_cache *c, bool memory) {
+    if (!c) return ": null cache";
+    if (c->kv_heads < 1 || c->kv_heads > 4096) return ": kv_heads must be 1 to 4096";
+    if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8) return ": head_dim must be a multiple of 8 up to 256";
+    if (c->page_tokens < 32 || c->page_tokens > 4096 || c->page_tokens % 32)
+        return ": page_tokens must be a multiple of 32 up to 4096";
+    if (c->value_bytes != 1 && c->value_bytes != 2) return ": value_bytes must be 1 or 2";
+    if (!memory) return nullptr;
+    if (!c->data || (reinterpret_cast<uintptr_t>(c->data) & 15)) return ": the cache's data must be 16-byte aligned";
+    if (c->layers < 1 || c->pages < 1 || c->pages > 0x7FFFFFFF) return ": layers and pages must be >= 1, pages below 2^31";
+    return nullptr;
+}
+
+// The same of a step's rows; `pointers`: those too.
+static const char *wrong_rows(const usp_cache_rows *r, const usp_cache &c, bool pointers) {
+    if (!r) return ": null rows";
+    if (r->rows < 0 || r->rows > (int64_t)1 << 20) return ": rows must be 0 to 2^20";
+    if (r->sequences < 1 || r->sequences > (int64_t)1 << 20) return ": sequences must be 1 to 2^20";
+    if (!r->offsets && r->rows != r->sequences && r->rows != 0) return ": without offsets there is one row for each sequence";
+    if (!pointers) return nullptr;
+    if (!r->table || !r->lengths) return ": null table or lengths";
+    if (r->table_pages < 1 || r->table_pages > (0x7FFFFFFF - 4096) / c.page_tokens)
+        return ": table_pages must be >= 1, its tokens below 2^31 - 4096";
+    if (r->ld_table < r->table_pages) return ": ld_table must be >= table_pages";
+    for (const void *p : {(const void *)r->table, (const void *)r->lengths, (const void *)r->offsets})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return ": table, lengths and offsets must be 4-byte aligned";
+    return nullptr;
+}
+
+// Whether rows of heads of an output lie apart from each other.
+static bool lie_apart(int64_t ld, int64_t head, int64_t rows, int64_t heads, int64_t dim) {
+    const auto inside = [dim](int64_t inner, int64_t n, int64_t outer, int64_t m) {
+        return (n == 1 || inner >= dim) && (m == 1 || (outer >= dim && (outer - dim) / (n > 1 ? n - 1 : 1) >= (n > 1 ? inner : 0)));
+    };
+    return inside(head, heads, ld, rows) || inside(ld, rows, head, heads);
+}
+
+static bool select_device(int device, DeviceGuard &g) {
+    int ndev = 0;
+    return device >= 0 && hipGetDeviceCount(&ndev) == hipSuccess && device < ndev && g.ok;
+}
+
+// What usp_cache_append and usp_cache_read check and do alike.
+static usp_status cache_rows_common(const std::string &f, const usp_cache *cache, const usp_cache_rows *rows, int64_t layer,
+                                    usp::HeadRows K, usp::HeadRows V, bool write, void *stream) {
+    if (const char *why = wrong_cache(cache, true)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
+    if (const char *why = wrong_rows(rows, *cache, true)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
+    if (layer < 0 || layer >= cache->layers) return usp::fail(USP_ERR_INVALID_ARG, f + ": no such layer");
+    if (rows->rows == 0) return USP_OK;
+    if (!K.p || !V.p) return usp::fail(USP_ERR_INVALID_ARG, f + ": null K or V");
+    if ((reinterpret_cast<uintptr_t>(K.p) | reinterpret_cast<uintptr_t>(V.p)) & 1)
+        return usp::fail(USP_ERR_INVALID_ARG, f + ": K and V must be 2-byte aligned");
+    for (const usp::HeadRows &r : {K, V}) {
+        if (r.ld < 0 || r.head < 0) return usp::fail(USP_ERR_INVALID_ARG, f + ": strides must be >= 0");
+        if (!write && !lie_apart(r.ld, r.head, rows->rows, cache->kv_heads, cache->head_dim))
+            return usp::fail(USP_ERR_INVALID_ARG, f + ": rows and heads of K and V must lie apart");
+    }
+    DeviceGuard g(cache->device);
+    if (!select_device(cache->device, g)) return usp::fail(USP_ERR_INVALID_ARG, f + ": no such device");
+    const usp::CacheView c = usp::cache_view(*cache, layer);
+    const usp::RowsView r = usp::rows_view(*rows, *cache);
+    const int rc = write ? usp::launch_cache_append(c, r, K, V, stream) : usp::launch_cache_read(c, r, K, V, stream);
     if (rc != 0) return hip_fail((hipError_t)rc, (f + ": launch").c_str());
     return USP_OK;
 }
@@ -607,6 +675,117 @@ usp_status usp_spmm_grouped(const usp_group *G, const void *X, int64_t ldx, int6
     c.ldb = ldb;
     c.weight = row_weight;
     return product_common(f, usp::product_shape(G), G->device, c, workspace, ws_bytes, stream);
+}
+
+size_t usp_cache_page_bytes(const usp_cache *cache) {
+    if (wrong_cache(cache, false)) return 0;
+    usp_cache c = *cache;
+    c.data = nullptr;
+    c.layers = c.pages = 1;
+    return (size_t)usp::cache_view(c, 0).page_bytes;
+}
+
+usp_status usp_cache_append(const usp_cache *cache, const usp_cache_rows *rows, int64_t layer, const void *K,
+                            int64_t ld_k, int64_t head_k, const void *V, int64_t ld_v, int64_t head_v, void *stream) {
+    return cache_rows_common("usp_cache_append", cache, rows, layer, {const_cast<void *>(K), ld_k, head_k},
+                             {const_cast<void *>(V), ld_v, head_v}, true, stream);
+}
+
+usp_status usp_cache_read(const usp_cache *cache, const usp_cache_rows *rows, int64_t layer, void *K, int64_t ld_k,
+                          int64_t head_k, void *V, int64_t ld_v, int64_t head_v, void *stream) {
+    return cache_rows_common("usp_cache_read", cache, rows, layer, {K, ld_k, head_k}, {V, ld_v, head_v}, false, stream);
+}
+
+usp_status usp_cache_copy(const usp_cache *cache, const int32_t *src, const int32_t *dst, int64_t n, void *stream) {
+    const std::string f("usp_cache_copy");
+    if (const char *why = wrong_cache(cache, true)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
+    if (n < 0 || n > cache->pages) return usp::fail(USP_ERR_INVALID_ARG, f + ": n must be 0 to pages");
+    if (n == 0) return USP_OK;
+    if (!src || !dst) return usp::fail(USP_ERR_INVALID_ARG, f + ": null pages");
+    std::vector<int32_t> from, to;
+    try {
+        std::vector<int32_t> sorted(dst, dst + n);
+        std::sort(sorted.begin(), sorted.end());
+        if (sorted.front() < 0 || sorted.back() >= cache->pages)
+            return usp::fail(USP_ERR_INVALID_ARG, f + ": a destination is no page of the cache");
+        if (std::adjacent_find(sorted.begin(), sorted.end()) != sorted.end())
+            return usp::fail(USP_ERR_INVALID_ARG, f + ": a destination is named twice");
+        from.reserve((size_t)n);
+        to.reserve((size_t)n);
+        for (int64_t i = 0; i < n; ++i) {
+            if (src[i] < 0 || src[i] >= cache->pages)
+                return usp::fail(USP_ERR_INVALID_ARG, f + ": a source is no page of the cache");
+            if (src[i] == dst[i]) continue;
+            if (std::binary_search(sorted.begin(), sorted.end(), src[i]))
+                return usp::fail(USP_ERR_INVALID_ARG, f + ": a page is both a source and a destination");
+            from.push_back(src[i]);
+            to.push_back(dst[i]);
+        }
+    } catch (const std::bad_alloc &) {
+        return usp::fail(USP_ERR_OOM, f + ": host allocation failed");
+    }
+    DeviceGuard g(cache->device);
+    if (!select_device(cache->device, g)) return usp::fail(USP_ERR_INVALID_ARG, f + ": no such device");
+    const int rc = usp::launch_cache_copy(usp::cache_view(*cache, 0), cache->layers, from.data(), to.data(), (int64_t)from.size(), stream);
+    if (rc != 0) return hip_fail((hipError_t)rc, (f + ": launch").c_str());
+    return USP_OK;
+}
+
+// Why heads of q do not go with a cache's; null where they do.
+static const char *wrong_heads(const usp_cache &c, int32_t heads) {
+    return heads < 1 || heads > 65536 || heads % c.kv_heads ? ": heads must be a multiple of kv_heads up to 65536" : nullptr;
+}
+
+size_t usp_attention_workspace_size(const usp_cache *cache, const usp_cache_rows *rows, int32_t heads) {
+    if (wrong_cache(cache, false) || wrong_rows(rows, *cache, false) || wrong_heads(*cache, heads) || rows->rows == 0) return 0;
+    return usp::attention_workspace_bytes(usp::cache_view(*cache, 0), usp::rows_view(*rows, *cache), heads);
+}
+
+usp_status usp_attention_plan(const usp_cache *cache, const usp_cache_rows *rows, int32_t heads, char *buf, size_t len) {
+    const std::string f("usp_attention_plan");
+    if (const char *why = wrong_cache(cache, false)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
+    if (const char *why = wrong_rows(rows, *cache, false)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
+    if (const char *why = wrong_heads(*cache, heads)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
+    if (rows->rows < 1 || !buf || len == 0) return usp::fail(USP_ERR_INVALID_ARG, f + ": need rows >= 1 and a buffer");
+    return copy_text(usp::describe_attention(usp::cache_view(*cache, 0), usp::rows_view(*rows, *cache), heads), buf, len);
+}
+
+usp_status usp_attention(const usp_cache *cache, const usp_cache_rows *rows, const usp_attention_args *args,
+                         void *workspace, size_t ws_bytes, void *stream) {
+    const std::string f("usp_attention");
+    if (const char *why = wrong_cache(cache, true)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
+    if (const char *why = wrong_rows(rows, *cache, true)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
+    if (!args) return usp::fail(USP_ERR_INVALID_ARG, f + ": null arguments");
+    const usp_attention_args &p = *args;
+    if (const char *why = wrong_heads(*cache, p.heads)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
+    if (p.layer < 0 || p.layer >= cache->layers) return usp::fail(USP_ERR_INVALID_ARG, f + ": no such layer");
+    if (!std::isfinite(p.scale)) return usp::fail(USP_ERR_INVALID_ARG, f + ": scale must be finite");
+    if (!std::isfinite(p.cap) || p.cap < 0.f) return usp::fail(USP_ERR_INVALID_ARG, f + ": cap must be >= 0 and finite");
+    if (p.cap > 0.f && !std::isfinite(2.f * p.scale / p.cap * 2.f))
+        return usp::fail(USP_ERR_INVALID_ARG, f + ": scale / cap is not finite");
+    if (p.window < 0) return usp::fail(USP_ERR_INVALID_ARG, f + ": window must be >= 0");
+    if (rows->rows == 0) return USP_OK;
+    if (!p.q || !p.out) return usp::fail(USP_ERR_INVALID_ARG, f + ": null q or out");
+    if ((reinterpret_cast<uintptr_t>(p.q) | reinterpret_cast<uintptr_t>(p.out)) & 1)
+        return usp::fail(USP_ERR_INVALID_ARG, f + ": q and out must be 2-byte aligned");
+    for (const void *q : {(const void *)p.first, (const void *)p.last, (const void *)p.slopes})
+        if (reinterpret_cast<uintptr_t>(q) & 3)
+            return usp::fail(USP_ERR_INVALID_ARG, f + ": first, last and slopes must be 4-byte aligned");
+    if (p.ld_q < 0 || p.head_q < 0) return usp::fail(USP_ERR_INVALID_ARG, f + ": strides must be >= 0");
+    if (!lie_apart(p.ld_out, p.head_out, rows->rows, p.heads, cache->head_dim))
+        return usp::fail(USP_ERR_INVALID_ARG, f + ": rows and heads of out must lie apart");
+    const usp::CacheView c = usp::cache_view(*cache, p.layer);
+    const usp::RowsView r = usp::rows_view(*rows, *cache);
+    if (!usp::attention_fits(c, r, p.heads)) return usp::fail(USP_ERR_UNSUPPORTED, f + ": too many rows and heads");
+    const size_t need = usp::attention_workspace_bytes(c, r, p.heads);
+    if (need && (!workspace || ws_bytes < need)) return usp::fail(USP_ERR_INVALID_ARG, f + ": workspace too small");
+    if (need && (reinterpret_cast<uintptr_t>(workspace) & 15))
+        return usp::fail(USP_ERR_INVALID_ARG, f + ": workspace must be 16-byte aligned");
+    DeviceGuard g(cache->device);
+    if (!select_device(cache->device, g)) return usp::fail(USP_ERR_INVALID_ARG, f + ": no such device");
+    const int rc = usp::launch_attention(c, r, p, workspace, stream);
+    if (rc != 0) return hip_fail((hipError_t)rc, (f + ": launch").c_str());
+    return USP_OK;
 }
 
 }  // extern "C"

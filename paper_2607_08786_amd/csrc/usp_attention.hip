@@ -1,0 +1,785 @@
+// usp_attention.hip -- attention of a step's rows over a paged cache (include/usp.h,
+// usp_attention).
+//
+// Both kernels take a tile of columns (a column: one head of one row, all columns of a tile
+// reading one head of the cache) through the blocks of 32 keys that it sees, once, with the
+// running maximum m and sum l of each column's softmax:
+//
+//     S^T = K Q^T     (keys x columns; rows of K are the matrix unit's A operand)
+//     p = exp2(s - m),  l = l exp2(m_old - m) + sum p
+//     O^T = O^T exp2(m_old - m) + V^T P^T    (channels x columns; rows of V^T are A)
+//
+// S^T leaves a lane the scores of one column, and with the cache's order of a block's
+// keys they are the 8 consecutive keys of which it hands over P^T's B operand: softmax and
+// P stay in registers, without an exchange but the maximum over the lanes of a column. K and V
+// are read in the order that they lie in (usp_cache.h).
+#include "usp_cache.h"
+#include "usp_device.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace usp {
+namespace {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef uint32_t v2u32 __attribute__((ext_vector_type(2)));
+typedef _Float16 half2a __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNothing = -__builtin_inff();
+
+struct AttendArgs {
+    CacheView c;
+    RowsView r;
+    const int32_t *first, *last;
+    const uint16_t *q;
+    uint16_t *out;
+    const float *slopes;
+    int64_t ld_q, head_q, ld_out, head_out;
+    float scale;           // score of q . K in the exponent of 2, or the argument of the cap's exponential
+    float cap;             // in the exponent of 2; 0: none
+    int heads, group, window;
+    int tiles;             // tiles of 16 heads of a row (rows kernel)
+    int q_vec, out_vec;
+    int split;             // whether tiles are cut into pieces (rows kernel)
+    int pieces_bits;       // 2^pieces_bits pieces of all tiles and heads together are aimed at
+    int limit, slot_limit; // items of a head in the grid, and slots of a head in the workspace
+    uint32_t *counters;
+    float *partials;
+};
+
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The larger of a value and what the lanes 16 (32) away hold.
+__device__ inline float max_16(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)s[0]), __builtin_bit_cast(float, (uint32_t)s[1]));
+}
+__device__ inline float max_32(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)s[0]), __builtin_bit_cast(float, (uint32_t)s[1]));
+}
+__device__ inline float sum_16(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]);
+}
+__device__ inline float sum_32(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]);
+}
+
+// Eight codes as fp16: the byte 128 + c under the exponent of 1024 is 1152 + c, exactly.
+__device__ inline half8 halves_of(v2u32 codes) {
+    const half2a bias = {(_Float16)-1152.f, (_Float16)-1152.f};
+    v4u32 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t u = codes[i / 2] ^ 0x80808080u;
+        const uint32_t w = __builtin_amdgcn_perm(0x64646464u, u, i % 2 ? 0x07030602u : 0x05010400u);
+        out[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2a, w) + bias);
+    }
+    return __builtin_bit_cast(half8, out);
+}
+
+// Eight channels d .. d + 7 of a head of q, zeros behind head_dim and where there is no column.
+__device__ inline half8 load_q8(const AttendArgs &a, int t, int head, int d, bool there) {
+    half8 x = {};
+    if (!there || d >= a.c.head_dim) return x;
+    const uint16_t *from = a.q + (int64_t)t * a.ld_q + (int64_t)head * a.head_q + d;
+    if (a.q_vec) return *reinterpret_cast<const half8 *>(from);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __builtin_bit_cast(_Float16, from[i]);
+    return x;
+}
+
+// Channels d .. d + 3 of an output.
+__device__ inline void store_out4(const AttendArgs &a, int t, int head, int d, floatx4 v) {
+    uint16_t *to = a.out + (int64_t)t * a.ld_out + (int64_t)head * a.head_out + d;
+    uint16_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, (_Float16)v[i]);
+    if (a.out_vec) {
+        *reinterpret_cast<uint2 *>(to) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = h[i];
+    }
+}
+
+// The keys lo <= k < hi that row t, token p of a sequence of len, sees.
+__device__ inline void span_of(const AttendArgs &a, int t, int p, int len, int &lo, int &hi) {
+    lo = a.first ? a.first[t] : 0;
+    if (a.window && p - a.window + 1 > lo) lo = p - a.window + 1;
+    if (lo < 0) lo = 0;
+    hi = a.last ? a.last[t] : p + 1;
+    if (hi > len) hi = len;
+    if (p < 0) hi = 0;
+}
+
+// A score in the exponent of 2, from q . K: scaled, capped, biased.
+__device__ inline float score_of(const AttendArgs &a, float x, float slope, int p, int key) {
+    x *= a.scale;
+    if (a.cap > 0.f)  // cap tanh(y): 1 - 2 / (1 + exp(2 y)); x is 2 y in the exponent of 2
+        x = a.cap * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_of(x)));
+    if (a.slopes) x -= slope * fabsf((float)(p - key));
+    return x;
+}
+
+// ---- Few rows of each sequence: one tile of up to 16 heads of a row at a time.
+
+constexpr int kRowWaves = 4;
+constexpr int kMinBlocks = 8;     // blocks of a piece at least: two for each wavefront
+constexpr int kMostPieces = 256;  // of a tile: the join's weights lie in LDS
+
+// What a workgroup does: piece `piece` of at most `pieces`, of `blocks` blocks each, of tile `tile` of row t.
+struct Item {
+    int s, t, tile, piece, pieces, blocks;
+    int p, len;   // the row's token, and its sequence's
+    int slot;     // of the tile's first piece
+    int counter;
+};
+
+// Blocks that a row of a sequence may see.
+__device__ inline int most_blocks(const AttendArgs &a, int len) {
+    const int all = (len + kBlockTokens - 1) / kBlockTokens;
+    return a.window && !a.last ? min(all, (a.window - 1 + kBlockTokens - 1) / kBlockTokens + 1) : all;
+}
+
+// Inclusive sums over the lanes of a wavefront.
+__device__ inline uint32_t scan_lanes(uint32_t v) {
+#pragma unroll
+    for (int d = 1; d < kLanes; d *= 2) {
+        const uint32_t o = (uint32_t)__shfl_up((int)v, d, kLanes);
+        if ((threadIdx.x & (kLanes - 1)) >= d) v += o;
+    }
+    return v;
+}
+
+// Item number `item` of a head. Where tiles are cut, a piece has as many blocks as make
+// 2^pieces_bits pieces of all of them, and every wavefront finds its item by itself: each
+// lane counts the pieces of as many sequences as it takes. False: there is no such item.
+__device__ inline bool find_item(const AttendArgs &a, int item, Item &it) {
+    const int S = a.r.sequences, lane = threadIdx.x & (kLanes - 1);
+    if (!a.split) {
+        it.t = item / a.tiles;
+        it.tile = item - it.t * a.tiles;
+        if (it.t >= a.r.rows) return false;
+        it.s = sequence_of(a.r, it.t);
+        if (it.s >= S || offset_of(a.r, it.s) > it.t) return false;
+        it.len = length_of(a.r, it.s);
+        it.p = it.len - (offset_of(a.r, it.s + 1) - it.t);
+        it.piece = 0;
+        it.pieces = 1;
+        it.blocks = 0;
+        it.slot = it.counter = 0;
+        return true;
+    }
+    const int per = (S + kLanes - 1) / kLanes, s0 = lane * per;
+    uint64_t total = 0;
+    for (int i = 0; i < per; ++i) {
+        const int s = s0 + i;
+        if (s < S) total += (uint64_t)max(0, offset_of(a.r, s + 1) - offset_of(a.r, s)) * (uint32_t)most_blocks(a, length_of(a.r, s));
+    }
+#pragma unroll
+    for (int d = 1; d < kLanes; d *= 2) {
+        const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)total, d, kLanes);
+        const uint32_t hi = (uint32_t)__shfl_xor((int)(uint32_t)(total >> 32), d, kLanes);
+        total += (uint64_t)hi << 32 | lo;
+    }
+    total = total * (uint32_t)(a.tiles * a.c.kv_heads);
+    const uint64_t even = (total + (1ull << a.pieces_bits) - 1) >> a.pieces_bits;
+    const int blocks = (int)min((uint64_t)(1 << 30), max((uint64_t)kMinBlocks, even));
+    auto pieces_of = [&](int len) {
+        return min(kMostPieces, max(1, (most_blocks(a, len) + blocks - 1) / blocks));
+    };
+    constexpr uint32_t kFull = 1u << 24;  // more items than a grid has
+    uint32_t items = 0, slots = 0;
+    for (int i = 0; i < per; ++i) {
+        const int s = s0 + i;
+        if (s >= S) break;
+        const int n = max(0, offset_of(a.r, s + 1) - offset_of(a.r, s)), pieces = pieces_of(length_of(a.r, s));
+        const uint32_t of_s = min(kFull, (uint32_t)n * (uint32_t)a.tiles) * (uint32_t)pieces;  // below 2^32
+        items = min(kFull, items + min(kFull, of_s));
+        if (pieces > 1) slots = min(kFull, slots + min(kFull, of_s));
+    }
+    const uint32_t items_end = scan_lanes(items), slots_end = scan_lanes(slots);
+    const uint64_t has = __ballot((uint32_t)item < items_end);
+    if (!has) return false;
+    const int owner = __ffsll((unsigned long long)has) - 1;
+    uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)(items_end - items), owner);
+    uint32_t slot = (uint32_t)__builtin_amdgcn_readlane((int)(slots_end - slots), owner);
+    for (int i = 0; i < per; ++i) {
+        const int s = owner * per + i;
+        if (s >= S) break;
+        const int off = offset_of(a.r, s), n = max(0, offset_of(a.r, s + 1) - off), len = length_of(a.r, s);
+        const int pieces = pieces_of(len);
+        const uint32_t of_s = (uint32_t)n * (uint32_t)a.tiles * (uint32_t)pieces;
+        if ((uint32_t)item - at < of_s) {
+            const int in = item - (int)at, tile = in / pieces;
+            it.s = s;
+            it.piece = in - tile * pieces;
+            it.t = off + tile / a.tiles;
+            it.tile = tile % a.tiles;
+            it.len = len;
+            it.p = len - n + tile / a.tiles;
+            it.pieces = pieces;
+            it.blocks = blocks;
+            it.slot = (int)slot + tile * pieces;
+            it.counter = (int)at + tile * pieces;
+            // Offsets that decrease may give more items than the grid and the workspace were made for.
+            return it.counter + pieces <= a.limit && (pieces == 1 || it.slot + pieces <= a.slot_limit);
+        }
+        at += of_s;
+        if (pieces > 1) slot += of_s;
+    }
+    return false;
+}
+
+// Floats of a piece's partial result: maxima, sums, and the output of each of its columns.
+__host__ __device__ inline int partial_floats(int columns, int width) { return 32 + columns * width; }
+
+template <int DS, int VB>
+__global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendArgs a) {
+    constexpr int W = 32 * DS, kBlockBytes = (int)cache_block_bytes(W, VB);
+    constexpr int kStride = W + 4;
+    constexpr int kJoinFloats = kMostPieces * 32;
+    constexpr int kShared = kRowWaves * 16 * kStride > kJoinFloats ? kRowWaves * 16 * kStride : kJoinFloats;
+    __shared__ __attribute__((aligned(16))) float so[kShared];
+    __shared__ float sm[kRowWaves][16], sl[kRowWaves][16];
+    __shared__ uint32_t arrived;
+
+    const int h = blockIdx.x % a.c.kv_heads;
+    Item it;
+    if (!find_item(a, blockIdx.x / a.c.kv_heads, it)) return;
+    const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+    const int r = lane & 15, g = lane >> 4;
+    const int columns = min(16, a.group - 16 * it.tile), head0 = h * a.group + 16 * it.tile;
+
+    int lo, hi;
+    span_of(a, it.t, it.p, it.len, lo, hi);
+    int b0 = lo / kBlockTokens, b1 = (hi + kBlockTokens - 1) / kBlockTokens;
+    if (hi <= lo) b0 = b1 = 0;
+    int pieces = 1;
+    if (it.pieces > 1) {
+        const int want = min(it.pieces, max(1, (b1 - b0 + it.blocks - 1) / it.blocks));
+        const int each = max(1, (b1 - b0 + want - 1) / want);
+        pieces = max(1, (b1 - b0 + each - 1) / each);
+        if (it.piece >= pieces) return;
+        b0 += it.piece * each;
+        b1 = min(b1, b0 + each);
+    }
+
+    half8 q[DS];
+#pragma unroll
+    for (int s = 0; s < DS; ++s) q[s] = load_q8(a, it.t, head0 + r, 32 * s + 8 * g, r < columns);
+    const float slope = a.slopes && r < columns ? a.slopes[head0 + r] * kLog2e : 0.f;
+
+    floatx4 o[2 * DS];
+#pragma unroll
+    for (int d = 0; d < 2 * DS; ++d) o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
+    float m = kNothing, l = 0.f;  // l: of this lane's keys alone
+    float unit = 1e-30f;          // 8 bits: the largest scale of values so far; o is in 2^-14 of it
+    const uint8_t *head_base = a.c.base + (int64_t)h * a.c.page_blocks * kBlockBytes;
+    const int32_t *table = a.r.table + (int64_t)it.s * a.r.ld_table;
+
+    int pages = 0, places = 0;  // lane i: page, and block in it, of this wavefront's i-th block from here
+    for (int n = 0, b = b0 + wave; b < b1; ++n, b += kRowWaves) {
+        if (n % kLanes == 0) {
+            const int mine = b + kRowWaves * lane;
+            if (mine < b1) {
+                const int in = mine / a.c.page_blocks;
+                pages = table[in];
+                places = mine - in * a.c.page_blocks;
+            }
+        }
+        const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(pages, n % kLanes);
+        if (page >= a.c.pages) continue;
+        const uint8_t *block = head_base + (int64_t)page * a.c.page_bytes + (int64_t)__builtin_amdgcn_readlane(places, n % kLanes) * kBlockBytes;
+
+        half8 k[DS][2], v[2 * DS];
+        floatx4 ks[2], vs[2];
+#pragma unroll
+        for (int s = 0; s < DS; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int unit8 = (4 * s + g) * kBlockTokens + 16 * (r / 8) + 8 * i + r % 8;
+                if (VB == 2)
+                    k[s][i] = reinterpret_cast<const half8 *>(block)[unit8];
+                else
+                    k[s][i] = halves_of(reinterpret_cast<const v2u32 *>(block)[unit8]);
+            }
+#pragma unroll
+        for (int d = 0; d < 2 * DS; ++d) {
+            const int unit8 = W / 8 * kBlockTokens + g * W + 16 * d + r;
+            if (VB == 2)
+                v[d] = reinterpret_cast<const half8 *>(block)[unit8];
+            else
+                v[d] = halves_of(reinterpret_cast<const v2u32 *>(block)[unit8]);
+        }
+        if (VB == 1) {
+            const floatx4 *scales = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                ks[i] = scales[2 * g + i];
+                vs[i] = scales[kBlockTokens / 4 + 2 * g + i];
+            }
+        }
+
+        floatx4 st[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int s = 0; s < DS; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) st[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[s][i], q[s], st[i], 0, 0, 0);
+
+        // The scores of keys key0 .. key0 + 7.
+        const int key0 = b * kBlockTokens + 8 * g;
+        float x[8];
+        bool seen[8];
+        float top = kNothing, top_scale = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = st[j / 4][j % 4];
+            if (VB == 1) x[j] *= ks[j / 4][j % 4];
+            x[j] = score_of(a, x[j], slope, it.p, key0 + j);
+            seen[j] = key0 + j >= lo && key0 + j < hi;
+            if (!seen[j]) x[j] = kNothing;
+            top = fmaxf(top, x[j]);
+            if (VB == 1) top_scale = fmaxf(top_scale, seen[j] ? vs[j / 4][j % 4] : 0.f);
+        }
+        const float m_new = fmaxf(m, max_32(max_16(top)));
+        const float base = m_new == kNothing ? 0.f : m_new;
+        float fade = exp2_of(m - base);
+        m = m_new;
+        l *= fade;
+        float to_unit = 1.f;
+        if (VB == 1) {
+            const float u = fmaxf(unit, max_32(max_16(top_scale)));
+            fade *= unit / u;
+            unit = u;
+            to_unit = 16384.f / u;
+        }
+        half8 p;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float w = exp2_of(x[j] - base);
+            w = seen[j] ? w : 0.f;
+            l += w;
+            if (VB == 1) w = seen[j] ? w * (vs[j / 4][j % 4] * to_unit) : 0.f;
+            p[j] = (_Float16)w;
+        }
+        // What the row does not see may hold anything, and nothing times infinity is not nothing.
+        if (VB == 2 && (b * kBlockTokens < lo || (b + 1) * kBlockTokens > hi)) {
+            v4u32 keep;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) keep[i] = (seen[2 * i] ? 0xFFFFu : 0u) | (seen[2 * i + 1] ? 0xFFFF0000u : 0u);
+#pragma unroll
+            for (int d = 0; d < 2 * DS; ++d) v[d] = __builtin_bit_cast(half8, __builtin_bit_cast(v4u32, v[d]) & keep);
+        }
+#pragma unroll
+        for (int d = 0; d < 2 * DS; ++d) {
+            o[d] *= fade;
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[d], p, o[d], 0, 0, 0);
+        }
+    }
+
+    // The wavefronts' results together, in their order.
+    l = sum_32(sum_16(l));
+    if (g == 0) {
+        sm[wave][r] = m;
+        sl[wave][r] = l;
+    }
+    if (r < columns) {
+        const float back = VB == 1 ? unit * (1.f / 16384.f) : 1.f;
+#pragma unroll
+        for (int d = 0; d < 2 * DS; ++d)
+            *reinterpret_cast<floatx4 *>(&so[(wave * 16 + r) * kStride + 16 * d + 4 * g]) = o[d] * back;
+    }
+    __syncthreads();
+    float *slots = a.partials;
+    const int slot_floats = partial_floats(min(16, a.group), W);
+    for (int e = threadIdx.x; e < columns * (W / 4); e += kRowWaves * kLanes) {
+        const int col = e / (W / 4), d = 4 * (e % (W / 4));
+        float top = sm[0][col];
+#pragma unroll
+        for (int w = 1; w < kRowWaves; ++w) top = fmaxf(top, sm[w][col]);
+        const float base = top == kNothing ? 0.f : top;
+        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+        float total = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) {
+            const float f = exp2_of(sm[w][col] - base);
+            total += sl[w][col] * f;
+            sum += *reinterpret_cast<const floatx4 *>(&so[(w * 16 + col) * kStride + d]) * f;
+        }
+        if (pieces == 1) {
+            if (d < a.c.head_dim) store_out4(a, it.t, head0 + col, d, total == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : sum * (1.f / total));
+        } else {
+            float *slot = slots + ((int64_t)(it.slot + it.piece) * a.c.kv_heads + h) * slot_floats;
+            const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(slot, (short)0, slot_floats * 4, kBufferRsrcWord3);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, sum), to, (32 + col * W + d) * 4, 0, kCachePolicyDevice);
+            if (d == 0) {
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, top), to, col * 4, 0, kCachePolicyDevice);
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, total), to, (16 + col) * 4, 0, kCachePolicyDevice);
+            }
+        }
+    }
+    if (pieces == 1) return;
+
+    // The last piece to arrive joins them, in their order.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's part lies in memory
+    __syncthreads();
+    uint32_t *counter = a.counters + (int64_t)it.counter * a.c.kv_heads + h;
+    if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (arrived != (uint32_t)pieces - 1) return;
+    const int64_t step = (int64_t)a.c.kv_heads * slot_floats;  // from a piece's slot to the next
+    float *first = slots + ((int64_t)it.slot * a.c.kv_heads + h) * slot_floats;
+    for (int e = threadIdx.x; e < pieces * 32; e += kRowWaves * kLanes) {
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(first, (short)0, -1, kBufferRsrcWord3);
+        so[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, (int)((e / 32 * step + e % 32) * 4), 0, kCachePolicyDevice));
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < columns * (W / 4); e += kRowWaves * kLanes) {
+        const int col = e / (W / 4), d = 4 * (e % (W / 4));
+        float top = kNothing;
+        for (int i = 0; i < pieces; ++i) top = fmaxf(top, so[i * 32 + col]);
+        const float base = top == kNothing ? 0.f : top;
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(first, (short)0, -1, kBufferRsrcWord3);
+        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+        float total = 0.f;
+        constexpr int kBatch = 8;
+        for (int i0 = 0; i0 < pieces; i0 += kBatch) {
+            v4u32 v[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (i0 + i < pieces)
+                    v[i] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(((i0 + i) * step + 32 + col * W + d) * 4), 0, kCachePolicyDevice);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (i0 + i < pieces) {
+                    const float f = exp2_of(so[(i0 + i) * 32 + col] - base);
+                    total += so[(i0 + i) * 32 + 16 + col] * f;
+                    sum += __builtin_bit_cast(floatx4, v[i]) * f;
+                }
+        }
+        if (d < a.c.head_dim) store_out4(a, it.t, head0 + col, d, total == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : sum * (1.f / total));
+    }
+    if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// ---- Many rows of each sequence: tiles of 128 columns of consecutive rows and the heads of a cache's head.
+
+constexpr int kTileWaves = 4;
+constexpr int kTileColumns = 32 * kTileWaves;
+
+// The first tile of sequence s: those before it have at most so many.
+__device__ inline int first_tile(const AttendArgs &a, int s) {
+    return (int)((int64_t)offset_of(a.r, s) * a.group / kTileColumns) + s;
+}
+
+template <int DS, int VB>
+__global__ __launch_bounds__(kTileWaves *kLanes) void attend_tiles_kernel(AttendArgs a) {
+    constexpr int W = 32 * DS, kBlockBytes = (int)cache_block_bytes(W, VB);
+    __shared__ half8 staged[W / 8 * kBlockTokens * 2];  // a block of keys, then of values, as in the cache
+    __shared__ floatx4 scales[2 * kBlockTokens / 4];
+    __shared__ int ends[2][kTileWaves];
+
+    const int h = blockIdx.x % a.c.kv_heads, tile = blockIdx.x / a.c.kv_heads;
+    int s = 0;
+    {
+        int below = a.r.sequences;  // first_tile(s) <= tile < first_tile(below)
+        while (below - s > 1) {
+            const int mid = (s + below) / 2;
+            if (first_tile(a, mid) <= tile)
+                s = mid;
+            else
+                below = mid;
+        }
+    }
+    const int off = offset_of(a.r, s), n = offset_of(a.r, s + 1) - off, len = length_of(a.r, s);
+    const int64_t column0 = (int64_t)(tile - first_tile(a, s)) * kTileColumns;
+    if (column0 < 0 || column0 >= (int64_t)n * a.group) return;
+
+    const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes, c = lane & 31, half = lane >> 5;
+    const int64_t column = column0 + 32 * wave + c;
+    const int row = (int)(column / a.group), t = off + row, head = h * a.group + (int)(column - (int64_t)row * a.group);
+    const bool there = row < n;
+    const int p = len - n + row;
+    int lo = 0, hi = 0;
+    if (there) span_of(a, t, p, len, lo, hi);
+
+    // The keys that the tile and this wavefront see any of, and those that all of its columns see.
+    const bool sees = hi > lo;
+    int any_lo = sees ? lo : 0x7FFFFFFF, any_hi = sees ? hi : 0, all_lo = there ? lo : 0, all_hi = there ? hi : 0x7FFFFFFF;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        any_lo = min(any_lo, __shfl_xor(any_lo, d, kLanes));
+        any_hi = max(any_hi, __shfl_xor(any_hi, d, kLanes));
+        all_lo = max(all_lo, __shfl_xor(all_lo, d, kLanes));
+        all_hi = min(all_hi, __shfl_xor(all_hi, d, kLanes));
+    }
+    any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+    any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+    if (lane == 0) {
+        ends[0][wave] = any_lo;
+        ends[1][wave] = any_hi;
+    }
+    __syncthreads();
+    int tile_lo = ends[0][0], tile_hi = ends[1][0];
+#pragma unroll
+    for (int w = 1; w < kTileWaves; ++w) {
+        tile_lo = min(tile_lo, ends[0][w]);
+        tile_hi = max(tile_hi, ends[1][w]);
+    }
+
+    half8 q[2 * DS];
+#pragma unroll
+    for (int i = 0; i < 2 * DS; ++i) q[i] = load_q8(a, t, head, 16 * i + 8 * half, there);
+    const float slope = a.slopes && there ? a.slopes[head] * kLog2e : 0.f;
+
+    floatx16 o[DS];
+#pragma unroll
+    for (int d = 0; d < DS; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    float m = kNothing, l = 0.f, unit = 1e-30f;
+    const int32_t *table = a.r.table + (int64_t)s * a.r.ld_table;
+    const int b1 = (tile_hi + kBlockTokens - 1) / kBlockTokens;
+    for (int b = tile_hi > tile_lo ? tile_lo / kBlockTokens : b1; b < b1; ++b) {
+        const int in = b / a.c.page_blocks;
+        const uint32_t page = (uint32_t)table[in];
+        if (page >= a.c.pages) continue;
+        const uint8_t *block = a.c.base + (int64_t)page * a.c.page_bytes + ((int64_t)h * a.c.page_blocks + (b - in * a.c.page_blocks)) * kBlockBytes;
+        __syncthreads();  // the block before has been read
+#pragma unroll
+        for (int i = 0; i < W / 8 * kBlockTokens * 2 / (kTileWaves * kLanes); ++i) {
+            const int unit8 = i * kTileWaves * kLanes + threadIdx.x;
+            if (VB == 2)
+                staged[unit8] = reinterpret_cast<const half8 *>(block)[unit8];
+            else
+                staged[unit8] = halves_of(reinterpret_cast<const v2u32 *>(block)[unit8]);
+        }
+        if (VB == 1 && threadIdx.x < 2 * kBlockTokens / 4)
+            scales[threadIdx.x] = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W)[threadIdx.x];
+        __syncthreads();
+        const int block_lo = b * kBlockTokens, block_hi = block_lo + kBlockTokens;
+        if (block_hi <= any_lo || block_lo >= any_hi) continue;  // this wavefront sees nothing of it
+        const bool whole = all_lo <= block_lo && block_hi <= all_hi;
+
+        floatx16 st;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2 * DS; ++i)
+            st = __builtin_amdgcn_mfma_f32_32x32x16_f16(staged[(2 * i + half) * kBlockTokens + c], q[i], st, 0, 0, 0);
+
+        // Register 8 u + j holds the score of key block_lo + 16 u + 8 half + j.
+        float top = kNothing, top_scale = 0.f;
+        floatx4 vs[4];
+        uint32_t seen = 0xFFFFu;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int in_block = 16 * (i / 8) + 8 * half + i % 8, key = block_lo + in_block;
+            if (VB == 1) {
+                st[i] *= scales[in_block / 4][i % 4];
+                if (i % 4 == 0) vs[i / 4] = scales[(kBlockTokens + in_block) / 4];
+                if (key < len) top_scale = fmaxf(top_scale, vs[i / 4][i % 4]);
+            }
+            st[i] = score_of(a, st[i], slope, p, key);
+            if (!whole && !(key >= lo && key < hi)) {
+                st[i] = kNothing;
+                seen &= ~(1u << i);
+            }
+            top = fmaxf(top, st[i]);
+        }
+        const float m_new = fmaxf(m, max_32(top));
+        const float base = m_new == kNothing ? 0.f : m_new;
+        float fade = exp2_of(m - base);
+        m = m_new;
+        l *= fade;
+        float to_unit = 1.f;
+        if (VB == 1) {
+            const float u = fmaxf(unit, max_32(top_scale));
+            fade *= unit / u;
+            unit = u;
+            to_unit = 16384.f / u;
+        }
+        half8 w[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float x = exp2_of(st[i] - base);
+            x = whole || (seen >> i & 1) ? x : 0.f;
+            l += x;
+            if (VB == 1) x = whole || (seen >> i & 1) ? x * (vs[i / 4][i % 4] * to_unit) : 0.f;
+            w[i / 8][i % 8] = (_Float16)x;
+        }
+#pragma unroll
+        for (int d = 0; d < DS; ++d) o[d] *= fade;
+        uint32_t odd = 0;  // values of this lane's that are not finite
+#pragma unroll
+        for (int d = 0; d < DS; ++d)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                half8 v = staged[W / 8 * kBlockTokens + (2 * u + half) * W + 32 * d + c];
+                if (VB == 2 && !whole) {
+                    // Nothing times infinity is not nothing: what is not finite is left out here.
+                    v4u32 bits = __builtin_bit_cast(v4u32, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t bad = ((bits[i] & 0x7C007C00u) + 0x04000400u) >> 15 & 0x00010001u;
+                        odd |= bad;
+                        bits[i] &= ~(bad * 0xFFFFu);
+                    }
+                    v = __builtin_bit_cast(half8, bits);
+                }
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[u], o[d], 0, 0, 0);
+            }
+        if (VB == 2 && !whole && __any(odd != 0)) {  // and added here to the columns that see it
+            const uint16_t *values = reinterpret_cast<const uint16_t *>(&staged[W / 8 * kBlockTokens]);
+#pragma unroll 1
+            for (int j = 0; j < kBlockTokens; ++j) {
+                const bool sees_j = block_lo + j >= lo && block_lo + j < hi;
+#pragma unroll
+                for (int d = 0; d < DS; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int channel = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
+                        const uint16_t u = values[((j / 8) * W + channel) * 8 + j % 8];
+                        if (sees_j && (u & 0x7C00) == 0x7C00) o[d][i] += (float)__builtin_bit_cast(_Float16, u);
+                    }
+            }
+        }
+    }
+
+    l = sum_32(l);
+    const float inv = (l == 0.f ? 0.f : 1.f / l) * (VB == 1 ? unit * (1.f / 16384.f) : 1.f);
+    if (!there) return;
+#pragma unroll
+    for (int d = 0; d < DS; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int channel = 32 * d + 8 * i + 4 * half;
+            floatx4 v = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+            v *= inv;
+            if (l == 0.f) v = floatx4{0.f, 0.f, 0.f, 0.f};
+            if (channel < a.c.head_dim) store_out4(a, t, head, channel, v);
+        }
+}
+
+typedef void (*AttendFn)(AttendArgs);
+
+template <int VB>
+AttendFn rows_kernel_of(int width) {
+    switch (width) {
+        case 32: return attend_rows_kernel<1, VB>;
+        case 64: return attend_rows_kernel<2, VB>;
+        case 96: return attend_rows_kernel<3, VB>;
+        case 128: return attend_rows_kernel<4, VB>;
+        case 192: return attend_rows_kernel<6, VB>;
+        default: return attend_rows_kernel<8, VB>;
+    }
+}
+template <int VB>
+AttendFn tiles_kernel_of(int width) {
+    switch (width) {
+        case 32: return attend_tiles_kernel<1, VB>;
+        case 64: return attend_tiles_kernel<2, VB>;
+        case 96: return attend_tiles_kernel<3, VB>;
+        case 128: return attend_tiles_kernel<4, VB>;
+        case 192: return attend_tiles_kernel<6, VB>;
+        default: return attend_tiles_kernel<8, VB>;
+    }
+}
+
+struct AttendPlan {
+    bool rows;             // the rows kernel; else the tiles kernel
+    bool split;
+    int tiles, pieces_bits;
+    int64_t limit, slots;  // items and partial results of a head
+    size_t partial_bytes;
+};
+
+constexpr int kPiecesBits = 10;
+
+AttendPlan plan_attention(const CacheView &c, const RowsView &r, int heads) {
+    const int64_t group = heads / c.kv_heads;
+    AttendPlan p = {};
+    p.pieces_bits = kPiecesBits;
+    p.rows = !r.offsets || (int64_t)r.rows <= 4 * (int64_t)r.sequences;
+    if (!p.rows) {
+        p.limit = (int64_t)r.rows * group / kTileColumns + r.sequences;
+        return p;
+    }
+    p.tiles = (int)((group + 15) / 16);
+    const int64_t all = (int64_t)r.rows * p.tiles;
+    const int64_t pieces = ((int64_t)1 << p.pieces_bits) / c.kv_heads;
+    // Cut where there are few tiles, and their counters and the lanes' sequences fit.
+    p.split = all * c.kv_heads <= 16384 && r.sequences <= 4096 && (all + pieces) * c.kv_heads <= kMaxCounters;
+    p.limit = p.split ? all + pieces : all;
+    if (p.split) {
+        // Tiles of more than one piece have at most twice their even share.
+        p.slots = std::min(p.limit, 2 * pieces + 2);
+        p.partial_bytes = (size_t)(p.slots * c.kv_heads) * partial_floats((int)std::min<int64_t>(16, group), c.width) * sizeof(float);
+    }
+    return p;
+}
+
+}  // namespace
+
+size_t attention_workspace_bytes(const CacheView &c, const RowsView &r, int heads) {
+    const AttendPlan p = plan_attention(c, r, heads);
+    return p.partial_bytes ? kCounterRegionBytes + p.partial_bytes : 0;
+}
+
+std::string describe_attention(const CacheView &c, const RowsView &r, int heads) {
+    const AttendPlan p = plan_attention(c, r, heads);
+    return std::string(p.rows ? "rows" : "tiles") + " W=" + std::to_string(c.width) +
+           (p.split ? " pieces=" + std::to_string(1 << p.pieces_bits) : "") + " grid=" + std::to_string(p.limit * c.kv_heads);
+}
+
+bool attention_fits(const CacheView &c, const RowsView &r, int heads) {
+    return plan_attention(c, r, heads).limit * c.kv_heads < (int64_t)1 << 31;
+}
+
+int launch_attention(const CacheView &c, const RowsView &r, const usp_attention_args &p, void *workspace, void *stream) {
+    const AttendPlan plan = plan_attention(c, r, p.heads);
+    AttendArgs a = {};
+    a.c = c;
+    a.r = r;
+    a.first = p.first;
+    a.last = p.last;
+    a.q = reinterpret_cast<const uint16_t *>(p.q);
+    a.out = reinterpret_cast<uint16_t *>(p.out);
+    a.slopes = p.slopes;
+    a.ld_q = p.ld_q;
+    a.head_q = p.head_q;
+    a.ld_out = p.ld_out;
+    a.head_out = p.head_out;
+    a.scale = p.cap > 0.f ? 2.f * kLog2e * p.scale / p.cap : p.scale * kLog2e;
+    a.cap = p.cap * kLog2e;
+    a.heads = p.heads;
+    a.group = p.heads / c.kv_heads;
+    a.window = p.window < r.capacity ? (int)p.window : 0;  // a longer one hides nothing
+    a.tiles = plan.tiles;
+    a.q_vec = (reinterpret_cast<uintptr_t>(p.q) & 15) == 0 && p.ld_q % 8 == 0 && p.head_q % 8 == 0;
+    a.out_vec = (reinterpret_cast<uintptr_t>(p.out) & 7) == 0 && p.ld_out % 4 == 0 && p.head_out % 4 == 0;
+    a.split = plan.split;
+    a.pieces_bits = plan.pieces_bits;
+    a.limit = (int)plan.limit;
+    a.slot_limit = (int)plan.slots;
+    a.counters = reinterpret_cast<uint32_t *>(workspace);
+    a.partials = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + kCounterRegionBytes);
+    const AttendFn fn = plan.rows ? c.value_bytes == 2 ? rows_kernel_of<2>(c.width) : rows_kernel_of<1>(c.width)
+                                  : c.value_bytes == 2 ? tiles_kernel_of<2>(c.width) : tiles_kernel_of<1>(c.width);
+    hipLaunchKernelGGL(fn, dim3((unsigned)(plan.limit * c.kv_heads)), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    return (int)hipGetLastError();
+}
+
+}  // namespace usp

@@ -39,7 +39,41 @@ def _(x, handle, out_features, bias, residual, activation, workspace):
     return x.new_empty((x.shape[0], out_features))
 
 
-class SparseLinear(torch.nn.Module):
+class Workspaces:
+    """The workspaces of a module's calls. Every completed call leaves a workspace ready for the next one of any size, so
+    each stream has one buffer for all its calls, replaced when one needs more bytes; it is allocated and used on that
+    stream alone, so its memory is reused in that stream's order.
+
+    A captured graph records the buffer's address. A capture takes a buffer that an earlier call (its
+    warm-up) left, which from then on belongs to the graphs, is kept as long as the module and is no
+    longer given to other calls. Without one of the size, the buffer is allocated and cleared in the
+    graph itself."""
+
+    def _no_workspaces(self) -> None:
+        self._ws: dict[int, torch.Tensor] = {}  # stream -> the workspace of the calls enqueued on it
+        self._graph_ws: list[torch.Tensor] = []  # workspaces whose addresses captured graphs hold
+
+    def _workspace(self, need: int, make) -> Optional[torch.Tensor]:
+        """A buffer of at least `need` bytes for a call on the current stream, or what `make` gives; None for none."""
+        if need == 0:
+            return None
+        if torch.cuda.is_current_stream_capturing():
+            ws = next((w for w in self._graph_ws if w.numel() >= need), None)
+            if ws is not None:
+                return ws
+            for stream, ws in list(self._ws.items()):  # another thread's call may add its stream meanwhile
+                if ws.numel() >= need and self._ws.pop(stream, None) is not None:
+                    self._graph_ws.append(ws)
+                    return ws
+            return make()
+        stream = self._stream()
+        ws = self._ws.get(stream)
+        if ws is None or ws.numel() < need:
+            ws = self._ws[stream] = make()
+        return ws
+
+
+class SparseLinear(Workspaces, torch.nn.Module):
     """``act(x W^T + b) (+ residual)`` with W pruned by ``mask`` (kept where nonzero).
 
     weight: [out_features, in_features] tensor (converted to fp16); mask: array or
@@ -68,8 +102,7 @@ class SparseLinear(torch.nn.Module):
         self.activation = activation
         self.register_buffer(
             "bias", None if bias is None else bias.detach().to(device=f"cuda:{dev}", dtype=torch.float16).contiguous())
-        self._ws: dict[int, torch.Tensor] = {}  # stream -> the workspace of the calls enqueued on it
-        self._graph_ws: list[torch.Tensor] = []  # workspaces whose addresses captured graphs hold
+        self._no_workspaces()
 
     @classmethod
     def from_linear(cls, linear: torch.nn.Linear, mask, activation: str = "none") -> "SparseLinear":
@@ -82,33 +115,8 @@ class SparseLinear(torch.nn.Module):
 
     def workspace(self, N: int) -> Optional[torch.Tensor]:
         """A zero-filled workspace of at least usp_workspace_size(N) bytes for a call enqueued on the
-        current stream.
-
-        Every completed call leaves a workspace ready for the next one with any N, so each stream has one
-        buffer for all token counts, replaced when a count needs more bytes; it is allocated and used on
-        that stream alone, so its memory is reused in that stream's order.
-
-        A captured graph records the buffer's address. A capture takes a buffer that an earlier call (its
-        warm-up) left, which from then on belongs to the graphs, is kept as long as the module and is no
-        longer given to other calls. Without one of the size, the buffer is allocated and cleared in the
-        graph itself."""
-        need = self.matrix.workspace_size(N)
-        if need == 0:
-            return None
-        if torch.cuda.is_current_stream_capturing():
-            ws = next((w for w in self._graph_ws if w.numel() >= need), None)
-            if ws is not None:
-                return ws
-            for stream, ws in list(self._ws.items()):  # another thread's call may add its stream meanwhile
-                if ws.numel() >= need and self._ws.pop(stream, None) is not None:
-                    self._graph_ws.append(ws)
-                    return ws
-            return self.matrix.make_workspace(N)
-        stream = self._stream()
-        ws = self._ws.get(stream)
-        if ws is None or ws.numel() < need:
-            ws = self._ws[stream] = self.matrix.make_workspace(N)
-        return ws
+        current stream (Workspaces says which)."""
+        return self._workspace(self.matrix.workspace_size(N), lambda: self.matrix.make_workspace(N))
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         lead = x.shape[:-1]

@@ -22,7 +22,8 @@ _STATUS = {0: "USP_OK", 1: "USP_ERR_INVALID_ARG", 2: "USP_ERR_UNSUPPORTED", 3: "
 
 EXPORTED = ("usp_encode", "usp_encode_q", "usp_workspace_size", "usp_spmm", "usp_spmm_ex", "usp_spmm_noalloc", "usp_spmm_q",
             "usp_quantize", "usp_plan", "usp_group_create", "usp_group_free", "usp_group_workspace_size", "usp_group_plan",
-            "usp_spmm_grouped", "usp_norm", "usp_decode_q", "usp_densify", "usp_decode", "usp_info", "usp_free", "usp_last_error")
+            "usp_spmm_grouped", "usp_norm", "usp_cache_page_bytes", "usp_cache_append", "usp_cache_read", "usp_cache_copy",
+            "usp_attention", "usp_attention_plan", "usp_attention_workspace_size", "usp_decode_q", "usp_densify", "usp_decode", "usp_info", "usp_free", "usp_last_error")
 
 # Bytes of the per-GPU device scratch usp_spmm_noalloc uses (USP_NOALLOC_SCRATCH_BYTES).
 NOALLOC_SCRATCH_BYTES = 32 << 20
@@ -57,6 +58,23 @@ class usp_norm_args(ctypes.Structure):
                 [(f, ctypes.c_int64) for f in ("ld_residual", "ld_y", "ld_gate", "ld_residual_out", "ld_out", "ld_out_q")] +
                 [("scale", ctypes.c_float), ("eps", ctypes.c_float), ("post_kind", ctypes.c_int),
                  ("pre_kind", ctypes.c_int), ("gate_activation", ctypes.c_int)])
+
+
+class usp_cache(ctypes.Structure):
+    _fields_ = ([("data", ctypes.c_void_p), ("layers", ctypes.c_int64), ("pages", ctypes.c_int64)] +
+                [(f, ctypes.c_int32) for f in ("kv_heads", "head_dim", "page_tokens", "value_bytes", "device")])
+
+
+class usp_cache_rows(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("table_pages", ctypes.c_int64),
+                ("lengths", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("sequences", ctypes.c_int64),
+                ("rows", ctypes.c_int64)]
+
+
+class usp_attention_args(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_void_p) for f in ("q", "out", "first", "last", "slopes")] +
+                [(f, ctypes.c_int64) for f in ("ld_q", "head_q", "ld_out", "head_out", "layer", "window")] +
+                [("heads", ctypes.c_int32), ("scale", ctypes.c_float), ("cap", ctypes.c_float)])
 
 
 _lib = None
@@ -111,6 +129,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     for name in ("usp_encode_q", "usp_decode_q", "usp_quantize", "usp_spmm_q", "usp_group_create", "usp_group_free",
                  "usp_spmm_grouped", "usp_norm", "usp_group_plan"):
         getattr(lib, name).restype = st
+    cache, rows = ctypes.POINTER(usp_cache), ctypes.POINTER(usp_cache_rows)
+    lib.usp_cache_page_bytes.argtypes = [cache]
+    lib.usp_cache_append.argtypes = [cache, rows, i64, p, i64, i64, p, i64, i64, p]
+    lib.usp_cache_read.argtypes = [cache, rows, i64, p, i64, i64, p, i64, i64, p]
+    lib.usp_cache_copy.argtypes = [cache, ctypes.c_void_p, ctypes.c_void_p, i64, p]
+    lib.usp_attention.argtypes = [cache, rows, ctypes.POINTER(usp_attention_args), p, sz, p]
+    lib.usp_attention_plan.argtypes = [cache, rows, ctypes.c_int32, ctypes.c_char_p, sz]
+    lib.usp_attention_workspace_size.argtypes = [cache, rows, ctypes.c_int32]
+    for name in ("usp_cache_append", "usp_cache_read", "usp_cache_copy", "usp_attention", "usp_attention_plan"):
+        getattr(lib, name).restype = st
+    lib.usp_cache_page_bytes.restype = lib.usp_attention_workspace_size.restype = sz
     lib.usp_group_workspace_size.argtypes = [p, i64]
     lib.usp_group_plan.argtypes = [p, i64, ctypes.c_char_p, sz]
     lib.usp_group_workspace_size.restype = sz
@@ -507,6 +536,210 @@ def usp_norm(residual: torch.Tensor, y: torch.Tensor | None = None, gate: torch.
                       _vector(out_scale, torch.float32, N, dev, "out_scale"), ld_res, ld_y, ld_g, ld_ro, ld_o, ld_q,
                       scale, eps, NORMS[post], NORMS[pre], GATES[gate_activation])
     _check((_lib or load_library()).usp_norm(ctypes.byref(a), N, K, dev, _stream_of(stream, dev)))
+
+
+class CacheRows:
+    """The rows of a step over a paged cache (usp_cache_rows): new tokens of some sequences.
+
+    table: int32 [sequences, pages], the pages of each sequence; lengths: int32 [sequences], its tokens in the cache, the
+    step's included; offsets: int32 [sequences + 1], where each sequence's rows start, or None for one row each. All on one
+    GPU, read there when a call runs (or a captured one is replayed); the object keeps the tensors alive."""
+
+    __slots__ = ("table", "lengths", "offsets", "device", "_structs")
+
+    def __init__(self, table: torch.Tensor, lengths: torch.Tensor, offsets: torch.Tensor | None = None):
+        dev = _gpu(table, "table")
+        _matrix(table, torch.int32, table.shape, dev, "table")
+        S = table.shape[0]
+        _vector(lengths, torch.int32, S, dev, "lengths")
+        _vector(offsets, torch.int32, S + 1, dev, "offsets")
+        self.table, self.lengths, self.offsets, self.device = table, lengths, offsets, dev
+        self._structs: dict[int, usp_cache_rows] = {}  # rows of a call -> the C description
+
+    def struct(self, T: int) -> usp_cache_rows:
+        """The C description for a call of T rows."""
+        got = self._structs.get(T)
+        if got is None:
+            S, pages = self.table.shape
+            if self.offsets is None and T != S:
+                raise ValueError(f"without offsets there is one row for each of the {S} sequences, got {T}")
+            got = usp_cache_rows(self.table.data_ptr(), self.table.stride(0) if S > 1 else pages, pages, self.lengths.data_ptr(),
+                                 None if self.offsets is None else self.offsets.data_ptr(), S, T)
+            if len(self._structs) > 64:
+                self._structs.clear()
+            self._structs[T] = got
+        return got
+
+
+class KVCache:
+    """The memory of a paged key-value cache (usp_cache): `layers` pools of `pages` pages of `page_tokens` tokens of
+    `kv_heads` heads of `head_dim` channels, as float16 or int8 (with a scale for each token and head).
+
+    data: uint8 [layers, pages, page bytes], allocated here unless given. It is not cleared: nothing reads what was never
+    written. Which sequence owns which page is the caller's business (attention.PagedCache keeps it)."""
+
+    def __init__(self, pages: int, kv_heads: int, head_dim: int, page_tokens: int = 64, layers: int = 1,
+                 dtype: torch.dtype = torch.float16, device: int | None = None, data: torch.Tensor | None = None):
+        if dtype not in (torch.float16, torch.int8):
+            raise TypeError("a cache holds float16 or int8 values")
+        if pages < 1 or layers < 1:
+            raise ValueError("pages and layers must be >= 1")
+        if data is not None:
+            device = _gpu(data, "data")
+        elif device is None:
+            device = torch.cuda.current_device()
+        self.pages, self.kv_heads, self.head_dim, self.page_tokens = pages, kv_heads, head_dim, page_tokens
+        self.layers, self.dtype, self.device = layers, dtype, device
+        self.description = usp_cache(None, layers, pages, kv_heads, head_dim, page_tokens, dtype.itemsize, device)
+        self.page_bytes = int(load_library().usp_cache_page_bytes(ctypes.byref(self.description)))
+        if not self.page_bytes:
+            raise ValueError("kv_heads must be 1 to 4096, head_dim a multiple of 8 up to 256, page_tokens a multiple of 32 up "
+                             f"to 4096: got {kv_heads}, {head_dim}, {page_tokens}")
+        shape = (layers, pages, self.page_bytes)
+        if data is None:
+            data = torch.empty(shape, dtype=torch.uint8, device=f"cuda:{device}")
+        elif data.dtype is not torch.uint8 or data.shape != shape or not data.is_contiguous():
+            raise ValueError(f"data must be a contiguous uint8 tensor {shape}")
+        self.data = data
+        self.description.data = data.data_ptr()
+
+    def workspace_size(self, rows: CacheRows, T: int, heads: int) -> int:
+        return usp_attention_workspace_size(self, rows, T, heads)
+
+    def make_workspace(self, rows: CacheRows, T: int, heads: int, stream=None) -> torch.Tensor | None:
+        """A workspace for attention of T rows, allocated on `stream` (default: the current one), the part cleared that has
+        to be."""
+        return _space(self.workspace_size(rows, T, heads), self.device, stream)
+
+    def plan(self, rows: CacheRows, T: int, heads: int) -> str:
+        return usp_attention_plan(self, rows, T, heads)
+
+    def append(self, rows: CacheRows, K: torch.Tensor, V: torch.Tensor, layer: int = 0, stream=None) -> None:
+        usp_cache_append(self, rows, K, V, layer, stream)
+
+    def read(self, rows: CacheRows, T: int, layer: int = 0, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+        """The keys and values [T, kv_heads, head_dim] of a step's rows as fp16; zeros for rows that are not there."""
+        with torch.cuda.stream(_torch_stream(stream)):
+            K, V = (torch.zeros((T, self.kv_heads, self.head_dim), dtype=torch.float16, device=self.data.device) for _ in range(2))
+        usp_cache_read(self, rows, K, V, layer, stream)
+        return K, V
+
+    def copy(self, src, dst, stream=None) -> None:
+        usp_cache_copy(self, src, dst, stream)
+
+    def attention(self, rows: CacheRows, q: torch.Tensor, out: torch.Tensor | None = None, workspace=None, stream=None,
+                  **operands) -> torch.Tensor:
+        """usp_attention into `out`, or into a new tensor of q's shape (zeros in rows that no sequence has); what the call
+        creates is allocated on `stream`."""
+        if out is None or workspace is None:
+            with torch.cuda.stream(_torch_stream(stream)):
+                if out is None:
+                    make = torch.empty if rows.offsets is None else torch.zeros
+                    out = make(q.shape, dtype=torch.float16, device=q.device)
+                if workspace is None:
+                    workspace = self.make_workspace(rows, q.shape[0], q.shape[1])
+        usp_attention(self, rows, q, out, workspace, stream=stream, **operands)
+        return out
+
+    def blocks(self) -> tuple[torch.Tensor, torch.Tensor]:
+        """Views of every key and value as they lie in memory: K [layers, pages, kv_heads, page_tokens / 32, 2, 2, 2, 4,
+        channels / 8, 8], whose dimensions 4 to 7 are the bits 4, 3, 2 and 1 to 0 of a token's place in its block, and V
+        [layers, pages, kv_heads, page_tokens / 32, 4, 8, channels], 4 and 5 the token; of 8 bits the codes."""
+        size, W = self.dtype.itemsize, cache_width(self.head_dim)
+        block = 64 * W * size + (256 if size == 1 else 0)
+        b = self.data.view(self.layers, self.pages, self.kv_heads, self.page_tokens // 32, block)
+        lead = b.shape[:-1]
+        k = b[..., :32 * W * size].view(self.dtype).unflatten(-1, (W // 8, 2, 2, 2, 4, 8))   # of a place: bits 4, 2, 3, 1-0
+        v = b[..., 32 * W * size:64 * W * size].view(self.dtype).unflatten(-1, (4, W, 8))
+        n = len(lead)
+        k = k.permute(*range(n), n + 1, n + 3, n + 2, n + 4, n, n + 5)
+        return k[..., :self.head_dim // 8, :], v.transpose(-1, -2)[..., :self.head_dim]
+
+
+def cache_width(head_dim: int) -> int:
+    """Channels of a head in a cache's memory."""
+    return next((w for w in (32, 64, 96, 128, 192) if head_dim <= w), 256)
+
+
+def _heads_of(t: torch.Tensor, shape, dev: int, name: str):
+    """(address, stride of rows, stride of heads) of an fp16 operand [rows, heads, channels] after its checks."""
+    if t.dtype is not torch.float16 or t.dim() != 3:
+        raise TypeError(f"{name} must be a 3-D torch.float16 tensor")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on GPU {dev}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}")
+    ld, head, inner = t.stride()
+    if inner != 1 and shape[2] > 1:
+        raise TypeError(f"{name} must have unit inner stride")
+    return t.data_ptr(), ld, head
+
+
+def _same_gpu(cache: KVCache, rows: CacheRows) -> int:
+    if rows.device != cache.device:
+        raise ValueError(f"the rows' table is on GPU {rows.device}, the cache on GPU {cache.device}")
+    return cache.device
+
+
+def usp_cache_page_bytes(cache: KVCache) -> int:
+    return int(load_library().usp_cache_page_bytes(ctypes.byref(cache.description)))
+
+
+def usp_cache_append(cache: KVCache, rows: CacheRows, K: torch.Tensor, V: torch.Tensor, layer: int = 0, stream=None) -> None:
+    """Writes the keys and values of a step's rows, K and V [T, kv_heads, head_dim] fp16 with unit inner stride, into their
+    pages of `layer` (8-bit caches: quantised as usp_quantize does, a scale for each row and head)."""
+    dev = _same_gpu(cache, rows)
+    shape = (K.shape[0], cache.kv_heads, cache.head_dim)
+    k, v = _heads_of(K, shape, dev, "K"), _heads_of(V, shape, dev, "V")
+    _check((_lib or load_library()).usp_cache_append(cache.description, rows.struct(shape[0]), layer, *k, *v, _stream_of(stream, dev)))
+
+
+def usp_cache_read(cache: KVCache, rows: CacheRows, K: torch.Tensor, V: torch.Tensor, layer: int = 0, stream=None) -> None:
+    """The reverse: a step's keys and values into K and V [T, kv_heads, head_dim] fp16; rows that are not there are left."""
+    dev = _same_gpu(cache, rows)
+    shape = (K.shape[0], cache.kv_heads, cache.head_dim)
+    k, v = _heads_of(K, shape, dev, "K"), _heads_of(V, shape, dev, "V")
+    _check((_lib or load_library()).usp_cache_read(cache.description, rows.struct(shape[0]), layer, *k, *v, _stream_of(stream, dev)))
+
+
+def usp_cache_copy(cache: KVCache, src, dst, stream=None) -> None:
+    """Copies page src[i] to page dst[i] in every layer. src and dst: sequences of page numbers on the host."""
+    n = len(src)
+    if len(dst) != n:
+        raise ValueError("src and dst must have the same number of pages")
+    pages = ctypes.c_int32 * n
+    _check((_lib or load_library()).usp_cache_copy(cache.description, pages(*src), pages(*dst), n, _stream_of(stream, cache.device)))
+
+
+def usp_attention_workspace_size(cache: KVCache, rows: CacheRows, T: int, heads: int) -> int:
+    return int((_lib or load_library()).usp_attention_workspace_size(cache.description, rows.struct(T), heads))
+
+
+def usp_attention_plan(cache: KVCache, rows: CacheRows, T: int, heads: int) -> str:
+    """The kernel usp_attention runs for T such rows, as text."""
+    buf = ctypes.create_string_buffer(128)
+    _check(load_library().usp_attention_plan(cache.description, rows.struct(T), heads, buf, len(buf)))
+    return buf.value.decode()
+
+
+def usp_attention(cache: KVCache, rows: CacheRows, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor | None = None,
+                  layer: int = 0, scale: float | None = None, cap: float = 0.0, slopes: torch.Tensor | None = None,
+                  window: int = 0, first: torch.Tensor | None = None, last: torch.Tensor | None = None, stream=None) -> None:
+    """Attention of a step's rows, q [T, heads, head_dim] fp16, over what the cache holds for them, into out (as q).
+    scale (default head_dim ** -0.5), cap, slopes [heads] fp32: of the scores; window, first [T] and last [T] int32: the
+    keys that a row sees (default: those up to its own)."""
+    dev = _same_gpu(cache, rows)
+    shape = q.shape
+    qp, ld_q, head_q = _heads_of(q, shape, dev, "q")
+    T, heads, dim = shape
+    if dim != cache.head_dim:
+        raise ValueError(f"q must have {cache.head_dim} channels for each head")
+    op, ld_o, head_o = _heads_of(out, shape, dev, "out")
+    a = usp_attention_args(qp, op, _vector(first, torch.int32, T, dev, "first"), _vector(last, torch.int32, T, dev, "last"),
+                           _vector(slopes, torch.float32, heads, dev, "slopes"), ld_q, head_q, ld_o, head_o, layer, window,
+                           heads, dim ** -0.5 if scale is None else scale, cap)
+    ws, ws_bytes = _workspace(workspace, dev)
+    _check((_lib or load_library()).usp_attention(cache.description, rows.struct(T), a, ws, ws_bytes, _stream_of(stream, dev)))
 
 
 def _zeros(n: int, device: int, stream) -> torch.Tensor | None:

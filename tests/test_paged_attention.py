@@ -1,0 +1,491 @@
+"""usp_attention, usp_cache_append, usp_cache_read and usp_cache_copy against plain forms in 64 bits (GPU)."""
+import numpy as np
+import pytest
+import torch
+
+import attention64
+from paper_2607_08786_amd import attention, usp
+
+pytestmark = pytest.mark.gpu
+
+
+def draw(seed, *shape, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).half()
+
+
+def int32(values):
+    return torch.as_tensor(values, dtype=torch.int32).cuda()
+
+
+class Setting:
+    """Sequences of given lengths in a cache whose memory held NaN, their pages in any order; keys and values on the host."""
+
+    def __init__(self, lengths, kv, D, page=32, values="f16", seed=0, layers=1, layer=0, extra_pages=3):
+        self.lengths, self.kv, self.D, self.layer = lengths, kv, D, layer
+        self.eight_bit = values == "q"
+        need = [-(-L // page) for L in lengths]
+        order = torch.randperm(sum(need) + extra_pages, generator=torch.Generator().manual_seed(seed)).int()
+        self.cache = usp.KVCache(sum(need) + extra_pages, kv, D, page, layers, torch.int8 if self.eight_bit else torch.float16)
+        self.cache.data.fill_(255)  # NaN, and codes of -1 with scales of NaN
+        self.table = torch.full((len(lengths), max(need + [1])), 2 ** 30, dtype=torch.int32)
+        at = 0
+        for s, n in enumerate(need):
+            self.table[s, :n] = order[at:at + n]
+            at += n
+        self.K = [draw(seed * 100 + 2 * s, L, kv, D) for s, L in enumerate(lengths)]
+        self.V = [draw(seed * 100 + 2 * s + 1, L, kv, D) for s, L in enumerate(lengths)]
+
+    def fill(self):
+        T = sum(self.lengths)
+        rows = self.rows(self.lengths)
+        if T:
+            self.cache.append(rows, torch.cat(self.K).cuda(), torch.cat(self.V).cuda(), layer=self.layer)
+        return self
+
+    def rows(self, counts=None):
+        offsets = None if counts is None else int32(np.concatenate([[0], np.cumsum(counts)]))
+        return usp.CacheRows(self.table.cuda(), int32(self.lengths), offsets)
+
+    def want(self, q, counts, **kw):
+        """(out, tolerance) of the last counts[s] tokens of each sequence."""
+        outs, tols, at = [], [], 0
+        first, last = kw.pop("first", None), kw.pop("last", None)
+        for s, n in enumerate(counts):
+            part = slice(at, at + n)
+            o, t = attention64.attend(q[part], attention64.held(self.K[s], self.eight_bit), attention64.held(self.V[s], self.eight_bit),
+                                      first=None if first is None else first[part], last=None if last is None else last[part], **kw)
+            outs.append(o)
+            tols.append(t)
+            at += n
+        return torch.cat(outs), torch.cat(tols)
+
+
+MODS = {"plain": {}, "cap": dict(cap=2.5), "bias": dict(slopes=True), "window": dict(window=45), "all": dict(cap=1.5, slopes=True, window=77, scale=0.3)}
+
+
+def operands(mods, heads):
+    kw = dict(MODS[mods])
+    if kw.get("slopes"):
+        kw["slopes"] = torch.tensor([2.0 ** (-(h % 7) - 1) for h in range(heads)])
+    return kw
+
+
+def on_gpu(kw):
+    return {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in kw.items()}
+
+
+ROWS = [(1, 1, 128, 32, [1]), (4, 4, 64, 64, [0, 1, 2, 31, 32, 33, 64, 65]), (8, 1, 8, 32, [7, 100, 257]), (6, 2, 80, 96, [300, 95, 96, 97]),
+        (40, 2, 128, 32, [129, 1, 700]), (3, 3, 256, 32, [5, 515]), (16, 1, 192, 64, [1000]), (5, 5, 24, 128, [127, 128, 129]),
+        (64, 8, 128, 64, [4500]), (2, 1, 96, 4096, [9000, 3])]
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("mods", MODS)
+@pytest.mark.parametrize("heads,kv,D,page,lengths", ROWS)
+def test_one_row(heads, kv, D, page, lengths, mods, values):
+    s = Setting(lengths, kv, D, page, values, seed=heads + D).fill()
+    q = draw(5, len(lengths), heads, D, scale=2.0)
+    kw = operands(mods, heads)
+    got = s.cache.attention(s.rows(), q.cuda(), **on_gpu(kw))
+    assert s.cache.plan(s.rows(), len(lengths), heads).startswith("rows")
+    # A sequence of no tokens has no row in the plain form: zeros.
+    counts = [min(1, L) for L in lengths]
+    has = torch.tensor(counts, dtype=torch.bool)
+    want, tol = s.want(q[has], counts, **kw)
+    assert (got[~has.cuda()] == 0).all()
+    attention64.close(got[has.cuda()], want, tol)
+
+
+TILES = [(1, 1, 128, 32, [40], [40]), (4, 2, 64, 64, [130, 7, 64, 300], [130, 0, 1, 200]), (6, 2, 80, 32, [100, 33], [33, 33]),
+         (20, 1, 128, 64, [70, 5], [64, 5]), (3, 3, 256, 32, [150], [150]), (2, 1, 96, 96, [401, 200], [129, 200]), (8, 8, 24, 32, [65], [65]),
+         (2, 2, 192, 64, [131], [100])]
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("mods", MODS)
+@pytest.mark.parametrize("heads,kv,D,page,lengths,counts", TILES)
+def test_many_rows(heads, kv, D, page, lengths, counts, mods, values):
+    s = Setting(lengths, kv, D, page, values, seed=heads + D + 1).fill()
+    T = sum(counts)
+    q = draw(6, T, heads, D, scale=2.0)
+    kw = operands(mods, heads)
+    rows = s.rows(counts)
+    assert s.cache.plan(rows, T, heads).startswith("tiles")
+    got = s.cache.attention(rows, q.cuda(), **on_gpu(kw))
+    attention64.close(got, *s.want(q, counts, **kw))
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("counts", [[1, 3, 0, 2], [60, 40, 0, 33]])
+def test_masks(counts, values):
+    """Documents, prefixes, and rows that nothing is left of, through both kernels; NaN and infinities where a row does not look."""
+    lengths = [90, 64, 17, 130]
+    s = Setting(lengths, 2, 64, 32, values, seed=9)
+    for L, V, K in zip(lengths, s.V, s.K):
+        V[L // 2, :, 3], V[L // 3, 1] = float("inf"), float("nan")
+        K[L // 4, 0, 5] = float("nan")
+    s.fill()
+    T = sum(counts)
+    g = torch.Generator().manual_seed(3)
+    q = draw(7, T, 4, 64)
+    position = torch.cat([torch.arange(L - n, L) for L, n in zip(lengths, counts)])
+    first = torch.randint(-3, 120, (T,), generator=g).int()
+    last = torch.randint(-5, 200, (T,), generator=g).int()
+    documents = (position // 20 * 20).int()
+    prefix = torch.maximum(position + 1, torch.tensor(40)).int()
+    for kw in (dict(first=first, last=last), dict(first=documents), dict(last=prefix), dict(first=first, window=9), dict(first=position.int() + 1)):
+        got = s.cache.attention(s.rows(counts), q.cuda(), **on_gpu(kw))
+        want, tol = s.want(q, counts, **kw)
+        if values == "f16":  # an infinity that a row sees is one; NaN where it is any
+            attention64.close(got, want, tol)
+        else:  # a token that is not finite is NaN in 8 bits, in every channel
+            attention64.close(got, want, torch.where(tol.isnan(), torch.zeros_like(tol), tol))
+    assert (got == 0).all()
+
+
+def test_scores_that_are_not_finite():
+    """A row that sees a NaN is NaN, also where an infinity of q meets K; others keep their bits."""
+    s = Setting([50], 1, 64, 32, seed=4).fill()
+    q = draw(8, 50, 1, 64)
+    clean = s.cache.attention(s.rows([50]), q.cuda())
+    bad = q.clone()
+    bad[13, 0, 2], bad[20, 0, 0] = float("nan"), float("inf")
+    got = s.cache.attention(s.rows([50]), bad.cuda())
+    others = [i for i in range(50) if i not in (13, 20)]
+    assert torch.equal(got[others], clean[others]) and got[13].isnan().all() and got[20].isnan().all()
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [40, 35]])
+def test_strides(counts):
+    """q as a part of a fused projection and at odd addresses, heads before rows, results between other values."""
+    heads, kv, D = 6, 2, 64
+    s = Setting([100, 70], kv, D, seed=11).fill()
+    T = sum(counts)
+    q = draw(9, T, heads, D)
+    rows = s.rows(counts)
+    want = s.cache.attention(rows, q.cuda())
+    fused = torch.zeros(T, (heads + 2 * kv) * D + 3, dtype=torch.float16, device="cuda")
+    places = [fused[:, :heads * D].unflatten(1, (heads, D)), fused[:, 1:1 + heads * D].unflatten(1, (heads, D)),
+              torch.zeros(heads, T, D, dtype=torch.float16, device="cuda").transpose(0, 1),
+              torch.zeros(T, heads, D + 5, dtype=torch.float16, device="cuda")[..., 3:3 + D]]
+    for place in places:
+        place.copy_(q)
+        assert torch.equal(s.cache.attention(rows, place), want)
+        base = torch.full_like(place._base, 7.0)
+        out = base.as_strided(place.shape, place.stride(), place.storage_offset())
+        s.cache.attention(rows, q.cuda(), out=out)
+        assert torch.equal(out, want)
+        out.fill_(7)
+        assert (base == 7).all()
+    one = q[:, :1].cuda().expand(T, heads, D)
+    assert torch.equal(s.cache.attention(rows, one), s.cache.attention(rows, one.contiguous()))
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("D", [8, 40, 64, 96, 128, 200, 256])
+def test_append_and_read(D, values):
+    """Every element where the layout says, codes and scales by the definition, nothing beside the rows written."""
+    lengths, counts, kv, page = [70, 33, 5, 64], [70, 2, 0, 33], 3, 64
+    s = Setting(lengths, kv, D, page, values, seed=D, layers=2, layer=1)
+    before = s.cache.data.clone()
+    K = torch.cat([k[L - n:] for k, L, n in zip(s.K, lengths, counts)])
+    V = torch.cat([v[L - n:] for v, L, n in zip(s.V, lengths, counts)])
+    V[3] = 0
+    V[5, 1, 2] = float("inf")
+    K[6, 0, 1] = float("nan")
+    s.cache.append(s.rows(counts), K.cuda(), V.cuda(), layer=1)
+    assert torch.equal(s.cache.data[0], before[0])
+    kb, vb = (x[1].cpu() for x in s.cache.blocks())
+    block = 64 * usp.cache_width(D) + 256
+    t = 0
+    written = torch.zeros(s.cache.pages, kv, page, dtype=torch.bool)
+    for i, (L, n) in enumerate(zip(lengths, counts)):
+        for j in range(L - n, L):
+            p, place = int(s.table[i, j // page]), j % page
+            written[p, :, place] = True
+            b = place % 32
+            for h in range(kv):
+                got_k = kb[p, h, place // 32, b >> 4, b >> 3 & 1, b >> 2 & 1, b & 3].reshape(-1)
+                got_v = vb[p, h, place // 32, b // 8, b % 8]
+                for got, x, which in ((got_k, K[t, h], 0), (got_v, V[t, h], 1)):
+                    if values == "f16":
+                        assert torch.equal(got.view(torch.int16), x.view(torch.int16))
+                        continue
+                    a = x.float().abs().max()
+                    ok = bool(torch.isfinite(a))
+                    inv = (127.0 / a.double()).float() if ok and a > 0 else torch.tensor(0.0)
+                    codes = (x.double() * inv.double()).float().round() if ok else torch.zeros(D)
+                    assert torch.equal(got, codes.to(torch.int8))
+                    raw = s.cache.data[1, p].view(kv, page // 32, block)[h, place // 32, -256:].view(torch.float32).cpu()
+                    scale = raw[32 * which + place % 32]
+                    assert scale.isnan() if not ok else scale == (a.double() / 127).float()
+            t += 1
+    # What was not written still holds the fill.
+    kk = kb.view(torch.int16 if values == "f16" else torch.int8)
+    empty = ~written.view(-1, kv, page // 32, 2, 2, 2, 4)
+    assert (kk[empty] == -1).all()
+    k2, v2 = s.cache.read(s.rows(counts), K.shape[0], layer=1)
+    for got, x in ((k2, K), (v2, V)):
+        want = attention64.held(x, s.eight_bit).half() if s.eight_bit else x
+        assert torch.equal(got.cpu().nan_to_num(9, 99, -99), want.nan_to_num(9, 99, -99))
+
+
+def test_append_strides():
+    kv, D = 2, 64
+    s = Setting([40], kv, D, seed=3)
+    fused = draw(1, 40, 2 * kv * D + 1).cuda()
+    for at in (0, 1):
+        K, V = fused[:, at:at + kv * D].unflatten(1, (kv, D)), fused[:, at + kv * D:at + 2 * kv * D].unflatten(1, (kv, D))
+        s.cache.append(s.rows([40]), K, V)
+        k, v = s.cache.read(s.rows([40]), 40)
+        assert torch.equal(k, K) and torch.equal(v, V)
+        out = torch.full((40, kv * D + 3), 5.0, dtype=torch.float16, device="cuda")
+        place = out[:, 1:1 + kv * D].unflatten(1, (kv, D))
+        usp.usp_cache_read(s.cache, s.rows([40]), place, torch.empty_like(place, memory_format=torch.contiguous_format))
+        assert torch.equal(place, K) and (out[:, 0] == 5).all() and (out[:, -2:] == 5).all()
+
+
+def test_rows_that_are_not_there():
+    """Pages outside the cache, lengths beyond the table, rows outside the offsets: no write, no influence, nothing read outside."""
+    kv, D, heads = 1, 64, 2
+    s = Setting([64, 96], kv, D, 32, seed=5).fill()
+    q = draw(2, 2, heads, D).cuda()
+    table = s.table.clone()
+    for page in (-1, s.cache.pages, 2 ** 31 - 1, -2 ** 31):
+        table[1, 1] = page
+        rows = usp.CacheRows(table.cuda(), int32(s.lengths))
+        K, V = s.K[1].clone(), s.V[1].clone()
+        keep = torch.ones(96, dtype=torch.bool)
+        keep[32:64] = False
+        want, tol = attention64.attend(q[1:].cpu(), K[keep].double(), V[keep].double())
+        attention64.close(s.cache.attention(rows, q)[1:], want, tol)
+        many = usp.CacheRows(table.cuda(), int32(s.lengths), int32([0, 0, 96]))
+        before = s.cache.data.clone()
+        s.cache.append(many, s.K[1].cuda(), s.V[1].cuda())
+        assert torch.equal(s.cache.data, before)
+        got = s.cache.attention(many, q[1:].expand(96, heads, D))
+        attention64.close(got[95:], want, tol)
+        assert torch.equal(got[:32], s.cache.attention(s.rows([0, 96]), q[1:].expand(96, heads, D))[:32])
+    table[1] = -5  # nothing at all
+    rows = usp.CacheRows(table.cuda(), int32(s.lengths))
+    assert (s.cache.attention(rows, q)[1] == 0).all()
+    # Lengths beyond the table and below zero.
+    full = s.cache.attention(s.rows(), q)
+    rows = usp.CacheRows(s.table[:, :3].contiguous().cuda(), int32([-7, 10 ** 6]))
+    got = s.cache.attention(rows, q)
+    assert (got[0] == 0).all() and torch.equal(got[1], full[1])
+    # Offsets out of range, decreasing, and rows that no sequence has.
+    out = torch.full((70, heads, D), 9.0, dtype=torch.float16, device="cuda")
+    q70 = draw(3, 70, heads, D).cuda()
+    usp.usp_attention(s.cache, usp.CacheRows(s.rows().table, s.rows().lengths, int32([3, 40, 60])), q70, out,
+                      s.cache.make_workspace(s.rows([3, 67]), 70, heads))
+    assert (out[:3] == 9).all() and (out[60:] == 9).all() and not (out[3:60] == 9).all(-1).any()
+    for offsets in ([-5, 40, 500], [50, 20, 70], [70, 0, 0], [2 ** 31 - 1, -2 ** 31, 3]):
+        for T in (70, 7):
+            out = torch.full((T + 40, heads, D), 9.0, dtype=torch.float16, device="cuda")
+            rows = usp.CacheRows(s.rows().table, s.rows().lengths, int32(offsets))
+            ws = s.cache.make_workspace(rows, T, heads)
+            usp.usp_attention(s.cache, rows, q70[:T], out[20:20 + T], ws)
+            assert (out[:20] == 9).all() and (out[20 + T:] == 9).all()
+            before = s.cache.data.clone()
+            s.cache.append(rows, torch.cat(s.K)[:T].cuda(), torch.cat(s.V)[:T].cuda())
+            assert s.cache.data.shape == before.shape
+            s.cache.data.copy_(before)
+            assert ws is None or (ws[:256 << 10] == 0).all()
+    assert torch.equal(s.cache.attention(s.rows(), q), full)
+
+
+def test_long_and_far():
+    """A long sequence in pieces, and pages behind 2^32 bytes."""
+    kv, D, heads, page = 2, 128, 16, 256
+    cache = usp.KVCache(24000, kv, D, page)  # 6.3 GB
+    assert cache.data.numel() > 2 ** 32
+    L = 70001
+    need = -(-L // page)
+    order = torch.cat([torch.arange(24000 - need // 2, 24000), torch.arange(need - need // 2)]).int()
+    K, V = draw(1, L, kv, D), draw(2, L, kv, D)
+    everything = usp.CacheRows(order[None].cuda(), int32([L]), int32([0, L]))
+    cache.append(everything, K.cuda(), V.cuda())
+    q = draw(3, 1, heads, D, scale=3.0)
+    rows = usp.CacheRows(order[None].cuda(), int32([L]))
+    want, tol = attention64.attend(q, K.double(), V.double())
+    attention64.close(cache.attention(rows, q.cuda()), want, tol)
+    k, v = cache.read(everything, L)
+    assert torch.equal(k.cpu(), K) and torch.equal(v.cpu(), V)
+    del k, v
+    cache.copy([0], [23990])
+    assert torch.equal(cache.data[:, 23990], cache.data[:, 0])
+
+
+@pytest.mark.parametrize("n,pages,layers", [(1, 4, 1), (5, 16, 3), (460, 1000, 2)])
+def test_copy(n, pages, layers):
+    cache = usp.KVCache(pages, 3, 40, 32, layers)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    cache.data.random_(0, 256, generator=g)
+    before = cache.data.clone()
+    order = torch.randperm(pages, generator=torch.Generator().manual_seed(n)).tolist()
+    src, dst = order[:n], order[n:2 * n]
+    src[0] = src[-1]  # a page may go to several
+    cache.copy(src, dst)
+    before[:, dst] = before[:, src]
+    assert torch.equal(cache.data, before)
+    cache.copy([], [])
+    cache.copy([src[0]], [src[0]])
+    assert torch.equal(cache.data, before)
+
+
+@pytest.mark.parametrize("counts", [[1, 1, 1], [30, 20, 9]])
+def test_captured_and_replayed(counts):
+    """A captured step of append and attention follows its tensors; a workspace that products use too stays ready."""
+    heads, kv, D = 8, 2, 64
+    s = Setting([2000, 900, 64], kv, D, 32, seed=21).fill()
+    T = sum(counts)
+    rows = s.rows(counts) if T > 3 else s.rows()
+    q, K, V = (draw(i, T, n, D).cuda() for i, n in ((1, heads), (2, kv), (3, kv)))
+    out = torch.empty_like(q)
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+
+    def step():
+        s.cache.append(rows, K, V)
+        usp.usp_attention(s.cache, rows, q, out, ws, window=1500)
+
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(5):
+        q.copy_(draw(30 + i, T, heads, D))
+        K.copy_(draw(40 + i, T, kv, D))
+        rows.lengths.copy_(int32([2000 - 300 * i, 900 - 100 * i, 64 - 2 * i]))
+        before = s.cache.data.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, cache = out.clone(), s.cache.data.clone()
+        s.cache.data.copy_(before)
+        out.fill_(float("nan"))
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.equal(cache, s.cache.data)
+        assert (ws[:256 << 10] == 0).all()
+
+
+def test_same_bits_and_streams():
+    """The same call gives the same bits, on other streams with workspaces of their own too."""
+    s = Setting([9000, 10, 3000], 2, 128, 64, seed=8).fill()
+    q = draw(1, 3, 16, 128).cuda()
+    want = s.cache.attention(s.rows(), q)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for i in range(12):
+        got.append(s.cache.attention(s.rows(), q, stream=streams[i % 3]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+
+
+def test_module():
+    """Prompts, forks, single tokens, a cut, a compaction: the module over a PagedCache against the plain form."""
+    heads, kv, D = 6, 2, 64
+    cache = attention.PagedCache(40, kv, D, page_tokens=32, layers=2)
+    cache.data.fill_(255)
+    mod = attention.PagedAttention(heads, kv, D, cap=20.0, slopes=torch.full((heads,), 0.01))
+    kept = {}
+    seed = [0]
+
+    def step(ids, counts, layer):
+        T = sum(counts)
+        seed[0] += 3
+        q, k, v = draw(seed[0], T, heads * D), draw(seed[0] + 1, T, kv, D), draw(seed[0] + 2, T, kv * D)
+        got = mod(q.cuda(), cache, step.rows, k.cuda(), v.cuda(), layer=layer)
+        assert got.shape == q.shape
+        at = 0
+        for i, n in zip(ids, counts):
+            K, V = kept.get((i, layer), (torch.empty(0, kv, D).half(), torch.empty(0, kv, D).half()))
+            kept[i, layer] = K, V = torch.cat([K, k[at:at + n]]), torch.cat([V, v[at:at + n].view(n, kv, D)])
+            want, tol = attention64.attend(q[at:at + n].view(n, heads, D), K.double(), V.double(), cap=20.0, slopes=torch.full((heads,), 0.01))
+            attention64.close(got[at:at + n].view(n, heads, D), want, tol)
+            at += n
+
+    def run(ids, counts=None):
+        step.rows = cache.extend(ids, counts)
+        for layer in range(2):
+            step(ids, counts or [1] * len(ids), layer)
+
+    a, b = cache.add(), cache.add()
+    run([a, b], [45, 64])
+    run([a, b])
+    c = cache.fork(a)
+    for layer in range(2):
+        kept[c, layer] = kept[a, layer]
+    assert cache.pages_of(c) == cache.pages_of(a)
+    run([b, c, a])
+    assert cache.pages_of(c)[0] == cache.pages_of(a)[0] and cache.pages_of(c)[1] != cache.pages_of(a)[1]
+    run([c, a], [20, 1])
+    cache.truncate(b, 40)
+    for layer in range(2):
+        kept[b, layer] = tuple(x[:40] for x in kept[b, layer])
+    cache.free(a)
+    run([b, c], [1, 30])
+    used = cache.compact()
+    assert used == 40 - cache.free_pages and max(cache.pages_of(b) + cache.pages_of(c)) < used
+    run([c, b])
+    single = cache.rows([c, b])
+    cache.update(single, [b, c])
+    assert single.lengths.tolist() == [cache.length(b), cache.length(c)]
+    # Through the operators, as a tracer sees them.
+    q = draw(90, 2, heads, D).cuda()
+    want = mod(q, cache, single)
+    with torch.overrides.BaseTorchFunctionMode():
+        assert torch.equal(mod(q, cache, single), want)
+    empty = mod(q[:0], cache, single)
+    assert empty.shape == (0, heads, D)
+
+
+def test_workspace_shared_with_products():
+    """One zero-filled workspace for a sparse product and an attention in pieces, in turn."""
+    g = torch.Generator().manual_seed(1)
+    W = torch.randn(512, 1024, generator=g).half().numpy()
+    A = usp.SparseMatrix(W, (torch.rand(512, 1024, generator=g) < 0.5).numpy())
+    X = draw(2, 16, 1024).cuda()
+    s = Setting([6000], 2, 64, 64, seed=2).fill()
+    q = draw(3, 1, 8, 64).cuda()
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    want_y, want_o = A.spmm(X), s.cache.attention(s.rows(), q)
+    for _ in range(3):
+        y, o = A.spmm(X, workspace=ws), s.cache.attention(s.rows(), q, workspace=ws)
+        assert torch.equal(y, want_y) and torch.equal(o, want_o)
+
+
+def test_binding_refusals():
+    s = Setting([40, 40], 2, 64, 32, seed=1).fill()
+    q = draw(1, 2, 4, 64).cuda()
+    rows = s.rows()
+    out = torch.empty_like(q)
+    ws = s.cache.make_workspace(rows, 2, 4)
+    call = lambda **kw: usp.usp_attention(**{**dict(cache=s.cache, rows=rows, q=q, out=out, workspace=ws), **kw})  # noqa: E731
+    call()
+    for bad in (dict(q=q.float()), dict(q=q[:, :, :32]), dict(q=q[:1]), dict(out=out[:, :2]), dict(out=out.cpu()), dict(first=int32([0])),
+                dict(last=torch.zeros(2, device="cuda")), dict(slopes=torch.zeros(3, device="cuda")), dict(q=q.transpose(1, 2).contiguous().transpose(1, 2))):
+        with pytest.raises((TypeError, ValueError)):
+            call(**bad)
+    for bad in (dict(workspace=None), dict(q=q[:, :3], out=out[:, :3]), dict(layer=1), dict(cap=-1.0), dict(scale=float("inf")), dict(window=-1),
+                dict(out=out[:, :1].expand(2, 4, 64)), dict(out=out[:1].expand(2, 4, 64))):
+        with pytest.raises(usp.UspError):
+            call(**bad)
+    K = draw(2, 2, 2, 64).cuda()
+    for bad in (lambda: s.cache.append(rows, K[:1], K[:1]), lambda: s.cache.append(rows, K, K[:, :1]), lambda: s.cache.append(rows, K.float(), K)):
+        with pytest.raises((TypeError, ValueError)):
+            bad()
+    with pytest.raises(usp.UspError):
+        s.cache.append(rows, K, K, layer=-1)
+    with pytest.raises(usp.UspError):
+        usp.usp_cache_read(s.cache, rows, K[:, :1].expand(2, 2, 64), K.clone())
+    for src, dst in (([0], [99]), ([-1], [0]), ([0, 1], [2, 2]), ([0, 1], [1, 2])):
+        with pytest.raises(usp.UspError):
+            s.cache.copy(src, dst)
+    with pytest.raises(ValueError):
+        s.cache.copy([0], [1, 2])
