@@ -11,7 +11,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libusp.so")
 SOURCES = ["usp_abi.cpp", "usp_encode.cpp", "usp_kernels.hip", "usp_wide.hip", "usp_norm.hip",
-           "usp_product.hip", "usp_product_wide.hip", "usp_cache.hip", "usp_attention.hip"]
+           "usp_product.hip", "usp_product_wide.hip", "usp_cache.hip", "usp_attention.hip",
+           "usp_attention_tiles.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # Packed fp32 VALU forms are disabled for all device code.

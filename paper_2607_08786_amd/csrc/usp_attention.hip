@@ -1,134 +1,12 @@
-// usp_attention.hip -- attention of a step's rows over a paged cache (include/usp.h,
-// usp_attention).
-//
-// Both kernels take a tile of columns (a column: one head of one row, all columns of a tile
-// reading one head of the cache) through the blocks of 32 keys that it sees, once, with the
-// running maximum m and sum l of each column's softmax:
-//
-//     S^T = K Q^T     (keys x columns; rows of K are the matrix unit's A operand)
-//     p = exp2(s - m),  l = l exp2(m_old - m) + sum p
-//     O^T = O^T exp2(m_old - m) + V^T P^T    (channels x columns; rows of V^T are A)
-//
-// S^T leaves a lane the scores of one column, and with the cache's order of a block's
-// keys they are the 8 consecutive keys of which it hands over P^T's B operand: softmax and
-// P stay in registers, without an exchange but the maximum over the lanes of a column. K and V
-// are read in the order that they lie in (usp_cache.h).
-#include "usp_cache.h"
-#include "usp_device.h"
+// usp_attention.hip -- attention of a step's rows over a paged cache: the planner, and the kernel
+// for few rows of each sequence (single tokens).
+#include "usp_attention.h"
 
 #include <algorithm>
 #include <cmath>
 
 namespace usp {
 namespace {
-
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef uint32_t v2u32 __attribute__((ext_vector_type(2)));
-typedef _Float16 half2a __attribute__((ext_vector_type(2)));
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNothing = -__builtin_inff();
-
-struct AttendArgs {
-    CacheView c;
-    RowsView r;
-    const int32_t *first, *last;
-    const uint16_t *q;
-    uint16_t *out;
-    const float *slopes;
-    int64_t ld_q, head_q, ld_out, head_out;
-    float scale;           // score of q . K in the exponent of 2, or the argument of the cap's exponential
-    float cap;             // in the exponent of 2; 0: none
-    int heads, group, window;
-    int tiles;             // tiles of 16 heads of a row (rows kernel)
-    int q_vec, out_vec;
-    int split;             // whether tiles are cut into pieces (rows kernel)
-    int pieces_bits;       // 2^pieces_bits pieces of all tiles and heads together are aimed at
-    int limit, slot_limit; // items of a head in the grid, and slots of a head in the workspace
-    uint32_t *counters;
-    float *partials;
-};
-
-__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// The larger of a value and what the lanes 16 (32) away hold.
-__device__ inline float max_16(float v) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, v);
-    const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)s[0]), __builtin_bit_cast(float, (uint32_t)s[1]));
-}
-__device__ inline float max_32(float v) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, v);
-    const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)s[0]), __builtin_bit_cast(float, (uint32_t)s[1]));
-}
-__device__ inline float sum_16(float v) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, v);
-    const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]);
-}
-__device__ inline float sum_32(float v) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, v);
-    const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]);
-}
-
-// Eight codes as fp16: the byte 128 + c under the exponent of 1024 is 1152 + c, exactly.
-__device__ inline half8 halves_of(v2u32 codes) {
-    const half2a bias = {(_Float16)-1152.f, (_Float16)-1152.f};
-    v4u32 out;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t u = codes[i / 2] ^ 0x80808080u;
-        const uint32_t w = __builtin_amdgcn_perm(0x64646464u, u, i % 2 ? 0x07030602u : 0x05010400u);
-        out[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2a, w) + bias);
-    }
-    return __builtin_bit_cast(half8, out);
-}
-
-// Eight channels d .. d + 7 of a head of q, zeros behind head_dim and where there is no column.
-__device__ inline half8 load_q8(const AttendArgs &a, int t, int head, int d, bool there) {
-    half8 x = {};
-    if (!there || d >= a.c.head_dim) return x;
-    const uint16_t *from = a.q + (int64_t)t * a.ld_q + (int64_t)head * a.head_q + d;
-    if (a.q_vec) return *reinterpret_cast<const half8 *>(from);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __builtin_bit_cast(_Float16, from[i]);
-    return x;
-}
-
-// Channels d .. d + 3 of an output.
-__device__ inline void store_out4(const AttendArgs &a, int t, int head, int d, floatx4 v) {
-    uint16_t *to = a.out + (int64_t)t * a.ld_out + (int64_t)head * a.head_out + d;
-    uint16_t h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, (_Float16)v[i]);
-    if (a.out_vec) {
-        *reinterpret_cast<uint2 *>(to) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to[i] = h[i];
-    }
-}
-
-// The keys lo <= k < hi that row t, token p of a sequence of len, sees.
-__device__ inline void span_of(const AttendArgs &a, int t, int p, int len, int &lo, int &hi) {
-    lo = a.first ? a.first[t] : 0;
-    if (a.window && p - a.window + 1 > lo) lo = p - a.window + 1;
-    if (lo < 0) lo = 0;
-    hi = a.last ? a.last[t] : p + 1;
-    if (hi > len) hi = len;
-    if (p < 0) hi = 0;
-}
-
-// A score in the exponent of 2, from q . K: scaled, capped, biased.
-__device__ inline float score_of(const AttendArgs &a, float x, float slope, int p, int key) {
-    x *= a.scale;
-    if (a.cap > 0.f)  // cap tanh(y): 1 - 2 / (1 + exp(2 y)); x is 2 y in the exponent of 2
-        x = a.cap * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_of(x)));
-    if (a.slopes) x -= slope * fabsf((float)(p - key));
-    return x;
-}
 
 // ---- Few rows of each sequence: one tile of up to 16 heads of a row at a time.
 
@@ -472,207 +350,6 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
     if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// ---- Many rows of each sequence: tiles of 128 columns of consecutive rows and the heads of a cache's head.
-
-constexpr int kTileWaves = 4;
-constexpr int kTileColumns = 32 * kTileWaves;
-
-// The first tile of sequence s: those before it have at most so many.
-__device__ inline int first_tile(const AttendArgs &a, int s) {
-    return (int)((int64_t)offset_of(a.r, s) * a.group / kTileColumns) + s;
-}
-
-template <int DS, int VB>
-__global__ __launch_bounds__(kTileWaves *kLanes) void attend_tiles_kernel(AttendArgs a) {
-    constexpr int W = 32 * DS, kBlockBytes = (int)cache_block_bytes(W, VB);
-    __shared__ half8 staged[W / 8 * kBlockTokens * 2];  // a block of keys, then of values, as in the cache
-    __shared__ floatx4 scales[2 * kBlockTokens / 4];
-    __shared__ int ends[2][kTileWaves];
-
-    const int h = blockIdx.x % a.c.kv_heads, tile = blockIdx.x / a.c.kv_heads;
-    int s = 0;
-    {
-        int below = a.r.sequences;  // first_tile(s) <= tile < first_tile(below)
-        while (below - s > 1) {
-            const int mid = (s + below) / 2;
-            if (first_tile(a, mid) <= tile)
-                s = mid;
-            else
-                below = mid;
-        }
-    }
-    const int off = offset_of(a.r, s), n = offset_of(a.r, s + 1) - off, len = length_of(a.r, s);
-    const int64_t column0 = (int64_t)(tile - first_tile(a, s)) * kTileColumns;
-    if (column0 < 0 || column0 >= (int64_t)n * a.group) return;
-
-    const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes, c = lane & 31, half = lane >> 5;
-    const int64_t column = column0 + 32 * wave + c;
-    const int row = (int)(column / a.group), t = off + row, head = h * a.group + (int)(column - (int64_t)row * a.group);
-    const bool there = row < n;
-    const int p = len - n + row;
-    int lo = 0, hi = 0;
-    if (there) span_of(a, t, p, len, lo, hi);
-
-    // The keys that the tile and this wavefront see any of, and those that all of its columns see.
-    const bool sees = hi > lo;
-    int any_lo = sees ? lo : 0x7FFFFFFF, any_hi = sees ? hi : 0, all_lo = there ? lo : 0, all_hi = there ? hi : 0x7FFFFFFF;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        any_lo = min(any_lo, __shfl_xor(any_lo, d, kLanes));
-        any_hi = max(any_hi, __shfl_xor(any_hi, d, kLanes));
-        all_lo = max(all_lo, __shfl_xor(all_lo, d, kLanes));
-        all_hi = min(all_hi, __shfl_xor(all_hi, d, kLanes));
-    }
-    any_lo = __builtin_amdgcn_readfirstlane(any_lo);
-    any_hi = __builtin_amdgcn_readfirstlane(any_hi);
-    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-    if (lane == 0) {
-        ends[0][wave] = any_lo;
-        ends[1][wave] = any_hi;
-    }
-    __syncthreads();
-    int tile_lo = ends[0][0], tile_hi = ends[1][0];
-#pragma unroll
-    for (int w = 1; w < kTileWaves; ++w) {
-        tile_lo = min(tile_lo, ends[0][w]);
-        tile_hi = max(tile_hi, ends[1][w]);
-    }
-
-    half8 q[2 * DS];
-#pragma unroll
-    for (int i = 0; i < 2 * DS; ++i) q[i] = load_q8(a, t, head, 16 * i + 8 * half, there);
-    const float slope = a.slopes && there ? a.slopes[head] * kLog2e : 0.f;
-
-    floatx16 o[DS];
-#pragma unroll
-    for (int d = 0; d < DS; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    float m = kNothing, l = 0.f, unit = 1e-30f;
-    const int32_t *table = a.r.table + (int64_t)s * a.r.ld_table;
-    const int b1 = (tile_hi + kBlockTokens - 1) / kBlockTokens;
-    for (int b = tile_hi > tile_lo ? tile_lo / kBlockTokens : b1; b < b1; ++b) {
-        const int in = b / a.c.page_blocks;
-        const uint32_t page = (uint32_t)table[in];
-        if (page >= a.c.pages) continue;
-        const uint8_t *block = a.c.base + (int64_t)page * a.c.page_bytes + ((int64_t)h * a.c.page_blocks + (b - in * a.c.page_blocks)) * kBlockBytes;
-        __syncthreads();  // the block before has been read
-#pragma unroll
-        for (int i = 0; i < W / 8 * kBlockTokens * 2 / (kTileWaves * kLanes); ++i) {
-            const int unit8 = i * kTileWaves * kLanes + threadIdx.x;
-            if (VB == 2)
-                staged[unit8] = reinterpret_cast<const half8 *>(block)[unit8];
-            else
-                staged[unit8] = halves_of(reinterpret_cast<const v2u32 *>(block)[unit8]);
-        }
-        if (VB == 1 && threadIdx.x < 2 * kBlockTokens / 4)
-            scales[threadIdx.x] = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W)[threadIdx.x];
-        __syncthreads();
-        const int block_lo = b * kBlockTokens, block_hi = block_lo + kBlockTokens;
-        if (block_hi <= any_lo || block_lo >= any_hi) continue;  // this wavefront sees nothing of it
-        const bool whole = all_lo <= block_lo && block_hi <= all_hi;
-
-        floatx16 st;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) st[i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 2 * DS; ++i)
-            st = __builtin_amdgcn_mfma_f32_32x32x16_f16(staged[(2 * i + half) * kBlockTokens + c], q[i], st, 0, 0, 0);
-
-        // Register 8 u + j holds the score of key block_lo + 16 u + 8 half + j.
-        float top = kNothing, top_scale = 0.f;
-        floatx4 vs[4];
-        uint32_t seen = 0xFFFFu;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int in_block = 16 * (i / 8) + 8 * half + i % 8, key = block_lo + in_block;
-            if (VB == 1) {
-                st[i] *= scales[in_block / 4][i % 4];
-                if (i % 4 == 0) vs[i / 4] = scales[(kBlockTokens + in_block) / 4];
-                if (key < len) top_scale = fmaxf(top_scale, vs[i / 4][i % 4]);
-            }
-            st[i] = score_of(a, st[i], slope, p, key);
-            if (!whole && !(key >= lo && key < hi)) {
-                st[i] = kNothing;
-                seen &= ~(1u << i);
-            }
-            top = fmaxf(top, st[i]);
-        }
-        const float m_new = fmaxf(m, max_32(top));
-        const float base = m_new == kNothing ? 0.f : m_new;
-        float fade = exp2_of(m - base);
-        m = m_new;
-        l *= fade;
-        float to_unit = 1.f;
-        if (VB == 1) {
-            const float u = fmaxf(unit, max_32(top_scale));
-            fade *= unit / u;
-            unit = u;
-            to_unit = 16384.f / u;
-        }
-        half8 w[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float x = exp2_of(st[i] - base);
-            x = whole || (seen >> i & 1) ? x : 0.f;
-            l += x;
-            if (VB == 1) x = whole || (seen >> i & 1) ? x * (vs[i / 4][i % 4] * to_unit) : 0.f;
-            w[i / 8][i % 8] = (_Float16)x;
-        }
-#pragma unroll
-        for (int d = 0; d < DS; ++d) o[d] *= fade;
-        uint32_t odd = 0;  // values of this lane's that are not finite
-#pragma unroll
-        for (int d = 0; d < DS; ++d)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                half8 v = staged[W / 8 * kBlockTokens + (2 * u + half) * W + 32 * d + c];
-                if (VB == 2 && !whole) {
-                    // Nothing times infinity is not nothing: what is not finite is left out here.
-                    v4u32 bits = __builtin_bit_cast(v4u32, v);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t bad = ((bits[i] & 0x7C007C00u) + 0x04000400u) >> 15 & 0x00010001u;
-                        odd |= bad;
-                        bits[i] &= ~(bad * 0xFFFFu);
-                    }
-                    v = __builtin_bit_cast(half8, bits);
-                }
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[u], o[d], 0, 0, 0);
-            }
-        if (VB == 2 && !whole && __any(odd != 0)) {  // and added here to the columns that see it
-            const uint16_t *values = reinterpret_cast<const uint16_t *>(&staged[W / 8 * kBlockTokens]);
-#pragma unroll 1
-            for (int j = 0; j < kBlockTokens; ++j) {
-                const bool sees_j = block_lo + j >= lo && block_lo + j < hi;
-#pragma unroll
-                for (int d = 0; d < DS; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int channel = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
-                        const uint16_t u = values[((j / 8) * W + channel) * 8 + j % 8];
-                        if (sees_j && (u & 0x7C00) == 0x7C00) o[d][i] += (float)__builtin_bit_cast(_Float16, u);
-                    }
-            }
-        }
-    }
-
-    l = sum_32(l);
-    const float inv = (l == 0.f ? 0.f : 1.f / l) * (VB == 1 ? unit * (1.f / 16384.f) : 1.f);
-    if (!there) return;
-#pragma unroll
-    for (int d = 0; d < DS; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int channel = 32 * d + 8 * i + 4 * half;
-            floatx4 v = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-            v *= inv;
-            if (l == 0.f) v = floatx4{0.f, 0.f, 0.f, 0.f};
-            if (channel < a.c.head_dim) store_out4(a, t, head, channel, v);
-        }
-}
-
 typedef void (*AttendFn)(AttendArgs);
 
 template <int VB>
@@ -686,27 +363,18 @@ AttendFn rows_kernel_of(int width) {
         default: return attend_rows_kernel<8, VB>;
     }
 }
-template <int VB>
-AttendFn tiles_kernel_of(int width) {
-    switch (width) {
-        case 32: return attend_tiles_kernel<1, VB>;
-        case 64: return attend_tiles_kernel<2, VB>;
-        case 96: return attend_tiles_kernel<3, VB>;
-        case 128: return attend_tiles_kernel<4, VB>;
-        case 192: return attend_tiles_kernel<6, VB>;
-        default: return attend_tiles_kernel<8, VB>;
-    }
-}
-
 struct AttendPlan {
     bool rows;             // the rows kernel; else the tiles kernel
     bool split;
     int tiles, pieces_bits;
+    int pieces;            // of a tile at most (tiles kernel)
     int64_t limit, slots;  // items and partial results of a head
     size_t partial_bytes;
 };
 
 constexpr int kPiecesBits = 10;
+constexpr int64_t kTilePlaces = 512;   // workgroups of the tiles kernel that run at once
+constexpr int64_t kMostTilePieces = 16;
 
 AttendPlan plan_attention(const CacheView &c, const RowsView &r, int heads) {
     const int64_t group = heads / c.kv_heads;
@@ -714,7 +382,10 @@ AttendPlan plan_attention(const CacheView &c, const RowsView &r, int heads) {
     p.pieces_bits = kPiecesBits;
     p.rows = !r.offsets || (int64_t)r.rows <= 4 * (int64_t)r.sequences;
     if (!p.rows) {
-        p.limit = (int64_t)r.rows * group / kTileColumns + r.sequences;
+        const int64_t columns = tile_columns(c.width);
+        p.limit = ((int64_t)r.rows * group + columns - 1) / columns + r.sequences - 1;
+        p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>(kMostTilePieces, kTilePlaces / (p.limit * c.kv_heads)));
+        if (p.pieces > 1) p.partial_bytes = (size_t)(p.limit * c.kv_heads * p.pieces * tile_slot_floats(c.width)) * sizeof(float);
         return p;
     }
     p.tiles = (int)((group + 15) / 16);
@@ -741,7 +412,8 @@ size_t attention_workspace_bytes(const CacheView &c, const RowsView &r, int head
 std::string describe_attention(const CacheView &c, const RowsView &r, int heads) {
     const AttendPlan p = plan_attention(c, r, heads);
     return std::string(p.rows ? "rows" : "tiles") + " W=" + std::to_string(c.width) +
-           (p.split ? " pieces=" + std::to_string(1 << p.pieces_bits) : "") + " grid=" + std::to_string(p.limit * c.kv_heads);
+           (p.rows ? p.split ? " pieces=" + std::to_string(1 << p.pieces_bits) : "" : " pieces=" + std::to_string(p.pieces)) +
+           " grid=" + std::to_string(p.limit * c.kv_heads * (p.rows ? 1 : p.pieces));
 }
 
 bool attention_fits(const CacheView &c, const RowsView &r, int heads) {
@@ -771,14 +443,16 @@ int launch_attention(const CacheView &c, const RowsView &r, const usp_attention_
     a.q_vec = (reinterpret_cast<uintptr_t>(p.q) & 15) == 0 && p.ld_q % 8 == 0 && p.head_q % 8 == 0;
     a.out_vec = (reinterpret_cast<uintptr_t>(p.out) & 7) == 0 && p.ld_out % 4 == 0 && p.head_out % 4 == 0;
     a.split = plan.split;
+    a.pieces = plan.pieces;
     a.pieces_bits = plan.pieces_bits;
     a.limit = (int)plan.limit;
     a.slot_limit = (int)plan.slots;
     a.counters = reinterpret_cast<uint32_t *>(workspace);
     a.partials = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + kCounterRegionBytes);
-    const AttendFn fn = plan.rows ? c.value_bytes == 2 ? rows_kernel_of<2>(c.width) : rows_kernel_of<1>(c.width)
-                                  : c.value_bytes == 2 ? tiles_kernel_of<2>(c.width) : tiles_kernel_of<1>(c.width);
-    hipLaunchKernelGGL(fn, dim3((unsigned)(plan.limit * c.kv_heads)), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    const int64_t grid = plan.limit * c.kv_heads * (plan.rows ? 1 : plan.pieces);
+    if (!plan.rows) return launch_tiles(&a, c.width, c.value_bytes, a.cap > 0.f || a.slopes || !(a.scale > 0.f), grid, stream);
+    const AttendFn fn = c.value_bytes == 2 ? rows_kernel_of<2>(c.width) : rows_kernel_of<1>(c.width);
+    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(kRowWaves * kLanes), 0, reinterpret_cast<hipStream_t>(stream), a);
     return (int)hipGetLastError();
 }
 

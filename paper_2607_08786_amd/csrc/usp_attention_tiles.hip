@@ -1,0 +1,434 @@
+// usp_attention_tiles.hip -- attention of many rows of each sequence (prompts and pieces of
+// prompts): tiles of columns of consecutive rows and the heads that a cache's head serves.
+#include "usp_attention.h"
+
+#include <utility>
+
+namespace usp {
+namespace {
+
+constexpr int kMinTileBlocks = 16;  // blocks of a piece at least
+
+// The first tile of sequence s: those before it have at most so many.
+template <int COLUMNS>
+__device__ inline int first_tile(const AttendArgs &a, int s) {
+    return (int)((int64_t)offset_of(a.r, s) * a.group / COLUMNS) + s;
+}
+
+// Eight codes of keys j .. j + 7 of a channel as fp16 values.
+__device__ inline half8 values_of(v2u32 codes, floatx4 s0, floatx4 s1) {
+    half8 out;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int8_t c = (int8_t)(codes[i / 4] >> (8 * (i % 4)));
+        out[i] = (_Float16)((float)c * (i < 4 ? s0[i % 4] : s1[i % 4]));
+    }
+    return out;
+}
+
+// Columns of a wavefront: CT tiles of 32. MOD: scores are capped, biased or not scaled by a positive number.
+template <int DS, int VB, bool MOD, int CT>
+__global__ __launch_bounds__(kTileWaves *kLanes, CT == 2 || DS > 4 ? 1 : 2) void attend_tiles_kernel(AttendArgs a) {
+    constexpr int W = 32 * DS, kBlockBytes = (int)cache_block_bytes(W, VB);
+    constexpr int kColumns = 32 * CT * kTileWaves;
+    constexpr int kKeyUnits = W / 8 * kBlockTokens;  // units of 8 keys' channels, and as many of values'
+    constexpr int kThreads = kTileWaves * kLanes;
+    __shared__ half8 staged[2][2 * kKeyUnits];  // blocks of keys, then of values, as in the cache
+    __shared__ floatx4 key_scales[2][kBlockTokens / 4];
+    __shared__ int ends[4][kTileWaves];
+    __shared__ int odd[2][kTileWaves];  // whether a wavefront's part of a block's values holds any that is not finite
+    __shared__ uint32_t arrived;
+
+    const int h = blockIdx.x % a.c.kv_heads, piece = (int)(blockIdx.x / a.c.kv_heads) % a.pieces;
+    const int tile = a.limit - 1 - (int)(blockIdx.x / a.c.kv_heads) / a.pieces;  // a prompt's last rows see most: they begin
+    int s = 0;
+    {
+        int below = a.r.sequences;  // first_tile(s) <= tile < first_tile(below)
+        while (below - s > 1) {
+            const int mid = (s + below) / 2;
+            if (first_tile<kColumns>(a, mid) <= tile)
+                s = mid;
+            else
+                below = mid;
+        }
+    }
+    const int off = offset_of(a.r, s), n = offset_of(a.r, s + 1) - off, len = length_of(a.r, s);
+    const int64_t column0 = (int64_t)(tile - first_tile<kColumns>(a, s)) * kColumns;
+    if (column0 < 0 || column0 >= (int64_t)n * a.group) return;
+
+    const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes, c = lane & 31, half = lane >> 5;
+    int row[CT], head[CT], p[CT], lo[CT], hi[CT];
+    bool there[CT];
+    float slope[CT];
+    // The keys that the wavefront sees any of, and those that all of its columns see.
+    int any_lo = 0x7FFFFFFF, any_hi = 0, all_lo = 0, all_hi = 0x7FFFFFFF;
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+        const int64_t column = column0 + 32 * (wave * CT + t) + c;
+        row[t] = (int)(column / a.group);
+        head[t] = h * a.group + (int)(column - (int64_t)row[t] * a.group);
+        there[t] = row[t] < n;
+        p[t] = len - n + row[t];
+        lo[t] = hi[t] = 0;
+        if (there[t]) {
+            span_of(a, off + row[t], p[t], len, lo[t], hi[t]);
+            if (hi[t] > lo[t]) {
+                any_lo = min(any_lo, lo[t]);
+                any_hi = max(any_hi, hi[t]);
+            }
+            all_lo = max(all_lo, lo[t]);
+            all_hi = min(all_hi, hi[t]);
+        }
+        slope[t] = MOD && a.slopes && there[t] ? a.slopes[head[t]] * kLog2e : 0.f;
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        any_lo = min(any_lo, __shfl_xor(any_lo, d, kLanes));
+        any_hi = max(any_hi, __shfl_xor(any_hi, d, kLanes));
+        all_lo = max(all_lo, __shfl_xor(all_lo, d, kLanes));
+        all_hi = min(all_hi, __shfl_xor(all_hi, d, kLanes));
+    }
+    any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+    any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+    if (lane == 0) {
+        ends[0][wave] = any_lo;
+        ends[1][wave] = any_hi;
+        ends[2][wave] = all_lo;
+        ends[3][wave] = all_hi;
+    }
+    __syncthreads();
+    int tile_lo = ends[0][0], tile_hi = ends[1][0], tile_all_lo = ends[2][0], tile_all_hi = ends[3][0];
+#pragma unroll
+    for (int w = 1; w < kTileWaves; ++w) {
+        tile_lo = min(tile_lo, ends[0][w]);
+        tile_hi = max(tile_hi, ends[1][w]);
+        tile_all_lo = max(tile_all_lo, ends[2][w]);
+        tile_all_hi = min(tile_all_hi, ends[3][w]);
+    }
+    tile_lo = __builtin_amdgcn_readfirstlane(tile_lo);
+    tile_hi = __builtin_amdgcn_readfirstlane(tile_hi);
+    tile_all_lo = __builtin_amdgcn_readfirstlane(tile_all_lo);
+    tile_all_hi = __builtin_amdgcn_readfirstlane(tile_all_hi);
+    int b1 = (tile_hi + kBlockTokens - 1) / kBlockTokens;
+    int b0 = tile_hi > tile_lo ? tile_lo / kBlockTokens : b1;
+    int pieces = 1;
+    if (a.pieces > 1) {
+        const int want = min(a.pieces, max(1, (b1 - b0) / kMinTileBlocks));
+        const int each = max(1, (b1 - b0 + want - 1) / want);
+        pieces = max(1, (b1 - b0 + each - 1) / each);
+        if (piece >= pieces) return;
+        b0 += piece * each;
+        b1 = min(b1, b0 + each);
+    }
+
+    half8 q[CT][2 * DS];
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2 * DS; ++i) q[t][i] = load_q8(a, off + row[t], head[t], 16 * i + 8 * half, there[t]);
+
+    floatx16 o[CT][DS];
+    float m[CT], l[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+#pragma unroll
+        for (int d = 0; d < DS; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][d][i] = 0.f;
+        m[t] = kNothing;
+        l[t] = 0.f;
+    }
+    // Plain scores are scaled in the exponential's argument, others before.
+    const float scale = MOD ? 1.f : a.scale;
+
+    const int32_t *table = a.r.table + (int64_t)s * a.r.ld_table;
+    const uint8_t *head_base = a.c.base + (int64_t)h * a.c.page_blocks * kBlockBytes;
+    int listed = b0 - kLanes, pages = 0, places = 0;  // lane i: page, and block in it, of block listed + i
+    // The first block from b on whose page is one of the cache's, or b1; its address.
+    auto next = [&](int b, const uint8_t *&block) {
+        for (; b < b1; ++b) {
+            if (b - listed >= kLanes) {
+                listed = b;
+                const int mine = b + lane;
+                if (mine < b1) {
+                    const int in = mine / a.c.page_blocks;
+                    pages = table[in];
+                    places = mine - in * a.c.page_blocks;
+                }
+            }
+            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(pages, b - listed);
+            if (page < a.c.pages) {
+                block = head_base + (int64_t)page * a.c.page_bytes + (int64_t)__builtin_amdgcn_readlane(places, b - listed) * kBlockBytes;
+                break;
+            }
+        }
+        return b;
+    };
+    // A block on its way into LDS: requested a block ahead, stored behind the products.
+    half8 unit[VB == 2 ? DS : 1];
+    v2u32 codes[VB == 1 ? DS : 1];
+    floatx4 unit_scales[VB == 1 ? DS : 1][2], lane_scales = {};
+    auto request = [&](const uint8_t *block) {
+#pragma unroll
+        for (int i = 0; i < DS; ++i) {
+            const int u = i * kThreads + (int)threadIdx.x;
+            if (VB == 2) {
+                unit[i] = reinterpret_cast<const half8 *>(block)[u];
+            } else {
+                codes[i] = reinterpret_cast<const v2u32 *>(block)[u];
+                if ((i + 1) * kThreads > kKeyUnits && u >= kKeyUnits) {
+                    const floatx4 *of = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W) + kBlockTokens / 4;
+                    unit_scales[i][0] = of[2 * ((u - kKeyUnits) / W)];
+                    unit_scales[i][1] = of[2 * ((u - kKeyUnits) / W) + 1];
+                }
+            }
+        }
+        if (VB == 1 && threadIdx.x < kBlockTokens / 4)
+            lane_scales = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W)[threadIdx.x];
+    };
+    // Nothing times infinity is not nothing: in a block that some column does not see the whole of, values that are not
+    // finite are left out of the product, and added to the columns that see them (below).
+    auto store = [&](int buffer, bool whole) {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < DS; ++i) {
+            const int u = i * kThreads + (int)threadIdx.x;
+            const bool value = (i + 1) * kThreads > kKeyUnits && u >= kKeyUnits;
+            half8 x = VB == 2 ? unit[VB == 2 ? i : 0]
+                    : value   ? values_of(codes[VB == 1 ? i : 0], unit_scales[VB == 1 ? i : 0][0], unit_scales[VB == 1 ? i : 0][1])
+                              : halves_of(codes[VB == 1 ? i : 0]);
+            if (!whole && value) {
+                v4u32 bits = __builtin_bit_cast(v4u32, x);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t inf = ((bits[j] & 0x7C007C00u) + 0x04000400u) >> 15 & 0x00010001u;
+                    bad |= inf;
+                    bits[j] &= ~(inf * 0xFFFFu);
+                }
+                x = __builtin_bit_cast(half8, bits);
+            }
+            staged[buffer][u] = x;
+        }
+        if (VB == 1 && threadIdx.x < kBlockTokens / 4) key_scales[buffer][threadIdx.x] = lane_scales;
+        if (!whole) {
+            const int any = __any(bad != 0);
+            if (lane == 0) odd[buffer][wave] = any;
+        }
+    };
+    auto all_see = [&](int b) { return tile_all_lo <= b * kBlockTokens && (b + 1) * kBlockTokens <= tile_all_hi; };
+
+    const uint8_t *block = nullptr;
+    int b = next(b0, block);
+    if (b < b1) {
+        request(block);
+        store(0, all_see(b));
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));  // of q: else the loop waits for what it requests ahead
+    __syncthreads();
+    for (int buffer = 0; b < b1; buffer ^= 1) {
+        const uint8_t *here = block;
+        const int b_next = next(b + 1, block);
+        if (b_next < b1) request(block);
+        const int block_lo = b * kBlockTokens, block_hi = block_lo + kBlockTokens;
+        if (block_hi > any_lo && block_lo < any_hi) {  // else this wavefront sees nothing of it
+            const half8 *keys = staged[buffer], *values = staged[buffer] + kKeyUnits;
+            const bool whole = all_lo <= block_lo && block_hi <= all_hi;
+            // Operands are read together, and the values ahead of the softmax: one wait instead of one for each product.
+            half8 k[2 * DS];
+#pragma unroll
+            for (int i = 0; i < 2 * DS; ++i) k[i] = keys[(2 * i + half) * kBlockTokens + c];
+            __builtin_amdgcn_sched_barrier(0);
+            floatx16 st[CT];
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[t][i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2 * DS; ++i)
+#pragma unroll
+                for (int t = 0; t < CT; ++t) st[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[i], q[t][i], st[t], 0, 0, 0);
+            half8 v[DS][2];
+#pragma unroll
+            for (int d = 0; d < DS; ++d)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) v[d][u] = values[(2 * u + half) * W + 32 * d + c];
+            __builtin_amdgcn_sched_barrier(0);
+            half8 w[CT][2];
+#pragma unroll
+            for (int t = 0; t < CT; ++t) {
+                // Register 8 u + j holds the score of key block_lo + 16 u + 8 half + j.
+                if (VB == 1) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) st[t][i] *= key_scales[buffer][(16 * (i / 8) + 8 * half + i % 8) / 4][i % 4];
+                }
+                if (MOD) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        st[t][i] = score_of(a, st[t][i], slope[t], p[t], block_lo + 16 * (i / 8) + 8 * half + i % 8);
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = block_lo + 16 * (i / 8) + 8 * half + i % 8;
+                        st[t][i] = key >= lo[t] && key < hi[t] ? st[t][i] : kNothing;
+                    }
+                }
+                float top = st[t][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fmaxf(top, st[t][i]);
+                top = fmaxf(m[t], max_32(top));
+                if (__any(top > m[t])) {
+                    const float fade = exp2_of((m[t] - (top == kNothing ? 0.f : top)) * scale);
+                    m[t] = top;
+                    l[t] *= fade;
+#pragma unroll
+                    for (int d = 0; d < DS; ++d) o[t][d] *= fade;
+                }
+                const float base = m[t] == kNothing ? 0.f : -m[t] * scale;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[t][i / 8][i % 8] = (_Float16)exp2_of(fmaf(st[t][i], scale, base));
+                // The sum takes the weights as the product does.
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const half2a pair = {w[t][i / 4][2 * (i % 4)], w[t][i / 4][2 * (i % 4) + 1]};
+                    l[t] = __builtin_amdgcn_fdot2(pair, half2a{(_Float16)1.f, (_Float16)1.f}, l[t], false);
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < DS; ++d)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int t = 0; t < CT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[d][u], w[t][u], o[t][d], 0, 0, 0);
+            if (!all_see(b) && (odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3])) {
+                // Rare, so straight from the cache.
+#pragma unroll 1
+                for (int j = 0; j < kBlockTokens; ++j)
+#pragma unroll
+                    for (int t = 0; t < CT; ++t) {
+                        const bool sees = block_lo + j >= lo[t] && block_lo + j < hi[t];
+#pragma unroll
+                        for (int d = 0; d < DS; ++d)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int at = kKeyUnits * 8 + ((j / 8) * W + 32 * d + 8 * (i / 4) + 4 * half + i % 4) * 8 + j % 8;
+                                float x;
+                                if (VB == 2)
+                                    x = (float)reinterpret_cast<const _Float16 *>(here)[at];
+                                else
+                                    x = reinterpret_cast<const float *>(here + 2 * kBlockTokens * W)[kBlockTokens + j];
+                                if (sees && !(fabsf(x) < __builtin_inff())) o[t][d][i] += x;
+                            }
+                    }
+            }
+        }
+        if (b_next < b1) store(buffer ^ 1, all_see(b_next));
+        __syncthreads();
+        b = b_next;
+    }
+
+#pragma unroll
+    for (int t = 0; t < CT; ++t) l[t] = sum_32(l[t]);
+    if (pieces > 1) {
+        // A piece's result lies as the lanes hold it. The last piece to arrive joins them, in their order.
+        constexpr int kParts = CT * (DS * 4 + 1);  // of 16 bytes a lane
+        constexpr int64_t kSlotFloats = (int64_t)kParts * 4 * kThreads;
+        float *slot = a.partials + ((int64_t)tile * a.pieces * a.c.kv_heads + h) * kSlotFloats;
+        const int64_t step = a.c.kv_heads * kSlotFloats;
+        const int at = (int)threadIdx.x * 16;
+        {
+            const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(slot + piece * step, (short)0, (int)(kSlotFloats * 4), kBufferRsrcWord3);
+#pragma unroll
+            for (int t = 0; t < CT; ++t) {
+#pragma unroll
+                for (int i = 0; i < DS * 4; ++i) {
+                    const floatx4 x = {o[t][i / 4][4 * (i % 4)], o[t][i / 4][4 * (i % 4) + 1], o[t][i / 4][4 * (i % 4) + 2], o[t][i / 4][4 * (i % 4) + 3]};
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, x), to, (t * (DS * 4 + 1) + i) * kThreads * 16 + at, 0, kCachePolicyDevice);
+                }
+                const floatx4 x = {m[t], l[t], 0.f, 0.f};
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, x), to, (t * (DS * 4 + 1) + DS * 4) * kThreads * 16 + at, 0, kCachePolicyDevice);
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's part lies in memory
+        __syncthreads();
+        uint32_t *counter = a.counters + (int64_t)tile * a.c.kv_heads + h;
+        if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (arrived != (uint32_t)pieces - 1) return;
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            float top = kNothing;
+            for (int i = 0; i < pieces; ++i) {
+                const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(slot + i * step, (short)0, (int)(kSlotFloats * 4), kBufferRsrcWord3);
+                top = fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, (t * (DS * 4 + 1) + DS * 4) * kThreads * 16 + at, 0, kCachePolicyDevice)));
+            }
+            const float base = top == kNothing ? 0.f : top;
+            l[t] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DS; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][d][i] = 0.f;
+            for (int i = 0; i < pieces; ++i) {
+                const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(slot + i * step, (short)0, (int)(kSlotFloats * 4), kBufferRsrcWord3);
+                v4u32 x[DS * 4 + 1];
+#pragma unroll
+                for (int j = 0; j < DS * 4 + 1; ++j)
+                    x[j] = __builtin_amdgcn_raw_buffer_load_b128(from, (t * (DS * 4 + 1) + j) * kThreads * 16 + at, 0, kCachePolicyDevice);
+                const floatx4 ml = __builtin_bit_cast(floatx4, x[DS * 4]);
+                const float f = exp2_of((ml[0] - base) * scale);
+                l[t] = fmaf(ml[1], f, l[t]);
+#pragma unroll
+                for (int j = 0; j < DS * 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[t][j / 4][4 * (j % 4) + e] = fmaf(__builtin_bit_cast(floatx4, x[j])[e], f, o[t][j / 4][4 * (j % 4) + e]);
+            }
+        }
+        if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+        const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
+        if (!there[t]) continue;
+#pragma unroll
+        for (int d = 0; d < DS; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int channel = 32 * d + 8 * i + 4 * half;
+                floatx4 v = {o[t][d][4 * i], o[t][d][4 * i + 1], o[t][d][4 * i + 2], o[t][d][4 * i + 3]};
+                v = l[t] == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : v * inv;
+                if (channel < a.c.head_dim) store_out4(a, off + row[t], head[t], channel, v);
+            }
+    }
+}
+
+constexpr int kTilesOfWave = 1;
+
+template <int VB, bool MOD>
+void (*tiles_kernel_of(int width))(AttendArgs) {
+    switch (width) {
+        case 32: return attend_tiles_kernel<1, VB, MOD, kTilesOfWave>;
+        case 64: return attend_tiles_kernel<2, VB, MOD, kTilesOfWave>;
+        case 96: return attend_tiles_kernel<3, VB, MOD, kTilesOfWave>;
+        case 128: return attend_tiles_kernel<4, VB, MOD, kTilesOfWave>;
+        case 192: return attend_tiles_kernel<6, VB, MOD, kTilesOfWave>;
+        default: return attend_tiles_kernel<8, VB, MOD, kTilesOfWave>;
+    }
+}
+
+}  // namespace
+
+int tile_columns(int) { return 32 * kTilesOfWave * kTileWaves; }
+
+int64_t tile_slot_floats(int width) { return (int64_t)kTilesOfWave * (width / 8 + 1) * 4 * kTileWaves * kLanes; }
+
+int launch_tiles(const void *args, int width, int value_bytes, bool modified, int64_t grid, void *stream) {
+    const AttendArgs &a = *reinterpret_cast<const AttendArgs *>(args);
+    const auto fn = value_bytes == 2 ? modified ? tiles_kernel_of<2, true>(width) : tiles_kernel_of<2, false>(width)
+                                     : modified ? tiles_kernel_of<1, true>(width) : tiles_kernel_of<1, false>(width);
+    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(kTileWaves * kLanes), 0, reinterpret_cast<hipStream_t>(stream), a);
+    return (int)hipGetLastError();
+}
+
+}  // namespace usp
