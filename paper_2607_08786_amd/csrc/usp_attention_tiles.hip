@@ -7,6 +7,7 @@
 namespace usp {
 namespace {
 
+constexpr int kAhead = 4;           // products that operands are read ahead
 constexpr int kMinTileBlocks = 16;  // blocks of a piece at least
 
 // The first tile of sequence s: those before it have at most so many.
@@ -28,7 +29,7 @@ __device__ inline half8 values_of(v2u32 codes, floatx4 s0, floatx4 s1) {
 
 // Columns of a wavefront: CT tiles of 32. MOD: scores are capped, biased or not scaled by a positive number.
 template <int DS, int VB, bool MOD, int CT>
-__global__ __launch_bounds__(kTileWaves *kLanes, CT == 2 || DS > 4 ? 1 : 2) void attend_tiles_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 2 ? 3 : 2) void attend_tiles_kernel(AttendArgs a) {
     constexpr int W = 32 * DS, kBlockBytes = (int)cache_block_bytes(W, VB);
     constexpr int kColumns = 32 * CT * kTileWaves;
     constexpr int kKeyUnits = W / 8 * kBlockTokens;  // units of 8 keys' channels, and as many of values'
@@ -36,7 +37,7 @@ __global__ __launch_bounds__(kTileWaves *kLanes, CT == 2 || DS > 4 ? 1 : 2) void
     __shared__ half8 staged[2][2 * kKeyUnits];  // blocks of keys, then of values, as in the cache
     __shared__ floatx4 key_scales[2][kBlockTokens / 4];
     __shared__ int ends[4][kTileWaves];
-    __shared__ int odd[2][kTileWaves];  // whether a wavefront's part of a block's values holds any that is not finite
+    __shared__ int odd[kTileWaves];  // whether a wavefront's part of a block's values holds any that is not finite
     __shared__ uint32_t arrived;
 
     const int h = blockIdx.x % a.c.kv_heads, piece = (int)(blockIdx.x / a.c.kv_heads) % a.pieces;
@@ -167,94 +168,109 @@ __global__ __launch_bounds__(kTileWaves *kLanes, CT == 2 || DS > 4 ? 1 : 2) void
         return b;
     };
     // A block on its way into LDS: requested a block ahead, stored behind the products.
-    half8 unit[VB == 2 ? DS : 1];
-    v2u32 codes[VB == 1 ? DS : 1];
-    floatx4 unit_scales[VB == 1 ? DS : 1][2], lane_scales = {};
-    auto request = [&](const uint8_t *block) {
+    v2u32 codes[DS];
+    floatx4 unit_scales[DS][2], lane_scales = {};
+    auto request = [&](const uint8_t *block, int buffer) {
+        if constexpr (VB == 2) {
+            // Straight into LDS: the compiler neither sees these transfers nor waits for them.
+            const uint64_t from = reinterpret_cast<uint64_t>(block);
+            const v4i32 rsrc = {(int)(uint32_t)from, (int)((uint32_t)(from >> 32) & 0xFFFFu), kBlockBytes, kBufferRsrcWord3};
+            const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)as_lds(staged[buffer]) + wave * kLanes * 16);
+#pragma unroll
+            for (int i = 0; i < DS; ++i)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                             :
+                             : "s"(to + 16u * kThreads * i), "v"(16 * (kThreads * i + (int)threadIdx.x)), "s"(rsrc)
+                             : "memory", "m0");
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < DS; ++i) {
             const int u = i * kThreads + (int)threadIdx.x;
-            if (VB == 2) {
-                unit[i] = reinterpret_cast<const half8 *>(block)[u];
-            } else {
-                codes[i] = reinterpret_cast<const v2u32 *>(block)[u];
-                if ((i + 1) * kThreads > kKeyUnits && u >= kKeyUnits) {
-                    const floatx4 *of = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W) + kBlockTokens / 4;
-                    unit_scales[i][0] = of[2 * ((u - kKeyUnits) / W)];
-                    unit_scales[i][1] = of[2 * ((u - kKeyUnits) / W) + 1];
-                }
+            codes[i] = reinterpret_cast<const v2u32 *>(block)[u];
+            if ((i + 1) * kThreads > kKeyUnits && u >= kKeyUnits) {
+                const floatx4 *of = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W) + kBlockTokens / 4;
+                unit_scales[i][0] = of[2 * ((u - kKeyUnits) / W)];
+                unit_scales[i][1] = of[2 * ((u - kKeyUnits) / W) + 1];
             }
         }
-        if (VB == 1 && threadIdx.x < kBlockTokens / 4)
+        if (threadIdx.x < kBlockTokens / 4)
             lane_scales = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W)[threadIdx.x];
     };
-    // Nothing times infinity is not nothing: in a block that some column does not see the whole of, values that are not
-    // finite are left out of the product, and added to the columns that see them (below).
-    auto store = [&](int buffer, bool whole) {
-        uint32_t bad = 0;
+    auto store = [&](int buffer) {
 #pragma unroll
         for (int i = 0; i < DS; ++i) {
             const int u = i * kThreads + (int)threadIdx.x;
             const bool value = (i + 1) * kThreads > kKeyUnits && u >= kKeyUnits;
-            half8 x = VB == 2 ? unit[VB == 2 ? i : 0]
-                    : value   ? values_of(codes[VB == 1 ? i : 0], unit_scales[VB == 1 ? i : 0][0], unit_scales[VB == 1 ? i : 0][1])
-                              : halves_of(codes[VB == 1 ? i : 0]);
-            if (!whole && value) {
-                v4u32 bits = __builtin_bit_cast(v4u32, x);
+            staged[buffer][u] = value ? values_of(codes[i], unit_scales[i][0], unit_scales[i][1]) : halves_of(codes[i]);
+        }
+        if (threadIdx.x < kBlockTokens / 4) key_scales[buffer][threadIdx.x] = lane_scales;
+    };
+    // Nothing times infinity is not nothing: in a block that some column does not see the whole of, values that are not
+    // finite are left out of the product, and added to the columns that see them (below).
+    auto clean = [&](int buffer) {
+        uint32_t bad = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t inf = ((bits[j] & 0x7C007C00u) + 0x04000400u) >> 15 & 0x00010001u;
-                    bad |= inf;
-                    bits[j] &= ~(inf * 0xFFFFu);
-                }
-                x = __builtin_bit_cast(half8, bits);
+        for (int i = 0; i < DS; ++i) {
+            const int u = i * kThreads + (int)threadIdx.x;
+            if ((i + 1) * kThreads <= kKeyUnits || u < kKeyUnits) continue;
+            v4u32 bits = __builtin_bit_cast(v4u32, staged[buffer][u]);
+            uint32_t any = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t inf = ((bits[j] & 0x7C007C00u) + 0x04000400u) >> 15 & 0x00010001u;
+                any |= inf;
+                bits[j] &= ~(inf * 0xFFFFu);
             }
-            staged[buffer][u] = x;
+            if (any) staged[buffer][u] = __builtin_bit_cast(half8, bits);
+            bad |= any;
         }
-        if (VB == 1 && threadIdx.x < kBlockTokens / 4) key_scales[buffer][threadIdx.x] = lane_scales;
-        if (!whole) {
-            const int any = __any(bad != 0);
-            if (lane == 0) odd[buffer][wave] = any;
-        }
+        const int any = __any(bad != 0);
+        if (lane == 0) odd[wave] = any;
+        lds_barrier();
     };
     auto all_see = [&](int b) { return tile_all_lo <= b * kBlockTokens && (b + 1) * kBlockTokens <= tile_all_hi; };
 
     const uint8_t *block = nullptr;
     int b = next(b0, block);
     if (b < b1) {
-        request(block);
-        store(0, all_see(b));
+        request(block, 0);
+        if (VB == 1) store(0);
     }
-    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));  // of q: else the loop waits for what it requests ahead
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));  // of q too: else the loop waits for what it requests ahead
     __syncthreads();
     for (int buffer = 0; b < b1; buffer ^= 1) {
         const uint8_t *here = block;
         const int b_next = next(b + 1, block);
-        if (b_next < b1) request(block);
+        if (b_next < b1) request(block, buffer ^ 1);
         const int block_lo = b * kBlockTokens, block_hi = block_lo + kBlockTokens;
+        if (!all_see(b)) clean(buffer);
         if (block_hi > any_lo && block_lo < any_hi) {  // else this wavefront sees nothing of it
             const half8 *keys = staged[buffer], *values = staged[buffer] + kKeyUnits;
             const bool whole = all_lo <= block_lo && block_hi <= all_hi;
-            // Operands are read together, and the values ahead of the softmax: one wait instead of one for each product.
-            half8 k[2 * DS];
+            constexpr int kProducts = 2 * DS;  // with the keys, and as many with the values
+            constexpr int ahead = kAhead < kProducts ? kAhead : kProducts;
+            half8 k[kProducts], v[kProducts];
 #pragma unroll
-            for (int i = 0; i < 2 * DS; ++i) k[i] = keys[(2 * i + half) * kBlockTokens + c];
-            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < ahead; ++i) k[i] = keys[(2 * i + half) * kBlockTokens + c];
             floatx16 st[CT];
 #pragma unroll
             for (int t = 0; t < CT; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) st[t][i] = 0.f;
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < 2 * DS; ++i)
+            for (int i = 0; i < kProducts; ++i) {
+                if (i + ahead < kProducts)
+                    k[i + ahead] = keys[(2 * (i + ahead) + half) * kBlockTokens + c];
+                else {
+                    const int j = i + ahead - kProducts;
+                    v[j] = values[(2 * (j % 2) + half) * W + 32 * (j / 2) + c];
+                }
 #pragma unroll
                 for (int t = 0; t < CT; ++t) st[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[i], q[t][i], st[t], 0, 0, 0);
-            half8 v[DS][2];
-#pragma unroll
-            for (int d = 0; d < DS; ++d)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) v[d][u] = values[(2 * u + half) * W + 32 * d + c];
-            __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             half8 w[CT][2];
 #pragma unroll
             for (int t = 0; t < CT; ++t) {
@@ -296,13 +312,16 @@ __global__ __launch_bounds__(kTileWaves *kLanes, CT == 2 || DS > 4 ? 1 : 2) void
                     l[t] = __builtin_amdgcn_fdot2(pair, half2a{(_Float16)1.f, (_Float16)1.f}, l[t], false);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int d = 0; d < DS; ++d)
+            for (int i = 0; i < kProducts; ++i) {
+                const int j = i + ahead;
+                if (j < kProducts) v[j] = values[(2 * (j % 2) + half) * W + 32 * (j / 2) + c];
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int t = 0; t < CT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[d][u], w[t][u], o[t][d], 0, 0, 0);
-            if (!all_see(b) && (odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3])) {
+                for (int t = 0; t < CT; ++t) o[t][i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i], w[t][i % 2], o[t][i / 2], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (!all_see(b) && (odd[0] | odd[1] | odd[2] | odd[3])) {
                 // Rare, so straight from the cache.
 #pragma unroll 1
                 for (int j = 0; j < kBlockTokens; ++j)
@@ -324,8 +343,9 @@ __global__ __launch_bounds__(kTileWaves *kLanes, CT == 2 || DS > 4 ? 1 : 2) void
                     }
             }
         }
-        if (b_next < b1) store(buffer ^ 1, all_see(b_next));
-        __syncthreads();
+        if (VB == 1 && b_next < b1) store(buffer ^ 1);
+        if (VB == 2) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next block lies in LDS
+        lds_barrier();
         b = b_next;
     }
 
