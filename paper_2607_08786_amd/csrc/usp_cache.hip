@@ -139,13 +139,227 @@ __global__ __launch_bounds__(kCacheThreads) void read_kernel(RowsArgs a) {
     }
 }
 
+// ---- Many rows of each sequence: a wavefront takes a head of eight tokens that lie together in their block, and turns
+// their values in LDS, so that a unit of a channel's eight tokens is written (read) at once. A value at a time, 2133
+// rows of 40 heads of 128 took 67 us into 8 bits and 57 back.
+
+constexpr int kGroup = 8;
+constexpr int kWavesOfGroups = kCacheThreads / kLanes64;
+
+// Groups of the sequences before s at most: of n rows there are up to n / 8 + 2.
+__device__ inline int first_group(const RowsView &r, int s) { return offset_of(r, s) / kGroup + 2 * s; }
+
+template <int DS, int VB, bool WRITE>
+__global__ __launch_bounds__(kCacheThreads) void group_kernel(RowsArgs a) {
+    constexpr int W = 32 * DS, kChunks = W / 8, kTurns = (DS + 1) / 2;  // turns of 64 lanes over 8 x kChunks units
+    __shared__ __attribute__((aligned(16))) _Float16 turned[kWavesOfGroups][kGroup][W + 8];
+    __shared__ uint32_t tops[kWavesOfGroups][2][kGroup];
+    const int lane = threadIdx.x & (kLanes64 - 1), wave = threadIdx.x / kLanes64;
+    const int64_t index = (int64_t)blockIdx.x * kWavesOfGroups + wave;
+    const int group = (int)(index / a.c.kv_heads), h = (int)(index - (int64_t)group * a.c.kv_heads);
+    int s = 0, below = a.r.sequences;  // first_group(s) <= group < first_group(below)
+    while (below - s > 1) {
+        const int mid = (s + below) / 2;
+        if (first_group(a.r, mid) <= group)
+            s = mid;
+        else
+            below = mid;
+    }
+    const int off = offset_of(a.r, s), n = offset_of(a.r, s + 1) - off, len = length_of(a.r, s);
+    const int begin = len - n > 0 ? len - n : 0, local = group - first_group(a.r, s);
+    const int64_t from = ((int64_t)begin / kGroup + local) * kGroup;  // the group's first token
+    uint8_t *block = nullptr;
+    if (local >= 0 && n > 0 && from < len) block = block_of(a.c, a.r, s, (int)from, h);
+    const int j0 = (int)(from % kBlockTokens);
+    auto there = [&](int token) { return block && from + token >= begin && from + token < len; };
+    const bool full = there(0) && there(kGroup - 1);
+    auto row_of = [&](const HeadRows &r, int token, int chunk) {
+        const int64_t t = off + (from + token - (len - n));
+        return reinterpret_cast<uint16_t *>(r.p) + t * r.ld + (int64_t)h * r.head + chunk * 8;
+    };
+    uint8_t *values = block + kBlockTokens * W * VB + (j0 / 8) * W * 8 * VB;  // units of eight tokens, channel after channel
+    float *scales = reinterpret_cast<float *>(block + 2 * kBlockTokens * W);
+    if (VB == 1 && lane < 2 * kGroup) tops[wave][lane / kGroup][lane % kGroup] = 0;
+
+    half8c k[kTurns], v[kTurns];
+    if (WRITE) {
+        if (VB == 1) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int u = i * kLanes64 + lane, token = u / kChunks, chunk = u % kChunks;
+            k[i] = v[i] = half8c{};
+            if (token < kGroup && there(token) && chunk * 8 < a.c.head_dim) {
+                const uint16_t *pk = row_of(a.k, token, chunk), *pv = row_of(a.v, token, chunk);
+                if (a.vec) {
+                    k[i] = *reinterpret_cast<const half8c *>(pk);
+                    v[i] = *reinterpret_cast<const half8c *>(pv);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        k[i][e] = __builtin_bit_cast(_Float16, pk[e]);
+                        v[i][e] = __builtin_bit_cast(_Float16, pv[e]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int u = i * kLanes64 + lane, token = u / kChunks, chunk = u % kChunks;
+            if (token >= kGroup) continue;
+            *reinterpret_cast<half8c *>(&turned[wave][token][chunk * 8]) = v[i];
+            if (VB == 1) {
+                uint32_t top_k = 0, top_v = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    top_k = std::max(top_k, magnitude_bits(k[i][e]));
+                    top_v = std::max(top_v, magnitude_bits(v[i][e]));
+                }
+                atomicMax(&tops[wave][0][token], top_k);
+                atomicMax(&tops[wave][1][token], top_v);
+            }
+        }
+        __syncthreads();
+        float scale, inv;
+        if (VB == 1 && lane < 2 * kGroup && there(lane % kGroup)) {
+            code_scale(tops[wave][lane / kGroup][lane % kGroup], scale, inv);
+            scales[(lane / kGroup) * kBlockTokens + j0 + lane % kGroup] = scale;
+        }
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int u = i * kLanes64 + lane, token = u / kChunks, chunk = u % kChunks;
+            if (token >= kGroup || !there(token)) continue;
+            const int at = (chunk * kBlockTokens + key_place(j0 + token)) * 8;
+            if (VB == 2) {
+                *reinterpret_cast<half8c *>(reinterpret_cast<uint16_t *>(block) + at) = k[i];
+            } else {
+                code_scale(tops[wave][0][token], scale, inv);
+                u32x2c w = {0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e / 4] |= code_bits(k[i][e], inv) << (8 * (e % 4));
+                *reinterpret_cast<u32x2c *>(block + at) = w;
+            }
+        }
+        float inv_v[kGroup];
+        if (VB == 1) {
+#pragma unroll
+            for (int e = 0; e < kGroup; ++e) code_scale(tops[wave][1][e], scale, inv_v[e]);
+        }
+#pragma unroll
+        for (int i = 0; i < (W + kLanes64 - 1) / kLanes64; ++i) {
+            const int d = i * kLanes64 + lane;
+            if (d >= W || !block) continue;
+            half8c x;
+#pragma unroll
+            for (int e = 0; e < kGroup; ++e) x[e] = turned[wave][e][d];
+            if (VB == 2) {
+                if (full) {
+                    *reinterpret_cast<half8c *>(reinterpret_cast<uint16_t *>(values) + d * 8) = x;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kGroup; ++e)
+                        if (there(e)) reinterpret_cast<uint16_t *>(values)[d * 8 + e] = __builtin_bit_cast(uint16_t, (_Float16)x[e]);
+                }
+            } else {
+                u32x2c w = {0, 0};
+#pragma unroll
+                for (int e = 0; e < kGroup; ++e) w[e / 4] |= code_bits(x[e], inv_v[e]) << (8 * (e % 4));
+                if (full) {
+                    *reinterpret_cast<u32x2c *>(values + d * 8) = w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kGroup; ++e)
+                        if (there(e)) values[d * 8 + e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
+                }
+            }
+        }
+        return;
+    }
+
+    float scale_v[kGroup];
+    if (VB == 1) {
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e) scale_v[e] = there(e) ? scales[kBlockTokens + j0 + e] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int u = i * kLanes64 + lane, token = u / kChunks, chunk = u % kChunks;
+        k[i] = half8c{};
+        if (token >= kGroup || !there(token)) continue;
+        const int at = (chunk * kBlockTokens + key_place(j0 + token)) * 8;
+        if (VB == 2) {
+            k[i] = *reinterpret_cast<const half8c *>(reinterpret_cast<const uint16_t *>(block) + at);
+        } else {
+            const u32x2c w = *reinterpret_cast<const u32x2c *>(block + at);
+            const float scale = scales[j0 + token];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) k[i][e] = (_Float16)((float)(int8_t)(w[e / 4] >> (8 * (e % 4))) * scale);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < (W + kLanes64 - 1) / kLanes64; ++i) {
+        const int d = i * kLanes64 + lane;
+        if (d >= W || !block) continue;
+        half8c x;
+        if (VB == 2) {
+            x = *reinterpret_cast<const half8c *>(reinterpret_cast<const uint16_t *>(values) + d * 8);
+        } else {
+            const u32x2c w = *reinterpret_cast<const u32x2c *>(values + d * 8);
+#pragma unroll
+            for (int e = 0; e < kGroup; ++e) x[e] = (_Float16)((float)(int8_t)(w[e / 4] >> (8 * (e % 4))) * scale_v[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e) turned[wave][e][d] = x[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int u = i * kLanes64 + lane, token = u / kChunks, chunk = u % kChunks;
+        if (token >= kGroup || !there(token) || chunk * 8 >= a.c.head_dim) continue;
+        const half8c x = *reinterpret_cast<const half8c *>(&turned[wave][token][chunk * 8]);
+        uint16_t *pk = row_of(a.k, token, chunk), *pv = row_of(a.v, token, chunk);
+        if (a.vec) {
+            *reinterpret_cast<half8c *>(pk) = k[i];
+            *reinterpret_cast<half8c *>(pv) = x;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                pk[e] = __builtin_bit_cast(uint16_t, (_Float16)k[i][e]);
+                pv[e] = __builtin_bit_cast(uint16_t, (_Float16)x[e]);
+            }
+        }
+    }
+}
+
+typedef void (*RowsFn)(RowsArgs);
+
+template <int VB, bool WRITE>
+RowsFn group_kernel_of(int width) {
+    switch (width) {
+        case 32: return group_kernel<1, VB, WRITE>;
+        case 64: return group_kernel<2, VB, WRITE>;
+        case 96: return group_kernel<3, VB, WRITE>;
+        case 128: return group_kernel<4, VB, WRITE>;
+        case 192: return group_kernel<6, VB, WRITE>;
+        default: return group_kernel<8, VB, WRITE>;
+    }
+}
+
 bool vector_heads(const HeadRows &r) {
     return (reinterpret_cast<uintptr_t>(r.p) & 15) == 0 && r.ld % 8 == 0 && r.head % 8 == 0;
 }
 
-int launch_rows(void (*fn)(RowsArgs), const CacheView &c, const RowsView &r, HeadRows K, HeadRows V, void *stream) {
+// Groups where sequences have four rows or more on average: at fewer, most of a group's lanes have nothing to do.
+template <bool WRITE>
+int launch_rows(const CacheView &c, const RowsView &r, HeadRows K, HeadRows V, void *stream) {
     const RowsArgs a = {c, r, K, V, vector_heads(K) && vector_heads(V)};
-    const int64_t grid = ((int64_t)r.rows * c.kv_heads + 3) / (kCacheThreads / kLanes64);
+    const bool groups = r.offsets && r.rows >= 4 * (int64_t)r.sequences;
+    RowsFn fn;
+    if (groups)
+        fn = c.value_bytes == 2 ? group_kernel_of<2, WRITE>(c.width) : group_kernel_of<1, WRITE>(c.width);
+    else
+        fn = WRITE ? c.value_bytes == 2 ? append_kernel<2> : append_kernel<1> : c.value_bytes == 2 ? read_kernel<2> : read_kernel<1>;
+    const int64_t waves = (groups ? (int64_t)r.rows / kGroup + 2 * (int64_t)r.sequences : (int64_t)r.rows) * c.kv_heads;
+    const int64_t grid = (waves + kWavesOfGroups - 1) / kWavesOfGroups;
     hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(kCacheThreads), 0, reinterpret_cast<hipStream_t>(stream), a);
     return (int)hipGetLastError();
 }
@@ -181,11 +395,11 @@ __global__ __launch_bounds__(kCacheThreads) void copy_kernel(CopyArgs a) {
 }  // namespace
 
 int launch_cache_append(const CacheView &c, const RowsView &r, HeadRows K, HeadRows V, void *stream) {
-    return launch_rows(c.value_bytes == 2 ? append_kernel<2> : append_kernel<1>, c, r, K, V, stream);
+    return launch_rows<true>(c, r, K, V, stream);
 }
 
 int launch_cache_read(const CacheView &c, const RowsView &r, HeadRows K, HeadRows V, void *stream) {
-    return launch_rows(c.value_bytes == 2 ? read_kernel<2> : read_kernel<1>, c, r, K, V, stream);
+    return launch_rows<false>(c, r, K, V, stream);
 }
 
 int launch_cache_copy(const CacheView &c, int64_t layers, const int32_t *src, const int32_t *dst, int64_t n, void *stream) {
