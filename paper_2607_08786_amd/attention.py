@@ -217,8 +217,7 @@ def _geometry(cache: usp.KVCache) -> List[int]:
 def _attend(cache: usp.KVCache, rows: usp.CacheRows, q: torch.Tensor, workspace: Optional[torch.Tensor], layer: int,
             scale: Optional[float], cap: float, slopes: Optional[torch.Tensor], window: int, first: Optional[torch.Tensor],
             last: Optional[torch.Tensor]) -> torch.Tensor:
-    make = torch.empty if rows.offsets is None else torch.zeros  # offsets may leave rows out
-    out = make(q.shape, dtype=torch.float16, device=q.device)
+    out = torch.empty_like(q) if rows.offsets is None else torch.zeros_like(q)  # offsets may leave rows out
     usp.usp_attention(cache, rows, q, out, workspace, layer, scale, cap, slopes, window, first, last)
     return out
 
@@ -313,7 +312,7 @@ class PagedAttention(torch.nn.Module):
         if T == 0:
             return q.to(torch.float16)
         slopes = self._buffers["slopes"]
-        seen = _seen((q, k, v, first, last, slopes, cache.data, rows.table, rows.lengths, rows.offsets))
+        seen = _seen((q, k, v, first, last))
         if k is not None:
             k3, v3 = _heads(k, self.kv_heads, self.head_dim, "k"), _heads(v, self.kv_heads, self.head_dim, "v")
             if seen:

@@ -41,7 +41,8 @@ struct AttendArgs {
     int q_vec, out_vec;
     int split;             // whether tiles are cut into pieces (rows kernel)
     int pieces;            // most pieces of a tile (tiles kernel)
-    int pieces_bits;       // 2^pieces_bits pieces of all tiles and heads together are aimed at
+    int pieces_bits;       // 2^pieces_bits pieces of all tiles and heads together are aimed at (rows kernel)
+    int min_blocks;        // of a piece at least (rows kernel)
     int limit, slot_limit; // items of a head in the grid, and slots of a head in the workspace
     uint32_t *counters;
     float *partials;
@@ -119,13 +120,21 @@ __device__ inline void span_of(const AttendArgs &a, int t, int p, int len, int &
     if (p < 0) hi = 0;
 }
 
-// A score in the exponent of 2, from q . K: scaled, capped, biased.
-__device__ inline float score_of(const AttendArgs &a, float x, float slope, int p, int key) {
-    x *= a.scale;
-    if (a.cap > 0.f)  // cap tanh(y): 1 - 2 / (1 + exp(2 y)); x is 2 y in the exponent of 2
-        x = a.cap * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_of(x)));
-    if (a.slopes) x -= slope * fabsf((float)(p - key));
-    return x;
+// Scores in the exponent of 2, from q . K: scaled, capped, biased. key(i): the key of x[i], less `key0`. (One branch for
+// all of them: behind a branch for each, their exponentials waited for one another.)
+template <class Scores, class Key>
+__device__ inline void modify_scores(const AttendArgs &a, Scores &x, int n, float slope, int p, int key0, Key key) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) x[i] *= a.scale;
+    if (a.cap > 0.f) {  // cap tanh(y) is cap (1 - 2 / (1 + exp(2 y))); x is 2 y in the exponent of 2
+#pragma unroll
+        for (int i = 0; i < n; ++i) x[i] = fmaf(-2.f * a.cap, __builtin_amdgcn_rcpf(1.f + exp2_of(x[i])), a.cap);
+    }
+    if (a.slopes) {
+        const int away = p - key0;
+#pragma unroll
+        for (int i = 0; i < n; ++i) x[i] = fmaf(-slope, fabsf((float)(away - key(i))), x[i]);
+    }
 }
 
 }  // namespace

@@ -11,7 +11,6 @@ namespace {
 // ---- Few rows of each sequence: one tile of up to 16 heads of a row at a time.
 
 constexpr int kRowWaves = 4;
-constexpr int kMinBlocks = 8;     // blocks of a piece at least: two for each wavefront
 constexpr int kMostPieces = 256;  // of a tile: the join's weights lie in LDS
 
 // What a workgroup does: piece `piece` of at most `pieces`, of `blocks` blocks each, of tile `tile` of row t.
@@ -28,14 +27,31 @@ __device__ inline int most_blocks(const AttendArgs &a, int len) {
     return a.window && !a.last ? min(all, (a.window - 1 + kBlockTokens - 1) / kBlockTokens + 1) : all;
 }
 
-// Inclusive sums over the lanes of a wavefront.
+// Lane by lane sums over a wavefront by DPP row shifts and broadcasts; the last lane has the whole.
+template <int CTRL, int ROWS>
+__device__ inline uint32_t dpp_add(uint32_t v) {
+    return v + __builtin_amdgcn_update_dpp(0u, v, CTRL, ROWS, 0xF, ROWS == 0xF);
+}
 __device__ inline uint32_t scan_lanes(uint32_t v) {
-#pragma unroll
-    for (int d = 1; d < kLanes; d *= 2) {
-        const uint32_t o = (uint32_t)__shfl_up((int)v, d, kLanes);
-        if ((threadIdx.x & (kLanes - 1)) >= d) v += o;
-    }
-    return v;
+    v = dpp_add<0x111, 0xF>(v);  // row_shr:1
+    v = dpp_add<0x112, 0xF>(v);
+    v = dpp_add<0x114, 0xF>(v);
+    v = dpp_add<0x118, 0xF>(v);
+    v = dpp_add<0x142, 0xA>(v);  // row_bcast:15
+    return dpp_add<0x143, 0xC>(v);  // row_bcast:31
+}
+template <int CTRL, int ROWS>
+__device__ inline float dpp_add(float v) {
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0u, __builtin_bit_cast(uint32_t, v), CTRL, ROWS, 0xF, ROWS == 0xF));
+}
+__device__ inline float sum_lanes(float v) {
+    v = dpp_add<0x111, 0xF>(v);
+    v = dpp_add<0x112, 0xF>(v);
+    v = dpp_add<0x114, 0xF>(v);
+    v = dpp_add<0x118, 0xF>(v);
+    v = dpp_add<0x142, 0xA>(v);
+    v = dpp_add<0x143, 0xC>(v);
+    return __builtin_bit_cast(float, (uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kLanes - 1));
 }
 
 // Item number `item` of a head. Where tiles are cut, a piece has as many blocks as make
@@ -57,33 +73,39 @@ __device__ inline bool find_item(const AttendArgs &a, int item, Item &it) {
         it.slot = it.counter = 0;
         return true;
     }
+    // The lane's sequences s0 .. s0 + per - 1; the first one's figures stay at hand.
     const int per = (S + kLanes - 1) / kLanes, s0 = lane * per;
-    uint64_t total = 0;
-    for (int i = 0; i < per; ++i) {
-        const int s = s0 + i;
-        if (s < S) total += (uint64_t)max(0, offset_of(a.r, s + 1) - offset_of(a.r, s)) * (uint32_t)most_blocks(a, length_of(a.r, s));
+    auto figures = [&](int s, int &off, int &n, int &len) {
+        off = n = len = 0;
+        if (s >= S) return;
+        off = offset_of(a.r, s);
+        n = max(0, offset_of(a.r, s + 1) - off);
+        len = length_of(a.r, s);
+    };
+    int off0, n0, len0;
+    figures(s0, off0, n0, len0);
+    float total = (float)n0 * (float)most_blocks(a, len0);
+    for (int i = 1; i < per; ++i) {
+        int off, n, len;
+        figures(s0 + i, off, n, len);
+        total += (float)n * (float)most_blocks(a, len);
     }
-#pragma unroll
-    for (int d = 1; d < kLanes; d *= 2) {
-        const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)total, d, kLanes);
-        const uint32_t hi = (uint32_t)__shfl_xor((int)(uint32_t)(total >> 32), d, kLanes);
-        total += (uint64_t)hi << 32 | lo;
-    }
-    total = total * (uint32_t)(a.tiles * a.c.kv_heads);
-    const uint64_t even = (total + (1ull << a.pieces_bits) - 1) >> a.pieces_bits;
-    const int blocks = (int)min((uint64_t)(1 << 30), max((uint64_t)kMinBlocks, even));
+    // The sum's roundings are fewer than 128, of 2^-24 each: 2^-16 more, and the pieces are no more than were made room for.
+    total = sum_lanes(total) * (float)(a.tiles * a.c.kv_heads) * (1.f + 1.f / 65536.f);
+    const int blocks = (int)fminf(1e9f, fmaxf((float)a.min_blocks, ceilf(ldexpf(total, -a.pieces_bits))));
     auto pieces_of = [&](int len) {
         return min(kMostPieces, max(1, (most_blocks(a, len) + blocks - 1) / blocks));
     };
     constexpr uint32_t kFull = 1u << 24;  // more items than a grid has
-    uint32_t items = 0, slots = 0;
-    for (int i = 0; i < per; ++i) {
-        const int s = s0 + i;
-        if (s >= S) break;
-        const int n = max(0, offset_of(a.r, s + 1) - offset_of(a.r, s)), pieces = pieces_of(length_of(a.r, s));
-        const uint32_t of_s = min(kFull, (uint32_t)n * (uint32_t)a.tiles) * (uint32_t)pieces;  // below 2^32
-        items = min(kFull, items + min(kFull, of_s));
-        if (pieces > 1) slots = min(kFull, slots + min(kFull, of_s));
+    // n tiles is at most 16384 where tiles are cut, so of one sequence there are fewer than 2^23 items.
+    const uint32_t items0 = (uint32_t)n0 * (uint32_t)a.tiles * (uint32_t)pieces_of(len0);
+    uint32_t items = items0, slots = pieces_of(len0) > 1 ? items0 : 0;
+    for (int i = 1; i < per; ++i) {
+        int off, n, len;
+        figures(s0 + i, off, n, len);
+        const uint32_t of_s = (uint32_t)n * (uint32_t)a.tiles * (uint32_t)pieces_of(len);
+        items = min(kFull, items + of_s);
+        if (pieces_of(len) > 1) slots = min(kFull, slots + of_s);
     }
     const uint32_t items_end = scan_lanes(items), slots_end = scan_lanes(slots);
     const uint64_t has = __ballot((uint32_t)item < items_end);
@@ -94,7 +116,14 @@ __device__ inline bool find_item(const AttendArgs &a, int item, Item &it) {
     for (int i = 0; i < per; ++i) {
         const int s = owner * per + i;
         if (s >= S) break;
-        const int off = offset_of(a.r, s), n = max(0, offset_of(a.r, s + 1) - off), len = length_of(a.r, s);
+        int off, n, len;
+        if (i == 0) {
+            off = __builtin_amdgcn_readlane(off0, owner);
+            n = __builtin_amdgcn_readlane(n0, owner);
+            len = __builtin_amdgcn_readlane(len0, owner);
+        } else {
+            figures(s, off, n, len);
+        }
         const int pieces = pieces_of(len);
         const uint32_t of_s = (uint32_t)n * (uint32_t)a.tiles * (uint32_t)pieces;
         if ((uint32_t)item - at < of_s) {
@@ -121,7 +150,8 @@ __device__ inline bool find_item(const AttendArgs &a, int item, Item &it) {
 // Floats of a piece's partial result: maxima, sums, and the output of each of its columns.
 __host__ __device__ inline int partial_floats(int columns, int width) { return 32 + columns * width; }
 
-template <int DS, int VB>
+// MOD: scores are capped, biased or not scaled by a positive number.
+template <int DS, int VB, bool MOD>
 __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendArgs a) {
     constexpr int W = 32 * DS, kBlockBytes = (int)cache_block_bytes(W, VB);
     constexpr int kStride = W + 4;
@@ -155,12 +185,13 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
     half8 q[DS];
 #pragma unroll
     for (int s = 0; s < DS; ++s) q[s] = load_q8(a, it.t, head0 + r, 32 * s + 8 * g, r < columns);
-    const float slope = a.slopes && r < columns ? a.slopes[head0 + r] * kLog2e : 0.f;
+    const float slope = MOD && a.slopes && r < columns ? a.slopes[head0 + r] * kLog2e : 0.f;
 
     floatx4 o[2 * DS];
 #pragma unroll
     for (int d = 0; d < 2 * DS; ++d) o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
     float m = kNothing, l = 0.f;  // l: of this lane's keys alone
+    const float scale = MOD ? 1.f : a.scale;  // plain scores are scaled in the exponential's argument, others before
     float unit = 1e-30f;          // 8 bits: the largest scale of values so far; o is in 2^-14 of it
     const uint8_t *head_base = a.c.base + (int64_t)h * a.c.page_blocks * kBlockBytes;
     const int32_t *table = a.r.table + (int64_t)it.s * a.r.ld_table;
@@ -187,17 +218,17 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
             for (int i = 0; i < 2; ++i) {
                 const int unit8 = (4 * s + g) * kBlockTokens + 16 * (r / 8) + 8 * i + r % 8;
                 if (VB == 2)
-                    k[s][i] = reinterpret_cast<const half8 *>(block)[unit8];
+                    k[s][i] = __builtin_nontemporal_load(reinterpret_cast<const half8 *>(block) + unit8);
                 else
-                    k[s][i] = halves_of(reinterpret_cast<const v2u32 *>(block)[unit8]);
+                    k[s][i] = halves_of(__builtin_nontemporal_load(reinterpret_cast<const v2u32 *>(block) + unit8));
             }
 #pragma unroll
         for (int d = 0; d < 2 * DS; ++d) {
             const int unit8 = W / 8 * kBlockTokens + g * W + 16 * d + r;
             if (VB == 2)
-                v[d] = reinterpret_cast<const half8 *>(block)[unit8];
+                v[d] = __builtin_nontemporal_load(reinterpret_cast<const half8 *>(block) + unit8);
             else
-                v[d] = halves_of(reinterpret_cast<const v2u32 *>(block)[unit8]);
+                v[d] = halves_of(__builtin_nontemporal_load(reinterpret_cast<const v2u32 *>(block) + unit8));
         }
         if (VB == 1) {
             const floatx4 *scales = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W);
@@ -217,51 +248,68 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
         // The scores of keys key0 .. key0 + 7.
         const int key0 = b * kBlockTokens + 8 * g;
         float x[8];
-        bool seen[8];
-        float top = kNothing, top_scale = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             x[j] = st[j / 4][j % 4];
             if (VB == 1) x[j] *= ks[j / 4][j % 4];
-            x[j] = score_of(a, x[j], slope, it.p, key0 + j);
-            seen[j] = key0 + j >= lo && key0 + j < hi;
-            if (!seen[j]) x[j] = kNothing;
+        }
+        if (MOD) modify_scores(a, x, 8, slope, it.p, key0, [](int j) { return j; });
+        if (b * kBlockTokens < lo || (b + 1) * kBlockTokens > hi) {
+            // What the row does not see may hold anything, and nothing times infinity is not nothing.
+            uint32_t keep[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool seen = key0 + j >= lo && key0 + j < hi;
+                keep[j] = seen ? 0xFFFFu : 0u;
+                x[j] = seen ? x[j] : kNothing;
+                if (VB == 1) vs[j / 4][j % 4] = seen ? vs[j / 4][j % 4] : 0.f;
+            }
+            if (VB == 2) {
+                const v4u32 both = {keep[0] | keep[1] << 16, keep[2] | keep[3] << 16, keep[4] | keep[5] << 16, keep[6] | keep[7] << 16};
+#pragma unroll
+                for (int d = 0; d < 2 * DS; ++d) v[d] = __builtin_bit_cast(half8, __builtin_bit_cast(v4u32, v[d]) & both);
+            }
+        }
+        float top = x[0], top_scale = VB == 1 ? vs[0][0] : 0.f;
+#pragma unroll
+        for (int j = 1; j < 8; ++j) {
             top = fmaxf(top, x[j]);
-            if (VB == 1) top_scale = fmaxf(top_scale, seen[j] ? vs[j / 4][j % 4] : 0.f);
+            if (VB == 1) top_scale = fmaxf(top_scale, vs[j / 4][j % 4]);
         }
         const float m_new = fmaxf(m, max_32(max_16(top)));
-        const float base = m_new == kNothing ? 0.f : m_new;
-        float fade = exp2_of(m - base);
+        const float base = m_new == kNothing ? 0.f : -m_new * scale;
+        float fade = exp2_of(fmaf(m, scale, base));
         m = m_new;
         l *= fade;
         float to_unit = 1.f;
         if (VB == 1) {
             const float u = fmaxf(unit, max_32(max_16(top_scale)));
-            fade *= unit / u;
+            fade *= unit * __builtin_amdgcn_rcpf(u);
             unit = u;
-            to_unit = 16384.f / u;
+            to_unit = 16384.f * __builtin_amdgcn_rcpf(u);
         }
-        half8 p;
+        half8 p, rest;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float w = exp2_of(x[j] - base);
-            w = seen[j] ? w : 0.f;
-            l += w;
-            if (VB == 1) w = seen[j] ? w * (vs[j / 4][j % 4] * to_unit) : 0.f;
+            float w = exp2_of(fmaf(x[j], scale, base));
+            if (VB == 1) {
+                l += w;
+                w *= vs[j / 4][j % 4] * to_unit;
+            }
             p[j] = (_Float16)w;
+            // Times its scale of values the largest weight is no longer 1, and its rounding the result's: what is rounded
+            // off takes part too. (The matrix unit idles.)
+            if (VB == 1) rest[j] = (_Float16)(w - (float)p[j]);
         }
-        // What the row does not see may hold anything, and nothing times infinity is not nothing.
-        if (VB == 2 && (b * kBlockTokens < lo || (b + 1) * kBlockTokens > hi)) {
-            v4u32 keep;
+        if (VB == 2) {  // the sum takes the weights as the product does
 #pragma unroll
-            for (int i = 0; i < 4; ++i) keep[i] = (seen[2 * i] ? 0xFFFFu : 0u) | (seen[2 * i + 1] ? 0xFFFF0000u : 0u);
-#pragma unroll
-            for (int d = 0; d < 2 * DS; ++d) v[d] = __builtin_bit_cast(half8, __builtin_bit_cast(v4u32, v[d]) & keep);
+            for (int j = 0; j < 8; j += 2) l = __builtin_amdgcn_fdot2(half2a{p[j], p[j + 1]}, half2a{(_Float16)1.f, (_Float16)1.f}, l, false);
         }
 #pragma unroll
         for (int d = 0; d < 2 * DS; ++d) {
             o[d] *= fade;
             o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[d], p, o[d], 0, 0, 0);
+            if (VB == 1) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[d], rest, o[d], 0, 0, 0);
         }
     }
 
@@ -285,12 +333,12 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
         float top = sm[0][col];
 #pragma unroll
         for (int w = 1; w < kRowWaves; ++w) top = fmaxf(top, sm[w][col]);
-        const float base = top == kNothing ? 0.f : top;
+        const float base = top == kNothing ? 0.f : -top * scale;
         floatx4 sum = {0.f, 0.f, 0.f, 0.f};
         float total = 0.f;
 #pragma unroll
         for (int w = 0; w < kRowWaves; ++w) {
-            const float f = exp2_of(sm[w][col] - base);
+            const float f = exp2_of(fmaf(sm[w][col], scale, base));
             total += sl[w][col] * f;
             sum += *reinterpret_cast<const floatx4 *>(&so[(w * 16 + col) * kStride + d]) * f;
         }
@@ -326,11 +374,11 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
         const int col = e / (W / 4), d = 4 * (e % (W / 4));
         float top = kNothing;
         for (int i = 0; i < pieces; ++i) top = fmaxf(top, so[i * 32 + col]);
-        const float base = top == kNothing ? 0.f : top;
+        const float base = top == kNothing ? 0.f : -top * scale;
         const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(first, (short)0, -1, kBufferRsrcWord3);
         floatx4 sum = {0.f, 0.f, 0.f, 0.f};
         float total = 0.f;
-        constexpr int kBatch = 8;
+        constexpr int kBatch = 32;  // loads of a turn, all under way at once
         for (int i0 = 0; i0 < pieces; i0 += kBatch) {
             v4u32 v[kBatch];
 #pragma unroll
@@ -340,7 +388,7 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
                 if (i0 + i < pieces) {
-                    const float f = exp2_of(so[(i0 + i) * 32 + col] - base);
+                    const float f = exp2_of(fmaf(so[(i0 + i) * 32 + col], scale, base));
                     total += so[(i0 + i) * 32 + 16 + col] * f;
                     sum += __builtin_bit_cast(floatx4, v[i]) * f;
                 }
@@ -352,34 +400,39 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
 
 typedef void (*AttendFn)(AttendArgs);
 
-template <int VB>
+template <int VB, bool MOD>
 AttendFn rows_kernel_of(int width) {
     switch (width) {
-        case 32: return attend_rows_kernel<1, VB>;
-        case 64: return attend_rows_kernel<2, VB>;
-        case 96: return attend_rows_kernel<3, VB>;
-        case 128: return attend_rows_kernel<4, VB>;
-        case 192: return attend_rows_kernel<6, VB>;
-        default: return attend_rows_kernel<8, VB>;
+        case 32: return attend_rows_kernel<1, VB, MOD>;
+        case 64: return attend_rows_kernel<2, VB, MOD>;
+        case 96: return attend_rows_kernel<3, VB, MOD>;
+        case 128: return attend_rows_kernel<4, VB, MOD>;
+        case 192: return attend_rows_kernel<6, VB, MOD>;
+        default: return attend_rows_kernel<8, VB, MOD>;
     }
 }
+
 struct AttendPlan {
     bool rows;             // the rows kernel; else the tiles kernel
     bool split;
-    int tiles, pieces_bits;
+    int tiles, pieces_bits, min_blocks;
     int pieces;            // of a tile at most (tiles kernel)
     int64_t limit, slots;  // items and partial results of a head
     size_t partial_bytes;
 };
 
-constexpr int kPiecesBits = 10;
+// Pieces that the rows kernel aims at, and blocks of a piece at least. Two workgroups of it fit a CU, 512 the chip. Few
+// tiles, so long ones or an idle chip: one round of pieces, down to two blocks for each wavefront (8 tiles of 4096
+// blocks of 16 KB: 92 us; 1024 pieces 105). Many tiles differ in length and are cut finer, so that the last to end are
+// short (64 sequences of 1024 to 8192 tokens, 8 tiles each, 8 bits: 129 us; 143 with 512), but not where a piece's start
+// and join would take as long as it (640 tiles of up to 32 blocks: 34.4 us whole, 43 in 1024 pieces).
+constexpr int kFewTiles = 128, kFewBits = 9, kFewMinBlocks = 8, kManyBits = 10, kManyMinBlocks = 32;
 constexpr int64_t kTilePlaces = 512;   // workgroups of the tiles kernel that run at once
 constexpr int64_t kMostTilePieces = 16;
 
 AttendPlan plan_attention(const CacheView &c, const RowsView &r, int heads) {
     const int64_t group = heads / c.kv_heads;
     AttendPlan p = {};
-    p.pieces_bits = kPiecesBits;
     p.rows = !r.offsets || (int64_t)r.rows <= 4 * (int64_t)r.sequences;
     if (!p.rows) {
         const int64_t columns = tile_columns(c.width);
@@ -390,9 +443,13 @@ AttendPlan plan_attention(const CacheView &c, const RowsView &r, int heads) {
     }
     p.tiles = (int)((group + 15) / 16);
     const int64_t all = (int64_t)r.rows * p.tiles;
+    const bool few = all * c.kv_heads <= kFewTiles;
+    p.pieces_bits = few ? kFewBits : kManyBits;
+    p.min_blocks = few ? kFewMinBlocks : kManyMinBlocks;
     const int64_t pieces = ((int64_t)1 << p.pieces_bits) / c.kv_heads;
     // Cut where there are few tiles, and their counters and the lanes' sequences fit.
-    p.split = all * c.kv_heads <= 16384 && r.sequences <= 4096 && (all + pieces) * c.kv_heads <= kMaxCounters;
+    p.split = all * c.kv_heads <= 16384 && r.sequences <= 4096 && (all + pieces) * c.kv_heads <= kMaxCounters &&
+              r.capacity > p.min_blocks * kBlockTokens;
     p.limit = p.split ? all + pieces : all;
     if (p.split) {
         // Tiles of more than one piece have at most twice their even share.
@@ -445,13 +502,16 @@ int launch_attention(const CacheView &c, const RowsView &r, const usp_attention_
     a.split = plan.split;
     a.pieces = plan.pieces;
     a.pieces_bits = plan.pieces_bits;
+    a.min_blocks = plan.min_blocks;
     a.limit = (int)plan.limit;
     a.slot_limit = (int)plan.slots;
     a.counters = reinterpret_cast<uint32_t *>(workspace);
     a.partials = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + kCounterRegionBytes);
     const int64_t grid = plan.limit * c.kv_heads * (plan.rows ? 1 : plan.pieces);
-    if (!plan.rows) return launch_tiles(&a, c.width, c.value_bytes, a.cap > 0.f || a.slopes || !(a.scale > 0.f), grid, stream);
-    const AttendFn fn = c.value_bytes == 2 ? rows_kernel_of<2>(c.width) : rows_kernel_of<1>(c.width);
+    const bool modified = a.cap > 0.f || a.slopes || !(a.scale > 0.f);
+    if (!plan.rows) return launch_tiles(&a, c.width, c.value_bytes, modified, grid, stream);
+    const AttendFn fn = c.value_bytes == 2 ? modified ? rows_kernel_of<2, true>(c.width) : rows_kernel_of<2, false>(c.width)
+                                           : modified ? rows_kernel_of<1, true>(c.width) : rows_kernel_of<1, false>(c.width);
     hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(kRowWaves * kLanes), 0, reinterpret_cast<hipStream_t>(stream), a);
     return (int)hipGetLastError();
 }

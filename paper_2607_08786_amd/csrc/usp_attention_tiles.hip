@@ -279,11 +279,7 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 2 ? 3 : 2) v
 #pragma unroll
                     for (int i = 0; i < 16; ++i) st[t][i] *= key_scales[buffer][(16 * (i / 8) + 8 * half + i % 8) / 4][i % 4];
                 }
-                if (MOD) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        st[t][i] = score_of(a, st[t][i], slope[t], p[t], block_lo + 16 * (i / 8) + 8 * half + i % 8);
-                }
+                if (MOD) modify_scores(a, st[t], 16, slope[t], p[t], block_lo + 8 * half, [](int i) { return 16 * (i / 8) + i % 8; });
                 if (!whole) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {

@@ -602,6 +602,7 @@ class KVCache:
             raise ValueError(f"data must be a contiguous uint8 tensor {shape}")
         self.data = data
         self.description.data = data.data_ptr()
+        self._blocks = None
 
     def workspace_size(self, rows: CacheRows, T: int, heads: int) -> int:
         return usp_attention_workspace_size(self, rows, T, heads)
@@ -645,6 +646,8 @@ class KVCache:
         """Views of every key and value as they lie in memory: K [layers, pages, kv_heads, page_tokens / 32, 2, 2, 2, 4,
         channels / 8, 8], whose dimensions 4 to 7 are the bits 4, 3, 2 and 1 to 0 of a token's place in its block, and V
         [layers, pages, kv_heads, page_tokens / 32, 4, 8, channels], 4 and 5 the token; of 8 bits the codes."""
+        if self._blocks is not None:
+            return self._blocks
         size, W = self.dtype.itemsize, cache_width(self.head_dim)
         block = 64 * W * size + (256 if size == 1 else 0)
         b = self.data.view(self.layers, self.pages, self.kv_heads, self.page_tokens // 32, block)
@@ -653,7 +656,8 @@ class KVCache:
         v = b[..., 32 * W * size:64 * W * size].view(self.dtype).unflatten(-1, (4, W, 8))
         n = len(lead)
         k = k.permute(*range(n), n + 1, n + 3, n + 2, n + 4, n, n + 5)
-        return k[..., :self.head_dim // 8, :], v.transpose(-1, -2)[..., :self.head_dim]
+        self._blocks = k[..., :self.head_dim // 8, :], v.transpose(-1, -2)[..., :self.head_dim]
+        return self._blocks
 
 
 def cache_width(head_dim: int) -> int:

@@ -461,7 +461,7 @@ def test_workspace_shared_with_products():
 
 
 def test_binding_refusals():
-    s = Setting([40, 40], 2, 64, 32, seed=1).fill()
+    s = Setting([400, 40], 2, 64, 32, seed=1).fill()
     q = draw(1, 2, 4, 64).cuda()
     rows = s.rows()
     out = torch.empty_like(q)

@@ -16,7 +16,7 @@ def described(**change):
     keep = ctypes.create_string_buffer(256)
     base = ctypes.addressof(keep) + 63 & ~63
     c = usp.usp_cache(base, 2, 8, 4, 64, 32, 2, 0)
-    r = usp.usp_cache_rows(base, 3, 3, base, base, 2, 5)
+    r = usp.usp_cache_rows(base, 300, 300, base, base, 2, 5)
     a = usp.usp_attention_args(base, base, None, None, None, 8 * 64, 64, 8 * 64, 64, 1, 0, 8, 0.1, 0.0)
     for name, v in change.items():
         where, field = name.split("_", 1)
