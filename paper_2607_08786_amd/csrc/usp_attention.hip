@@ -427,7 +427,7 @@ struct AttendPlan {
 // short (64 sequences of 1024 to 8192 tokens, 8 tiles each, 8 bits: 129 us; 143 with 512), but not where a piece's start
 // and join would take as long as it (640 tiles of up to 32 blocks: 34.4 us whole, 43 in 1024 pieces).
 constexpr int kFewTiles = 128, kFewBits = 9, kFewMinBlocks = 8, kManyBits = 10, kManyMinBlocks = 32;
-constexpr int64_t kTilePlaces = 512;   // workgroups of the tiles kernel that run at once
+constexpr int64_t kTilePlaces = 768;   // workgroups of the tiles kernel that run at once
 constexpr int64_t kMostTilePieces = 16;
 
 AttendPlan plan_attention(const CacheView &c, const RowsView &r, int heads) {

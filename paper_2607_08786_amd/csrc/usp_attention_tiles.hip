@@ -29,13 +29,14 @@ __device__ inline half8 values_of(v2u32 codes, floatx4 s0, floatx4 s1) {
 
 // Columns of a wavefront: CT tiles of 32. MOD: scores are capped, biased or not scaled by a positive number.
 template <int DS, int VB, bool MOD, int CT>
-__global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 2 ? 3 : 2) void attend_tiles_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : 3) void attend_tiles_kernel(AttendArgs a) {
     constexpr int W = 32 * DS, kBlockBytes = (int)cache_block_bytes(W, VB);
     constexpr int kColumns = 32 * CT * kTileWaves;
     constexpr int kKeyUnits = W / 8 * kBlockTokens;  // units of 8 keys' channels, and as many of values'
     constexpr int kThreads = kTileWaves * kLanes;
     __shared__ half8 staged[2][2 * kKeyUnits];  // blocks of keys, then of values, as in the cache
     __shared__ floatx4 key_scales[2][kBlockTokens / 4];
+    __shared__ v2u32 raw[2][VB == 1 ? kBlockBytes / 8 : 1];  // 8 bits: blocks as they lie in the cache
     __shared__ int ends[4][kTileWaves];
     __shared__ int odd[kTileWaves];  // whether a wavefront's part of a block's values holds any that is not finite
     __shared__ uint32_t arrived;
@@ -167,44 +168,35 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 2 ? 3 : 2) v
         }
         return b;
     };
-    // A block on its way into LDS: requested a block ahead, stored behind the products.
-    v2u32 codes[DS];
-    floatx4 unit_scales[DS][2], lane_scales = {};
+    // A block on its way into LDS, 16 bytes a lane: the compiler neither sees these transfers nor waits for them.
     auto request = [&](const uint8_t *block, int buffer) {
-        if constexpr (VB == 2) {
-            // Straight into LDS: the compiler neither sees these transfers nor waits for them.
-            const uint64_t from = reinterpret_cast<uint64_t>(block);
-            const v4i32 rsrc = {(int)(uint32_t)from, (int)((uint32_t)(from >> 32) & 0xFFFFu), kBlockBytes, kBufferRsrcWord3};
-            const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)as_lds(staged[buffer]) + wave * kLanes * 16);
+        const uint64_t from = reinterpret_cast<uint64_t>(block);
+        const v4i32 rsrc = {(int)(uint32_t)from, (int)((uint32_t)(from >> 32) & 0xFFFFu), kBlockBytes, kBufferRsrcWord3};
+        const void *base = VB == 2 ? (const void *)staged[buffer] : (const void *)raw[VB == 1 ? buffer : 0];
+        const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)as_lds(base) + wave * kLanes * 16);
 #pragma unroll
-            for (int i = 0; i < DS; ++i)
+        for (int i = 0; i * kThreads * 16 < kBlockBytes; ++i)
+            if ((i + 1) * kThreads * 16 <= kBlockBytes || (i * kThreads + (int)threadIdx.x) * 16 < kBlockBytes)
                 asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                              :
                              : "s"(to + 16u * kThreads * i), "v"(16 * (kThreads * i + (int)threadIdx.x)), "s"(rsrc)
                              : "memory", "m0");
-            return;
-        }
+    };
+    // 8 bits: codes as fp16, those of values times their scales.
+    auto convert = [&](int buffer) {
+        const v2u32 *from = raw[VB == 1 ? buffer : 0];
+        const floatx4 *scales = reinterpret_cast<const floatx4 *>(from + 2 * kKeyUnits);
 #pragma unroll
         for (int i = 0; i < DS; ++i) {
             const int u = i * kThreads + (int)threadIdx.x;
-            codes[i] = reinterpret_cast<const v2u32 *>(block)[u];
-            if ((i + 1) * kThreads > kKeyUnits && u >= kKeyUnits) {
-                const floatx4 *of = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W) + kBlockTokens / 4;
-                unit_scales[i][0] = of[2 * ((u - kKeyUnits) / W)];
-                unit_scales[i][1] = of[2 * ((u - kKeyUnits) / W) + 1];
+            if ((i + 1) * kThreads <= kKeyUnits || u < kKeyUnits) {
+                staged[buffer][u] = halves_of(from[u]);
+            } else {
+                const int keys8 = (u - kKeyUnits) / W;
+                staged[buffer][u] = values_of(from[u], scales[kBlockTokens / 4 + 2 * keys8], scales[kBlockTokens / 4 + 2 * keys8 + 1]);
             }
         }
-        if (threadIdx.x < kBlockTokens / 4)
-            lane_scales = reinterpret_cast<const floatx4 *>(block + 2 * kBlockTokens * W)[threadIdx.x];
-    };
-    auto store = [&](int buffer) {
-#pragma unroll
-        for (int i = 0; i < DS; ++i) {
-            const int u = i * kThreads + (int)threadIdx.x;
-            const bool value = (i + 1) * kThreads > kKeyUnits && u >= kKeyUnits;
-            staged[buffer][u] = value ? values_of(codes[i], unit_scales[i][0], unit_scales[i][1]) : halves_of(codes[i]);
-        }
-        if (threadIdx.x < kBlockTokens / 4) key_scales[buffer][threadIdx.x] = lane_scales;
+        if (threadIdx.x < kBlockTokens / 4) key_scales[buffer][threadIdx.x] = scales[threadIdx.x];
     };
     // Nothing times infinity is not nothing: in a block that some column does not see the whole of, values that are not
     // finite are left out of the product, and added to the columns that see them (below).
@@ -231,18 +223,33 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 2 ? 3 : 2) v
     };
     auto all_see = [&](int b) { return tile_all_lo <= b * kBlockTokens && (b + 1) * kBlockTokens <= tile_all_hi; };
 
-    const uint8_t *block = nullptr;
-    int b = next(b0, block);
-    if (b < b1) {
-        request(block, 0);
-        if (VB == 1) store(0);
+    const uint8_t *here = nullptr, *block = nullptr;
+    int b = next(b0, here);
+    if (b < b1) request(here, 0);
+    block = here;
+    int b_next = b1;
+    if (VB == 1) {
+        b_next = next(b + 1, block);
+        if (b_next < b1) request(block, 1);
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_only(0));  // of q too: else the loop waits for what it requests ahead
     __syncthreads();
+    if (VB == 1) {
+        if (b < b1) convert(0);
+        lds_barrier();
+    }
     for (int buffer = 0; b < b1; buffer ^= 1) {
-        const uint8_t *here = block;
-        const int b_next = next(b + 1, block);
-        if (b_next < b1) request(block, buffer ^ 1);
+        // fp16: the next block is requested; 8 bits: the one behind it, and the next converted.
+        const uint8_t *next_block = block;
+        int b_after = b1;
+        if (VB == 2) {
+            b_next = next(b + 1, next_block);
+            if (b_next < b1) request(next_block, buffer ^ 1);
+        } else {
+            b_after = next(b_next + 1, block);
+            if (b_after < b1) request(block, buffer);
+            if (b_next < b1) convert(buffer ^ 1);
+        }
         const int block_lo = b * kBlockTokens, block_hi = block_lo + kBlockTokens;
         if (!all_see(b)) clean(buffer);
         if (block_hi > any_lo && block_lo < any_hi) {  // else this wavefront sees nothing of it
@@ -339,10 +346,11 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 2 ? 3 : 2) v
                     }
             }
         }
-        if (VB == 1 && b_next < b1) store(buffer ^ 1);
-        if (VB == 2) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next block lies in LDS
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what was requested lies in LDS
         lds_barrier();
         b = b_next;
+        here = next_block;
+        if (VB == 1) b_next = b_after;
     }
 
 #pragma unroll
