@@ -404,8 +404,9 @@ size_t usp_cache_page_bytes(const usp_cache *cache);
  * offsets[s + 1]: row t is its token lengths[s] - offsets[s + 1] + t. Token j of it lies in page
  * table[s * ld_table + j / page_tokens]. All are read on the device, so a captured call takes what they
  * hold when it is replayed, and none makes a call read or write outside its operands: lengths count as at
- * most table_pages * page_tokens and at least 0, offsets as within [0, rows] and not below an earlier
- * one, a token before the sequence's start is not there, and neither is one in a page outside [0, pages).
+ * most table_pages * page_tokens and at least 0, offsets as within [0, rows] (where they decrease, which rows are
+ * computed is not defined), a token before the sequence's start is not there, and neither is one in a page outside
+ * [0, pages).
  */
 typedef struct {
     const int32_t *table;    /* device int32, sequences rows of table_pages entries with stride ld_table */
@@ -453,9 +454,11 @@ usp_status usp_cache_copy(const usp_cache *cache, const int32_t *src, const int3
  * h / (heads / kv_heads) of the cache:
  *     x[k] = scale * q . K[k];   x[k] <- cap * tanh(x[k] / cap)  (cap > 0);   x[k] <- x[k] - slopes[h] * |p - k|
  *     out  = sum_k exp(x[k]) V[k] / sum_k exp(x[k]),   zeros for a row that sees nothing
- * in fp32, the weights exp(x - max) rounded to fp16 for the product with V (relative 2^-11 each; the sum below the
- * line takes them unrounded), one rounding to fp16 at the end. What a row does not see has no influence on
- * it, NaN and infinities included. A row that sees a NaN, or a score of +infinity, is NaN.
+ * in fp32, the weights exp(x - max) rounded to fp16 for the product with V (relative 2^-11 each, above the line and below
+ * alike; 8-bit caches and single rows: to 22 bits), one rounding to fp16 at the end. What a row does not see has no
+ * influence on it, NaN and infinities included. A row that sees a NaN, or a score of +infinity, is NaN; one whose
+ * scores are all -infinity is zeros. Infinities in q, K or scale * q . K beyond fp32's range count as what they
+ * are there.
  */
 typedef struct {
     const void *q;          /* device fp16: channel d of head h of row t at q + t * ld_q + h * head_q + d */

@@ -427,17 +427,24 @@ struct AttendPlan {
 // short (64 sequences of 1024 to 8192 tokens, 8 tiles each, 8 bits: 129 us; 143 with 512), but not where a piece's start
 // and join would take as long as it (640 tiles of up to 32 blocks: 34.4 us whole, 43 in 1024 pieces).
 constexpr int kFewTiles = 128, kFewBits = 9, kFewMinBlocks = 8, kManyBits = 10, kManyMinBlocks = 32;
-constexpr int64_t kTilePlaces = 768;   // workgroups of the tiles kernel that run at once
+// Workgroups of the tiles kernel that run at once, by the bytes of a value: three on a CU, two that convert 8 bits (512
+// rows over 16512 tokens, 256 tiles: 438 us in two pieces each, 493 in three).
+constexpr int64_t kTilePlaces[] = {0, 512, 768};
 constexpr int64_t kMostTilePieces = 16;
 
 AttendPlan plan_attention(const CacheView &c, const RowsView &r, int heads) {
     const int64_t group = heads / c.kv_heads;
     AttendPlan p = {};
-    p.rows = !r.offsets || (int64_t)r.rows <= 4 * (int64_t)r.sequences;
+    // The rows kernel reads the cache for each row, the tiles kernel for 128 columns, with fewer workgroups where there are
+    // few sequences. 16 sequences of 4096 tokens, 8 heads for each of 8: 1 row each 46 against 67 us, 2 rows 66 / 66, 4
+    // rows 97 / 65; one sequence of 65536: 54 / 122, 74 / 125, 96 / 126, 6 rows 198 / 129; with a head for each of 40 there:
+    // 257 / 263, 2 rows 455 / 262.
+    const int64_t S = r.sequences, T = r.rows;
+    p.rows = T <= S || (T <= 4 * S && group >= 4 && S * c.kv_heads <= 64);
     if (!p.rows) {
         const int64_t columns = tile_columns(c.width);
         p.limit = ((int64_t)r.rows * group + columns - 1) / columns + r.sequences - 1;
-        p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>(kMostTilePieces, kTilePlaces / (p.limit * c.kv_heads)));
+        p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>(kMostTilePieces, kTilePlaces[c.value_bytes] / (p.limit * c.kv_heads)));
         if (p.pieces > 1) p.partial_bytes = (size_t)(p.limit * c.kv_heads * p.pieces * tile_slot_floats(c.width)) * sizeof(float);
         return p;
     }

@@ -8,7 +8,7 @@ namespace usp {
 namespace {
 
 constexpr int kAhead = 4;           // products that operands are read ahead
-constexpr int kMinTileBlocks = 16;  // blocks of a piece at least
+constexpr int kMinTileBlocks = 6;   // blocks of a piece at least
 
 // The first tile of sequence s: those before it have at most so many.
 template <int COLUMNS>
@@ -16,26 +16,34 @@ __device__ inline int first_tile(const AttendArgs &a, int s) {
     return (int)((int64_t)offset_of(a.r, s) * a.group / COLUMNS) + s;
 }
 
-// Eight codes of keys j .. j + 7 of a channel as fp16 values.
+// A scale of values is taken apart into one of 4 bits, whose products with codes fp16 holds exactly, and a factor near 1
+// that the weight of its key takes, in its exponent (so that the largest weight is 1 all the same, which has no
+// rounding): rounded products would add to the result's error as much as its own rounding.
+__device__ inline float short_scale(float s) { return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, s) + 0x80000u) & 0xFFF00000u); }
+
+// Eight codes of keys j .. j + 7 of a channel times their short scales, as fp16 values.
 __device__ inline half8 values_of(v2u32 codes, floatx4 s0, floatx4 s1) {
     half8 out;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int8_t c = (int8_t)(codes[i / 4] >> (8 * (i % 4)));
-        out[i] = (_Float16)((float)c * (i < 4 ? s0[i % 4] : s1[i % 4]));
+        out[i] = (_Float16)((float)c * short_scale(i < 4 ? s0[i % 4] : s1[i % 4]));
     }
     return out;
 }
 
 // Columns of a wavefront: CT tiles of 32. MOD: scores are capped, biased or not scaled by a positive number.
 template <int DS, int VB, bool MOD, int CT>
-__global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : 3) void attend_tiles_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) void attend_tiles_kernel(AttendArgs a) {
     constexpr int W = 32 * DS, kBlockBytes = (int)cache_block_bytes(W, VB);
     constexpr int kColumns = 32 * CT * kTileWaves;
     constexpr int kKeyUnits = W / 8 * kBlockTokens;  // units of 8 keys' channels, and as many of values'
     constexpr int kThreads = kTileWaves * kLanes;
     __shared__ half8 staged[2][2 * kKeyUnits];  // blocks of keys, then of values, as in the cache
-    __shared__ floatx4 key_scales[2][kBlockTokens / 4];
+    // 8 bits, of each key: its scale (times that of the scores), and the factor f of its weight as a logarithm and as
+    // 1 / f - 1 (near 0 both: in fp16 they are off by less than 2^-15).
+    __shared__ floatx4 key_scales[2][VB == 1 ? kBlockTokens / 4 : 1];
+    __shared__ half8 factors[2][2][VB == 1 ? kBlockTokens / 8 : 1];
     __shared__ v2u32 raw[2][VB == 1 ? kBlockBytes / 8 : 1];  // 8 bits: blocks as they lie in the cache
     __shared__ int ends[4][kTileWaves];
     __shared__ int odd[kTileWaves];  // whether a wavefront's part of a block's values holds any that is not finite
@@ -143,7 +151,7 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : 3) void attend_til
         l[t] = 0.f;
     }
     // Plain scores are scaled in the exponential's argument, others before.
-    const float scale = MOD ? 1.f : a.scale;
+    const float scale = MOD || VB == 1 ? 1.f : a.scale;
 
     const int32_t *table = a.r.table + (int64_t)s * a.r.ld_table;
     const uint8_t *head_base = a.c.base + (int64_t)h * a.c.page_blocks * kBlockBytes;
@@ -182,21 +190,29 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : 3) void attend_til
                              : "s"(to + 16u * kThreads * i), "v"(16 * (kThreads * i + (int)threadIdx.x)), "s"(rsrc)
                              : "memory", "m0");
     };
-    // 8 bits: codes as fp16, those of values times their scales.
+    // 8 bits: codes as fp16, those of values times their short scales.
     auto convert = [&](int buffer) {
         const v2u32 *from = raw[VB == 1 ? buffer : 0];
-        const floatx4 *scales = reinterpret_cast<const floatx4 *>(from + 2 * kKeyUnits);
 #pragma unroll
         for (int i = 0; i < DS; ++i) {
             const int u = i * kThreads + (int)threadIdx.x;
             if ((i + 1) * kThreads <= kKeyUnits || u < kKeyUnits) {
                 staged[buffer][u] = halves_of(from[u]);
             } else {
-                const int keys8 = (u - kKeyUnits) / W;
-                staged[buffer][u] = values_of(from[u], scales[kBlockTokens / 4 + 2 * keys8], scales[kBlockTokens / 4 + 2 * keys8 + 1]);
+                const floatx4 *scales = reinterpret_cast<const floatx4 *>(from + 2 * kKeyUnits) + kBlockTokens / 4 + 2 * ((u - kKeyUnits) / W);
+                staged[buffer][u] = values_of(from[u], scales[0], scales[1]);
             }
         }
-        if (threadIdx.x < kBlockTokens / 4) key_scales[buffer][threadIdx.x] = scales[threadIdx.x];
+    };
+    // What the scales of a block's 32 keys and values come to, one of each a lane.
+    auto put_scales = [&](int buffer) {
+        if (lane >= kBlockTokens) return;
+        const float *from = reinterpret_cast<const float *>(raw[VB == 1 ? buffer : 0] + 2 * kKeyUnits) + lane;
+        const float value = from[kBlockTokens], f = value * __builtin_amdgcn_rcpf(short_scale(value));
+        const _Float16 log = (_Float16)(fabsf(f - 1.f) < 0.5f ? __builtin_amdgcn_logf(f) : 0.f);  // of 0 and NaN: none
+        reinterpret_cast<float *>(key_scales[buffer])[lane] = from[0] * (MOD ? 1.f : a.scale);
+        reinterpret_cast<_Float16 *>(factors[buffer][0])[lane] = log;
+        reinterpret_cast<_Float16 *>(factors[buffer][1])[lane] = (_Float16)(exp2_of(-(float)log) - 1.f);
     };
     // Nothing times infinity is not nothing: in a block that some column does not see the whole of, values that are not
     // finite are left out of the product, and added to the columns that see them (below).
@@ -235,7 +251,10 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : 3) void attend_til
     __builtin_amdgcn_s_waitcnt(vmcnt_only(0));  // of q too: else the loop waits for what it requests ahead
     __syncthreads();
     if (VB == 1) {
-        if (b < b1) convert(0);
+        if (b < b1) {
+            convert(0);
+            if (wave == 0) put_scales(0);
+        }
         lds_barrier();
     }
     for (int buffer = 0; b < b1; buffer ^= 1) {
@@ -252,6 +271,7 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : 3) void attend_til
         }
         const int block_lo = b * kBlockTokens, block_hi = block_lo + kBlockTokens;
         if (!all_see(b)) clean(buffer);
+        if (VB == 1 && b_next < b1 && wave == (b_next & (kTileWaves - 1))) put_scales(buffer ^ 1);  // in turn
         if (block_hi > any_lo && block_lo < any_hi) {  // else this wavefront sees nothing of it
             const half8 *keys = staged[buffer], *values = staged[buffer] + kKeyUnits;
             const bool whole = all_lo <= block_lo && block_hi <= all_hi;
@@ -282,11 +302,24 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : 3) void attend_til
 #pragma unroll
             for (int t = 0; t < CT; ++t) {
                 // Register 8 u + j holds the score of key block_lo + 16 u + 8 half + j.
+                half8 log_factor[2], less_one[2];
                 if (VB == 1) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) st[t][i] *= key_scales[buffer][(16 * (i / 8) + 8 * half + i % 8) / 4][i % 4];
+                    for (int u = 0; u < 2; ++u) {
+                        log_factor[u] = factors[buffer][0][VB == 1 ? 2 * u + half : 0];
+                        less_one[u] = factors[buffer][1][VB == 1 ? 2 * u + half : 0];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float by = key_scales[buffer][VB == 1 ? 4 * (i / 8) + 2 * half + i % 8 / 4 : 0][i % 4];
+                        st[t][i] = fmaf(st[t][i], by, MOD ? 0.f : (float)log_factor[i / 8][i % 8]);
+                    }
                 }
                 if (MOD) modify_scores(a, st[t], 16, slope[t], p[t], block_lo + 8 * half, [](int i) { return 16 * (i / 8) + i % 8; });
+                if (MOD && VB == 1) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) st[t][i] += (float)log_factor[i / 8][i % 8];
+                }
                 if (!whole) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
@@ -306,13 +339,14 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : 3) void attend_til
                     for (int d = 0; d < DS; ++d) o[t][d] *= fade;
                 }
                 const float base = m[t] == kNothing ? 0.f : -m[t] * scale;
+                // The sum takes the weights as the product does.
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[t][i / 8][i % 8] = (_Float16)exp2_of(fmaf(st[t][i], scale, base));
-                // The sum takes the weights as the product does.
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const half2a pair = {w[t][i / 4][2 * (i % 4)], w[t][i / 4][2 * (i % 4) + 1]};
                     l[t] = __builtin_amdgcn_fdot2(pair, half2a{(_Float16)1.f, (_Float16)1.f}, l[t], false);
+                    if (VB == 1) l[t] = __builtin_amdgcn_fdot2(pair, half2a{less_one[i / 4][2 * (i % 4)], less_one[i / 4][2 * (i % 4) + 1]}, l[t], false);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);

@@ -2,8 +2,11 @@
 
 out = sum_k w_k V_k / sum_k w_k. With p_k = w_k / sum w and A = sum_k p_k |V_k| (per channel), the errors are
 * the result's rounding to fp16: 2^-11 |out|, 2^-25 where it is subnormal;
-* the weights' rounding to fp16: 2^-11 of each, so 2^-11 A, and 2^-25 each where they are subnormal, so
-  2^-25 sum |V_k| over sum w, which is at least 1 (weights are relative to the largest);
+* the weights' rounding to fp16, relative d_k of at most 2^-11 above and below the line alike: sum_k p_k d_k (V_k - out), so
+  2^-11 (A + |out|), and 2^-25 each where they are subnormal, so 2^-25 sum |V_k| over sum w, which is at least 1 (weights
+  are relative to the largest);
+* in 8 bits a weight's factor f between 16 / 17 and 17 / 16, held as log2 f (below 0.0875, so half a step of fp16 is 2^-15) and as
+  1 / f - 1 (the same): relative 2^-15 ln 2 + 2^-15 < 2^-14 of each weight, so 2^-14 (A + |out|);
 * an error e of the scores, which moves p_k by p_k (e_k - sum p e), so at most 2 e A;
 * fp32 sums over n keys and the rescaling of what was summed: fewer than 4 (n + 40) roundings of A.
 e in roundings U = 2^-24: 2 (D + 40) of sum_d |q_d K_d| scale (products and their sum, twice over for what the matrix unit
@@ -70,7 +73,8 @@ def attend(q, K, V, scale=None, cap=0.0, slopes=None, first=None, last=None, win
             A = w @ vv.abs()
             e = U * (2 * (D + 40) * size[i, at].max() + 16 * (z.abs().max() + cap + bias[i, at].abs().max()))
             subnormal = 2.0 ** -25 * vv.abs().sum(0) * w.max()
-            tol[i, h] = 2.0 ** -25 + 2.0 ** -11 * out[i, h].abs() + 2.0 ** -11 * A + subnormal + 2 * e * A + 4 * (len(at) + 40) * U * A
+            tol[i, h] = (2.0 ** -25 + 2.0 ** -11 * out[i, h].abs() + (2.0 ** -11 + 2.0 ** -14) * (A + out[i, h].abs()) + subnormal +
+                         2 * e * A + 4 * (len(at) + 40) * U * A)
     return out, tol
 
 

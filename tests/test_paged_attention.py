@@ -128,7 +128,8 @@ def test_masks(counts, values):
     s.fill()
     T = sum(counts)
     g = torch.Generator().manual_seed(3)
-    q = draw(7, T, 4, 64)
+    q = draw(7, T, 8, 64)
+    assert s.cache.plan(s.rows(counts), T, 8).startswith("rows" if T == 6 else "tiles")
     position = torch.cat([torch.arange(L - n, L) for L, n in zip(lengths, counts)])
     first = torch.randint(-3, 120, (T,), generator=g).int()
     last = torch.randint(-5, 200, (T,), generator=g).int()
@@ -248,7 +249,7 @@ def test_append_strides():
 
 def test_rows_that_are_not_there():
     """Pages outside the cache, lengths beyond the table, rows outside the offsets: no write, no influence, nothing read outside."""
-    kv, D, heads = 1, 64, 2
+    kv, D, heads = 1, 64, 4
     s = Setting([64, 96], kv, D, 32, seed=5).fill()
     q = draw(2, 2, heads, D).cuda()
     table = s.table.clone()
