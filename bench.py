@@ -44,6 +44,9 @@ def parse():
     ap.add_argument("--workload", default="ffn70b")
     ap.add_argument("--N", type=int, default=16)
     ap.add_argument("--sparsity", type=int, default=50)
+    ap.add_argument("--context", type=int, default=0,
+                    help="block workloads: attention over so many cached tokens of each of the N sequences, the step's "
+                         "included (0: q stands in for its output)")
     ap.add_argument("--rotate-gib", type=float, default=1.0)
     ap.add_argument("--mode", choices=("graph", "eager"), default="graph")
     ap.add_argument("--no-cpu", action="store_true", help="skip the CPU oracle baseline")
@@ -334,11 +337,13 @@ def block_main(args):
     """Decode step of one decoder block (--workload block13b / block70b): its six
     linear layers in order, each one fused usp_spmm_ex launch (bias, ReLU on the
     FFN's first layer, residual adds), against the same chain done densely with
-    hipBLASLt (torch.addmm) and separate elementwise kernels."""
+    hipBLASLt (torch.addmm) and separate elementwise kernels. With --context the step's
+    keys and values go into a paged cache and attention over it (usp_cache_append,
+    usp_attention) stands between the projections, in both chains."""
     import torch
 
     import workloads as wl
-    from paper_2607_08786_amd import usp
+    from paper_2607_08786_amd import attention, usp
 
     torch.cuda.set_device(0)
     sp = args.sparsity or 50
@@ -360,15 +365,35 @@ def block_main(args):
                      (layers[0], layers[1], layers[2], layers[3], layers[5]))
     u = torch.empty((N, layers[4].M), dtype=torch.float16, device="cuda")
 
-    def sparse_step(ms):
+    heads, kv_heads, dim = cfg["heads"], cfg["kv_heads"], cfg["head_dim"]
+    if args.context:  # one layer of the cache for each copy of the block
+        pages = N * math.ceil(args.context / 64)
+        cache = attention.PagedCache(pages, kv_heads, dim, page_tokens=64, layers=copies)
+        ids = [cache.add() for _ in range(N)]
+        prompt = cache.extend(ids, [args.context] * N)
+        draw = torch.Generator(device="cuda").manual_seed(cfg["cfg_id"])
+        for layer in range(copies):
+            K0, V0 = (torch.randn(N * args.context, kv_heads, dim, generator=draw, device="cuda", dtype=torch.float16) for _ in range(2))
+            cache.append(prompt, K0, V0, layer=layer)
+        rows, a = cache.rows(ids), torch.empty_like(q)
+        space = cache.make_workspace(rows, N, heads)
+
+    def attended(q, k, v, layer):
+        if not args.context:
+            return q  # stands in for the attention's output
+        cache.append(rows, k.view(N, kv_heads, dim), v.view(N, kv_heads, dim), layer=layer)
+        usp.usp_attention(cache, rows, q.view(N, heads, dim), a.view(N, heads, dim), space, layer=layer)
+        return a
+
+    def sparse_step(ms, layer=0):
         ms[0].spmm(X, Y=q, workspace=ws, bias=biases[0])
         ms[1].spmm(X, Y=k, workspace=ws, bias=biases[1])
         ms[2].spmm(X, Y=v, workspace=ws, bias=biases[2])
-        ms[3].spmm(q, Y=o, workspace=ws, bias=biases[3], residual=X)      # attention output stand-in: q
+        ms[3].spmm(attended(q, k, v, layer), Y=o, workspace=ws, bias=biases[3], residual=X)
         ms[4].spmm(o, Y=u, workspace=ws, bias=biases[4], activation="relu")
         ms[5].spmm(u, Y=y, workspace=ws, bias=biases[5], residual=o)
 
-    steps = [lambda ms=ms: sparse_step(ms) for ms in mats]
+    steps = [lambda ms=ms, i=i: sparse_step(ms, i) for i, ms in enumerate(mats)]
     ms_sparse = timed_steps(torch, steps, args.steps, args.warmup, args.mode)
 
     # Check the block's output against the same pruned block in fp32 (dense).
@@ -377,6 +402,10 @@ def block_main(args):
     torch.cuda.synchronize()
     f = lambda t: t.float()
     q32 = f(X) @ f(dws[0]).t() + f(biases[0])
+    if args.context:
+        Kc, Vc = (f(t).view(N, args.context, kv_heads, dim).permute(0, 2, 1, 3) for t in cache.read(prompt, N * args.context))
+        p32 = torch.softmax(q32.half().float().view(N, kv_heads, -1, dim) @ Kc.transpose(2, 3).contiguous() * dim ** -0.5, -1)
+        q32 = (p32 @ Vc.contiguous()).reshape(N, heads * dim)
     o32 = q32.half().float() @ f(dws[3]).t() + f(biases[3]) + f(X)
     u32 = torch.relu(o32.half().float() @ f(dws[4]).t() + f(biases[4]))
     y32 = u32.half().float() @ f(dws[5]).t() + f(biases[5]) + o32.half().float()
@@ -390,18 +419,18 @@ def block_main(args):
         qd, kd, vd, od, yd = (torch.empty_like(t) for t in (q, k, v, o, y))
         ud = torch.empty_like(u)
 
-        def dense_step(wsd):
+        def dense_step(wsd, layer=0):
             torch.addmm(biases[0], X, wsd[0].t(), out=qd)
             torch.addmm(biases[1], X, wsd[1].t(), out=kd)
             torch.addmm(biases[2], X, wsd[2].t(), out=vd)
-            torch.addmm(biases[3], qd, wsd[3].t(), out=od)
+            torch.addmm(biases[3], attended(qd, kd, vd, layer), wsd[3].t(), out=od)
             od.add_(X)
             torch.addmm(biases[4], od, wsd[4].t(), out=ud)
             ud.relu_()
             torch.addmm(biases[5], ud, wsd[5].t(), out=yd)
             yd.add_(od)
 
-        dsteps = [lambda wsd=wsd: dense_step(wsd) for wsd in dsets]
+        dsteps = [lambda wsd=wsd, i=i: dense_step(wsd, i % copies) for i, wsd in enumerate(dsets)]
         ms_dense = timed_steps(torch, dsteps, args.steps, args.warmup, args.mode)
         dense = {"ms_per_step": ms_dense, "copies": dcopies,
                  "library": "hipBLASLt via torch.addmm (bias) + separate add / relu kernels, default heuristic"}
@@ -409,6 +438,8 @@ def block_main(args):
 
     flops = sum(2.0 * L.M * L.K * N for L in layers)
     alg_bytes = sbytes + sum(2 * L.K * N + 2 * L.M * N for L in layers) + sum(2 * L.M for L in layers)
+    flops += 4.0 * N * args.context * heads * dim
+    alg_bytes += 4 * N * args.context * kv_heads * dim
     achieved = alg_bytes / (ms_sparse * 1e-3) / 1e9
     out = {
         "metric": METRIC,
@@ -425,12 +456,13 @@ def block_main(args):
         "data": "synthetic",
         "config": {"workload": f"{args.workload}: decode step of one decoder block, {len(layers)} linear layers "
                                f"({', '.join(f'{L.name} {L.M}x{L.K}' for L in layers)}), {sp}% per-row "
-                               f"magnitude pruning, N={N}, fused bias / ReLU / residual epilogues",
-                   "N": N, "sparsity_pct": sp, "hidden": H},
+                               f"magnitude pruning, N={N}, fused bias / ReLU / residual epilogues"
+                               + (f", attention over {args.context} cached tokens a sequence" if args.context else ""),
+                   "N": N, "sparsity_pct": sp, "hidden": H, "context": args.context},
         "roofline": {"bound": "hbm", "achieved": achieved, "peak": HBM_PEAK_GBS, "unit": "GB/s",
                      "frac": achieved / HBM_PEAK_GBS, "traffic": None},
         "us_per_block": ms_sparse * 1e3,
-        "launches_per_block": len(layers),
+        "launches_per_block": len(layers) + (2 if args.context else 0),
         "compressed_bytes": sbytes,
         "encode_seconds": encode_s,
         "check_rel_frobenius_vs_fp32_dense": check,

@@ -475,8 +475,9 @@ typedef struct {
     float cap;              /* >= 0, finite; 0: none */
 } usp_attention_args;
 
-/* usp_attention_workspace_size -- bytes of device workspace usp_attention needs for such a step (sequences, rows and
- * whether there are offsets are looked at; no pointer is read); 0 for an invalid description. */
+/* usp_attention_workspace_size -- bytes of device workspace usp_attention needs for such a step (sequences, rows,
+ * table_pages and whether there are offsets are looked at; no pointer is read); 0 when none, or for an invalid
+ * description. */
 size_t usp_attention_workspace_size(const usp_cache *cache, const usp_cache_rows *rows, int32_t heads);
 
 /* usp_attention_plan -- which kernel usp_attention runs for such a step, as usp_plan. */

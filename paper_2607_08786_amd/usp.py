@@ -7,6 +7,7 @@ There is no fallback: if the library is not built, loading it raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -592,7 +593,7 @@ class KVCache:
         self.layers, self.dtype, self.device = layers, dtype, device
         self.description = usp_cache(None, layers, pages, kv_heads, head_dim, page_tokens, dtype.itemsize, device)
         self.page_bytes = int(load_library().usp_cache_page_bytes(ctypes.byref(self.description)))
-        if not self.page_bytes:
+        if not self.page_bytes or max(kv_heads, head_dim, page_tokens) >= 2 ** 31:
             raise ValueError("kv_heads must be 1 to 4096, head_dim a multiple of 8 up to 256, page_tokens a multiple of 32 up "
                              f"to 4096: got {kv_heads}, {head_dim}, {page_tokens}")
         shape = (layers, pages, self.page_bytes)
@@ -711,8 +712,9 @@ def usp_cache_copy(cache: KVCache, src, dst, stream=None) -> None:
     n = len(src)
     if len(dst) != n:
         raise ValueError("src and dst must have the same number of pages")
-    pages = ctypes.c_int32 * n
-    _check((_lib or load_library()).usp_cache_copy(cache.description, pages(*src), pages(*dst), n, _stream_of(stream, cache.device)))
+    src, dst = array.array("i", src), array.array("i", dst)  # OverflowError beyond 32 bits, which ctypes would cut
+    _check((_lib or load_library()).usp_cache_copy(cache.description, src.buffer_info()[0], dst.buffer_info()[0], n,
+                                                   _stream_of(stream, cache.device)))
 
 
 def usp_attention_workspace_size(cache: KVCache, rows: CacheRows, T: int, heads: int) -> int:

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import attention64
-from paper_2607_08786_amd import attention, usp
+from paper_2607_08786_amd import attention, linear, usp
 
 pytestmark = pytest.mark.gpu
 
@@ -446,6 +446,69 @@ def test_module():
     assert empty.shape == (0, heads, D)
 
 
+@pytest.mark.parametrize("values", [torch.float16, torch.int8])
+def test_decoder_block_step(values):
+    """A block's attention half as a program runs it, captured: norm, the pruned projections, keys and values into the cache,
+    attention, the output projection; every replay against the eager step, the cache growing between them."""
+    heads, kv, D, S = 8, 2, 64, 3
+    H = heads * D
+    g = torch.Generator().manual_seed(5)
+    layer = lambda out, into: linear.SparseLinear(torch.randn(out, into, generator=g) * 0.05, torch.rand(out, into, generator=g) < 0.5)  # noqa: E731
+    norm, qkv, o = linear.BlockNorm(H), layer(H + 2 * kv * D, H), layer(H, H)
+    attend = attention.PagedAttention(heads, kv, D, window=900)
+    cache = attention.PagedCache(80, kv, D, page_tokens=32, dtype=values)
+    ids = [cache.add() for _ in range(S)]
+    prompt = [700, 33, 300]
+    cache.append(cache.extend(ids, prompt), draw(1, sum(prompt), kv, D).cuda(), draw(2, sum(prompt), kv, D).cuda())
+    x = draw(3, S, H).cuda()
+    tables = torch.zeros(S, 40, dtype=torch.int32, device="cuda")
+    rows = usp.CacheRows(tables, torch.zeros(S, dtype=torch.int32, device="cuda"))
+
+    def step():
+        r, h = norm(x)
+        p = qkv(h)
+        return o(attend(p[:, :H], cache, rows, p[:, H:H + kv * D], p[:, H + kv * D:]), r)
+
+    cache.extend(ids)
+    cache.update(rows, ids)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = step()
+    for i in range(5):
+        x.copy_(draw(10 + i, S, H))
+        cache.extend(ids)
+        cache.update(rows, ids)
+        want = step().clone()
+        kept = cache.data.clone()
+        y.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(cache.data, kept) and torch.isfinite(y).all()
+
+
+def test_capture_without_warm_up():
+    """The workspace is then the graph's own, cleared in it."""
+    s = Setting([6000], 2, 64, 64, seed=2).fill()
+    rows, q = s.rows(), draw(3, 1, 8, 64).cuda()
+    mod = attention.PagedAttention(8, 2, 64)
+    want = attention.PagedAttention(8, 2, 64)(q, s.cache, rows)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = mod(q, s.cache, rows)
+    for i in range(4):
+        got.zero_()
+        graph.replay()
+        again = mod(q, s.cache, rows)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(again, want)
+
+
 def test_workspace_shared_with_products():
     """One zero-filled workspace for a sparse product and an attention in pieces, in turn."""
     g = torch.Generator().manual_seed(1)
@@ -490,3 +553,5 @@ def test_binding_refusals():
             s.cache.copy(src, dst)
     with pytest.raises(ValueError):
         s.cache.copy([0], [1, 2])
+    with pytest.raises(OverflowError):
+        s.cache.copy([2 ** 32], [1])

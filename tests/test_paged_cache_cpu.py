@@ -77,7 +77,8 @@ def test_more_refusals():
     assert lib.usp_cache_copy(c, None, None, 0, None) == 0
     buf = ctypes.create_string_buffer(64)
     err(lib.usp_attention_plan(c, r, 7, buf, 64), "multiple")
-    assert lib.usp_attention_plan(c, r, 8, buf, 64) == 0 and buf.value.startswith(b"rows")
+    assert lib.usp_attention_plan(c, r, 16, buf, 64) == 0 and buf.value.startswith(b"rows")
+    assert lib.usp_attention_plan(c, r, 8, buf, 64) == 0 and buf.value.startswith(b"tiles")
     r.rows = 0  # nothing to do, whatever else
     assert lib.usp_attention(c, r, a, None, 0, None) == 0 and lib.usp_attention_workspace_size(c, r, 8) == 0
     assert lib.usp_cache_append(c, r, 0, None, 0, 0, None, 0, 0, None) == 0

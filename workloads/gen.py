@@ -279,15 +279,15 @@ def make_small_int(M: int, K: int, N: int, density: float, seed: int, lo: int = 
 # Decoder blocks of the synthetic decode-step benchmark: one block's linear
 # layers in execution order, (name, out, in, epilogue), with 13B shapes (hidden
 # 5120, FFN 13824) and 70B-like shapes (hidden 8192, grouped K/V projections of
-# 1024, FFN 28672); the FFN's first layer carries the activation, the output
+# 1024, FFN 28672) and the heads of the attention between q, k, v and o; the FFN's first layer carries the activation, the output
 # projection and the FFN's last layer a residual add. Weights as the workload
 # set draws them, pruned per row to the given sparsity by magnitude.
 BLOCKS = {
-    "block13b": dict(cfg_id=70, hidden=5120, dist="normal", scale=0.02,
+    "block13b": dict(cfg_id=70, hidden=5120, dist="normal", scale=0.02, heads=40, kv_heads=40, head_dim=128,
                      layers=[("q", 5120, 5120, "bias"), ("k", 5120, 5120, "bias"), ("v", 5120, 5120, "bias"),
                              ("o", 5120, 5120, "bias+residual"), ("up", 13824, 5120, "bias+relu"),
                              ("down", 5120, 13824, "bias+residual")]),
-    "block70b": dict(cfg_id=80, hidden=8192, dist="student_t4", scale=0.02,
+    "block70b": dict(cfg_id=80, hidden=8192, dist="student_t4", scale=0.02, heads=64, kv_heads=8, head_dim=128,
                      layers=[("q", 8192, 8192, "bias"), ("k", 1024, 8192, "bias"), ("v", 1024, 8192, "bias"),
                              ("o", 8192, 8192, "bias+residual"), ("up", 28672, 8192, "bias+relu"),
                              ("down", 8192, 28672, "bias+residual")]),
