@@ -1,5 +1,22 @@
 // usp_attention_tiles.hip -- attention of many rows of each sequence (prompts and pieces of
 // prompts): tiles of columns of consecutive rows and the heads that a cache's head serves.
+//
+// A workgroup of four wavefronts has 128 columns, 32 each; a block of keys and values goes through
+// LDS once for all of them, double buffered, by transfers straight into LDS (fp16), where its
+// units already lie in operand order. Products are v_mfma_f32_32x32x16_f16.
+//
+// What bounds it: one prompt of 4096 tokens, 64 heads on 8 of 128 channels, takes 311 us, 885 TFLOP/s;
+// an 8192^3 library product reaches 1157 on the same card, a 16384^3 one 1310. A wavefront's step over a
+// block is 16 products (512 cycles of the matrix unit) and about 135 vector instructions, 16 of them
+// exponentials (600 cycles), of which half overlap at best: a matrix and eight vector instructions took 19.6 ns
+// a step where the one alone takes 14.6 and the others 11.3. And the clock falls under this load, from
+// 2.3 to 1.9 GHz. Steps on the way: a plain loop 779 us; blocks requested ahead and operands read together 348; straight
+// into LDS, operands four products ahead, three wavefronts a SIMD 311. Without gain: priorities of
+// wavefronts, 2 or 6 products ahead. Slower: softmax of a block between the products of its neighbours (369,
+// two wavefronts a SIMD), two tiles of columns a wavefront (556, one a SIMD).
+//
+// 8 bits: 512 rows over 16512 tokens, the same heads, 442 us, 617 TFLOP/s: codes go raw into LDS and are converted
+// there once for the four wavefronts, two wavefronts a SIMD for want of registers.
 #include "usp_attention.h"
 
 #include <utility>
@@ -32,11 +49,11 @@ __device__ inline half8 values_of(v2u32 codes, floatx4 s0, floatx4 s1) {
     return out;
 }
 
-// Columns of a wavefront: CT tiles of 32. MOD: scores are capped, biased or not scaled by a positive number.
-template <int DS, int VB, bool MOD, int CT>
+// A wavefront has 32 of the tile's columns. MOD: scores are capped, biased or not scaled by a positive number.
+template <int DS, int VB, bool MOD>
 __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) void attend_tiles_kernel(AttendArgs a) {
     constexpr int W = 32 * DS, kBlockBytes = (int)cache_block_bytes(W, VB);
-    constexpr int kColumns = 32 * CT * kTileWaves;
+    constexpr int kColumns = 32 * kTileWaves;
     constexpr int kKeyUnits = W / 8 * kBlockTokens;  // units of 8 keys' channels, and as many of values'
     constexpr int kThreads = kTileWaves * kLanes;
     __shared__ half8 staged[2][2 * kKeyUnits];  // blocks of keys, then of values, as in the cache
@@ -67,30 +84,22 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
     if (column0 < 0 || column0 >= (int64_t)n * a.group) return;
 
     const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes, c = lane & 31, half = lane >> 5;
-    int row[CT], head[CT], p[CT], lo[CT], hi[CT];
-    bool there[CT];
-    float slope[CT];
-    // The keys that the wavefront sees any of, and those that all of its columns see.
-    int any_lo = 0x7FFFFFFF, any_hi = 0, all_lo = 0, all_hi = 0x7FFFFFFF;
-#pragma unroll
-    for (int t = 0; t < CT; ++t) {
-        const int64_t column = column0 + 32 * (wave * CT + t) + c;
-        row[t] = (int)(column / a.group);
-        head[t] = h * a.group + (int)(column - (int64_t)row[t] * a.group);
-        there[t] = row[t] < n;
-        p[t] = len - n + row[t];
-        lo[t] = hi[t] = 0;
-        if (there[t]) {
-            span_of(a, off + row[t], p[t], len, lo[t], hi[t]);
-            if (hi[t] > lo[t]) {
-                any_lo = min(any_lo, lo[t]);
-                any_hi = max(any_hi, hi[t]);
-            }
-            all_lo = max(all_lo, lo[t]);
-            all_hi = min(all_hi, hi[t]);
+    const int64_t column = column0 + 32 * wave + c;
+    const int row = (int)(column / a.group), head = h * a.group + (int)(column - (int64_t)row * a.group);
+    const bool there = row < n;
+    const int p = len - n + row;
+    // The keys that this column sees, that the wavefront's see any of, and that all of them see.
+    int lo = 0, hi = 0, any_lo = 0x7FFFFFFF, any_hi = 0, all_lo = 0, all_hi = 0x7FFFFFFF;
+    if (there) {
+        span_of(a, off + row, p, len, lo, hi);
+        if (hi > lo) {
+            any_lo = min(any_lo, lo);
+            any_hi = max(any_hi, hi);
         }
-        slope[t] = MOD && a.slopes && there[t] ? a.slopes[head[t]] * kLog2e : 0.f;
+        all_lo = lo;
+        all_hi = hi;
     }
+    const float slope = MOD && a.slopes && there ? a.slopes[head] * kLog2e : 0.f;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
         any_lo = min(any_lo, __shfl_xor(any_lo, d, kLanes));
@@ -133,23 +142,16 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
         b1 = min(b1, b0 + each);
     }
 
-    half8 q[CT][2 * DS];
+    half8 q[2 * DS];
 #pragma unroll
-    for (int t = 0; t < CT; ++t)
-#pragma unroll
-        for (int i = 0; i < 2 * DS; ++i) q[t][i] = load_q8(a, off + row[t], head[t], 16 * i + 8 * half, there[t]);
+    for (int i = 0; i < 2 * DS; ++i) q[i] = load_q8(a, off + row, head, 16 * i + 8 * half, there);
 
-    floatx16 o[CT][DS];
-    float m[CT], l[CT];
+    floatx16 o[DS];
 #pragma unroll
-    for (int t = 0; t < CT; ++t) {
+    for (int d = 0; d < DS; ++d)
 #pragma unroll
-        for (int d = 0; d < DS; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[t][d][i] = 0.f;
-        m[t] = kNothing;
-        l[t] = 0.f;
-    }
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    float m = kNothing, l = 0.f;
     // Plain scores are scaled in the exponential's argument, others before.
     const float scale = MOD || VB == 1 ? 1.f : a.scale;
 
@@ -258,7 +260,7 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
         lds_barrier();
     }
     for (int buffer = 0; b < b1; buffer ^= 1) {
-        // fp16: the next block is requested; 8 bits: the one behind it, and the next converted.
+        // fp16: the next block is requested. 8 bits: the one behind it, and the next is converted.
         const uint8_t *next_block = block;
         int b_after = b1;
         if (VB == 2) {
@@ -280,11 +282,9 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
             half8 k[kProducts], v[kProducts];
 #pragma unroll
             for (int i = 0; i < ahead; ++i) k[i] = keys[(2 * i + half) * kBlockTokens + c];
-            floatx16 st[CT];
+            floatx16 st;
 #pragma unroll
-            for (int t = 0; t < CT; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st[t][i] = 0.f;
+            for (int i = 0; i < 16; ++i) st[i] = 0.f;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < kProducts; ++i) {
@@ -294,90 +294,83 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
                     const int j = i + ahead - kProducts;
                     v[j] = values[(2 * (j % 2) + half) * W + 32 * (j / 2) + c];
                 }
-#pragma unroll
-                for (int t = 0; t < CT; ++t) st[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[i], q[t][i], st[t], 0, 0, 0);
+                st = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[i], q[i], st, 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            half8 w[CT][2];
+            half8 w[2];
+            // Register 8 u + j holds the score of key block_lo + 16 u + 8 half + j.
+            half8 log_factor[2], less_one[2];
+            if (VB == 1) {
 #pragma unroll
-            for (int t = 0; t < CT; ++t) {
-                // Register 8 u + j holds the score of key block_lo + 16 u + 8 half + j.
-                half8 log_factor[2], less_one[2];
-                if (VB == 1) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        log_factor[u] = factors[buffer][0][VB == 1 ? 2 * u + half : 0];
-                        less_one[u] = factors[buffer][1][VB == 1 ? 2 * u + half : 0];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float by = key_scales[buffer][VB == 1 ? 4 * (i / 8) + 2 * half + i % 8 / 4 : 0][i % 4];
-                        st[t][i] = fmaf(st[t][i], by, MOD ? 0.f : (float)log_factor[i / 8][i % 8]);
-                    }
+                for (int u = 0; u < 2; ++u) {
+                    log_factor[u] = factors[buffer][0][VB == 1 ? 2 * u + half : 0];
+                    less_one[u] = factors[buffer][1][VB == 1 ? 2 * u + half : 0];
                 }
-                if (MOD) modify_scores(a, st[t], 16, slope[t], p[t], block_lo + 8 * half, [](int i) { return 16 * (i / 8) + i % 8; });
-                if (MOD && VB == 1) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) st[t][i] += (float)log_factor[i / 8][i % 8];
+                for (int i = 0; i < 16; ++i) {
+                    const float by = key_scales[buffer][VB == 1 ? 4 * (i / 8) + 2 * half + i % 8 / 4 : 0][i % 4];
+                    st[i] = fmaf(st[i], by, MOD ? 0.f : (float)log_factor[i / 8][i % 8]);
                 }
-                if (!whole) {
+            }
+            if (MOD) modify_scores(a, st, 16, slope, p, block_lo + 8 * half, [](int i) { return 16 * (i / 8) + i % 8; });
+            if (MOD && VB == 1) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int key = block_lo + 16 * (i / 8) + 8 * half + i % 8;
-                        st[t][i] = key >= lo[t] && key < hi[t] ? st[t][i] : kNothing;
-                    }
+                for (int i = 0; i < 16; ++i) st[i] += (float)log_factor[i / 8][i % 8];
+            }
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = block_lo + 16 * (i / 8) + 8 * half + i % 8;
+                    st[i] = key >= lo && key < hi ? st[i] : kNothing;
                 }
-                float top = st[t][0];
+            }
+            float top = st[0];
 #pragma unroll
-                for (int i = 1; i < 16; ++i) top = fmaxf(top, st[t][i]);
-                top = fmaxf(m[t], max_32(top));
-                if (__any(top > m[t])) {
-                    const float fade = exp2_of((m[t] - (top == kNothing ? 0.f : top)) * scale);
-                    m[t] = top;
-                    l[t] *= fade;
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, st[i]);
+            top = fmaxf(m, max_32(top));
+            if (__any(top > m)) {
+                const float fade = exp2_of((m - (top == kNothing ? 0.f : top)) * scale);
+                m = top;
+                l *= fade;
 #pragma unroll
-                    for (int d = 0; d < DS; ++d) o[t][d] *= fade;
-                }
-                const float base = m[t] == kNothing ? 0.f : -m[t] * scale;
-                // The sum takes the weights as the product does.
+                for (int d = 0; d < DS; ++d) o[d] *= fade;
+            }
+            const float base = m == kNothing ? 0.f : -m * scale;
+            // The sum takes the weights as the product does.
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[t][i / 8][i % 8] = (_Float16)exp2_of(fmaf(st[t][i], scale, base));
+            for (int i = 0; i < 16; ++i) w[i / 8][i % 8] = (_Float16)exp2_of(fmaf(st[i], scale, base));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const half2a pair = {w[t][i / 4][2 * (i % 4)], w[t][i / 4][2 * (i % 4) + 1]};
-                    l[t] = __builtin_amdgcn_fdot2(pair, half2a{(_Float16)1.f, (_Float16)1.f}, l[t], false);
-                    if (VB == 1) l[t] = __builtin_amdgcn_fdot2(pair, half2a{less_one[i / 4][2 * (i % 4)], less_one[i / 4][2 * (i % 4) + 1]}, l[t], false);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const half2a pair = {w[i / 4][2 * (i % 4)], w[i / 4][2 * (i % 4) + 1]};
+                l = __builtin_amdgcn_fdot2(pair, half2a{(_Float16)1.f, (_Float16)1.f}, l, false);
+                if (VB == 1) l = __builtin_amdgcn_fdot2(pair, half2a{less_one[i / 4][2 * (i % 4)], less_one[i / 4][2 * (i % 4) + 1]}, l, false);
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < kProducts; ++i) {
                 const int j = i + ahead;
                 if (j < kProducts) v[j] = values[(2 * (j % 2) + half) * W + 32 * (j / 2) + c];
-#pragma unroll
-                for (int t = 0; t < CT; ++t) o[t][i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i], w[t][i % 2], o[t][i / 2], 0, 0, 0);
+                o[i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i], w[i % 2], o[i / 2], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (!all_see(b) && (odd[0] | odd[1] | odd[2] | odd[3])) {
                 // Rare, so straight from the cache.
 #pragma unroll 1
-                for (int j = 0; j < kBlockTokens; ++j)
+                for (int j = 0; j < kBlockTokens; ++j) {
+                    const bool sees = block_lo + j >= lo && block_lo + j < hi;
 #pragma unroll
-                    for (int t = 0; t < CT; ++t) {
-                        const bool sees = block_lo + j >= lo[t] && block_lo + j < hi[t];
+                    for (int d = 0; d < DS; ++d)
 #pragma unroll
-                        for (int d = 0; d < DS; ++d)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const int at = kKeyUnits * 8 + ((j / 8) * W + 32 * d + 8 * (i / 4) + 4 * half + i % 4) * 8 + j % 8;
-                                float x;
-                                if (VB == 2)
-                                    x = (float)reinterpret_cast<const _Float16 *>(here)[at];
-                                else
-                                    x = reinterpret_cast<const float *>(here + 2 * kBlockTokens * W)[kBlockTokens + j];
-                                if (sees && !(fabsf(x) < __builtin_inff())) o[t][d][i] += x;
-                            }
-                    }
+                        for (int i = 0; i < 16; ++i) {
+                            const int at = kKeyUnits * 8 + ((j / 8) * W + 32 * d + 8 * (i / 4) + 4 * half + i % 4) * 8 + j % 8;
+                            float x;
+                            if (VB == 2)
+                                x = (float)reinterpret_cast<const _Float16 *>(here)[at];
+                            else
+                                x = reinterpret_cast<const float *>(here + 2 * kBlockTokens * W)[kBlockTokens + j];
+                            if (sees && !(fabsf(x) < __builtin_inff())) o[d][i] += x;
+                        }
+                }
             }
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what was requested lies in LDS
@@ -387,11 +380,10 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
         if (VB == 1) b_next = b_after;
     }
 
-#pragma unroll
-    for (int t = 0; t < CT; ++t) l[t] = sum_32(l[t]);
+    l = sum_32(l);
     if (pieces > 1) {
         // A piece's result lies as the lanes hold it. The last piece to arrive joins them, in their order.
-        constexpr int kParts = CT * (DS * 4 + 1);  // of 16 bytes a lane
+        constexpr int kParts = DS * 4 + 1;  // of 16 bytes a lane
         constexpr int64_t kSlotFloats = (int64_t)kParts * 4 * kThreads;
         float *slot = a.partials + ((int64_t)tile * a.pieces * a.c.kv_heads + h) * kSlotFloats;
         const int64_t step = a.c.kv_heads * kSlotFloats;
@@ -399,15 +391,12 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
         {
             const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(slot + piece * step, (short)0, (int)(kSlotFloats * 4), kBufferRsrcWord3);
 #pragma unroll
-            for (int t = 0; t < CT; ++t) {
-#pragma unroll
-                for (int i = 0; i < DS * 4; ++i) {
-                    const floatx4 x = {o[t][i / 4][4 * (i % 4)], o[t][i / 4][4 * (i % 4) + 1], o[t][i / 4][4 * (i % 4) + 2], o[t][i / 4][4 * (i % 4) + 3]};
-                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, x), to, (t * (DS * 4 + 1) + i) * kThreads * 16 + at, 0, kCachePolicyDevice);
-                }
-                const floatx4 x = {m[t], l[t], 0.f, 0.f};
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, x), to, (t * (DS * 4 + 1) + DS * 4) * kThreads * 16 + at, 0, kCachePolicyDevice);
+            for (int i = 0; i < DS * 4; ++i) {
+                const floatx4 x = {o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, x), to, i * kThreads * 16 + at, 0, kCachePolicyDevice);
             }
+            const floatx4 x = {m, l, 0.f, 0.f};
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, x), to, DS * 4 * kThreads * 16 + at, 0, kCachePolicyDevice);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's part lies in memory
         __syncthreads();
@@ -415,71 +404,63 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
         if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         if (arrived != (uint32_t)pieces - 1) return;
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-            float top = kNothing;
-            for (int i = 0; i < pieces; ++i) {
-                const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(slot + i * step, (short)0, (int)(kSlotFloats * 4), kBufferRsrcWord3);
-                top = fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, (t * (DS * 4 + 1) + DS * 4) * kThreads * 16 + at, 0, kCachePolicyDevice)));
-            }
-            const float base = top == kNothing ? 0.f : top;
-            l[t] = 0.f;
-#pragma unroll
-            for (int d = 0; d < DS; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[t][d][i] = 0.f;
-            for (int i = 0; i < pieces; ++i) {
-                const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(slot + i * step, (short)0, (int)(kSlotFloats * 4), kBufferRsrcWord3);
-                v4u32 x[DS * 4 + 1];
-#pragma unroll
-                for (int j = 0; j < DS * 4 + 1; ++j)
-                    x[j] = __builtin_amdgcn_raw_buffer_load_b128(from, (t * (DS * 4 + 1) + j) * kThreads * 16 + at, 0, kCachePolicyDevice);
-                const floatx4 ml = __builtin_bit_cast(floatx4, x[DS * 4]);
-                const float f = exp2_of((ml[0] - base) * scale);
-                l[t] = fmaf(ml[1], f, l[t]);
-#pragma unroll
-                for (int j = 0; j < DS * 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[t][j / 4][4 * (j % 4) + e] = fmaf(__builtin_bit_cast(floatx4, x[j])[e], f, o[t][j / 4][4 * (j % 4) + e]);
-            }
+        float top = kNothing;
+        for (int i = 0; i < pieces; ++i) {
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(slot + i * step, (short)0, (int)(kSlotFloats * 4), kBufferRsrcWord3);
+            top = fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, DS * 4 * kThreads * 16 + at, 0, kCachePolicyDevice)));
         }
-        if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-#pragma unroll
-    for (int t = 0; t < CT; ++t) {
-        const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
-        if (!there[t]) continue;
+        const float base = top == kNothing ? 0.f : top;
+        l = 0.f;
 #pragma unroll
         for (int d = 0; d < DS; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int channel = 32 * d + 8 * i + 4 * half;
-                floatx4 v = {o[t][d][4 * i], o[t][d][4 * i + 1], o[t][d][4 * i + 2], o[t][d][4 * i + 3]};
-                v = l[t] == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : v * inv;
-                if (channel < a.c.head_dim) store_out4(a, off + row[t], head[t], channel, v);
-            }
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        for (int i = 0; i < pieces; ++i) {
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(slot + i * step, (short)0, (int)(kSlotFloats * 4), kBufferRsrcWord3);
+            v4u32 x[DS * 4 + 1];
+#pragma unroll
+            for (int j = 0; j < DS * 4 + 1; ++j)
+                x[j] = __builtin_amdgcn_raw_buffer_load_b128(from, j * kThreads * 16 + at, 0, kCachePolicyDevice);
+            const floatx4 ml = __builtin_bit_cast(floatx4, x[DS * 4]);
+            const float f = exp2_of((ml[0] - base) * scale);
+            l = fmaf(ml[1], f, l);
+#pragma unroll
+            for (int j = 0; j < DS * 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j / 4][4 * (j % 4) + e] = fmaf(__builtin_bit_cast(floatx4, x[j])[e], f, o[j / 4][4 * (j % 4) + e]);
+        }
+        if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (!there) return;
+#pragma unroll
+    for (int d = 0; d < DS; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int channel = 32 * d + 8 * i + 4 * half;
+            floatx4 v = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+            v = l == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : v * inv;
+            if (channel < a.c.head_dim) store_out4(a, off + row, head, channel, v);
+        }
 }
-
-constexpr int kTilesOfWave = 1;
 
 template <int VB, bool MOD>
 void (*tiles_kernel_of(int width))(AttendArgs) {
     switch (width) {
-        case 32: return attend_tiles_kernel<1, VB, MOD, kTilesOfWave>;
-        case 64: return attend_tiles_kernel<2, VB, MOD, kTilesOfWave>;
-        case 96: return attend_tiles_kernel<3, VB, MOD, kTilesOfWave>;
-        case 128: return attend_tiles_kernel<4, VB, MOD, kTilesOfWave>;
-        case 192: return attend_tiles_kernel<6, VB, MOD, kTilesOfWave>;
-        default: return attend_tiles_kernel<8, VB, MOD, kTilesOfWave>;
+        case 32: return attend_tiles_kernel<1, VB, MOD>;
+        case 64: return attend_tiles_kernel<2, VB, MOD>;
+        case 96: return attend_tiles_kernel<3, VB, MOD>;
+        case 128: return attend_tiles_kernel<4, VB, MOD>;
+        case 192: return attend_tiles_kernel<6, VB, MOD>;
+        default: return attend_tiles_kernel<8, VB, MOD>;
     }
 }
 
 }  // namespace
 
-int tile_columns(int) { return 32 * kTilesOfWave * kTileWaves; }
+int tile_columns(int) { return 32 * kTileWaves; }
 
-int64_t tile_slot_floats(int width) { return (int64_t)kTilesOfWave * (width / 8 + 1) * 4 * kTileWaves * kLanes; }
+int64_t tile_slot_floats(int width) { return (int64_t)(width / 8 + 1) * 4 * kTileWaves * kLanes; }
 
 int launch_tiles(const void *args, int width, int value_bytes, bool modified, int64_t grid, void *stream) {
     const AttendArgs &a = *reinterpret_cast<const AttendArgs *>(args);
