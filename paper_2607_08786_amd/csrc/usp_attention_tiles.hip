@@ -15,8 +15,9 @@
 // wavefronts, 2 or 6 products ahead. Slower: softmax of a block between the products of its neighbours (369,
 // two wavefronts a SIMD), two tiles of columns a wavefront (556, one a SIMD).
 //
-// 8 bits: 512 rows over 16512 tokens, the same heads, 442 us, 617 TFLOP/s: codes go raw into LDS and are converted
-// there once for the four wavefronts, two wavefronts a SIMD for want of registers.
+// 8 bits: 512 rows over 16512 tokens, the same heads, 422 us, 647 TFLOP/s: codes go raw into LDS and are converted
+// there once for the four wavefronts, two wavefronts a SIMD for want of registers. Scales of values taken apart, for
+// exact products with the codes, cost 50 us of it (374 without, at an error against 64 bits of 3.1e-4 instead of 2.4e-4).
 #include "usp_attention.h"
 
 #include <utility>
@@ -44,7 +45,7 @@ __device__ inline half8 values_of(v2u32 codes, floatx4 s0, floatx4 s1) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int8_t c = (int8_t)(codes[i / 4] >> (8 * (i % 4)));
-        out[i] = (_Float16)((float)c * short_scale(i < 4 ? s0[i % 4] : s1[i % 4]));
+        out[i] = (_Float16)((float)c * (i < 4 ? s0[i % 4] : s1[i % 4]));
     }
     return out;
 }
@@ -57,11 +58,12 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
     constexpr int kKeyUnits = W / 8 * kBlockTokens;  // units of 8 keys' channels, and as many of values'
     constexpr int kThreads = kTileWaves * kLanes;
     __shared__ half8 staged[2][2 * kKeyUnits];  // blocks of keys, then of values, as in the cache
-    // 8 bits, of each key: its scale (times that of the scores), and the factor f of its weight as a logarithm and as
-    // 1 / f - 1 (near 0 both: in fp16 they are off by less than 2^-15).
-    __shared__ floatx4 key_scales[2][VB == 1 ? kBlockTokens / 4 : 1];
-    __shared__ half8 factors[2][2][VB == 1 ? kBlockTokens / 8 : 1];
-    __shared__ v2u32 raw[2][VB == 1 ? kBlockBytes / 8 : 1];  // 8 bits: blocks as they lie in the cache
+    // 8 bits: blocks as they lie in the cache, and of the keys of four blocks their scales (times that of the scores), the
+    // short scales of their values, and the factors f of their weights as logarithms and as 1 / f - 1 (near 0 both: in
+    // fp16 they are off by less than 2^-15).
+    __shared__ v2u32 raw[3][VB == 1 ? kBlockBytes / 8 : 1];
+    __shared__ floatx4 key_scales[4][VB == 1 ? kBlockTokens / 4 : 1], value_scales[4][VB == 1 ? kBlockTokens / 4 : 1];
+    __shared__ half8 factors[4][2][VB == 1 ? kBlockTokens / 8 : 1];
     __shared__ int ends[4][kTileWaves];
     __shared__ int odd[kTileWaves];  // whether a wavefront's part of a block's values holds any that is not finite
     __shared__ uint32_t arrived;
@@ -193,28 +195,29 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
                              : "memory", "m0");
     };
     // 8 bits: codes as fp16, those of values times their short scales.
-    auto convert = [&](int buffer) {
-        const v2u32 *from = raw[VB == 1 ? buffer : 0];
+    auto convert = [&](int from, int slot, int buffer) {
+        const v2u32 *codes = raw[VB == 1 ? from : 0];
 #pragma unroll
         for (int i = 0; i < DS; ++i) {
             const int u = i * kThreads + (int)threadIdx.x;
             if ((i + 1) * kThreads <= kKeyUnits || u < kKeyUnits) {
-                staged[buffer][u] = halves_of(from[u]);
+                staged[buffer][u] = halves_of(codes[u]);
             } else {
-                const floatx4 *scales = reinterpret_cast<const floatx4 *>(from + 2 * kKeyUnits) + kBlockTokens / 4 + 2 * ((u - kKeyUnits) / W);
-                staged[buffer][u] = values_of(from[u], scales[0], scales[1]);
+                const floatx4 *scales = &value_scales[slot][VB == 1 ? 2 * ((u - kKeyUnits) / W) : 0];
+                staged[buffer][u] = values_of(codes[u], scales[0], scales[1]);
             }
         }
     };
     // What the scales of a block's 32 keys and values come to, one of each a lane.
-    auto put_scales = [&](int buffer) {
+    auto put_scales = [&](int from, int slot) {
         if (lane >= kBlockTokens) return;
-        const float *from = reinterpret_cast<const float *>(raw[VB == 1 ? buffer : 0] + 2 * kKeyUnits) + lane;
-        const float value = from[kBlockTokens], f = value * __builtin_amdgcn_rcpf(short_scale(value));
+        const float *scales = reinterpret_cast<const float *>(raw[VB == 1 ? from : 0] + 2 * kKeyUnits) + lane;
+        const float value = scales[kBlockTokens], brief = short_scale(value), f = value * __builtin_amdgcn_rcpf(brief);
         const _Float16 log = (_Float16)(fabsf(f - 1.f) < 0.5f ? __builtin_amdgcn_logf(f) : 0.f);  // of 0 and NaN: none
-        reinterpret_cast<float *>(key_scales[buffer])[lane] = from[0] * (MOD ? 1.f : a.scale);
-        reinterpret_cast<_Float16 *>(factors[buffer][0])[lane] = log;
-        reinterpret_cast<_Float16 *>(factors[buffer][1])[lane] = (_Float16)(exp2_of(-(float)log) - 1.f);
+        reinterpret_cast<float *>(key_scales[slot])[lane] = scales[0] * (MOD ? 1.f : a.scale);
+        reinterpret_cast<float *>(value_scales[slot])[lane] = brief;
+        reinterpret_cast<_Float16 *>(factors[slot][0])[lane] = log;
+        reinterpret_cast<_Float16 *>(factors[slot][1])[lane] = (_Float16)(exp2_of(-(float)log) - 1.f);
     };
     // Nothing times infinity is not nothing: in a block that some column does not see the whole of, values that are not
     // finite are left out of the product, and added to the columns that see them (below).
@@ -241,39 +244,39 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
     };
     auto all_see = [&](int b) { return tile_all_lo <= b * kBlockTokens && (b + 1) * kBlockTokens <= tile_all_hi; };
 
-    const uint8_t *here = nullptr, *block = nullptr;
-    int b = next(b0, here);
-    if (b < b1) request(here, 0);
-    block = here;
-    int b_next = b1;
-    if (VB == 1) {
-        b_next = next(b + 1, block);
-        if (b_next < b1) request(block, 1);
+    // Blocks under way: the one at work, and those after it, b1 where there is none. fp16: the next is requested while one is
+    // at work. 8 bits: of the three after it the first is converted, the second's scales are taken apart, the third requested.
+    constexpr int kUnderWay = VB == 1 ? 3 : 1;
+    int blocks[4];
+    const uint8_t *at[4] = {nullptr, nullptr, nullptr, nullptr};
+    blocks[0] = next(b0, at[0]);
+    if (blocks[0] < b1) request(at[0], 0);
+#pragma unroll
+    for (int i = 1; i < kUnderWay; ++i) {
+        at[i] = at[i - 1];
+        blocks[i] = next(blocks[i - 1] + 1, at[i]);
+        if (blocks[i] < b1) request(at[i], i);
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_only(0));  // of q too: else the loop waits for what it requests ahead
     __syncthreads();
     if (VB == 1) {
-        if (b < b1) {
-            convert(0);
-            if (wave == 0) put_scales(0);
-        }
+        if (wave < 2 && blocks[wave] < b1) put_scales(wave, wave);
+        lds_barrier();
+        if (blocks[0] < b1) convert(0, 0, 0);
         lds_barrier();
     }
-    for (int buffer = 0; b < b1; buffer ^= 1) {
-        // fp16: the next block is requested. 8 bits: the one behind it, and the next is converted.
-        const uint8_t *next_block = block;
-        int b_after = b1;
-        if (VB == 2) {
-            b_next = next(b + 1, next_block);
-            if (b_next < b1) request(next_block, buffer ^ 1);
-        } else {
-            b_after = next(b_next + 1, block);
-            if (b_after < b1) request(block, buffer);
-            if (b_next < b1) convert(buffer ^ 1);
-        }
+    int ring = 0;  // the first block's place among the raw ones
+    for (int step = 0; blocks[0] < b1; ++step) {
+        const int buffer = step & 1, slot = step & 3, b = blocks[0];
+        const uint8_t *here = at[0];
+        at[kUnderWay] = at[kUnderWay - 1];
+        blocks[kUnderWay] = next(blocks[kUnderWay - 1] + 1, at[kUnderWay]);
+        if (blocks[kUnderWay] < b1) request(at[kUnderWay], VB == 1 ? ring : buffer ^ 1);
+        const int second = ring == 2 ? 0 : ring + 1, third = second == 2 ? 0 : second + 1;
+        if (VB == 1 && blocks[1] < b1) convert(second, (slot + 1) & 3, buffer ^ 1);
         const int block_lo = b * kBlockTokens, block_hi = block_lo + kBlockTokens;
         if (!all_see(b)) clean(buffer);
-        if (VB == 1 && b_next < b1 && wave == (b_next & (kTileWaves - 1))) put_scales(buffer ^ 1);  // in turn
+        if (VB == 1 && blocks[VB == 1 ? 2 : 0] < b1 && wave == slot) put_scales(third, (slot + 2) & 3);  // in turn
         if (block_hi > any_lo && block_lo < any_hi) {  // else this wavefront sees nothing of it
             const half8 *keys = staged[buffer], *values = staged[buffer] + kKeyUnits;
             const bool whole = all_lo <= block_lo && block_hi <= all_hi;
@@ -303,12 +306,12 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
             if (VB == 1) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    log_factor[u] = factors[buffer][0][VB == 1 ? 2 * u + half : 0];
-                    less_one[u] = factors[buffer][1][VB == 1 ? 2 * u + half : 0];
+                    log_factor[u] = factors[slot][0][VB == 1 ? 2 * u + half : 0];
+                    less_one[u] = factors[slot][1][VB == 1 ? 2 * u + half : 0];
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float by = key_scales[buffer][VB == 1 ? 4 * (i / 8) + 2 * half + i % 8 / 4 : 0][i % 4];
+                    const float by = key_scales[slot][VB == 1 ? 4 * (i / 8) + 2 * half + i % 8 / 4 : 0][i % 4];
                     st[i] = fmaf(st[i], by, MOD ? 0.f : (float)log_factor[i / 8][i % 8]);
                 }
             }
@@ -375,9 +378,12 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what was requested lies in LDS
         lds_barrier();
-        b = b_next;
-        here = next_block;
-        if (VB == 1) b_next = b_after;
+#pragma unroll
+        for (int i = 0; i < kUnderWay; ++i) {
+            blocks[i] = blocks[i + 1];
+            at[i] = at[i + 1];
+        }
+        ring = second;
     }
 
     l = sum_32(l);
