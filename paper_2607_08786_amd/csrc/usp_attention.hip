@@ -437,7 +437,7 @@ struct AttendPlan {
 // and join would take as long as it (640 tiles of up to 32 blocks: 34.4 us whole, 43 in 1024 pieces).
 constexpr int kFewTiles = 128, kFewBits = 9, kFewMinBlocks = 8, kManyBits = 10, kManyMinBlocks = 32;
 // Workgroups of the tiles kernel that run at once, by the bytes of a value: three on a CU, two that convert 8 bits (512
-// rows over 16512 tokens, 256 tiles: 422 us in two pieces each; 438 against 493 in three a step before).
+// rows over 16512 tokens, 256 tiles: 426 us in two pieces each; a step before this one 438, and 493 in three).
 constexpr int64_t kTilePlaces[] = {0, 512, 768};
 constexpr int64_t kMostTilePieces = 16;
 

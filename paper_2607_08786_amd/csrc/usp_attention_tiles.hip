@@ -5,17 +5,17 @@
 // LDS once for all of them, double buffered, by transfers straight into LDS (fp16), where its
 // units already lie in operand order. Products are v_mfma_f32_32x32x16_f16.
 //
-// What bounds it: one prompt of 4096 tokens, 64 heads on 8 of 128 channels, takes 311 us, 885 TFLOP/s;
+// What bounds it: one prompt of 4096 tokens, 64 heads on 8 of 128 channels, takes 312 us, 882 TFLOP/s;
 // an 8192^3 library product reaches 1157 on the same card, a 16384^3 one 1310. A wavefront's step over a
 // block is 16 products (512 cycles of the matrix unit) and about 135 vector instructions, 16 of them
 // exponentials (600 cycles), of which half overlap at best: a matrix and eight vector instructions took 19.6 ns
 // a step where the one alone takes 14.6 and the others 11.3. And the clock falls under this load, from
-// 2.3 to 1.9 GHz. Steps on the way: a plain loop 779 us; blocks requested ahead and operands read together 348; straight
-// into LDS, operands four products ahead, three wavefronts a SIMD 311. Without gain: priorities of
+// 2.5 (a long cache's single token) to 1.9 GHz. Steps on the way: a plain loop 779 us; blocks requested ahead and operands read together 348; straight
+// into LDS, operands four products ahead, three wavefronts a SIMD 312. Without gain: priorities of
 // wavefronts, 2 or 6 products ahead. Slower: softmax of a block between the products of its neighbours (369,
 // two wavefronts a SIMD), two tiles of columns a wavefront (556, one a SIMD).
 //
-// 8 bits: 512 rows over 16512 tokens, the same heads, 422 us, 647 TFLOP/s: codes go raw into LDS and are converted
+// 8 bits: 512 rows over 16512 tokens, the same heads, 426 us, 640 TFLOP/s: codes go raw into LDS and are converted
 // there once for the four wavefronts, two wavefronts a SIMD for want of registers. Scales of values taken apart, for
 // exact products with the codes, cost 50 us of it (374 without, at an error against 64 bits of 3.1e-4 instead of 2.4e-4).
 #include "usp_attention.h"
