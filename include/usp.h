@@ -471,7 +471,7 @@ typedef struct {
     int64_t layer;
     int64_t window;         /* >= 0 */
     int32_t heads;          /* a multiple of kv_heads, up to 65536 */
-    float scale;            /* finite */
+    float scale;            /* finite, |scale| at most 2^127 */
     float cap;              /* >= 0, finite; 0: none */
 } usp_attention_args;
 

@@ -759,7 +759,7 @@ usp_status usp_attention(const usp_cache *cache, const usp_cache_rows *rows, con
     const usp_attention_args &p = *args;
     if (const char *why = wrong_heads(*cache, p.heads)) return usp::fail(USP_ERR_INVALID_ARG, f + why);
     if (p.layer < 0 || p.layer >= cache->layers) return usp::fail(USP_ERR_INVALID_ARG, f + ": no such layer");
-    if (!std::isfinite(p.scale)) return usp::fail(USP_ERR_INVALID_ARG, f + ": scale must be finite");
+    if (!(std::fabs(p.scale) <= 0x1p127f)) return usp::fail(USP_ERR_INVALID_ARG, f + ": scale must be finite, of at most 2^127");
     if (!std::isfinite(p.cap) || p.cap < 0.f) return usp::fail(USP_ERR_INVALID_ARG, f + ": cap must be >= 0 and finite");
     if (p.cap > 0.f && !std::isfinite(2.f * p.scale / p.cap * 2.f))
         return usp::fail(USP_ERR_INVALID_ARG, f + ": scale / cap is not finite");

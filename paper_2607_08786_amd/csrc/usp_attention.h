@@ -36,6 +36,7 @@ struct AttendArgs {
     int64_t ld_q, head_q, ld_out, head_out;
     float scale;           // score of q . K in the exponent of 2, or the argument of the cap's exponential
     float cap;             // in the exponent of 2; 0: none
+    float cap_inv;         // of a large cap 1 / cap (scale is then the score's), else 0
     int heads, group, window;
     int tiles;             // tiles of 16 heads of a row (rows kernel)
     int q_vec, out_vec;
@@ -126,7 +127,17 @@ template <class Scores, class Key>
 __device__ inline void modify_scores(const AttendArgs &a, Scores &x, int n, float slope, int p, int key0, Key key) {
 #pragma unroll
     for (int i = 0; i < n; ++i) x[i] *= a.scale;
-    if (a.cap > 0.f) {  // cap tanh(y) is cap (1 - 2 / (1 + exp(2 y))); x is 2 y in the exponent of 2
+    if (a.cap_inv > 0.f) {
+        // The form below is off by some 2^-22 of the cap, however small the score. Here x is the score, y = x / cap, and
+        // tanh(y) for |y| < 1 / 8 the series to y^7, off by 2^-29 of itself.
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float y = x[i] * a.cap_inv, z = y * y;
+            const float series = fmaf(x[i] * z, fmaf(z, fmaf(z, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), x[i]);
+            const float whole = fmaf(-2.f * a.cap, __builtin_amdgcn_rcpf(1.f + exp2_of(2.f * kLog2e * y)), a.cap);
+            x[i] = fabsf(y) < 0.125f ? series : whole;
+        }
+    } else if (a.cap > 0.f) {  // cap tanh(y) is cap (1 - 2 / (1 + exp(2 y))); x is 2 y in the exponent of 2
 #pragma unroll
         for (int i = 0; i < n; ++i) x[i] = fmaf(-2.f * a.cap, __builtin_amdgcn_rcpf(1.f + exp2_of(x[i])), a.cap);
     }

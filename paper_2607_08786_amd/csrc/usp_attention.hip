@@ -440,6 +440,8 @@ constexpr int kFewTiles = 128, kFewBits = 9, kFewMinBlocks = 8, kManyBits = 10, 
 // rows over 16512 tokens, 256 tiles: 426 us in two pieces each; a step before this one 438, and 493 in three).
 constexpr int64_t kTilePlaces[] = {0, 512, 768};
 constexpr int64_t kMostTilePieces = 16;
+// The largest cap whose scores may be off by 2^-22 of it: 2^-14, a quarter of a weight's rounding to fp16.
+constexpr float kPlainCap = 256.f;
 
 AttendPlan plan_attention(const CacheView &c, const RowsView &r, int heads) {
     const int64_t group = heads / c.kv_heads;
@@ -507,8 +509,9 @@ int launch_attention(const CacheView &c, const RowsView &r, const usp_attention_
     a.head_q = p.head_q;
     a.ld_out = p.ld_out;
     a.head_out = p.head_out;
-    a.scale = p.cap > 0.f ? 2.f * kLog2e * p.scale / p.cap : p.scale * kLog2e;
-    a.cap = p.cap * kLog2e;
+    a.cap = std::min(p.cap, 1e38f) * kLog2e;  // twice it is finite
+    a.cap_inv = p.cap > kPlainCap ? 1.f / a.cap : 0.f;
+    a.scale = p.cap > 0.f && !a.cap_inv ? 2.f * kLog2e * p.scale / p.cap : p.scale * kLog2e;
     a.heads = p.heads;
     a.group = p.heads / c.kv_heads;
     a.window = p.window < r.capacity ? (int)p.window : 0;  // a longer one hides nothing

@@ -10,7 +10,9 @@ out = sum_k w_k V_k / sum_k w_k. With p_k = w_k / sum w and A = sum_k p_k |V_k| 
 * an error e of the scores, which moves p_k by p_k (e_k - sum p e), so at most 2 e A;
 * fp32 sums over n keys and the rescaling of what was summed: fewer than 4 (n + 40) roundings of A.
 e in roundings U = 2^-24: 2 (D + 40) of sum_d |q_d K_d| scale (products and their sum, twice over for what the matrix unit
-drops), 16 of the largest score, cap and bias each (scaling, cap, bias, subtraction of the maximum, exponential)."""
+drops), 16 of the largest score, cap and bias each (scaling, cap, bias, subtraction of the maximum, exponential). A cap
+counts as at most 512 or 32 times the largest score: cap tanh(y) for |y| < 1 / 8 has a series, with an error relative to the
+score itself, and elsewhere the cap is less than 9 times the score."""
 import numpy as np
 import torch
 
@@ -66,12 +68,13 @@ def attend(q, K, V, scale=None, cap=0.0, slopes=None, first=None, last=None, win
             if not len(at):
                 continue
             z, vv = s[i, at], v[at]
+            most = min(cap, max(512.0, 32 * float(z.abs().nan_to_num(0, 0).max())))
             top = z.max()
             w = torch.exp(z - (top if torch.isfinite(top) else 0))
             w = w / w.sum()
             out[i, h] = w @ vv
             A = w @ vv.abs()
-            e = U * (2 * (D + 40) * size[i, at].max() + 16 * (z.abs().max() + cap + bias[i, at].abs().max()))
+            e = U * (2 * (D + 40) * size[i, at].max() + 16 * (z.abs().max() + most + bias[i, at].abs().max()))
             subnormal = 2.0 ** -25 * vv.abs().sum(0) * w.max()
             tol[i, h] = (2.0 ** -25 + 2.0 ** -11 * out[i, h].abs() + (2.0 ** -11 + 2.0 ** -14) * (A + out[i, h].abs()) + subnormal +
                          2 * e * A + 4 * (len(at) + 40) * U * A)

@@ -117,6 +117,20 @@ def test_many_rows(heads, kv, D, page, lengths, counts, mods, values):
 
 
 @pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("n", [1, 70])
+def test_large_caps(n, values):
+    """A cap far above the scores changes them by less than their rounding, however large it is; one among them bends them."""
+    s = Setting([200], 2, 64, 32, values, seed=21).fill()
+    rows, counts = s.rows([n]), [n]
+    for size in (2.0, 200.0):
+        q = draw(22, n, 4, 64, scale=size)
+        for cap in (255.0, 257.0, 1e4, 1e6, 1e30, 3.4e38):
+            attention64.close(s.cache.attention(rows, q.cuda(), cap=cap), *s.want(q, counts, cap=cap))
+    q = draw(23, n, 4, 64)
+    attention64.close(s.cache.attention(rows, q.cuda(), cap=600.0, scale=300.0), *s.want(q, counts, cap=600.0, scale=300.0))
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
 @pytest.mark.parametrize("counts", [[1, 3, 0, 2], [60, 40, 0, 33]])
 def test_masks(counts, values):
     """Documents, prefixes, and rows that nothing is left of, through both kernels; NaN and infinities where a row does not look."""

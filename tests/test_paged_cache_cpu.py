@@ -33,7 +33,7 @@ def described(**change):
     (dict(r_table_pages=2 ** 26), "table_pages"), (dict(r_ld_table=2), "ld_table"), (dict(r_sequences=0), "sequences"),
     (dict(r_sequences=2 ** 20 + 1), "sequences"), (dict(r_rows=-1), "rows must"), (dict(r_rows=2 ** 20 + 1), "rows must"),
     (dict(r_offsets=None), "one row for each"), (dict(a_heads=6), "multiple"), (dict(a_heads=0), "multiple"), (dict(a_heads=65540), "multiple"),
-    (dict(a_layer=2), "layer"), (dict(a_layer=-1), "layer"), (dict(a_scale=float("nan")), "scale"), (dict(a_cap=float("inf")), "cap"),
+    (dict(a_layer=2), "layer"), (dict(a_layer=-1), "layer"), (dict(a_scale=float("nan")), "scale"), (dict(a_scale=2.0 ** 127.5), "scale"), (dict(a_cap=float("inf")), "cap"),
     (dict(a_cap=-1.0), "cap"), (dict(a_cap=1e-45), "scale / cap"), (dict(a_window=-1), "window"), (dict(a_q=None), "null q"),
     (dict(a_out=None), "null q"), (dict(a_q=1), "2-byte"), (dict(a_first=2), "4-byte"), (dict(a_slopes=2), "4-byte"),
     (dict(a_ld_q=-1), "strides"), (dict(a_ld_out=63), "apart"), (dict(a_head_out=32), "apart"), (dict(a_ld_out=7 * 64), "apart"),
