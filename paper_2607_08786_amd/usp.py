@@ -544,9 +544,13 @@ class CacheRows:
 
     table: int32 [sequences, pages], the pages of each sequence; lengths: int32 [sequences], its tokens in the cache, the
     step's included; offsets: int32 [sequences + 1], where each sequence's rows start, or None for one row each. All on one
-    GPU, read there when a call runs (or a captured one is replayed); the object keeps the tensors alive."""
+    GPU, read there when a call runs (or a captured one is replayed): write into them for another step. The object keeps
+    them alive, and stays with them."""
 
-    __slots__ = ("table", "lengths", "offsets", "device", "_structs")
+    __slots__ = ("_table", "_lengths", "_offsets", "device", "_structs")
+    table = property(lambda self: self._table)
+    lengths = property(lambda self: self._lengths)
+    offsets = property(lambda self: self._offsets)
 
     def __init__(self, table: torch.Tensor, lengths: torch.Tensor, offsets: torch.Tensor | None = None):
         dev = _gpu(table, "table")
@@ -554,18 +558,18 @@ class CacheRows:
         S = table.shape[0]
         _vector(lengths, torch.int32, S, dev, "lengths")
         _vector(offsets, torch.int32, S + 1, dev, "offsets")
-        self.table, self.lengths, self.offsets, self.device = table, lengths, offsets, dev
+        self._table, self._lengths, self._offsets, self.device = table, lengths, offsets, dev
         self._structs: dict[int, usp_cache_rows] = {}  # rows of a call -> the C description
 
     def struct(self, T: int) -> usp_cache_rows:
         """The C description for a call of T rows."""
         got = self._structs.get(T)
         if got is None:
-            S, pages = self.table.shape
-            if self.offsets is None and T != S:
+            S, pages = self._table.shape
+            if self._offsets is None and T != S:
                 raise ValueError(f"without offsets there is one row for each of the {S} sequences, got {T}")
-            got = usp_cache_rows(self.table.data_ptr(), self.table.stride(0) if S > 1 else pages, pages, self.lengths.data_ptr(),
-                                 None if self.offsets is None else self.offsets.data_ptr(), S, T)
+            got = usp_cache_rows(self._table.data_ptr(), self._table.stride(0) if S > 1 else pages, pages, self._lengths.data_ptr(),
+                                 None if self._offsets is None else self._offsets.data_ptr(), S, T)
             if len(self._structs) > 64:
                 self._structs.clear()
             self._structs[T] = got
@@ -601,9 +605,11 @@ class KVCache:
             data = torch.empty(shape, dtype=torch.uint8, device=f"cuda:{device}")
         elif data.dtype is not torch.uint8 or data.shape != shape or not data.is_contiguous():
             raise ValueError(f"data must be a contiguous uint8 tensor {shape}")
-        self.data = data
+        self._data = data
         self.description.data = data.data_ptr()
         self._blocks = None
+
+    data = property(lambda self: self._data)
 
     def workspace_size(self, rows: CacheRows, T: int, heads: int) -> int:
         return usp_attention_workspace_size(self, rows, T, heads)

@@ -130,6 +130,17 @@ def test_large_caps(n, values):
     attention64.close(s.cache.attention(rows, q.cuda(), cap=600.0, scale=300.0), *s.want(q, counts, cap=600.0, scale=300.0))
 
 
+def test_tensors_are_not_exchanged():
+    """The C descriptions name the tensors that an object was made of."""
+    s = Setting([40], 1, 64, 32)
+    rows = s.rows()
+    for name in ("table", "lengths", "offsets"):
+        with pytest.raises(AttributeError):
+            setattr(rows, name, getattr(rows, name))
+    with pytest.raises(AttributeError):
+        s.cache.data = s.cache.data
+
+
 @pytest.mark.parametrize("values", ["f16", "q"])
 @pytest.mark.parametrize("counts", [[1, 3, 0, 2], [60, 40, 0, 33]])
 def test_masks(counts, values):

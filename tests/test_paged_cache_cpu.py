@@ -110,7 +110,7 @@ class Host(attention.PagedCache):
     """A PagedCache without a GPU: tokens are numbers in a list of pages, copies are made there."""
 
     def __init__(self, pages, page_tokens):
-        self.pages, self.page_tokens, self.data = pages, page_tokens, torch.empty(0)
+        self.pages, self.page_tokens, self._data = pages, page_tokens, torch.empty(0)
         self._free, self._users = list(range(pages)), [0] * pages
         self._pages, self._lengths, self._next = {}, {}, 0
         self.memory = [[None] * page_tokens for _ in range(pages)]
