@@ -164,10 +164,10 @@ static const char *wrong_rows(const usp_cache_rows *r, const usp_cache &c, bool 
     if (r->rows < 0 || r->rows > (int64_t)1 << 20) return ": rows must be 0 to 2^20";
     if (r->sequences < 1 || r->sequences > (int64_t)1 << 20) return ": sequences must be 1 to 2^20";
     if (!r->offsets && r->rows != r->sequences && r->rows != 0) return ": without offsets there is one row for each sequence";
-    if (!pointers) return nullptr;
-    if (!r->table || !r->lengths) return ": null table or lengths";
     if (r->table_pages < 1 || r->table_pages > (0x7FFFFFFF - 4096) / c.page_tokens)
         return ": table_pages must be >= 1, its tokens below 2^31 - 4096";
+    if (!pointers) return nullptr;
+    if (!r->table || !r->lengths) return ": null table or lengths";
     if (r->ld_table < r->table_pages) return ": ld_table must be >= table_pages";
     for (const void *p : {(const void *)r->table, (const void *)r->lengths, (const void *)r->offsets})
         if (reinterpret_cast<uintptr_t>(p) & 3) return ": table, lengths and offsets must be 4-byte aligned";

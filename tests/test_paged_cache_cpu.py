@@ -89,6 +89,15 @@ def test_too_many_workgroups():
     assert usp.load_library().usp_attention(c, r, a, base, 1 << 50, None) == 2 and "too many" in usp.usp_last_error()
 
 
+@pytest.mark.parametrize("table_pages", [0, -1, 2 ** 26, 2 ** 62])
+def test_sizes_of_no_table(table_pages):
+    """A table of no or too many pages has no workspace and no plan."""
+    keep, base, c, r, a = described(r_table_pages=table_pages, r_ld_table=2 ** 62, r_offsets=None, r_rows=1, r_sequences=1)
+    lib, buf = usp.load_library(), ctypes.create_string_buffer(64)
+    assert lib.usp_attention_workspace_size(c, r, 8) == 0
+    assert lib.usp_attention_plan(c, r, 8, buf, 64) == 1 and "table_pages" in usp.usp_last_error()
+
+
 def test_sizes():
     lib = usp.load_library()
     for value_bytes, D, block in ((2, 128, 64 * 128 * 2), (1, 128, 64 * 128 + 256), (2, 40, 64 * 64 * 2), (1, 136, 64 * 192 + 256), (2, 256, 64 * 512)):
