@@ -415,7 +415,8 @@ typedef struct {
     const int32_t *lengths;  /* device int32 [sequences] */
     const int32_t *offsets;  /* device int32 [sequences + 1]; or NULL: row s is sequence s's only one */
     int64_t sequences;       /* 1 to 2^20; without offsets: rows */
-    int64_t rows;            /* T, 0 to 2^20 (0: nothing is done) */
+    int64_t rows;            /* T, 0 to 2^20 (0: nothing is done); more than one launch takes, which begins at 2^24 rows
+                                times heads, is USP_ERR_UNSUPPORTED */
 } usp_cache_rows;
 
 /*

@@ -202,10 +202,11 @@ static usp_status cache_rows_common(const std::string &f, const usp_cache *cache
         if (!write && !lie_apart(r.ld, r.head, rows->rows, cache->kv_heads, cache->head_dim))
             return usp::fail(USP_ERR_INVALID_ARG, f + ": rows and heads of K and V must lie apart");
     }
-    DeviceGuard g(cache->device);
-    if (!select_device(cache->device, g)) return usp::fail(USP_ERR_INVALID_ARG, f + ": no such device");
     const usp::CacheView c = usp::cache_view(*cache, layer);
     const usp::RowsView r = usp::rows_view(*rows, *cache);
+    if (!usp::cache_rows_fit(c, r)) return usp::fail(USP_ERR_UNSUPPORTED, f + ": too many rows and heads");
+    DeviceGuard g(cache->device);
+    if (!select_device(cache->device, g)) return usp::fail(USP_ERR_INVALID_ARG, f + ": no such device");
     const int rc = write ? usp::launch_cache_append(c, r, K, V, stream) : usp::launch_cache_read(c, r, K, V, stream);
     if (rc != 0) return hip_fail((hipError_t)rc, (f + ": launch").c_str());
     return USP_OK;

@@ -492,7 +492,8 @@ std::string describe_attention(const CacheView &c, const RowsView &r, int heads)
 }
 
 bool attention_fits(const CacheView &c, const RowsView &r, int heads) {
-    return plan_attention(c, r, heads).limit * c.kv_heads < (int64_t)1 << 31;
+    const AttendPlan p = plan_attention(c, r, heads);
+    return p.limit * c.kv_heads * (p.rows ? 1 : p.pieces) <= kMostWorkgroups;
 }
 
 int launch_attention(const CacheView &c, const RowsView &r, const usp_attention_args &p, void *workspace, void *stream) {

@@ -86,17 +86,20 @@ __device__ inline uint8_t *block_of(const CacheView &c, const RowsView &r, int s
            ((int64_t)h * c.page_blocks + rest / kBlockTokens) * cache_block_bytes(c.width, c.value_bytes);
 }
 
+constexpr int64_t kMostWorkgroups = ((int64_t)1 << 24) - 1;  // of a launch of 256 threads each: they are counted in 32 bits
+
 // Launchers (usp_cache.hip, usp_attention.hip): hipSuccess or the launch's error.
 struct HeadRows {          // rows of heads of fp16
     void *p;
     int64_t ld, head;      // strides of rows and heads in elements
 };
+bool cache_rows_fit(const CacheView &c, const RowsView &r);  // one launch takes them
 int launch_cache_append(const CacheView &c, const RowsView &r, HeadRows K, HeadRows V, void *stream);
 int launch_cache_read(const CacheView &c, const RowsView &r, HeadRows K, HeadRows V, void *stream);
 int launch_cache_copy(const CacheView &c, int64_t layers, const int32_t *src, const int32_t *dst, int64_t n, void *stream);
 size_t attention_workspace_bytes(const CacheView &c, const RowsView &r, int heads);
 std::string describe_attention(const CacheView &c, const RowsView &r, int heads);
-bool attention_fits(const CacheView &c, const RowsView &r, int heads);  // its workgroups are counted in 31 bits
+bool attention_fits(const CacheView &c, const RowsView &r, int heads);  // one launch takes it
 int launch_attention(const CacheView &c, const RowsView &r, const usp_attention_args &p, void *workspace, void *stream);
 
 }  // namespace usp

@@ -353,18 +353,23 @@ bool vector_heads(const HeadRows &r) {
 }
 
 // Groups where sequences have four rows or more on average: at fewer, most of a group's lanes have nothing to do.
+bool in_groups(const RowsView &r) { return r.offsets && r.rows >= 4 * (int64_t)r.sequences; }
+
+int64_t rows_grid(const CacheView &c, const RowsView &r) {
+    const int64_t waves = (in_groups(r) ? (int64_t)r.rows / kGroup + 2 * (int64_t)r.sequences : (int64_t)r.rows) * c.kv_heads;
+    return (waves + kWavesOfGroups - 1) / kWavesOfGroups;
+}
+
 template <bool WRITE>
 int launch_rows(const CacheView &c, const RowsView &r, HeadRows K, HeadRows V, void *stream) {
     const RowsArgs a = {c, r, K, V, vector_heads(K) && vector_heads(V)};
-    const bool groups = r.offsets && r.rows >= 4 * (int64_t)r.sequences;
+    const bool groups = in_groups(r);
     RowsFn fn;
     if (groups)
         fn = c.value_bytes == 2 ? group_kernel_of<2, WRITE>(c.width) : group_kernel_of<1, WRITE>(c.width);
     else
         fn = WRITE ? c.value_bytes == 2 ? append_kernel<2> : append_kernel<1> : c.value_bytes == 2 ? read_kernel<2> : read_kernel<1>;
-    const int64_t waves = (groups ? (int64_t)r.rows / kGroup + 2 * (int64_t)r.sequences : (int64_t)r.rows) * c.kv_heads;
-    const int64_t grid = (waves + kWavesOfGroups - 1) / kWavesOfGroups;
-    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(kCacheThreads), 0, reinterpret_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(fn, dim3((unsigned)rows_grid(c, r)), dim3(kCacheThreads), 0, reinterpret_cast<hipStream_t>(stream), a);
     return (int)hipGetLastError();
 }
 
@@ -398,6 +403,8 @@ __global__ __launch_bounds__(kCacheThreads) void copy_kernel(CopyArgs a) {
 
 }  // namespace
 
+bool cache_rows_fit(const CacheView &c, const RowsView &r) { return rows_grid(c, r) <= kMostWorkgroups; }
+
 int launch_cache_append(const CacheView &c, const RowsView &r, HeadRows K, HeadRows V, void *stream) {
     return launch_rows<true>(c, r, K, V, stream);
 }
@@ -412,7 +419,7 @@ int launch_cache_copy(const CacheView &c, int64_t layers, const int32_t *src, co
     a.page_bytes = c.page_bytes;
     a.layer_bytes = (int64_t)c.pages * c.page_bytes;
     a.parts = (int)((c.page_bytes + kCopyBytes - 1) / kCopyBytes);
-    const int64_t most = std::max<int64_t>(1, (((int64_t)1 << 30) / a.parts) / kPairs);  // layers of a launch
+    const int64_t most = std::max<int64_t>(1, kMostWorkgroups / a.parts / kPairs);  // layers of a launch
     for (int64_t i = 0; i < n; i += kPairs) {
         a.pairs = (int)std::min<int64_t>(kPairs, n - i);
         std::copy(src + i, src + i + a.pairs, a.src);

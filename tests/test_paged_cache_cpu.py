@@ -98,6 +98,17 @@ def test_sizes_of_no_table(table_pages):
     assert lib.usp_attention_plan(c, r, 8, buf, 64) == 1 and "table_pages" in usp.usp_last_error()
 
 
+def test_launches_beyond_the_grid():
+    """A launch has fewer than 2^32 threads: 2^24 workgroups of 256 are refused, not cut."""
+    lib = usp.load_library()
+    for offsets in (None, "r_offsets"):
+        change = dict(c_kv_heads=256, a_heads=256, r_rows=2 ** 20, r_sequences=2 ** 20, a_ld_out=2 ** 15, a_ld_q=2 ** 15)
+        keep, base, c, r, a = described(**change, **({"r_offsets": None} if offsets is None else {}))
+        assert lib.usp_attention(c, r, a, base, 1 << 50, None) == 2 and "too many" in usp.usp_last_error()
+        for call in (lib.usp_cache_append, lib.usp_cache_read):
+            assert call(c, r, 0, base, 2 ** 15, 64, base, 2 ** 15, 64, None) == 2 and "too many" in usp.usp_last_error()
+
+
 def test_sizes():
     lib = usp.load_library()
     for value_bytes, D, block in ((2, 128, 64 * 128 * 2), (1, 128, 64 * 128 + 256), (2, 40, 64 * 64 * 2), (1, 136, 64 * 192 + 256), (2, 256, 64 * 512)):
