@@ -142,9 +142,9 @@ __device__ inline void modify_scores(const AttendArgs &a, Scores &x, int n, floa
         for (int i = 0; i < n; ++i) x[i] = fmaf(-2.f * a.cap, __builtin_amdgcn_rcpf(1.f + exp2_of(x[i])), a.cap);
     }
     if (a.slopes) {
-        const int away = p - key0;
+        const float away = (float)(p - key0);  // and the differences are exact below 2^24
 #pragma unroll
-        for (int i = 0; i < n; ++i) x[i] = fmaf(-slope, fabsf((float)(away - key(i))), x[i]);
+        for (int i = 0; i < n; ++i) x[i] = fmaf(-slope, fabsf(away - (float)key(i)), x[i]);
     }
 }
 
