@@ -10,10 +10,10 @@
 // block is 16 products (512 cycles of the matrix unit) and about 135 vector instructions, 16 of them
 // exponentials (600 cycles), of which half overlap at best: a matrix and eight vector instructions took 19.6 ns
 // a step where the one alone takes 14.6 and the others 11.3. And the clock falls under this load, from
-// 2.5 (a long cache's single token) to 1.8-1.9 GHz. Steps on the way: a plain loop 779 us; blocks requested ahead and operands read together 348; straight
-// into LDS, operands four products ahead, three wavefronts a SIMD 312. Without gain: priorities of
-// wavefronts, 2 or 6 products ahead. Slower: softmax of a block between the products of its neighbours (369,
-// two wavefronts a SIMD), two tiles of columns a wavefront (556, one a SIMD).
+// 2.5 (a long cache's single token) to 1.8-1.9 GHz. Steps on the way: a plain loop 779 us; blocks requested ahead and
+// operands read together 348; straight into LDS, operands four products ahead, three wavefronts a SIMD 312. Without gain:
+// priorities of wavefronts, 2 or 6 products ahead. Slower: two blocks under way (339, registers spilled), softmax of a
+// block between the products of its neighbours (369, two wavefronts a SIMD), two tiles of columns a wavefront (556, one).
 //
 // 8 bits: 512 rows over 16512 tokens, the same heads, 426 us, 640 TFLOP/s: codes go raw into LDS and are converted
 // there once for the four wavefronts, two wavefronts a SIMD for want of registers. Scales of values taken apart, for
