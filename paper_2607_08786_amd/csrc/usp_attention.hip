@@ -200,7 +200,6 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
 #pragma unroll
     for (int d = 0; d < 2 * DS; ++d) o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
     float m = kNothing, l = 0.f;  // l: of this lane's keys alone
-    const float scale = MOD ? 1.f : a.scale;  // plain scores are scaled in the exponential's argument, others before
     float unit = 1e-30f;          // 8 bits: the largest scale of values so far; o is in 2^-14 of it
     const uint8_t *head_base = a.c.base + (int64_t)h * a.c.page_blocks * kBlockBytes;
     const int32_t *table = a.r.table + (int64_t)it.s * a.r.ld_table;
@@ -262,7 +261,15 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
             x[j] = st[j / 4][j % 4];
             if (VB == 1) x[j] *= ks[j / 4][j % 4];
         }
-        if (MOD) modify_scores(a, x, 8, slope, it.p, key0, [](int j) { return j; });
+        // Scores are scaled and rounded before their maximum is taken: m is one of them, so the largest weight is 1 and a
+        // maximum that stays fades nothing, whatever the scores. (Scaled in the exponent's sum instead, the maximum's own
+        // rounding came in at every block.)
+        if (MOD) {
+            modify_scores(a, x, 8, slope, it.p, key0, [](int j) { return j; });
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] *= a.scale;
+        }
         if (b * kBlockTokens < lo || (b + 1) * kBlockTokens > hi) {
             // What the row does not see may hold anything, and nothing times infinity is not nothing.
             uint32_t keep[8];
@@ -286,8 +293,8 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
             if (VB == 1) top_scale = fmaxf(top_scale, vs[j / 4][j % 4]);
         }
         const float m_new = fmaxf(m, max_32(max_16(top)));
-        const float base = m_new == kNothing ? 0.f : -m_new * scale;
-        float fade = exp2_of(fmaf(m, scale, base));
+        const float base = m_new == kNothing ? 0.f : m_new;
+        float fade = exp2_of(m - base);
         m = m_new;
         l *= fade;
         float to_unit = 1.f;
@@ -300,7 +307,7 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
         half8 p, rest;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float w = exp2_of(fmaf(x[j], scale, base));
+            float w = exp2_of(x[j] - base);
             if (VB == 1) {
                 l += w;
                 w *= vs[j / 4][j % 4] * to_unit;
@@ -342,12 +349,12 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
         float top = sm[0][col];
 #pragma unroll
         for (int w = 1; w < kRowWaves; ++w) top = fmaxf(top, sm[w][col]);
-        const float base = top == kNothing ? 0.f : -top * scale;
+        const float base = top == kNothing ? 0.f : top;
         floatx4 sum = {0.f, 0.f, 0.f, 0.f};
         float total = 0.f;
 #pragma unroll
         for (int w = 0; w < kRowWaves; ++w) {
-            const float f = exp2_of(fmaf(sm[w][col], scale, base));
+            const float f = exp2_of(sm[w][col] - base);
             total += sl[w][col] * f;
             sum += *reinterpret_cast<const floatx4 *>(&so[(w * 16 + col) * kStride + d]) * f;
         }
@@ -383,7 +390,7 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
         const int col = e / (W / 4), d = 4 * (e % (W / 4));
         float top = kNothing;
         for (int i = 0; i < pieces; ++i) top = fmaxf(top, so[i * 32 + col]);
-        const float base = top == kNothing ? 0.f : -top * scale;
+        const float base = top == kNothing ? 0.f : top;
         const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(first, (short)0, -1, kBufferRsrcWord3);
         floatx4 sum = {0.f, 0.f, 0.f, 0.f};
         float total = 0.f;
@@ -397,7 +404,7 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
                 if (i0 + i < pieces) {
-                    const float f = exp2_of(fmaf(so[(i0 + i) * 32 + col], scale, base));
+                    const float f = exp2_of(so[(i0 + i) * 32 + col] - base);
                     total += so[(i0 + i) * 32 + 16 + col] * f;
                     sum += __builtin_bit_cast(floatx4, v[i]) * f;
                 }

@@ -1,0 +1,125 @@
+"""usp_attention where the arithmetic of its softmax could go wrong: long chains of blocks, large scores, weights far below
+the largest, extreme scales (GPU). Each case has an answer in closed form or by sums in 64 bits, and a tolerance of its own."""
+import numpy as np
+import pytest
+import torch
+
+import attention64
+from paper_2607_08786_amd import usp
+
+pytestmark = pytest.mark.gpu
+
+PAGE = 4096
+
+
+def draw(seed, *shape, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).half()
+
+
+def int32(values):
+    return torch.as_tensor(values, dtype=torch.int32).cuda()
+
+
+def one_sequence(K, V, values, page=64):
+    """A cache that holds one sequence's K and V [L, kv, D], and a function that makes the rows of its last n tokens."""
+    L, kv, D = K.shape
+    pages = -(-L // page)
+    cache = usp.KVCache(pages, kv, D, page, dtype=torch.int8 if values == "q" else torch.float16)
+    table, length = int32([list(range(pages))]), int32([L])
+    cache.append(usp.CacheRows(table, length, int32([0, L])), K.cuda(), V.cuda())
+    return cache, lambda n: usp.CacheRows(table, length, None if n == 1 else int32([0, n]))
+
+
+def uncut(cache, tables):
+    """Rows of one token for each of 4097 sequences, of which the first have the pages of `tables` and the others nothing: too
+    many sequences for tiles to be cut, so that one workgroup takes each of the first ones whole."""
+    table = torch.zeros(4097, len(tables[0]), dtype=torch.int32)
+    lengths = torch.zeros(4097, dtype=torch.int32)
+    table[:len(tables)], lengths[:len(tables)] = torch.tensor(tables, dtype=torch.int32), PAGE * len(tables[0])
+    rows = usp.CacheRows(table.cuda(), lengths.cuda())
+    plan = cache.plan(rows, 4097, cache.kv_heads)
+    assert plan.startswith("rows") and "pieces" not in plan
+    return rows
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("score", [300.0, 1e4, 1e8])
+def test_long_chains_of_equal_scores(score, values):
+    """1024 blocks a wavefront, values 1 in the first half of the keys and 0 in the second: 1 / 2 whatever the score. Weights
+    are equal, so their roundings cancel. What is left: the result's rounding, 2^-12; sums of 1024 terms of one size each,
+    1024 2^-24 = 2^-14 of 1 / 2 for the numerator and the same for the sum of weights."""
+    D = 64
+    cache = usp.KVCache(2, 1, D, PAGE, dtype=torch.int8 if values == "q" else torch.float16)
+    K, V = torch.zeros(2 * PAGE, 1, D).half(), torch.zeros(2 * PAGE, 1, D).half()
+    K[..., :61], V[:PAGE] = 1, 1
+    cache.append(usp.CacheRows(int32([[0, 1]]), int32([2 * PAGE]), int32([0, 2 * PAGE])), K.cuda(), V.cuda())
+    rows = uncut(cache, [[0] * 16 + [1] * 16])
+    q = torch.ones(4097, 1, D, dtype=torch.float16, device="cuda")
+    got = cache.attention(rows, q, scale=score / 61)
+    assert (got[1:] == 0).all()
+    assert ((got[0].double() - 0.5).abs() <= 2.0 ** -12 + 2.0 ** -14).all(), got[0, 0, :4]
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("n", [1])
+@pytest.mark.parametrize("L", [90, 4000])
+@pytest.mark.parametrize("size,step", [(4096, 4), (57344, 32)])
+def test_large_scores(size, step, L, n, values):
+    """Scores of some 1e8 and 1e10 that lie far apart between seven kinds of keys and are one number within each: the mean
+    of the values of the largest kind that a row sees. Products are multiples of size * step and their sums below 2^24 of
+    them, so scores are exact up to their scale. (Values have one largest magnitude, so one scale in 8 bits.)
+    Errors: the result's rounding; sums of up to L terms in fp32, twice over for the matrix unit; in 8 bits a weight's factor,
+    the same for all here, 2^-14 of each."""
+    D, kv, heads = 128, 2, 4
+    kind = (torch.arange(L) * 3 + 1) % 7
+    K = (size + step * kind.float())[:, None, None].expand(L, kv, D).half()
+    V = draw(1, L, kv, D).clamp(-3, 3)
+    V[..., 0] = 4
+    q = torch.full((n, heads, D), float(size)).half()
+    q[:, 1::2] *= -1  # half of the heads: the smallest kind, its score far below zero
+    cache, rows = one_sequence(K, V, values)
+    got = cache.attention(rows(n), q.cuda()).cpu().double()
+    held = attention64.held(V, values == "q")
+    for i in range(n):
+        seen = kind[:L - n + i + 1]
+        for h in range(heads):
+            at = (seen == (seen.min() if h % 2 else seen.max())).nonzero()[:, 0]
+            v = held[at, h // 2]
+            want, A = v.mean(0), v.abs().mean(0)
+            tol = 2.0 ** -25 + 2.0 ** -11 * want.abs() + (4 * (L + 40) * 2.0 ** -24 + (2.0 ** -13 if values == "q" else 0)) * A
+            assert ((got[i, h] - want).abs() <= tol).all(), (i, h, got[i, h, :4], want[:4])
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("n", [1])
+def test_scores_beyond_fp32(n, values):
+    """A score beyond fp32's range counts as an infinity: above, the row is NaN; below, the key has no weight; all below: zeros.
+    Errors as above."""
+    D, L = 64, 500
+    sign = torch.where(torch.arange(L) % 5 == 0, 0.0, -1.0)  # scores of 0 and of -2^130
+    K = (sign * 32)[:, None, None].expand(L, 1, D).half()
+    V = draw(2, L, 1, D)
+    V[..., 0] = 4
+    V = V.clamp(-4, 4)
+    cache, rows = one_sequence(K, V, values)
+    q = torch.full((n, 3, D), 32.0).half()
+    q[:, 1] *= -1
+    scale = 2.0 ** 114
+    first = torch.arange(L - n, L).int()
+    got = cache.attention(rows(n), q.cuda(), scale=scale).cpu().double()
+    assert got[:, 1].isnan().all()
+    held = attention64.held(V, values == "q")[:, 0]
+    for i in range(n):
+        v = held[:L - n + i + 1][::5]
+        want, A = v.mean(0), v.abs().mean(0)
+        tol = 2.0 ** -25 + 2.0 ** -11 * want.abs() + (4 * (L + 40) * 2.0 ** -24 + (2.0 ** -13 if values == "q" else 0)) * A
+        for h in (0, 2):
+            assert ((got[i, h] - want).abs() <= tol).all()
+    alone = cache.attention(rows(n), q.cuda(), scale=scale, first=first.cuda()).cpu()  # each row its own key alone
+    for i in range(n):
+        if (L - n + i) % 5:
+            assert (alone[i, 0] == 0).all()
+        else:
+            want = held[L - n + i]
+            assert ((alone[i, 0].double() - want).abs() <= 2.0 ** -25 + (2.0 ** -11 + 2.0 ** -13) * want.abs()).all()
