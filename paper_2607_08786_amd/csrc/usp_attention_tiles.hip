@@ -27,6 +27,7 @@ namespace {
 
 constexpr int kAhead = 4;           // products that operands are read ahead
 constexpr int kMinTileBlocks = 6;   // blocks of a piece at least
+constexpr float kLargeScore = 0x1.fp25f;
 
 // The first tile of sequence s: those before it have at most so many.
 template <int COLUMNS>
@@ -154,8 +155,26 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     float m = kNothing, l = 0.f;
-    // Plain scores are scaled in the exponential's argument, others before.
-    const float scale = MOD || VB == 1 ? 1.f : a.scale;
+    // m is a scaled score, rounded. Plain scores are scaled in the exponent's one sum, which holds their product exactly, so
+    // all weights of a column are off by m's rounding, the largest too: by up to 2 in the exponent below kLargeScore, and by
+    // anything beyond. Where q alone does not rule that out (|q . K| is at most 65504 sum |q|), scores are scaled and rounded
+    // first, as the other kernels' are, on the way past the masks. (Branches in the loop that look at m took 1.4 to 10% of a
+    // prompt; this takes nothing at 64 and 128 channels and 1% at 256, and `late` in a vector register spilled 16 others.)
+    constexpr bool kPlain = !MOD && VB == 2;
+    bool scale_first = false;
+    if (kPlain) {
+        float sum = W * 0x1p-14f;  // covers subnormal channels, whether or not the sum takes them as zeros
+#pragma unroll
+        for (int i = 0; i < 2 * DS; ++i) {
+            const v4u32 bits = __builtin_bit_cast(v4u32, q[i]) & 0x7FFF7FFFu;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2a, bits[j]), half2a{(_Float16)1.f, (_Float16)1.f}, sum, false);
+        }
+        scale_first = __any(!(sum_32(sum) * 65504.f * a.scale < kLargeScore));
+    }
+    const float late = kPlain ? __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, scale_first ? 1.f : a.scale)))
+                              : 1.f;  // what is left to multiply scores by in the exponent
 
     const int32_t *table = a.r.table + (int64_t)s * a.r.ld_table;
     const uint8_t *head_base = a.c.base + (int64_t)h * a.c.page_blocks * kBlockBytes;
@@ -320,7 +339,11 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
 #pragma unroll
                 for (int i = 0; i < 16; ++i) st[i] += (float)log_factor[i / 8][i % 8];
             }
-            if (!whole) {
+            if (!whole || scale_first) {
+                if (scale_first) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) st[i] *= a.scale;
+                }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int key = block_lo + 16 * (i / 8) + 8 * half + i % 8;
@@ -330,18 +353,18 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
             float top = st[0];
 #pragma unroll
             for (int i = 1; i < 16; ++i) top = fmaxf(top, st[i]);
-            top = fmaxf(m, max_32(top));
+            top = fmaxf(m, max_32(top) * late);  // the largest product rounds to the largest rounded one
             if (__any(top > m)) {
-                const float fade = exp2_of((m - (top == kNothing ? 0.f : top)) * scale);
+                const float fade = exp2_of(m - (top == kNothing ? 0.f : top));
                 m = top;
                 l *= fade;
 #pragma unroll
                 for (int d = 0; d < DS; ++d) o[d] *= fade;
             }
-            const float base = m == kNothing ? 0.f : -m * scale;
+            const float base = m == kNothing ? 0.f : -m;
             // The sum takes the weights as the product does.
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i / 8][i % 8] = (_Float16)exp2_of(fmaf(st[i], scale, base));
+            for (int i = 0; i < 16; ++i) w[i / 8][i % 8] = (_Float16)exp2_of(fmaf(st[i], late, base));
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const half2a pair = {w[i / 4][2 * (i % 4)], w[i / 4][2 * (i % 4) + 1]};
@@ -428,7 +451,7 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
             for (int j = 0; j < DS * 4 + 1; ++j)
                 x[j] = __builtin_amdgcn_raw_buffer_load_b128(from, j * kThreads * 16 + at, 0, kCachePolicyDevice);
             const floatx4 ml = __builtin_bit_cast(floatx4, x[DS * 4]);
-            const float f = exp2_of((ml[0] - base) * scale);
+            const float f = exp2_of(ml[0] - base);
             l = fmaf(ml[1], f, l);
 #pragma unroll
             for (int j = 0; j < DS * 4; ++j)
