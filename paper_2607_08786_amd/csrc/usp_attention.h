@@ -26,6 +26,10 @@ typedef _Float16 half2a __attribute__((ext_vector_type(2)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNothing = -__builtin_inff();
 
+// Weights in fp16 are 2^(score - m), m being the largest score less one of these: the larger below kLargeScore, where m's
+// rounding moves it by 2 at most, and one that rounds to 8 at most beyond, so that no weight passes fp16's 65504.
+constexpr float kLift = 13.f, kLargeLift = 7.f, kLargeScore = 0x1.fp25f;
+
 struct AttendArgs {
     CacheView c;
     RowsView r;
@@ -49,6 +53,7 @@ struct AttendArgs {
     float *partials;
 };
 
+__device__ inline float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The larger of a value and what the lanes 16 (32) away hold.

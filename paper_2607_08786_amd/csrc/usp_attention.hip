@@ -261,9 +261,8 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
             x[j] = st[j / 4][j % 4];
             if (VB == 1) x[j] *= ks[j / 4][j % 4];
         }
-        // Scores are scaled and rounded before their maximum is taken: m is one of them, so the largest weight is 1 and a
-        // maximum that stays fades nothing, whatever the scores. (Scaled in the exponent's sum instead, the maximum's own
-        // rounding came in at every block.)
+        // Scores are scaled and rounded before their maximum is taken, so a maximum that stays fades nothing, whatever the
+        // scores. (Scaled in the exponent's sum instead, the maximum's own rounding came in at every block.)
         if (MOD) {
             modify_scores(a, x, 8, slope, it.p, key0, [](int j) { return j; });
         } else {
@@ -292,7 +291,9 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
             top = fmaxf(top, x[j]);
             if (VB == 1) top_scale = fmaxf(top_scale, vs[j / 4][j % 4]);
         }
-        const float m_new = fmaxf(m, max_32(max_16(top)));
+        top = max_32(max_16(top));
+        if (VB == 2) top -= fabsf(top) < kLargeScore ? kLift : kLargeLift;  // small weights in fp16's full precision
+        const float m_new = fmaxf(m, top);
         const float base = m_new == kNothing ? 0.f : m_new;
         float fade = exp2_of(m - base);
         m = m_new;
@@ -305,11 +306,12 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
             to_unit = 16384.f * __builtin_amdgcn_rcpf(u);
         }
         half8 p, rest;
+        float block_sum = 0.f;  // to a large weight, single small ones may add nothing
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float w = exp2_of(x[j] - base);
             if (VB == 1) {
-                l += w;
+                block_sum += w;
                 w *= vs[j / 4][j % 4] * to_unit;
             }
             p[j] = (_Float16)w;
@@ -319,8 +321,10 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
         }
         if (VB == 2) {  // the sum takes the weights as the product does
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) l = __builtin_amdgcn_fdot2(half2a{p[j], p[j + 1]}, half2a{(_Float16)1.f, (_Float16)1.f}, l, false);
+            for (int j = 0; j < 8; j += 2)
+                block_sum = __builtin_amdgcn_fdot2(half2a{p[j], p[j + 1]}, half2a{(_Float16)1.f, (_Float16)1.f}, block_sum, false);
         }
+        l += block_sum;
 #pragma unroll
         for (int d = 0; d < 2 * DS; ++d) {
             o[d] *= fade;

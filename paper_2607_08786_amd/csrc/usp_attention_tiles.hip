@@ -27,7 +27,6 @@ namespace {
 
 constexpr int kAhead = 4;           // products that operands are read ahead
 constexpr int kMinTileBlocks = 6;   // blocks of a piece at least
-constexpr float kLargeScore = 0x1.fp25f;
 
 // The first tile of sequence s: those before it have at most so many.
 template <int COLUMNS>
@@ -155,14 +154,16 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     float m = kNothing, l = 0.f;
-    // m is a scaled score, rounded. Plain scores are scaled in the exponent's one sum, which holds their product exactly, so
-    // all weights of a column are off by m's rounding, the largest too: by up to 2 in the exponent below kLargeScore, and by
-    // anything beyond. Where q alone does not rule that out (|q . K| is at most 65504 sum |q|), scores are scaled and rounded
-    // first, as the other kernels' are, on the way past the masks. (Branches in the loop that look at m took 1.4 to 10% of a
-    // prompt; this takes nothing at 64 and 128 channels and 1% at 256, and `late` in a vector register spilled 16 others.)
+    // Weights are taken relative to m, a column's largest scaled score less `lift`, so that fp16 holds the largest one as some
+    // 2^lift and small ones to its full precision down to 2^(-14 - lift) of it. Plain scores are scaled in the exponent's one
+    // sum, which holds their product exactly, so all weights of a column are off by m's rounding: by 2 in the exponent below
+    // kLargeScore, and by anything beyond. Where q and the biases do not rule that out (|q . K| is at most 65504 sum |q|),
+    // scores are scaled and rounded first, as the other kernels' are, on the way past the masks, and lifted less. (Branches in
+    // the loop that look at m took 1.4 to 10% of a prompt; this takes nothing at 64 and 128 channels and 1% at 256, and
+    // `late` in a vector register spilled 16 others.)
     constexpr bool kPlain = !MOD && VB == 2;
-    bool scale_first = false;
-    if (kPlain) {
+    float bound = a.cap;
+    if (!MOD || a.cap == 0.f) {
         float sum = W * 0x1p-14f;  // covers subnormal channels, whether or not the sum takes them as zeros
 #pragma unroll
         for (int i = 0; i < 2 * DS; ++i) {
@@ -171,10 +172,12 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
             for (int j = 0; j < 4; ++j)
                 sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2a, bits[j]), half2a{(_Float16)1.f, (_Float16)1.f}, sum, false);
         }
-        scale_first = __any(!(sum_32(sum) * 65504.f * a.scale < kLargeScore));
+        bound = sum_32(sum) * 65504.f * fabsf(a.scale);
     }
-    const float late = kPlain ? __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, scale_first ? 1.f : a.scale)))
-                              : 1.f;  // what is left to multiply scores by in the exponent
+    if (MOD) bound += fabsf(slope) * (float)len;
+    const bool large = __any(!(bound < kLargeScore)), scale_first = kPlain && large;
+    const float lift = uniform(large ? kLargeLift : kLift);
+    const float late = kPlain ? uniform(large ? 1.f : a.scale) : 1.f;  // what is left to multiply scores by in the exponent
 
     const int32_t *table = a.r.table + (int64_t)s * a.r.ld_table;
     const uint8_t *head_base = a.c.base + (int64_t)h * a.c.page_blocks * kBlockBytes;
@@ -353,7 +356,7 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
             float top = st[0];
 #pragma unroll
             for (int i = 1; i < 16; ++i) top = fmaxf(top, st[i]);
-            top = fmaxf(m, max_32(top) * late);  // the largest product rounds to the largest rounded one
+            top = fmaxf(m, fmaf(max_32(top), late, -lift));
             if (__any(top > m)) {
                 const float fade = exp2_of(m - (top == kNothing ? 0.f : top));
                 m = top;
@@ -362,15 +365,17 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
                 for (int d = 0; d < DS; ++d) o[d] *= fade;
             }
             const float base = m == kNothing ? 0.f : -m;
-            // The sum takes the weights as the product does.
+            // The sum takes the weights as the product does. (A block's first: to a large weight, two small ones may add nothing.)
+            float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i / 8][i % 8] = (_Float16)exp2_of(fmaf(st[i], late, base));
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const half2a pair = {w[i / 4][2 * (i % 4)], w[i / 4][2 * (i % 4) + 1]};
-                l = __builtin_amdgcn_fdot2(pair, half2a{(_Float16)1.f, (_Float16)1.f}, l, false);
-                if (VB == 1) l = __builtin_amdgcn_fdot2(pair, half2a{less_one[i / 4][2 * (i % 4)], less_one[i / 4][2 * (i % 4) + 1]}, l, false);
+                sum = __builtin_amdgcn_fdot2(pair, half2a{(_Float16)1.f, (_Float16)1.f}, sum, false);
+                if (VB == 1) sum = __builtin_amdgcn_fdot2(pair, half2a{less_one[i / 4][2 * (i % 4)], less_one[i / 4][2 * (i % 4) + 1]}, sum, false);
             }
+            l += sum;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < kProducts; ++i) {

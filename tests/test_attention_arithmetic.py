@@ -122,3 +122,35 @@ def test_scores_beyond_fp32(n, values):
         else:
             want = held[L - n + i]
             assert ((alone[i, 0].double() - want).abs() <= 2.0 ** -25 + (2.0 ** -11 + 2.0 ** -13) * want.abs()).all()
+
+
+@pytest.mark.parametrize("spread", [0.0, 1.0])
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("n", [1, 64])
+@pytest.mark.parametrize("L", [16384, 131072])
+def test_one_key_far_above_the_others(L, n, values, spread):
+    """A first token that draws attention, its score 17.4 above the others', its value 0: the result is what the others add
+    up to. Errors relative to it: its rounding 2^-11; each weight's rounding, 2^-11 in fp16 and 2^-14 more in 8 bits, in the
+    numerator (in the sum of weights the others are less than 2^-4), and 2^-25 of the few that are subnormal, in units in which
+    the others are 2^-10 and more, 2^-15; an exponent of up to 64 off by 8 roundings, 2^-15; the
+    numerator's sum of two terms a block of 32 keys and the sum of weights' of one, (L / 16 + L / 32) 2^-24, twice over."""
+    D = 64
+    g = torch.Generator().manual_seed(L + n)
+    K = torch.zeros(L, 1, D).half()
+    K[1:, 0, 0] = (torch.randn(L - 1, generator=g) * spread).half()
+    K[0, 0, 0] = 17.40625
+    V = (torch.rand(L, 1, D, generator=g) + 0.5).half()
+    V[0] = 0
+    cache, rows = one_sequence(K, V, values, page=PAGE)
+    q = torch.zeros(n, 1, D).half()
+    q[..., 0] = 1
+    assert cache.plan(rows(n), n, 1).startswith("rows" if n == 1 else "tiles")
+    got = cache.attention(rows(n), q.cuda(), scale=1.0)[:, 0].cpu().double()
+    s = attention64.held(K, values == "q")[:, 0, 0]
+    w = torch.exp(s - s[0])
+    v = attention64.held(V, values == "q")[:, 0]
+    total, above = torch.cumsum(w, 0)[L - n:], torch.cumsum(w[:, None] * v, 0)[L - n:]
+    want = above / total[:, None]
+    assert total.max() < 1 + 2.0 ** -4
+    off = (got / want - 1).abs().max()
+    assert off <= 2.0 ** -11 + 2.0 ** -11 + 2.0 ** -14 + 2.0 ** -14 + 2 * (L / 16 + L / 32) * 2.0 ** -24, off
