@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
         float to_unit = 1.f;
         if (VB == 1) {
             const float u = fmaxf(unit, max_32(max_16(top_scale)));
-            fade *= unit * __builtin_amdgcn_rcpf(u);
+            if (u > unit) fade *= unit * __builtin_amdgcn_rcpf(u);  // a unit that stays leaves o as it is: the product need not be 1
             unit = u;
             to_unit = 16384.f * __builtin_amdgcn_rcpf(u);
         }

@@ -60,6 +60,23 @@ def test_long_chains_of_equal_scores(score, values):
     assert ((got[0].double() - 0.5).abs() <= 2.0 ** -12 + 2.0 ** -14).all(), got[0, 0, :4]
 
 
+def test_long_chains_in_units_of_a_scale():
+    """32768 blocks a wavefront of an 8-bit cache, values v in the first half of the keys and 0 in the second: v / 2. All
+    weights are 1, so the sums are of whole numbers below 2^24 times a power of two, and exact. What is left: the result's
+    rounding, 2^-11 of it, the value's scale and the result's way back from its units, a few 2^-24 of it."""
+    D, L = 32, 1024
+    v = torch.linspace(1.0, 2.0, 17)[:16].half()
+    cache = usp.KVCache(17, 1, D, PAGE, dtype=torch.int8)
+    K, V = torch.zeros(17 * PAGE, 1, D).half(), torch.zeros(17, PAGE, 1, D).half()
+    V[:16] = v[:, None, None, None]
+    everything = usp.CacheRows(int32([list(range(17))]), int32([17 * PAGE]), int32([0, 17 * PAGE]))
+    cache.append(everything, K.cuda(), V.view(17 * PAGE, 1, D).cuda())
+    rows = uncut(cache, [[i] * (L // 2) + [16] * (L // 2) for i in range(16)])
+    got = cache.attention(rows, torch.zeros(4097, 1, D, dtype=torch.float16, device="cuda"))
+    want = attention64.held(V[:16, 0], True).view(16, 1, D) / 2
+    assert ((got[:16].cpu().double() - want).abs() <= (2.0 ** -11 + 2.0 ** -20) * want).all(), (got[:16, 0, 0].cpu() / want[:, 0, 0] - 1)
+
+
 @pytest.mark.parametrize("values", ["f16", "q"])
 @pytest.mark.parametrize("n", [1, 40])
 @pytest.mark.parametrize("L", [90, 4000])
