@@ -539,7 +539,8 @@ int launch_attention(const CacheView &c, const RowsView &r, const usp_attention_
     a.counters = reinterpret_cast<uint32_t *>(workspace);
     a.partials = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + kCounterRegionBytes);
     const int64_t grid = plan.limit * c.kv_heads * (plan.rows ? 1 : plan.pieces);
-    const bool modified = a.cap > 0.f || a.slopes || !(a.scale > 0.f);
+    // (The tiles kernel multiplies plain scores by the product of their scale and the key's: up to 2^10, a finite one.)
+    const bool modified = a.cap > 0.f || a.slopes || !(a.scale > 0.f) || (c.value_bytes == 1 && a.scale > 0x1p64f);
     if (!plan.rows) return launch_tiles(&a, c.width, c.value_bytes, modified, grid, stream);
     const AttendFn fn = c.value_bytes == 2 ? modified ? rows_kernel_of<2, true>(c.width) : rows_kernel_of<2, false>(c.width)
                                            : modified ? rows_kernel_of<1, true>(c.width) : rows_kernel_of<1, false>(c.width);

@@ -171,3 +171,17 @@ def test_one_key_far_above_the_others(L, n, values, spread):
     assert total.max() < 1 + 2.0 ** -4
     off = (got / want - 1).abs().max()
     assert off <= 2.0 ** -11 + 2.0 ** -11 + 2.0 ** -14 + 2.0 ** -14 + 2 * (L / 16 + L / 32) * 2.0 ** -24, off
+
+
+@pytest.mark.parametrize("modified", [False, True])
+@pytest.mark.parametrize("n", [1, 40])
+def test_scale_times_the_keys_scale(n, modified):
+    """8 bits: a scale of 2^126 and keys of up to 60000. A score of 0 is 0, although the two scales' product is beyond fp32."""
+    D, L = 64, 70
+    K = torch.full((L, 1, D), 60000.0).half()
+    V = draw(3, L, 1, D)
+    cache, rows = one_sequence(K, V, "q")
+    slopes = torch.zeros(2, device="cuda") if modified else None
+    got = cache.attention(rows(n), torch.zeros(n, 2, D, dtype=torch.float16, device="cuda"), scale=2.0 ** 126, slopes=slopes)
+    zero = cache.attention(rows(n), torch.zeros(n, 2, D, dtype=torch.float16, device="cuda"), scale=1.0, slopes=slopes)
+    assert torch.isfinite(got).all() and torch.equal(got, zero)
