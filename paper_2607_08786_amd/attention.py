@@ -217,7 +217,7 @@ def _geometry(cache: usp.KVCache) -> List[int]:
 def _attend(cache: usp.KVCache, rows: usp.CacheRows, q: torch.Tensor, workspace: Optional[torch.Tensor], layer: int,
             scale: Optional[float], cap: float, slopes: Optional[torch.Tensor], window: int, first: Optional[torch.Tensor],
             last: Optional[torch.Tensor]) -> torch.Tensor:
-    out = torch.empty_like(q) if rows.offsets is None else torch.zeros_like(q)  # offsets may leave rows out
+    out = q.new_empty(q.shape) if rows.offsets is None else q.new_zeros(q.shape)  # offsets may leave rows out
     usp.usp_attention(cache, rows, q, out, workspace, layer, scale, cap, slopes, window, first, last)
     return out
 
