@@ -20,7 +20,7 @@ from typing import List, Optional, Sequence
 import torch
 
 from . import usp
-from .linear import Workspaces, _seen
+from .linear import Workspaces, _operand, _seen
 
 
 class OutOfPages(RuntimeError):
@@ -321,8 +321,8 @@ class PagedAttention(torch.nn.Module):
                 usp.usp_cache_append(cache, rows, k3, v3, layer)
         ws = self._workspace_of(cache, rows, T)
         if seen:
-            out = torch.ops.usp.paged_attention(q3, cache.data, _geometry(cache), rows.table, rows.lengths, rows.offsets, ws, layer,
-                                                self.scale, self.cap, slopes, self.window, first, last)
+            out = torch.ops.usp.paged_attention(q3, cache.data, _geometry(cache), rows.table, rows.lengths, rows.offsets,
+                                                _operand(ws, q3), layer, self.scale, self.cap, slopes, self.window, first, last)
         else:
             out = _attend(cache, rows, q3, ws, layer, self.scale, self.cap, slopes, self.window, first, last)
         return out if q.dim() == 3 else out.flatten(1)

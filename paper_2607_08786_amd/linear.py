@@ -73,6 +73,12 @@ class Workspaces:
         return ws
 
 
+def _operand(workspace: Optional[torch.Tensor], x: torch.Tensor) -> Optional[torch.Tensor]:
+    """A workspace as an operator's operand. A compiled program has an empty tensor for none: inductor takes no None for an
+    operand that the operator writes."""
+    return x.new_empty(0, dtype=torch.uint8) if workspace is None and torch.compiler.is_compiling() else workspace
+
+
 class SparseLinear(Workspaces, torch.nn.Module):
     """``act(x W^T + b) (+ residual)`` with W pruned by ``mask`` (kept where nonzero).
 
@@ -130,7 +136,7 @@ class SparseLinear(Workspaces, torch.nn.Module):
             if r2.dtype != torch.float16 or not r2.is_contiguous():
                 r2 = r2.to(torch.float16).contiguous()
         y = torch.ops.usp.sparse_linear(x2, self.matrix.handle, self.out_features, self.bias, r2,
-                                        usp.ACTIVATIONS[self.activation], self.workspace(N))
+                                        usp.ACTIVATIONS[self.activation], _operand(self.workspace(N), x2))
         return y.reshape(*lead, self.out_features)
 
     def extra_repr(self) -> str:
@@ -316,7 +322,7 @@ class SparseLinearQ(SparseLinear):
         if r2 is not None and r2.shape[0] != N:
             raise ValueError("residual must have one row per token")
         y = _call(sparse_linear_q, _linear_q, x2, x_scale, self.matrix.handle, self.out_features, self._buffers["bias"],
-                  r2, usp.ACTIVATIONS[self.activation], self.workspace(N))
+                  r2, usp.ACTIVATIONS[self.activation], _operand(self.workspace(N), x2))
         return y if x.dim() == 2 else y.reshape(*x.shape[:-1], self.out_features)
 
 
@@ -374,7 +380,8 @@ class SparseExperts(SparseLinear):
         if T == 0 or x2.shape[0] == 0:
             return x2.new_zeros((T, self.out_features), dtype=torch.float16)
         return _call(sparse_experts, _experts, x2, x_scale, offsets, rows, row_weight, self.matrix.handle,
-                     self.out_features, self.eight_bit, self._buffers["bias"], usp.ACTIVATIONS[self.activation], self.workspace(T))
+                     self.out_features, self.eight_bit, self._buffers["bias"], usp.ACTIVATIONS[self.activation],
+                     _operand(self.workspace(T), x2))
 
     def extra_repr(self) -> str:
         return (f"experts={len(self.matrix.experts)}, in_features={self.in_features}, "

@@ -4,7 +4,7 @@ from types import SimpleNamespace
 import pytest
 import torch
 
-from paper_2607_08786_amd import attention, usp
+from paper_2607_08786_amd import attention, linear, usp
 
 KV, HEADS, D, T = 2, 4, 64, 5
 
@@ -51,3 +51,54 @@ def test_compiled_operator(layout, offsets, backend):
     assert torch.equal(compiled(q), 2 * q.flatten(1) + 1)
     got = called(q, where, workspace)
     assert got.is_contiguous() and torch.equal(got, 2 * q)
+
+
+def attention_module(need):
+    data, _, table, lengths = operands()
+    cache = SimpleNamespace(kv_heads=KV, head_dim=D, page_tokens=32, dtype=torch.float16, device=0, data=data, workspace_size=lambda *a: need,
+                            make_workspace=lambda *a: torch.zeros(need, dtype=torch.uint8))
+    rows = SimpleNamespace(table=table, lengths=lengths, offsets=None)
+    module = attention.PagedAttention(HEADS, KV, D)
+    return lambda q: module(q, cache, rows), torch.randn(T, HEADS * D).half(), lambda q: 2 * q
+
+
+IN, OUT = 32, 24
+
+
+def layer(cls, need, **also):
+    m = cls.__new__(cls)
+    torch.nn.Module.__init__(m)
+    m._set_up((OUT, IN), None, "none", 0)
+    m.matrix = SimpleNamespace(handle=1, device=0, workspace_size=lambda n: need, make_workspace=lambda n: torch.zeros(need, dtype=torch.uint8), **also)
+    return m
+
+
+def linear_module(need):
+    return layer(linear.SparseLinear, need), torch.randn(T, IN).half(), lambda x: 2 * x[:, :OUT]
+
+
+def linear_q_module(need):
+    return layer(linear.SparseLinearQ, need), torch.randn(T, IN).half(), lambda x: 2 * x[:, :OUT]
+
+
+def experts_module(need):
+    m = layer(linear.SparseExperts, need, experts=[None])
+    m.eight_bit = False
+    offsets = torch.tensor([0, T], dtype=torch.int32)
+    return lambda x: m(x, offsets), torch.randn(T, IN).half(), lambda x: 2 * x[:, :OUT]
+
+
+@pytest.mark.parametrize("backend", ["aot_eager", "inductor"])
+@pytest.mark.parametrize("need", [0, 16])
+@pytest.mark.parametrize("make", [attention_module, linear_module, linear_q_module, experts_module])
+def test_compiled_modules(make, need, backend, monkeypatch):
+    """Also where a step needs no workspace."""
+    for name, at in (("usp_spmm_ex", 2), ("usp_spmm_q", 3), ("usp_spmm_grouped", 3)):
+        def product(*args, at=at, **kw):
+            args[at].detach().numpy()[:] = 2 * args[1].detach().numpy()[:, :OUT]
+        monkeypatch.setattr(usp, name, product)
+    module, x, want = make(need)
+    compiled = torch.compile(lambda x: module(x) + 1, backend=backend)
+    for factor in (1, 3):
+        assert torch.equal(compiled(x * factor), want(x * factor) + 1)
+        assert torch.equal(module(x * factor), want(x * factor))

@@ -80,3 +80,12 @@ def test_prompts_beside_single_tokens(values):
     rows = s.rows(counts)
     assert s.cache.plan(rows, T, heads).startswith("tiles")
     attention64.close(s.cache.attention(rows, q.cuda()), *s.want(q, counts))
+
+
+def test_empty_workspace():
+    """An empty tensor where a step needs no workspace, as compiled programs have it."""
+    s = Setting([200, 60], 2, 64, 64, seed=7).fill()
+    q, rows = draw(15, 2, 8, 64).cuda(), s.rows()
+    assert s.cache.workspace_size(rows, 2, 8) == 0
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    assert torch.equal(s.cache.attention(rows, q, workspace=none), s.cache.attention(rows, q))
