@@ -296,6 +296,14 @@ class PagedAttention(torch.nn.Module):
         self.register_buffer("slopes", slopes)
         self._spaces: dict[int, _DeviceWorkspaces] = {}
 
+    def _apply(self, fn, recurse=True):
+        """Moves and casts: slopes stay fp32, as the kernels take them, in a model that is cast."""
+        slopes = self._buffers["slopes"]
+        super()._apply(fn, recurse)
+        if slopes is not None and self._buffers["slopes"].dtype is not torch.float32:
+            self._buffers["slopes"] = slopes.to(self._buffers["slopes"].device)
+        return self
+
     def forward(self, q: torch.Tensor, cache: usp.KVCache, rows: usp.CacheRows, k: Optional[torch.Tensor] = None,
                 v: Optional[torch.Tensor] = None, layer: int = 0, first: Optional[torch.Tensor] = None,
                 last: Optional[torch.Tensor] = None) -> torch.Tensor:
