@@ -455,13 +455,14 @@ usp_status usp_cache_copy(const usp_cache *cache, const int32_t *src, const int3
  * h / (heads / kv_heads) of the cache:
  *     x[k] = scale * q . K[k];   x[k] <- cap * tanh(x[k] / cap)  (cap > 0);   x[k] <- x[k] - slopes[h] * |p - k|
  *     out  = sum_k exp(x[k]) V[k] / sum_k exp(x[k]),   zeros for a row that sees nothing
- * in fp32, with one rounding to fp16 at the end. The weights exp(x - max) are rounded to fp16 for the product with V and taken
- * as rounded in the sum below the line too: relative 2^-11 each down to 2^-27 of the largest, and to 2^-38 of it below
- * that (2^-14 and 2^-25 where q and the biases allow scores beyond 2^25); over 8-bit caches 2^-14 more in prompts (the tiles
- * kernel of usp_attention_plan), and to 22 bits instead for few rows (its rows kernel). Values of 8-bit prompts that are
- * below 2^-14 are rounded to multiples of 2^-24. What a row does not see has no influence on it, NaN and infinities included. A row that
- * sees a NaN, or a score of +infinity, is NaN; one whose scores are all -infinity is zeros. Infinities in q and K, and
- * scores beyond fp32's range (log2(e) times them, so from 2.3e38 on), count as what they are there.
+ * in fp32, with one rounding to fp16 at the end. For the product with V the weights exp(x - max) are taken to 22 bits and
+ * to 2^-38 of the largest where a step has few rows (the rows kernel of usp_attention_plan). In prompts (its tiles kernel)
+ * they are rounded to fp16, in the sum below the line too: relative 2^-11 each down to 2^-27 of the largest, and to 2^-38
+ * of it below that (2^-14 and 2^-25 where q and the biases allow scores beyond 2^25), and 2^-14 more over 8-bit caches, whose
+ * values below 2^-14 are rounded to multiples of 2^-24 there. What a row does not see has no influence on it, NaN and
+ * infinities included. A row that sees a NaN, or a score of +infinity, is NaN; one whose scores are all -infinity is zeros.
+ * Infinities in q and K, and scores beyond fp32's range (log2(e) times them, so from 2.3e38 on), count as what they are
+ * there.
  */
 typedef struct {
     const void *q;          /* device fp16: channel d of head h of row t at q + t * ld_q + h * head_q + d */

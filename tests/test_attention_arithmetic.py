@@ -185,3 +185,28 @@ def test_scale_times_the_keys_scale(n, modified):
     got = cache.attention(rows(n), torch.zeros(n, 2, D, dtype=torch.float16, device="cuda"), scale=2.0 ** 126, slopes=slopes)
     zero = cache.attention(rows(n), torch.zeros(n, 2, D, dtype=torch.float16, device="cuda"), scale=1.0, slopes=slopes)
     assert torch.isfinite(got).all() and torch.equal(got, zero)
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("L", [40, 130, 700])
+def test_weights_of_few_rows(L, values):
+    """Weights are not rounded to fp16 where a row is alone. q and K are whole numbers of few bits, so scores are exact up to
+    their scale (8-bit keys: four values whose largest is 2, so codes and scales of one key are too), and V's signs leave a
+    result far below its terms A = sum p |V|. Errors: the result's rounding, 2^-11 of it; weights, 2^-20 of A and it; scores
+    off by 16 roundings, twice over; sums of L / 16 terms and a join, twice over."""
+    D, heads, kv = 64, 8, 2
+    g = torch.Generator().manual_seed(L)
+    K = torch.randint(-2, 3, (L, kv, D), generator=g).half()
+    K[..., 0] = 2
+    q = torch.randint(-2, 3, (1, heads, D), generator=g).half()
+    V = ((torch.rand(L, kv, D, generator=g) + 0.5) * (torch.randint(0, 2, (L, kv, D), generator=g) * 2 - 1)).half()
+    cache, rows = one_sequence(K, V, values)
+    got = cache.attention(rows(1), q.cuda(), scale=0.11).cpu().double()[0]
+    k, v = attention64.held(K, values == "q"), attention64.held(V, values == "q")
+    for h in range(heads):
+        z = k[:, h // 4] @ q[0, h].double() * float(torch.tensor(0.11))
+        w = torch.softmax(z, 0)
+        out, A = w @ v[:, h // 4], w @ v[:, h // 4].abs()
+        e = 16 * 2.0 ** -24 * (z.abs().max() + (D * 2.0 * 2.0 * 0.11 if values == "q" else 0))
+        tol = 2.0 ** -25 + 2.0 ** -11 * out.abs() + 2.0 ** -20 * (A + out.abs()) + (2 * e + 2 * (L / 16 + 40) * 2.0 ** -24) * A
+        assert ((got[h] - out).abs() <= tol).all(), ((got[h] - out).abs() / tol).max()
