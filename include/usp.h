@@ -456,7 +456,7 @@ usp_status usp_cache_copy(const usp_cache *cache, const int32_t *src, const int3
  *     x[k] = scale * q . K[k];   x[k] <- cap * tanh(x[k] / cap)  (cap > 0);   x[k] <- x[k] - slopes[h] * |p - k|
  *     out  = sum_k exp(x[k]) V[k] / sum_k exp(x[k]),   zeros for a row that sees nothing
  * in fp32, with one rounding to fp16 at the end. For the product with V the weights exp(x - max) are taken to 22 bits and
- * to 2^-38 of the largest where a step has few rows (the rows kernel of usp_attention_plan). In prompts (its tiles kernel)
+ * to 2^-37 of the largest where a step has few rows (the rows kernel of usp_attention_plan). In prompts (its tiles kernel)
  * they are rounded to fp16, in the sum below the line too: relative 2^-11 each down to 2^-27 of the largest, and to 2^-38
  * of it below that (2^-14 and 2^-25 where q and the biases allow scores beyond 2^25), and 2^-14 more over 8-bit caches, whose
  * values below 2^-14 are rounded to multiples of 2^-24 there. What a row does not see has no influence on it, NaN and

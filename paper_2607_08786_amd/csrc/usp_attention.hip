@@ -305,17 +305,26 @@ __global__ __launch_bounds__(kRowWaves *kLanes) void attend_rows_kernel(AttendAr
             unit = u;
             to_unit = 16384.f * __builtin_amdgcn_rcpf(u);
         }
-        half8 p, rest;
-        float block_sum = 0.f;  // to a large weight, single small ones may add nothing
+        float w[8], block_sum = 0.f;  // a block's first: to a large sum, single small ones may add nothing
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float w = exp2_of(x[j] - base);
-            block_sum += w;
-            if (VB == 1) w *= vs[j / 4][j % 4] * to_unit;
-            p[j] = (_Float16)w;
-            // What is rounded off takes part too: the matrix unit idles. (16 sequences of up to 1023 tokens 34.8 -> 35.4 us, long
-            // ones and 8 bits nothing; errors against 64 bits 2.2e-4 -> 2.1e-4, of which the result's rounding is most.)
-            rest[j] = (_Float16)(w - (float)p[j]);
+            w[j] = exp2_of(x[j] - base);
+            block_sum += w[j];
+            if (VB == 1) w[j] *= vs[j / 4][j % 4] * to_unit;
+        }
+        // What is rounded off the weights takes part too: the matrix unit idles. (16 sequences of up to 1023 tokens 34.8 ->
+        // 35.2 us, long ones and 8 bits nothing; errors against 64 bits 2.2e-4 -> 2.1e-4, of which the result's rounding is
+        // most.) fp16 values may be infinite, so it must be neither negative nor nothing: weights are rounded down, and it is
+        // 2^-24 at least where there is a weight.
+        half8 p, rest;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            half2a high = {(_Float16)w[j], (_Float16)w[j + 1]};
+            if (VB == 2) high = __builtin_bit_cast(half2a, __builtin_amdgcn_cvt_pkrtz(w[j], w[j + 1]));
+            half2a low = {(_Float16)(w[j] - (float)high[0]), (_Float16)(w[j + 1] - (float)high[1])};
+            if (VB == 2) low = __builtin_elementwise_max(low, __builtin_elementwise_min(high, half2a{(_Float16)0x1p-24f, (_Float16)0x1p-24f}));
+            p[j] = high[0], p[j + 1] = high[1];
+            rest[j] = low[0], rest[j + 1] = low[1];
         }
         l += block_sum;
 #pragma unroll

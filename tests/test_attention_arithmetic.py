@@ -210,3 +210,25 @@ def test_weights_of_few_rows(L, values):
         e = 16 * 2.0 ** -24 * (z.abs().max() + (D * 2.0 * 2.0 * 0.11 if values == "q" else 0))
         tol = 2.0 ** -25 + 2.0 ** -11 * out.abs() + 2.0 ** -20 * (A + out.abs()) + (2 * e + 2 * (L / 16 + 40) * 2.0 ** -24) * A
         assert ((got[h] - out).abs() <= tol).all(), ((got[h] - out).abs() / tol).max()
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_infinite_values(n):
+    """An infinity that a row sees is one, whatever its weight down to 2^-36 of the largest, and equal weights too; two of
+    opposite signs are NaN."""
+    D, L, heads = 64, 200, 40
+    K = torch.zeros(L, 1, D).half()
+    K[7, 0, 0] = -1  # head h: a score of -h / 40 of 24.95, 2^-36
+    V = draw(5, L, 1, D)
+    V[7, 0, 3], V[7, 0, 5], V[7, 0, 8] = float("inf"), float("-inf"), float("inf")
+    V[9, 0, 8] = float("-inf")
+    q = torch.zeros(n, heads, D).half()
+    q[..., 0] = torch.arange(heads) / 40 * 24.95
+    cache, rows = one_sequence(K, V, "f16")
+    assert cache.plan(rows(n), n, heads).startswith("rows" if n == 1 else "tiles")
+    got = cache.attention(rows(n), q.cuda(), scale=1.0).cpu()
+    assert (got[..., 3] == float("inf")).all() and (got[..., 5] == -float("inf")).all() and got[..., 8].isnan().all()
+    others = [d for d in range(D) if d not in (3, 5, 8)]
+    assert torch.isfinite(got[..., others]).all()
+    hidden = cache.attention(rows(n), q.cuda(), scale=1.0, first=int32([8] * n)).cpu()
+    assert torch.isfinite(hidden[..., :8]).all() and (hidden[..., 8] == -float("inf")).all()
