@@ -232,3 +232,22 @@ def test_infinite_values(n):
     assert torch.isfinite(got[..., others]).all()
     hidden = cache.attention(rows(n), q.cuda(), scale=1.0, first=int32([8] * n)).cpu()
     assert torch.isfinite(hidden[..., :8]).all() and (hidden[..., 8] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("size,step", [(4096, 4), (57344, 32)])
+def test_large_biased_scores(size, step, n, values):
+    """Scores of 1e8 and 1e10 that pass the biases, here of nothing, and under a cap far above them: as without, to roundings."""
+    D, L = 128, 900
+    kind = (torch.arange(L) * 3 + 1) % 7
+    K = (size + step * kind.float())[:, None, None].expand(L, 1, D).half()
+    V = draw(6, L, 1, D).clamp(-3, 3)
+    V[..., 0] = 4
+    q = torch.full((n, 2, D), float(size)).half()
+    q[:, 1] *= -1
+    cache, rows = one_sequence(K, V, values)
+    want = cache.attention(rows(n), q.cuda())
+    for kw in (dict(slopes=torch.zeros(2, device="cuda")), dict(cap=1e30)):
+        got = cache.attention(rows(n), q.cuda(), **kw)
+        assert ((got - want).abs() <= 2.0 ** -10 * want.abs() + 2.0 ** -12).all()
