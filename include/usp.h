@@ -462,7 +462,7 @@ usp_status usp_cache_copy(const usp_cache *cache, const int32_t *src, const int3
  * values below 2^-14 are rounded to multiples of 2^-24 there. What a row does not see has no influence on it, NaN and
  * infinities included. A row that sees a NaN, or a score of +infinity, is NaN; one whose scores are all -infinity is zeros.
  * Infinities in q and K, and scores beyond fp32's range (log2(e) times them, so from 2.3e38 on), count as what they are
- * there.
+ * there; an infinite value as what it is under a weight of at least 2^-36 of the largest (2^-24 where scores may pass 2^25).
  */
 typedef struct {
     const void *q;          /* device fp16: channel d of head h of row t at q + t * ld_q + h * head_q + d */

@@ -1,14 +1,14 @@
 // usp_attention.hip -- attention of a step's rows over a paged cache: the planner, and the kernel
 // for few rows of each sequence (single tokens).
 //
-// Bound by the cache's bytes, each read once: one token over 131072, 8 heads of 128 for 64 of q's, 537 MB, takes 92 us
+// Bound by the cache's bytes, each read once: one token over 131072, 8 heads of 128 for 64 of q's, 537 MB, takes 93 us
 // (5.8 TB/s; a 2 GB copy moves 5.1); 64 sequences of 1024 to 8191 tokens in 8 bits, 633 MB with the scales, 129 us (4.9);
 // 16 sequences of up to 1023 tokens, 40 heads each, 199 MB, 34 us (5.8, part of it from the 256 MB cache). So K and V go
 // from memory to the matrix unit's operands with nothing between, 16 KB a wavefront under way, eight wavefronts a CU; a
 // tile fills 16 of the unit's columns with as many heads as share a head of the cache, down to one, which costs
 // nothing: the unit idles. Loads that pass L2 by (43.9 -> 39.4 us for the 16 sequences) and one test for all of a
 // block's masks, caps and biases instead of one a key (8 bits: 160 -> 129) brought most. The smallest calls are launch,
-// the lengths, the table, the keys, one after the other: 4.6 us for one sequence of 101 tokens.
+// the lengths, the table, the keys, one after the other: 4.9 us for one sequence of 101 tokens.
 #include "usp_attention.h"
 
 #include <algorithm>
@@ -450,7 +450,8 @@ struct AttendPlan {
 // and join would take as long as it (640 tiles of up to 32 blocks: 34.4 us whole, 43 in 1024 pieces).
 constexpr int kFewTiles = 128, kFewBits = 9, kFewMinBlocks = 8, kManyBits = 10, kManyMinBlocks = 32;
 // Workgroups of the tiles kernel that run at once, by the bytes of a value: three on a CU, two that convert 8 bits (512
-// rows over 16512 tokens, 256 tiles: 426 us in two pieces each; a step before this one 438, and 493 in three).
+// rows over 16512 tokens, 256 tiles: 426 us in two pieces each; a step before this one 438, and 493 in three). Counted at
+// widths of up to 128; at 192 and 256 one workgroup fits a CU, and fewer pieces were not tried there.
 constexpr int64_t kTilePlaces[] = {0, 512, 768};
 constexpr int64_t kMostTilePieces = 16;
 // The largest cap whose scores may be off by 2^-22 of it: 2^-14, a quarter of a weight's rounding to fp16.

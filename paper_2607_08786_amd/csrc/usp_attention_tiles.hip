@@ -5,19 +5,24 @@
 // LDS once for all of them, double buffered, by transfers straight into LDS (fp16), where its
 // units already lie in operand order. Products are v_mfma_f32_32x32x16_f16.
 //
-// What bounds it: one prompt of 4096 tokens, 64 heads on 8 of 128 channels, takes 312 us, 882 TFLOP/s;
+// What bounds it: one prompt of 4096 tokens, 64 heads on 8 of 128 channels, takes 317 us, 869 TFLOP/s;
 // an 8192^3 library product reaches 1157 on the same card, a 16384^3 one 1310. A wavefront's step over a
-// block is 16 products (512 cycles of the matrix unit) and about 135 vector instructions, 16 of them
-// exponentials (600 cycles), of which half overlap at best: a matrix and eight vector instructions took 19.6 ns
-// a step where the one alone takes 14.6 and the others 11.3. And the clock falls under this load, from
-// 2.5 (a long cache's single token) to 1.8-1.9 GHz. Steps on the way: a plain loop 779 us; blocks requested ahead and
-// operands read together 348; straight into LDS, operands four products ahead, three wavefronts a SIMD 312. Without gain:
-// priorities of wavefronts, 2 or 6 products ahead. Slower: two blocks under way (339, registers spilled), softmax of a
-// block between the products of its neighbours (369, two wavefronts a SIMD), two tiles of columns a wavefront (556, one).
+// block is 16 products (512 cycles of the matrix unit) and 157 vector instructions, all else counted in, 16 of them
+// exponentials, of which half overlap at best: a matrix and eight vector instructions took 19.6 ns a step where the one
+// alone takes 14.6 and the others 11.3. About 40 of the 157 are o and l faded: 66 in each step where one of 32 columns
+// finds a larger maximum, which for scores in random order is 1 - (1 - 1 / b)^32 at block b, 61% of this prompt's steps. That
+// part need not be: a maximum that grows little could stay. And the clock falls under this load, from 2.5 (a long cache's
+// single token) to 1.8-1.9 GHz. Steps on the way: a plain loop 779 us; blocks requested ahead and operands read together
+// 348; straight into LDS, operands four products ahead, three wavefronts a SIMD 312; weights lifted into fp16's range, sums
+// by blocks, large scores 317. Without gain: priorities of wavefronts, 2 or 6 products ahead. Slower: two blocks under way
+// (339, registers spilled), softmax of a block between the products of its neighbours (369, two wavefronts a SIMD), two
+// tiles of columns a wavefront (556, one). At 192 and 256 channels one wavefront a SIMD is left: the same prompt takes 838
+// and 993 us, 493 and 554 TFLOP/s.
 //
-// 8 bits: 512 rows over 16512 tokens, the same heads, 426 us, 640 TFLOP/s: codes go raw into LDS and are converted
-// there once for the four wavefronts, two wavefronts a SIMD for want of registers. Scales of values taken apart, for
-// exact products with the codes, cost 50 us of it (374 without, at an error against 64 bits of 3.1e-4 instead of 2.4e-4).
+// 8 bits: 512 rows over 16512 tokens, the same heads, 428 us, 638 TFLOP/s (at 256 channels 1323, 412): codes go raw into
+// LDS and are converted there once for the four wavefronts, two wavefronts a SIMD for want of registers. Scales of values
+// taken apart, for exact products with the codes, cost 50 us of it (374 without, at an error against 64 bits of 3.1e-4
+// instead of 2.4e-4).
 #include "usp_attention.h"
 
 #include <utility>
@@ -34,9 +39,10 @@ __device__ inline int first_tile(const AttendArgs &a, int s) {
     return (int)((int64_t)offset_of(a.r, s) * a.group / COLUMNS) + s;
 }
 
-// A scale of values is taken apart into one of 4 bits, whose products with codes fp16 holds exactly, and a factor near 1
-// that the weight of its key takes, in its exponent (so that the largest weight is 1 all the same, which has no
-// rounding): rounded products would add to the result's error as much as its own rounding.
+// A scale of values is taken apart into one of 4 bits, whose products with codes fp16 holds exactly (from 2^-21 on; those of
+// smaller ones are rounded to multiples of 2^-24, as the result is), and a factor near 1 that the weight of its key takes,
+// in its exponent (so that the largest weight is a power of two all the same, which has no rounding): rounded products would
+// add to the result's error as much as its own rounding.
 __device__ inline float short_scale(float s) { return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, s) + 0x80000u) & 0xFFF00000u); }
 
 // Eight codes of keys j .. j + 7 of a channel times their short scales, as fp16 values.
