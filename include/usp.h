@@ -494,7 +494,8 @@ usp_status usp_attention_plan(const usp_cache *cache, const usp_cache_rows *rows
  *              operator; not used by another call in flight
  * The kernel is chosen by the number of rows for each sequence, so a step that mixes single tokens with
  * prompts is faster as two calls. Asynchronous on `stream`; no allocation, capturable; the same bits for the same
- * operands (which other sequences a step has may move a result by roundings of its fp32 sums).
+ * operands (which other sequences a step has, and whether a row near it has a q that allows scores beyond 2^25, may move a
+ * result by roundings of its fp32 sums).
  */
 usp_status usp_attention(const usp_cache *cache, const usp_cache_rows *rows, const usp_attention_args *args,
                          void *workspace, size_t ws_bytes, void *stream);

@@ -178,7 +178,8 @@ __global__ __launch_bounds__(kTileWaves *kLanes, DS > 4 ? 1 : VB == 1 ? 2 : 3) v
             for (int j = 0; j < 4; ++j)
                 sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2a, bits[j]), half2a{(_Float16)1.f, (_Float16)1.f}, sum, false);
         }
-        bound = sum_32(sum) * 65504.f * fabsf(a.scale);
+        sum = sum_32(sum);
+        bound = sum < __builtin_inff() ? sum * 65504.f * fabsf(a.scale) : 0.f;  // a row of NaN: no cause to round others otherwise
     }
     if (MOD) bound += fabsf(slope) * (float)len;
     const bool large = __any(!(bound < kLargeScore)), scale_first = kPlain && large;

@@ -251,3 +251,22 @@ def test_large_biased_scores(size, step, n, values):
     for kw in (dict(slopes=torch.zeros(2, device="cuda")), dict(cap=1e30)):
         got = cache.attention(rows(n), q.cuda(), **kw)
         assert ((got - want).abs() <= 2.0 ** -10 * want.abs() + 2.0 ** -12).all()
+
+
+@pytest.mark.parametrize("values", ["f16", "q"])
+@pytest.mark.parametrize("biased", [False, True])
+def test_neighbours_of_rows_that_are_not_finite(biased, values):
+    """Rows with a NaN or an infinity in q are NaN, and all others keep their bits."""
+    D, L, n, heads = 128, 700, 300, 4
+    cache, rows = one_sequence(draw(8, L, 2, D), draw(9, L, 2, D), values)
+    kw = dict(slopes=torch.full((heads,), 0.01, device="cuda")) if biased else {}
+    q = draw(10, n, heads, D, scale=2.0)
+    clean = cache.attention(rows(n), q.cuda(), **kw)
+    assert torch.isfinite(clean).all()
+    bad = torch.zeros(n, heads, dtype=torch.bool)
+    for i, value in enumerate((float("nan"), float("inf"), -float("inf"))):
+        for row in range(5 + i, n, 41):
+            q[row, row % heads, 3 * i] = value
+            bad[row, row % heads] = True
+    got = cache.attention(rows(n), q.cuda(), **kw)
+    assert got[bad.cuda()].isnan().all() and torch.equal(got[~bad.cuda()], clean[~bad.cuda()])
